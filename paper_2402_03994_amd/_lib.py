@@ -1,5 +1,5 @@
-"""ctypes declarations of the C ABI in include/sketch.h and include/sketch_hvp.h (argument
-marshalling only)."""
+"""ctypes declarations of the C ABI in include/sketch.h, include/sketch_hvp.h and include/sketch_train.h
+(argument marshalling only)."""
 from __future__ import annotations
 
 import ctypes
@@ -10,6 +10,8 @@ LIB_PATH = os.path.join(HERE, "libsketch.so")
 
 SK_FJL, SK_FFD, SK_AFFD, SK_AFJL, SK_QK, SK_QKH, SK_AFJLQ, SK_AFFDQ, SK_AFJLF = range(9)
 SK_F32, SK_BF16 = 0, 1
+SK_I32, SK_I64 = 0, 1
+SK_ADAMW_F32, SK_ADAMW_8BIT = 0, 1
 STATUS = {0: "SK_OK", -1: "SK_EINVAL", -2: "SK_EDTYPE", -3: "SK_ENOMEM", -4: "SK_EHIP", -5: "SK_EUNSUPPORTED"}
 STREAMS = {"sign": 1, "gauss": 2, "index": 3, "ffdperm": 4, "pi1": 5, "pi2": 6, "qka": 7, "qkb": 8, "qh": 9,
            "hvp": 10}
@@ -17,7 +19,10 @@ EXPORTS = ("sketch_create", "sketch_apply", "sketch_apply_noalloc", "sketch_appl
            "sketch_debug_stream", "sketch_profile", "sketch_profile_read", "sketch_last_error",
            "sketch_status_string", "sk_hvp_create", "sk_hvp_apply", "sk_hvp_destroy", "sketch_hvp",
            "sketch_arnoldi_work_floats", "sketch_arnoldi_step", "sketch_arnoldi", "sk_hvp_profile",
-           "sk_hvp_profile_read", "sketch_id_search_work_floats", "sketch_id_search")
+           "sk_hvp_profile_read", "sketch_id_search_work_floats", "sketch_id_search", "sketch_embed", "sketch_embed_grad",
+           "sketch_embed_grad_work_bytes", "sketch_token_logp", "sketch_token_logp_grad", "sketch_policy_loss",
+           "sketch_preference_work_bytes", "sketch_preference_loss", "sketch_adamw_create",
+           "sketch_adamw_state_elems", "sketch_adamw_apply", "sketch_adamw_moments", "sketch_adamw_destroy")
 HVP_PROF_CLASSES = ["hvp_dots", "hvp_combine", "arnoldi_orth"]
 HVP_MAX_RANK = 32
 PROF_CLASSES = ["afjl_fold", "afjl_tail", "fwht", "prolog", "affd_fold", "gather", "ffd", "qk", "other",
@@ -39,6 +44,20 @@ class Info(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("D", ctypes.c_int64),
                 ("seed", ctypes.c_uint64), ("total_numel", ctypes.c_int64), ("total_padded", ctypes.c_int64),
                 ("workspace_bytes", ctypes.c_int64), ("rng_version", ctypes.c_int32), ("device", ctypes.c_int32)]
+
+
+class Logits(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("targets", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("vocab", ctypes.c_int64), ("ld", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("dtype", ctypes.c_int), ("index", ctypes.c_int), ("device", ctypes.c_int32)]
+
+
+class AdamWStep(ctypes.Structure):
+    _fields_ = [("step", ctypes.c_int64), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
+                ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("max_norm", ctypes.c_double), ("grad_scale", ctypes.c_void_p), ("norm", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p)]
 
 
 _lib = None
@@ -101,6 +120,27 @@ def load() -> ctypes.CDLL:
     L.sketch_id_search.argtypes = [P, P, ctypes.POINTER(P), i64, f32, f32, i32, i32, P, P, P,
                                    ctypes.POINTER(IdResult), P]
     L.sketch_id_search.restype = ctypes.c_int
+    LP, SP = ctypes.POINTER(Logits), ctypes.POINTER(AdamWStep)
+    for name, restype, args in (
+            ("sketch_embed", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, ctypes.c_int, i64, f32, P, ctypes.c_int,
+                                            i32, P]),
+            ("sketch_embed_grad_work_bytes", i64, [i64, i64, i64]),
+            ("sketch_embed_grad", ctypes.c_int, [P, ctypes.c_int, i64, P, ctypes.c_int, i64, i64, i64, i64, f32, P,
+                                                 ctypes.c_int, i32, P, i64, i32, P]),
+            ("sketch_token_logp", ctypes.c_int, [LP, P, P, P]),
+            ("sketch_token_logp_grad", ctypes.c_int, [LP, P, P, P, i64, P]),
+            ("sketch_policy_loss", ctypes.c_int, [LP, P, P, P, P, f32, f32, f32, P, P, P, P, i64, P]),
+            ("sketch_preference_work_bytes", i64, [i64]),
+            ("sketch_preference_loss", ctypes.c_int, [LP, P, ctypes.c_int, i64, P, f32, f32, i32, P, P, P, P, i64, P,
+                                                      i64, P]),
+            ("sketch_adamw_create", ctypes.c_int, [P, P, i32, ctypes.c_int, u64, i32, ctypes.POINTER(P)]),
+            ("sketch_adamw_state_elems", i64, [P]),
+            ("sketch_adamw_apply", ctypes.c_int, [P, SP, ctypes.POINTER(P), ctypes.c_int, ctypes.POINTER(P),
+                                                  ctypes.c_int, ctypes.POINTER(P), P]),
+            ("sketch_adamw_moments", ctypes.c_int, [P, P, P, P, P, P, P, P]),
+            ("sketch_adamw_destroy", None, [P])):
+        fn = getattr(L, name)
+        fn.argtypes, fn.restype = args, restype
     _lib = L
     return L
 

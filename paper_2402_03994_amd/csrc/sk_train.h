@@ -1,0 +1,90 @@
+// sk_train.h -- what the training-step operators (sk_embed.hip, sk_loss.hip,
+// sk_adamw.hip) share: argument failures, the device guard, element access and
+// ordered workgroup reductions.
+#pragma once
+
+#include <cmath>
+#include <new>
+#include <string>
+
+#include "../../include/sketch_train.h"
+#include "sk_launch.h"
+
+namespace sk {
+
+inline int train_fail(int code, const char *msg) noexcept {
+  try {
+    set_error(code, msg);
+  } catch (...) {  // no memory for the message: the code alone
+  }
+  return code;
+}
+
+inline int train_launched() noexcept {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SK_OK : train_fail(SK_EHIP, hipGetErrorString(e));
+}
+
+struct TrainGuard {  // the caller's current device again on scope exit
+  int prev = -1, dev;
+  explicit TrainGuard(int d) : dev(d) {
+    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+    if (prev != dev) (void)hipSetDevice(dev);
+  }
+  ~TrainGuard() {
+    if (prev >= 0 && prev != dev) (void)hipSetDevice(prev);
+  }
+};
+
+// Elements: float or bf16 (held as its 16 bits).
+struct bf16 {
+  uint16_t u;
+};
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(bf16 x) { return __uint_as_float((uint32_t)x.u << 16); }
+// to nearest even, NaN kept
+__device__ __forceinline__ uint32_t bf16_bits(float f) {
+  return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)f);
+}
+template <typename T>
+__device__ __forceinline__ T from_f32(float f);
+template <>
+__device__ __forceinline__ float from_f32<float>(float f) {
+  return f;
+}
+template <>
+__device__ __forceinline__ bf16 from_f32<bf16>(float f) {
+  return bf16{(uint16_t)bf16_bits(f)};
+}
+
+template <typename Op, typename T>
+__device__ __forceinline__ T wave_all(T v, Op op) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v = op(v, __shfl_xor(v, d, 64));
+  return v;
+}
+struct OpMax {
+  __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct OpAdd {
+  template <typename T>
+  __device__ T operator()(T a, T b) const {
+    return a + b;
+  }
+};
+
+// Reduction over a workgroup of W waves, in a fixed order; every thread gets the result.  `lds` holds W entries and
+// is free again after the next barrier.
+template <int W, typename Op, typename T>
+__device__ __forceinline__ T block_all(T v, Op op, T *lds) {
+  v = wave_all(v, op);
+  if (W == 1) return v;
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  T r = lds[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) r = op(r, lds[i]);
+  return r;
+}
+
+}  // namespace sk
