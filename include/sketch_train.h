@@ -46,14 +46,15 @@ int sketch_embed(const void *weight, sk_dtype dtype, int64_t vocab, int64_t widt
 /*
  * Gradient of the lookup: for each of `batch` groups of n tokens
  *   out[v] (+)= scale * sum over t with ids[t] = v of dy[t]
- * with the sum in fp32 in the order of t (long runs of one id in pieces of
- * fixed length), rounded once to out_dtype; ids outside [0, vocab) add nothing.
+ * with the sum in fp32 in an order that the ids alone set (that of t in pieces of
+ * 16 or 64 tokens, then the pieces), rounded once to out_dtype; ids outside [0, vocab) add nothing.
  * batch > 1 gives one gradient per example.  Rows that no id names are zeroed
  * (accumulate = 0) or kept (accumulate = 1).
  *   dy       [batch, n, width], row stride ld >= width elements.
  *   out      [batch, vocab, width] contiguous.
  *   work     sketch_embed_grad_work_bytes(batch, n, width) bytes, 256-byte aligned.
- * SK_EUNSUPPORTED for vocab > 2^20 or batch * n > 2^30.
+ * SK_EUNSUPPORTED for vocab > 2^20, batch > 2^18, batch * n > 2^28, width > 2^24 or
+ * about batch * n * width > 2^42.
  */
 int64_t sketch_embed_grad_work_bytes(int64_t batch, int64_t n, int64_t width);
 int sketch_embed_grad(const void *dy, sk_dtype dtype, int64_t ld, const void *ids, sk_index index, int64_t batch,
@@ -81,8 +82,8 @@ typedef struct {
 
 /*
  * logp[t] = log softmax(scale x_t)[targets[t]] (fp32).  stats [rows, 2] fp32
- * (NULL if not wanted): the row's largest logit m and log sum exp(scale (x - m)),
- * what sketch_token_logp_grad needs.  A row without a logit above -inf has
+ * (NULL if not wanted): the row's largest logit m and sum exp(scale (x - m)), what
+ * sketch_token_logp_grad needs (0, 0 at masked rows).  A row without a logit above -inf has
  * logp = -inf and a gradient of zeros; NaN and +inf follow the formula.
  */
 int sketch_token_logp(const sk_logits *x, float *logp, float *stats, void *stream);

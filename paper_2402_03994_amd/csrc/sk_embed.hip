@@ -1,82 +1,386 @@
 // sk_embed.hip -- embedding lookup and its gradient (C ABI of
 // include/sketch_train.h).
+//
+// Lookup: a wave copies up to 4 KB of a row (64 lanes x 4 vectors of 16
+// bytes), so that a row needs no more waves than its bytes ask for and one id
+// is read per wave; bound by memory.
+//
+// Gradient, in three or four launches, without atomics on floats:
+//   k_eg_rank   sorts each run of up to 4096 tokens of a group by (id,
+//               position): an entry's place is how many entries are smaller,
+//               counted by brute force (64 entries a workgroup against all of
+//               the run; 4096 comparisons an entry over the whole chip take
+//               less time than the barriers of a sort in one workgroup's LDS).
+//   k_eg_merge  joins up to 16 sorted runs: an entry's place is its own plus
+//               what a binary search in each other run gives, one lane a run.
+//   k_eg_sum    a wave adds up R sorted entries for 64 vectors of columns and
+//               writes out every id that begins and ends among them; what
+//               crosses the cut is written to the workspace (head: the part of
+//               an id that began earlier, tail: of one that goes on).  The
+//               launch's other workgroups zero the rows that no id names.
+//   k_eg_join   tail + heads of the ids that cross cuts.
+// Every sum has a fixed order: the sorted one within R entries, then piece by
+// piece.  Bound by writing the gradient (vocab x width per group).
+#include <algorithm>
+
 #include "sk_train.h"
 
 using namespace sk;
 
 namespace {
 
+constexpr uint32_t kNoId = 0xFFFFFFFFu;  // of a masked token: sorts to the end
+constexpr int kRun = 4096;               // tokens ranked by brute force
+constexpr int kMergeRuns = 16;
+
 __device__ __forceinline__ int64_t id_at(const void *ids, int index, int64_t t) {
   return index == SK_I64 ? ((const int64_t *)ids)[t] : ((const int32_t *)ids)[t];
 }
 
-template <typename W, typename O>
-__global__ __launch_bounds__(256) void k_embed(const W *__restrict__ w, int64_t vocab, int64_t width, int64_t ld,
-                                               const void *__restrict__ ids, int index, float scale,
-                                               O *__restrict__ out) {
-  const int64_t t = blockIdx.x, v = id_at(ids, index, t);
-  const bool live = v >= 0 && v < vocab;
-  for (int64_t c = threadIdx.x; c < width; c += 256)
-    out[t * width + c] = from_f32<O>(live ? scale * to_f32(w[v * ld + c]) : 0.0f);
-}
-
-template <typename O>
-__global__ __launch_bounds__(256) void k_eg_zero(O *__restrict__ out, int64_t n) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
-    out[i] = from_f32<O>(0.0f);
-}
-
-// One workgroup per token: the first one of its id in the group adds up all of them in order.
-template <typename G, typename O>
-__global__ __launch_bounds__(256) void k_eg_sum(const G *__restrict__ dy, int64_t ld, const void *__restrict__ ids,
-                                                int index, int64_t n, int64_t vocab, int64_t width, float scale,
-                                                O *__restrict__ out, int accumulate) {
-  __shared__ int found;
-  __shared__ int match[256];
-  const int64_t b = blockIdx.y, t = blockIdx.x, base = b * n, v = id_at(ids, index, base + t);
-  if (v < 0 || v >= vocab) return;
-  if (threadIdx.x == 0) found = 0;
-  __syncthreads();
-  for (int64_t i = threadIdx.x; i < t; i += 256)
-    if (id_at(ids, index, base + i) == v) found = 1;
-  __syncthreads();
-  if (found) return;
-  O *o = out + (b * vocab + v) * width;
-  for (int64_t c0 = 0; c0 < width; c0 += 256) {
-    const int64_t c = c0 + threadIdx.x;
-    float sum = 0.0f;
-    for (int64_t i0 = t; i0 < n; i0 += 256) {
-      const int64_t i = i0 + threadIdx.x;
-      __syncthreads();
-      match[threadIdx.x] = i < n && id_at(ids, index, base + i) == v;
-      __syncthreads();
-      for (int k = 0; k < 256; ++k)
-        if (match[k] && c < width) sum += to_f32(dy[(base + i0 + k) * ld + c]);
-    }
-    if (c < width) o[c] = from_f32<O>(scale * sum + (accumulate ? to_f32(o[c]) : 0.0f));
+// N elements from floats, at an address aligned to one element
+template <typename O, int N>
+__device__ __forceinline__ void store_n(O *p, const float *f) {
+  if (sizeof(O) == 4) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) Vec<O>::store(p + i, Vec<O>::pack(f + i));
+  } else if (N == 8) {
+    Vec<O>::store(p, Vec<O>::pack(f));
+  } else {  // four bf16
+    struct __attribute__((packed, aligned(2))) Half {
+      uint32_t a, b;
+    };
+    *(Half *)p = Half{bf16_bits(f[0]) | bf16_bits(f[1]) << 16, bf16_bits(f[2]) | bf16_bits(f[3]) << 16};
   }
 }
 
-template <typename W>
+template <typename W, typename O>
+__global__ __launch_bounds__(256) void k_embed(const W *__restrict__ w, int64_t vocab, int width, int64_t ld,
+                                               const void *__restrict__ ids, int index, int64_t n, int pieces,
+                                               float scale, O *__restrict__ out) {
+  constexpr int N = Vec<W>::N, NV = 4;
+  const int64_t job = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = job / pieces;
+  if (t >= n) return;
+  const int lane = threadIdx.x & 63, nv = width / N, v0 = (int)(job % pieces) * 64 * NV + lane;
+  const int64_t v = id_at(ids, index, t);
+  const bool live = v >= 0 && v < vocab;
+  const W *x = w + (live ? v : 0) * ld;
+  O *o = out + t * width;
+  u32x4 raw[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    raw[k] = u32x4{0, 0, 0, 0};
+    if (live && v0 + 64 * k < nv) raw[k] = Vec<W>::load(x + (int64_t)(v0 + 64 * k) * N);
+  }
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (v0 + 64 * k < nv) {
+      float f[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i] = scale * Vec<W>::get(raw[k], i);
+      store_n<O, N>(o + (int64_t)(v0 + 64 * k) * N, f);
+    }
+  const int c = nv * N + lane;  // the width % N last columns, by the first piece
+  if (v0 == lane && c < width) o[c] = from_f32<O>(live ? scale * to_f32(x[c]) : 0.0f);
+}
+
+struct Entry {  // a token of its group: id and position
+  uint32_t id, pos;
+};
+
+// Ranks 64 entries of a run against the whole run, eight waves taking turns at its blocks of 64.
+__global__ __launch_bounds__(512) void k_eg_rank(const void *__restrict__ ids, int index, int64_t n, int64_t vocab,
+                                                 int runs, int tiles, Entry *__restrict__ sorted) {
+  __shared__ int part[8][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t run = blockIdx.x / (unsigned)tiles, b = run / runs, p0 = (run % runs) * kRun;
+  const int tile = blockIdx.x % (unsigned)tiles, len = (int)(n - p0 < kRun ? n - p0 : kRun);
+  if (tile * 64 >= len) return;
+  auto key = [&](int i) -> uint32_t {
+    if (i >= len) return kNoId;
+    const int64_t v = id_at(ids, index, b * n + p0 + i);
+    return v >= 0 && v < vocab ? (uint32_t)v : kNoId;
+  };
+  const uint32_t mine = key(tile * 64 + lane);
+  int count = 0;
+  for (int blk = wave; blk * 64 < len; blk += 8) {
+    const uint32_t theirs = key(blk * 64 + lane);
+    if (blk < tile) {  // earlier entries of the same id come first
+#pragma unroll
+      for (int j = 0; j < 64; ++j) count += (uint32_t)__builtin_amdgcn_readlane((int)theirs, j) <= mine;
+    } else if (blk > tile) {
+#pragma unroll
+      for (int j = 0; j < 64; ++j) count += (uint32_t)__builtin_amdgcn_readlane((int)theirs, j) < mine;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 64; ++j) {
+        const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)theirs, j);
+        count += k < mine || (k == mine && j < lane);
+      }
+    }
+  }
+  part[wave][lane] = count;
+  __syncthreads();
+  if (wave == 0 && tile * 64 + lane < len) {
+    int rank = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rank += part[i][lane];
+    sorted[b * n + p0 + rank] = Entry{mine, (uint32_t)(p0 + tile * 64 + lane)};
+  }
+}
+
+// Sorted runs of `len` entries, 16 at a time: 16 lanes an entry.
+__global__ __launch_bounds__(256) void k_eg_merge(const Entry *__restrict__ in, Entry *__restrict__ out, int64_t n,
+                                                  int64_t len, int64_t total) {
+  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kMergeRuns;
+  const int r = threadIdx.x % kMergeRuns;
+  if (e >= total) return;  // all 16 lanes of an entry
+  const int64_t b = e / n, i = e % n, g0 = i / (len * kMergeRuns) * (len * kMergeRuns);
+  const int own = (int)((i - g0) / len);
+  const Entry mine = in[e];
+  // lower bound in later runs, upper bound in earlier ones: entries of one id stay in order
+  const int64_t r0 = g0 + r * len;
+  int64_t lo = 0, hi = r0 >= n ? 0 : (n - r0 < len ? n - r0 : len);
+  if (r == own) {
+    lo = hi = i - r0;
+  }
+  const Entry *run = in + b * n + r0;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    const uint32_t k = run[mid].id;
+    if (r < own ? k <= mine.id : k < mine.id)
+      lo = mid + 1;
+    else
+      hi = mid;
+  }
+  int64_t rank = lo;
+#pragma unroll
+  for (int d = 8; d >= 1; d >>= 1) rank += __shfl_xor(rank, d, 16);
+  if (r == 0) out[b * n + g0 + rank] = mine;
+}
+
+// What the sums work on: groups of n sorted entries, cut into tiles of R, and columns cut into pieces of 64 vectors.
+struct Sums {
+  const Entry *sorted;
+  int64_t n, vocab, ld, tiles;
+  int width, pieces, R, accumulate;
+  float scale;
+  float *head, *tail;  // [batch, tiles, width]
+};
+
+// the N columns from c on of a row of sums to out or (accumulate) onto it
+template <typename O, int N>
+__device__ __forceinline__ void put(O *row, int c, int width, const float *acc, float scale, int accumulate) {
+  if (c + N <= width) {
+    float f[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = scale * acc[i] + (accumulate ? to_f32(row[c + i]) : 0.0f);
+    store_n<O, N>(row + c, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (c + i < width) row[c + i] = from_f32<O>(scale * acc[i] + (accumulate ? to_f32(row[c + i]) : 0.0f));
+  }
+}
+template <int N>
+__device__ __forceinline__ void put_part(float *row, int c, int width, const float *acc) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (c + i < width) row[c + i] = acc[i];
+}
+
+template <typename G, typename O>
+__global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, unsigned sum_blocks, const G *__restrict__ dy,
+                                                O *__restrict__ out) {
+  constexpr int N = Vec<G>::N, U = 32 / N;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (blockIdx.x >= sum_blocks) {
+    // zeros to the rows without an entry: 64 rows a wave, each lane looks one up
+    const int64_t per = (s.vocab + 255) / 256, j = blockIdx.x - sum_blocks, b = j / per;
+    const int64_t r0 = (j % per) * 256 + wave * 64, r = r0 + lane;
+    const Entry *k = s.sorted + b * s.n;
+    int64_t lo = 0, hi = s.n;
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) >> 1;
+      if ((int64_t)k[mid].id < r)
+        lo = mid + 1;
+      else
+        hi = mid;
+    }
+    uint64_t absent = __ballot(r < s.vocab && (lo >= s.n || (int64_t)k[lo].id != r));
+    constexpr int NO = Vec<O>::N;
+    while (absent) {
+      const int at = __builtin_ctzll(absent);
+      absent &= absent - 1;
+      O *row = out + (b * s.vocab + r0 + at) * s.width;
+      const int nv = s.width / NO;
+      for (int v = lane; v < nv; v += 64) Vec<O>::store(row + (int64_t)v * NO, u32x4{0, 0, 0, 0});
+      if (nv * NO + lane < s.width) row[nv * NO + lane] = from_f32<O>(0.0f);
+    }
+    return;
+  }
+  const int64_t job = (int64_t)blockIdx.x * 4 + wave;
+  if (job >= jobs) return;
+  const int64_t bt = job / s.pieces, b = bt / s.tiles, tile = bt % s.tiles, e0 = tile * s.R;
+  const int c = (int)(job % s.pieces) * 64 * N + lane * N;
+  const Entry *k = s.sorted + b * s.n;
+  Entry e{kNoId, 0};
+  if (lane < s.R && e0 + lane < s.n) e = k[e0 + lane];
+  const uint32_t before = e0 > 0 ? k[e0 - 1].id : kNoId, after = e0 + s.R < s.n ? k[e0 + s.R].id : kNoId;
+  float acc[N];
+  uint32_t cur = kNoId;
+  bool began = true;
+  O *const o = out + b * s.vocab * s.width;
+  auto flush = [&](bool ends) {
+    if (cur == kNoId) return;
+    if (began && ends)
+      put<O, N>(o + (int64_t)cur * s.width, c, s.width, acc, s.scale, s.accumulate);
+    else
+      put_part<N>((began ? s.tail : s.head) + bt * s.width, c, s.width, acc);
+  };
+  for (int i0 = 0; i0 < s.R; i0 += U) {
+    float x[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)e.id, i0 + u);
+      const uint32_t pos = (uint32_t)__builtin_amdgcn_readlane((int)e.pos, i0 + u);
+      if (id == kNoId) continue;  // the rest of the tile is empty
+      const G *row = dy + (b * s.n + pos) * s.ld;
+      if (c + N <= s.width) {
+        const u32x4 v = Vec<G>::load(row + c);
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[u][i] = Vec<G>::get(v, i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[u][i] = c + i < s.width ? to_f32(row[c + i]) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)e.id, i0 + u);
+      if (id == kNoId) continue;
+      if (id != cur) {
+        flush(true);
+        began = i0 + u > 0 || before != id;
+        cur = id;
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) acc[i] += x[u][i];
+    }
+  }
+  flush(after != cur);
+}
+
+// An id that begins in a tile and goes on: its tail there and the heads of the tiles that follow, four waves in turn.
+template <typename O>
+__global__ __launch_bounds__(256) void k_eg_join(Sums s, O *__restrict__ out) {
+  constexpr int N = 4;
+  __shared__ float part[3][64 * N];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int pieces = (s.width + 64 * N - 1) / (64 * N);
+  const int64_t bt = blockIdx.x / (unsigned)pieces, b = bt / s.tiles, tile = bt % s.tiles, e1 = (tile + 1) * s.R;
+  if (e1 >= s.n) return;
+  const Entry *k = s.sorted + b * s.n;
+  const uint32_t id = k[e1 - 1].id;
+  if (id == kNoId || k[e1].id != id) return;
+  if (k[e1 - s.R].id == id && e1 > s.R && k[e1 - s.R - 1].id == id) return;  // began earlier
+  int64_t heads = 0;
+  for (;;) {
+    const int64_t at = e1 + (heads + lane) * s.R;
+    const uint64_t no = ~__ballot(at < s.n && k[at].id == id);
+    if (no) {
+      heads += __builtin_ctzll(no);
+      break;
+    }
+    heads += 64;
+  }
+  const int c = (int)(blockIdx.x % (unsigned)pieces) * 64 * N + lane * N;
+  float acc[N] = {0.0f, 0.0f, 0.0f, 0.0f};
+  auto add = [&](const float *row) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (c + i < s.width) acc[i] += row[c + i];
+  };
+  if (wave == 0) add(s.tail + bt * s.width);
+#pragma unroll 4
+  for (int64_t h = wave; h < heads; h += 4) add(s.head + (bt + 1 + h) * s.width);
+  if (wave)
+#pragma unroll
+    for (int i = 0; i < N; ++i) part[wave - 1][lane * N + i] = acc[i];
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] += part[w][lane * N + i];
+  if (c < s.width) put<O, N>(out + (b * s.vocab + id) * s.width, c, s.width, acc, s.scale, s.accumulate);
+}
+
+template <typename W, typename O>
 void run_embed(const void *w, int64_t vocab, int64_t width, int64_t ld, const void *ids, int index, int64_t n,
-               float scale, void *out, sk_dtype od, hipStream_t st) {
-  const dim3 g((unsigned)n), b(256);
-  if (od == SK_F32)
-    hipLaunchKernelGGL((k_embed<W, float>), g, b, 0, st, (const W *)w, vocab, width, ld, ids, index, scale,
-                       (float *)out);
-  else
-    hipLaunchKernelGGL((k_embed<W, bf16>), g, b, 0, st, (const W *)w, vocab, width, ld, ids, index, scale,
-                       (bf16 *)out);
+               float scale, void *out, hipStream_t st) {
+  const int64_t pieces = std::max<int64_t>(1, (width / Vec<W>::N + 255) / 256);
+  hipLaunchKernelGGL((k_embed<W, O>), dim3((unsigned)((n * pieces + 3) / 4)), dim3(256), 0, st, (const W *)w, vocab,
+                     (int)width, ld, ids, index, n, (int)pieces, scale, (O *)out);
+}
+
+// Entries a wave adds up: few where there are few waves (8192 fill the chip), else enough that little is left to join.
+int eg_tile(int64_t batch, int64_t n, int64_t width) {
+  return batch * n * ((width + 255) / 256) > 8192 * 16 ? 64 : 16;
+}
+
+struct EgWork {
+  int64_t tiles, entries, sums, bytes;  // bytes of one list of entries, of one set of partial sums, of all
+};
+EgWork eg_work(int64_t batch, int64_t n, int64_t width) {
+  EgWork w;
+  const int R = eg_tile(batch, n, width);
+  w.tiles = (n + R - 1) / R;
+  w.entries = (batch * n * (int64_t)sizeof(Entry) + 255) / 256 * 256;
+  w.sums = w.tiles > 1 ? (batch * w.tiles * width * 4 + 255) / 256 * 256 : 0;
+  w.bytes = w.entries * (n > kRun ? 2 : 1) + 2 * w.sums;
+  return w;
 }
 
 template <typename G, typename O>
 void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batch, int64_t n, int64_t vocab,
-            int64_t width, float scale, O *out, int accumulate, hipStream_t st) {
-  if (!accumulate)
-    hipLaunchKernelGGL((k_eg_zero<O>), dim3(4096), dim3(256), 0, st, out, batch * vocab * width);
-  if (n)
-    hipLaunchKernelGGL((k_eg_sum<G, O>), dim3((unsigned)n, (unsigned)batch), dim3(256), 0, st, (const G *)dy, ld, ids,
-                       index, n, vocab, width, scale, out, accumulate);
+            int64_t width, float scale, O *out, int accumulate, void *work, hipStream_t st) {
+  const EgWork w = eg_work(batch, n, width);
+  Entry *sorted = (Entry *)work, *other = (Entry *)((char *)work + w.entries);
+  Sums s;
+  s.head = (float *)((char *)work + w.entries * (n > kRun ? 2 : 1));
+  s.tail = s.head + w.sums / 4;
+  if (n) {
+    const int64_t runs = (n + kRun - 1) / kRun;
+    const int64_t tiles = (std::min<int64_t>(n, kRun) + 63) / 64;  // of a run
+    hipLaunchKernelGGL(k_eg_rank, dim3((unsigned)(batch * runs * tiles)), dim3(512), 0, st, ids, index, n, vocab,
+                       (int)runs, (int)tiles, sorted);
+    for (int64_t len = kRun; len < n; len *= kMergeRuns) {
+      hipLaunchKernelGGL(k_eg_merge, dim3((unsigned)((batch * n * kMergeRuns + 255) / 256)), dim3(256), 0, st, sorted,
+                         other, n, len, batch * n);
+      std::swap(sorted, other);
+    }
+  }
+  s.sorted = sorted;
+  s.n = n;
+  s.vocab = vocab;
+  s.ld = ld;
+  s.tiles = w.tiles;
+  s.width = (int)width;
+  s.pieces = (int)((width + 64 * Vec<G>::N - 1) / (64 * Vec<G>::N));
+  s.R = eg_tile(batch, n, width);
+  s.accumulate = accumulate;
+  s.scale = scale;
+  const int64_t jobs = batch * w.tiles * s.pieces, sum_blocks = (jobs + 3) / 4;
+  const int64_t blocks = sum_blocks + (accumulate ? 0 : batch * ((vocab + 255) / 256));
+  if (blocks)
+    hipLaunchKernelGGL((k_eg_sum<G, O>), dim3((unsigned)blocks), dim3(256), 0, st, s, jobs, (unsigned)sum_blocks,
+                       (const G *)dy, out);
+  if (w.tiles > 1)
+    hipLaunchKernelGGL((k_eg_join<O>), dim3((unsigned)(batch * w.tiles * ((width + 255) / 256))), dim3(256), 0, st, s,
+                       out);
 }
 
 bool dtype_ok(int d) { return d == SK_F32 || d == SK_BF16; }
@@ -91,20 +395,26 @@ int sketch_embed(const void *weight, sk_dtype dtype, int64_t vocab, int64_t widt
   if (index != SK_I32 && index != SK_I64) return train_fail(SK_EDTYPE, "unknown index type");
   if (vocab < 1 || width < 1 || n < 0 || ld < width)
     return train_fail(SK_EINVAL, "need vocab, width >= 1, n >= 0 and ld >= width");
-  if (n > INT32_MAX) return train_fail(SK_EUNSUPPORTED, "more than 2^31 - 1 ids");
+  if (n > INT32_MAX || width > (1 << 24) || n * ((width + 1023) / 1024) > INT32_MAX)
+    return train_fail(SK_EUNSUPPORTED, "too many ids, or a width above 2^24");
   if (n == 0) return SK_OK;
   if (!weight || !ids || !out) return train_fail(SK_EINVAL, "NULL argument");
   TrainGuard guard(device);
-  if (dtype == SK_F32)
-    run_embed<float>(weight, vocab, width, ld, ids, index, n, scale, out, out_dtype, (hipStream_t)stream);
+  hipStream_t st = (hipStream_t)stream;
+  if (dtype == SK_F32 && out_dtype == SK_F32)
+    run_embed<float, float>(weight, vocab, width, ld, ids, index, n, scale, out, st);
+  else if (dtype == SK_F32)
+    run_embed<float, bf16>(weight, vocab, width, ld, ids, index, n, scale, out, st);
+  else if (out_dtype == SK_F32)
+    run_embed<bf16, float>(weight, vocab, width, ld, ids, index, n, scale, out, st);
   else
-    run_embed<bf16>(weight, vocab, width, ld, ids, index, n, scale, out, out_dtype, (hipStream_t)stream);
+    run_embed<bf16, bf16>(weight, vocab, width, ld, ids, index, n, scale, out, st);
   return train_launched();
 }
 
 int64_t sketch_embed_grad_work_bytes(int64_t batch, int64_t n, int64_t width) {
-  if (batch < 1 || n < 0 || width < 1) return 0;
-  return 256;
+  if (batch < 1 || n < 0 || width < 1 || batch > (1 << 30) || n > (1 << 30) || batch * n > (1 << 30)) return 0;
+  return std::max<int64_t>(256, eg_work(batch, n, width).bytes);
 }
 
 int sketch_embed_grad(const void *dy, sk_dtype dtype, int64_t ld, const void *ids, sk_index index, int64_t batch,
@@ -114,21 +424,23 @@ int sketch_embed_grad(const void *dy, sk_dtype dtype, int64_t ld, const void *id
   if (index != SK_I32 && index != SK_I64) return train_fail(SK_EDTYPE, "unknown index type");
   if (batch < 1 || vocab < 1 || width < 1 || n < 0 || ld < width)
     return train_fail(SK_EINVAL, "need batch, vocab, width >= 1, n >= 0 and ld >= width");
-  if (vocab > (1 << 20) || batch > (1 << 30) || n > (1 << 30) || batch * n > (1 << 30))
-    return train_fail(SK_EUNSUPPORTED, "vocab above 2^20 or batch * n above 2^30");
+  // what the launches' grids and 32-bit entries hold
+  if (vocab > (1 << 20) || width > (1 << 24) || batch > (1 << 18) || n > (1 << 28) || batch * n > (1 << 28) ||
+      batch * ((n + 15) / 16 * ((width + 255) / 256)) > (1 << 30))
+    return train_fail(SK_EUNSUPPORTED, "sizes above what the kernels take");
   if (!out || (n && (!dy || !ids || !work))) return train_fail(SK_EINVAL, "NULL argument");
   if (n && work_bytes < sketch_embed_grad_work_bytes(batch, n, width))
     return train_fail(SK_EINVAL, "work is smaller than sketch_embed_grad_work_bytes");
   TrainGuard guard(device);
   hipStream_t st = (hipStream_t)stream;
   if (dtype == SK_F32 && out_dtype == SK_F32)
-    run_eg<float>(dy, ld, ids, index, batch, n, vocab, width, scale, (float *)out, accumulate, st);
+    run_eg<float>(dy, ld, ids, index, batch, n, vocab, width, scale, (float *)out, accumulate, work, st);
   else if (dtype == SK_F32)
-    run_eg<float>(dy, ld, ids, index, batch, n, vocab, width, scale, (bf16 *)out, accumulate, st);
+    run_eg<float>(dy, ld, ids, index, batch, n, vocab, width, scale, (bf16 *)out, accumulate, work, st);
   else if (out_dtype == SK_F32)
-    run_eg<bf16>(dy, ld, ids, index, batch, n, vocab, width, scale, (float *)out, accumulate, st);
+    run_eg<bf16>(dy, ld, ids, index, batch, n, vocab, width, scale, (float *)out, accumulate, work, st);
   else
-    run_eg<bf16>(dy, ld, ids, index, batch, n, vocab, width, scale, (bf16 *)out, accumulate, st);
+    run_eg<bf16>(dy, ld, ids, index, batch, n, vocab, width, scale, (bf16 *)out, accumulate, work, st);
   return train_launched();
 }
 

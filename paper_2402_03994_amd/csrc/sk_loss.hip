@@ -7,6 +7,9 @@
 // a number c of the row times scale (onehot - p).  The exponentials are at most
 // 1, so a row whose entries are all the type's lowest value is the uniform
 // distribution; a row of -inf alone has m taken as 0 and z = 0.
+#include <algorithm>
+#include <type_traits>
+
 #include "sk_train.h"
 
 using namespace sk;
@@ -30,62 +33,157 @@ __device__ __forceinline__ int target_at(const Rows &r, int64_t t) {
   return v >= 0 && v < r.vocab ? (int)v : -1;
 }
 
-// (m, log z) of one row by a workgroup of 256
-template <typename T>
-__device__ __forceinline__ float2 row_stats(const T *x, int vocab, float scale, float *lds) {
-  float m = -INFINITY;
-  for (int j = threadIdx.x; j < vocab; j += 256) m = fmaxf(m, to_f32(x[j]));
-  m = block_all<4>(m, OpMax(), lds);
-  if (m == -INFINITY) m = 0.0f;
-  float z = 0.0f;
-  for (int j = threadIdx.x; j < vocab; j += 256) z += __builtin_amdgcn_exp2f((to_f32(x[j]) - m) * (scale * kLog2e));
-  z = block_all<4>(z, OpAdd(), lds + 4);
-  return make_float2(m, logf(z));
+// A row's numbers: the largest entry m and z = sum_j exp(scale (x_j - m)).
+struct Stats {
+  float m, z;
+};
+
+__device__ __forceinline__ float logp_of(float xt, Stats s, float scale) {
+  return s.z == 0.0f ? -INFINITY : (xt - s.m) * scale - logf(s.z);
 }
 
-__device__ __forceinline__ float logp_of(float xt, float2 s, float scale) {
-  return s.y == -INFINITY ? -INFINITY : (xt - s.x) * scale - s.y;
-}
+// The part of a row that a thread of THREADS holds: up to NV vectors of 16 bytes, THREADS vectors apart, from vector
+// v0 on, and (one tile only) one of the vocab % N entries after the last whole vector.  What is beyond the row is -inf.
+template <typename T, int THREADS, int NV>
+struct Tile {
+  static constexpr int N = Vec<T>::N;
+  static constexpr uint32_t kNone = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+  u32x4 raw[NV];
+  float rest;
 
-// row of c scale (onehot - p); zeros where c = 0 or the row is empty
-template <typename T>
-__device__ __forceinline__ void row_grad(const T *x, T *d, int vocab, float scale, float2 s, int target, float c) {
-  const bool none = c == 0.0f || s.y == -INFINITY;
-  for (int j = threadIdx.x; j < vocab; j += 256) {
-    float g = 0.0f;
-    if (!none) {
-      const float p = __builtin_amdgcn_exp2f(((to_f32(x[j]) - s.x) * scale - s.y) * kLog2e);
-      g = c * scale * ((j == target ? 1.0f : 0.0f) - p);
+  __device__ __forceinline__ void load(const T *x, int vocab, int v0, int tid) {
+    const int nv = vocab / N;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int i = v0 + k * THREADS + tid;
+      raw[k] = u32x4{kNone, kNone, kNone, kNone};
+      if (i < nv) raw[k] = Vec<T>::load(x + (int64_t)i * N);
     }
-    d[j] = from_f32<T>(g);
+    const int j = nv * N + tid;
+    rest = v0 == 0 && j < vocab ? to_f32(x[j]) : -INFINITY;
   }
+  // The vectors stay packed between two uses: without this the compiler carries the unpacked bf16 values along, twice
+  // the registers.
+  __device__ __forceinline__ void stay() {
+    if (sizeof(T) == 2) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(raw[k]));
+    }
+  }
+  __device__ __forceinline__ float largest() const {
+    float m = rest;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < N; ++i) m = fmaxf(m, Vec<T>::get(raw[k], i));
+    return m;
+  }
+  __device__ __forceinline__ float expsum(float m, float k2) const {
+    float z = __builtin_amdgcn_exp2f((rest - m) * k2);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((Vec<T>::get(raw[k], i) - m) * k2);
+      z += s;
+    }
+    return z;
+  }
+  // w exp(scale (x - m)) to the row d
+  __device__ __forceinline__ void store(T *d, int vocab, int v0, int tid, float m, float k2, float w) const {
+    const int nv = vocab / N;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int i = v0 + k * THREADS + tid;
+      if (i < nv) {
+        float f[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = w * __builtin_amdgcn_exp2f((Vec<T>::get(raw[k], e) - m) * k2);
+        Vec<T>::store(d + (int64_t)i * N, Vec<T>::pack(f));
+      }
+    }
+    const int j = nv * N + tid;
+    if (v0 == 0 && j < vocab) d[j] = from_f32<T>(w * __builtin_amdgcn_exp2f((rest - m) * k2));
+  }
+};
+
+// exp(scale (x - m)) of what a thread has summed under its own largest entry, moved to the common m
+__device__ __forceinline__ float moved(Stats s, float m, float k2) {
+  return s.z == 0.0f ? 0.0f : s.z * __builtin_amdgcn_exp2f((s.m - m) * k2);
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_logp(Rows r, float *__restrict__ logp, float2 *__restrict__ stats) {
-  __shared__ float lds[8];
-  const int64_t t = blockIdx.x;
-  const int target = target_at(r, t);
-  const T *x = (const T *)r.x + t * r.ld;
-  float2 s = make_float2(0.0f, 0.0f);
-  float lp = 0.0f;
-  if (target >= 0) {
-    s = row_stats(x, r.vocab, r.scale, lds);
-    lp = logp_of(to_f32(x[target]), s, r.scale);
+// Joins the threads' (m, z): within the waves, then the waves' through LDS (two rows of THREADS / 64 entries).
+template <int THREADS>
+__device__ __forceinline__ Stats join(Stats s, float k2, float (*lds)[16]) {
+  constexpr int W = THREADS / 64;
+  const float mw = wave_all(s.m, OpMax());
+  Stats r{mw, wave_all(moved(s, mw, k2), OpAdd())};
+  if (W > 1) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (lane == 0) {
+      lds[0][wave] = r.m;
+      lds[1][wave] = r.z;
+    }
+    __syncthreads();
+    Stats q{lane < W ? lds[0][lane] : -INFINITY, lane < W ? lds[1][lane] : 0.0f};
+    r.m = wave_all(q.m, OpMax());
+    r.z = wave_all(moved(q, r.m, k2), OpAdd());
   }
-  if (threadIdx.x == 0) {
-    logp[t] = lp;
-    if (stats) stats[t] = s;
-  }
+  if (r.m == -INFINITY) r.m = 0.0f;
+  return r;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_logp_grad(Rows r, const float2 *__restrict__ stats,
-                                                   const float *__restrict__ dlogp, void *d, int64_t ldd) {
-  const int64_t t = blockIdx.x;
-  const int target = target_at(r, t);
-  const float c = target >= 0 ? dlogp[t] : 0.0f;
-  row_grad((const T *)r.x + t * r.ld, (T *)d + t * ldd, r.vocab, r.scale, stats[t], target, c);
+// (m, z) of a tile's entries by one thread; an exponent of no entry at all is left out
+template <typename TileT>
+__device__ __forceinline__ Stats thread_stats(TileT &t, float k2) {
+  const float m = t.largest();
+  t.stay();
+  return Stats{m, t.expsum(m == -INFINITY ? 0.0f : m, k2)};
+}
+
+// Writes the row c scale (onehot - p) of a target; called with what the threads hold of the row, or (RESIDENT false)
+// with nothing: the row is read again, tile by tile.
+template <typename T, int THREADS, int NV, bool RESIDENT>
+__device__ __forceinline__ void row_grad(const T *x, T *d, int vocab, float scale, Stats s, int target, float xt, float c,
+                                         Tile<T, THREADS, NV> &t, int tid) {
+  constexpr int N = Vec<T>::N;
+  const int nv = vocab / N;
+  if (c == 0.0f || s.z == 0.0f) {
+    for (int i = tid; i < nv; i += THREADS) Vec<T>::store(d + (int64_t)i * N, u32x4{0, 0, 0, 0});
+    if (nv * N + tid < vocab) d[nv * N + tid] = from_f32<T>(0.0f);
+    return;
+  }
+  const float k2 = scale * kLog2e, cs = c * scale, w = -cs / s.z;
+  if (RESIDENT) {
+    t.stay();
+    t.store(d, vocab, 0, tid, s.m, k2, w);
+  } else {
+    for (int v0 = 0; v0 < nv || v0 == 0; v0 += THREADS * NV) {
+      t.load(x, vocab, v0, tid);
+      t.store(d, vocab, v0, tid, s.m, k2, w);
+    }
+  }
+  // the target's entry, again by the thread that has just stored it
+  const int i = target / N;
+  if (tid == (i < nv ? i % THREADS : target - nv * N))
+    d[target] = from_f32<T>(cs * (1.0f - __builtin_amdgcn_exp2f((xt - s.m) * k2) / s.z));
+}
+
+template <typename T, int THREADS, int NV, bool RESIDENT>
+__device__ __forceinline__ Stats row_stats(const T *x, int vocab, float k2, Tile<T, THREADS, NV> &t, int tid,
+                                           float (*lds)[16]) {
+  t.load(x, vocab, 0, tid);
+  Stats s = thread_stats(t, k2);
+  if (!RESIDENT) {
+    const int nv = vocab / Vec<T>::N;
+    for (int v0 = THREADS * NV; v0 < nv; v0 += THREADS * NV) {
+      t.load(x, vocab, v0, tid);
+      const Stats o = thread_stats(t, k2);
+      const float m = fmaxf(s.m, o.m);
+      s = Stats{m, moved(s, m, k2) + moved(o, m, k2)};
+    }
+  }
+  return join<THREADS>(s, k2, lds);
 }
 
 struct Policy {
@@ -107,28 +205,100 @@ __device__ __forceinline__ void policy_token(const Policy &p, int64_t t, float l
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_policy(Rows r, Policy p, float *__restrict__ logp, float *__restrict__ loss_t,
-                                                void *d, int64_t ldd) {
-  __shared__ float lds[8];
-  const int64_t t = blockIdx.x;
+// One row by THREADS threads; rows of one wave share a workgroup of four.
+template <int THREADS>
+__device__ __forceinline__ int64_t row_of_thread(int &tid) {
+  if (THREADS > 64) {
+    tid = threadIdx.x;
+    return blockIdx.x;
+  }
+  tid = threadIdx.x & 63;
+  return (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+}
+
+template <typename T, int THREADS, int NV, bool RESIDENT>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_logp(Rows r, int64_t rows, float *__restrict__ logp,
+                                                                       float2 *__restrict__ stats) {
+  __shared__ float lds[2][16];
+  int tid;
+  const int64_t t = row_of_thread<THREADS>(tid);
+  if (t >= rows) return;
+  const int target = target_at(r, t);
+  const T *x = (const T *)r.x + t * r.ld;
+  Stats s{0.0f, 0.0f};
+  float lp = 0.0f;
+  if (target >= 0) {
+    const float xt = to_f32(x[target]);
+    Tile<T, THREADS, NV> tile;
+    s = row_stats<T, THREADS, NV, RESIDENT>(x, r.vocab, r.scale * kLog2e, tile, tid, lds);
+    lp = logp_of(xt, s, r.scale);
+  }
+  if (tid == 0) {
+    logp[t] = lp;
+    if (stats) stats[t] = make_float2(s.m, s.z);
+  }
+}
+
+// d (NULL: the loss alone) may be the logits: a row's threads hold it, or have all read it, before any of them writes.
+template <typename T, int THREADS, int NV, bool RESIDENT>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_policy(Rows r, int64_t rows, Policy p,
+                                                                         float *__restrict__ logp,
+                                                                         float *__restrict__ loss_t, void *d,
+                                                                         int64_t ldd) {
+  __shared__ float lds[2][16];
+  int tid;
+  const int64_t t = row_of_thread<THREADS>(tid);
+  if (t >= rows) return;
   const int target = target_at(r, t);
   const float w = target >= 0 ? p.weights[t] : 0.0f;
   const T *x = (const T *)r.x + t * r.ld;
-  float2 s = make_float2(0.0f, 0.0f);
-  float lp = 0.0f, l = 0.0f, c = 0.0f;
+  Tile<T, THREADS, NV> tile;
+  Stats s{0.0f, 0.0f};
+  float lp = 0.0f, l = 0.0f, c = 0.0f, xt = 0.0f;
   if (w != 0.0f) {
-    s = row_stats(x, r.vocab, r.scale, lds);
-    lp = logp_of(to_f32(x[target]), s, r.scale);
+    xt = to_f32(x[target]);
+    s = row_stats<T, THREADS, NV, RESIDENT>(x, r.vocab, r.scale * kLog2e, tile, tid, lds);
+    lp = logp_of(xt, s, r.scale);
     policy_token(p, t, lp, l, c);
     c *= w;
   }
-  __syncthreads();  // x[target] is read before the row may be overwritten
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     logp[t] = lp;
     loss_t[t] = l;
   }
-  if (d) row_grad(x, (T *)d + t * ldd, r.vocab, r.scale, s, target, c);
+  if (d) row_grad<T, THREADS, NV, RESIDENT>(x, (T *)d + t * ldd, r.vocab, r.scale, s, target, xt, c, tile, tid);
+}
+
+// The gradient from known (m, z): nothing of a row has to be held, so a row is cut into pieces of 256 x NV vectors, one
+// workgroup each.
+template <typename T, int NV>
+__global__ __launch_bounds__(256) void k_logp_grad(Rows r, int pieces, const float2 *__restrict__ stats,
+                                                   const float *__restrict__ dlogp, void *dl, int64_t ldd) {
+  constexpr int N = Vec<T>::N;
+  const int64_t t = blockIdx.x / (unsigned)pieces;
+  const int piece = blockIdx.x % (unsigned)pieces, tid = threadIdx.x;
+  const int target = target_at(r, t), vocab = r.vocab, nv = vocab / N;
+  const T *x = (const T *)r.x + t * r.ld;
+  T *d = (T *)dl + t * ldd;
+  const float c = target >= 0 ? dlogp[t] : 0.0f;
+  const float2 s = stats[t];
+  const int v0 = piece * 256 * NV;
+  if (c == 0.0f || s.y == 0.0f) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (v0 + k * 256 + tid < nv) Vec<T>::store(d + (int64_t)(v0 + k * 256 + tid) * N, u32x4{0, 0, 0, 0});
+    if (v0 == 0 && nv * N + tid < vocab) d[nv * N + tid] = from_f32<T>(0.0f);
+    return;
+  }
+  const float k2 = r.scale * kLog2e, cs = c * r.scale;
+  const int i = target / N;
+  const bool mine = i < nv ? (i >= v0 && i < v0 + 256 * NV && tid == (i - v0) % 256)
+                           : (v0 == 0 && tid == target - nv * N);
+  const float xt = mine ? to_f32(x[target]) : 0.0f;  // read before the thread's stores, for the gradient in place
+  Tile<T, 256, NV> tile;
+  tile.load(x, vocab, v0, tid);
+  tile.store(d, vocab, v0, tid, s.x, k2, -cs / s.y);
+  if (mine) d[target] = from_f32<T>(cs * (1.0f - __builtin_amdgcn_exp2f((xt - s.x) * k2) / s.y));
 }
 
 // sum_t w_t l_t over the unmasked rows, in fp64 in a fixed order
@@ -232,20 +402,76 @@ Rows rows_of(const sk_logits *x) {
   return Rows{x->data, x->targets, x->ld, (int32_t)x->vocab, (int32_t)x->index, x->scale};
 }
 
-void run_logp(const sk_logits *x, float *logp, float *stats, hipStream_t st) {
-  const dim3 g((unsigned)x->rows), b(256);
-  if (x->dtype == SK_F32)
-    hipLaunchKernelGGL((k_logp<float>), g, b, 0, st, rows_of(x), logp, (float2 *)stats);
+// Threads and vectors for a row of nv whole vectors: the fewest that hold it.  Beyond 1024 x 16 vectors a row is
+// streamed.
+template <typename T, typename F>
+void with_row_shape(int64_t nv, F f) {
+  if (nv <= 64 * 4)
+    f(std::integral_constant<int, 64>(), std::integral_constant<int, 4>(), std::true_type());
+  else if (nv <= 256 * 4)
+    f(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), std::true_type());
+  else if (nv <= 256 * 8)
+    f(std::integral_constant<int, 256>(), std::integral_constant<int, 8>(), std::true_type());
+  else if (nv <= 1024 * 4)
+    f(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>(), std::true_type());
+  else if (nv <= 1024 * 8)
+    f(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>(), std::true_type());
+  else if (nv <= 1024 * 16)
+    f(std::integral_constant<int, 1024>(), std::integral_constant<int, 16>(), std::true_type());
   else
-    hipLaunchKernelGGL((k_logp<bf16>), g, b, 0, st, rows_of(x), logp, (float2 *)stats);
+    f(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>(), std::false_type());
+}
+
+template <typename T>
+void run_logp_t(const sk_logits *x, float *logp, float *stats, hipStream_t st) {
+  with_row_shape<T>(x->vocab / Vec<T>::N, [&](auto th, auto nv, auto res) {
+    constexpr int TH = decltype(th)::value;
+    const int64_t blocks = TH == 64 ? (x->rows + 3) / 4 : x->rows;
+    hipLaunchKernelGGL((k_logp<T, TH, decltype(nv)::value, decltype(res)::value>), dim3((unsigned)blocks),
+                       dim3(TH == 64 ? 256 : TH), 0, st, rows_of(x), x->rows, logp, (float2 *)stats);
+  });
+}
+
+void run_logp(const sk_logits *x, float *logp, float *stats, hipStream_t st) {
+  if (x->dtype == SK_F32)
+    run_logp_t<float>(x, logp, stats, st);
+  else
+    run_logp_t<bf16>(x, logp, stats, st);
+}
+
+template <typename T>
+void run_policy_t(const sk_logits *x, const Policy &p, float *logp, float *token_loss, void *d, int64_t ldd,
+                  hipStream_t st) {
+  with_row_shape<T>(x->vocab / Vec<T>::N, [&](auto th, auto nv, auto res) {
+    constexpr int TH = decltype(th)::value;
+    const int64_t blocks = TH == 64 ? (x->rows + 3) / 4 : x->rows;
+    hipLaunchKernelGGL((k_policy<T, TH, decltype(nv)::value, decltype(res)::value>), dim3((unsigned)blocks),
+                       dim3(TH == 64 ? 256 : TH), 0, st, rows_of(x), x->rows, p, logp, token_loss, d, ldd);
+  });
+}
+
+template <typename T>
+void run_logp_grad_t(const sk_logits *x, const float *stats, const float *dlogp, void *d, int64_t ldd,
+                     hipStream_t st) {
+  constexpr int NV = 4;
+  const int64_t pieces = std::max<int64_t>(1, (x->vocab / Vec<T>::N + 256 * NV - 1) / (256 * NV));
+  // a grid holds fewer than 2^31 workgroups
+  const int64_t most = std::max<int64_t>(1, INT32_MAX / pieces);
+  for (int64_t r0 = 0; r0 < x->rows; r0 += most) {
+    Rows r = rows_of(x);
+    r.x = (const T *)r.x + r0 * r.ld;
+    r.targets = (const char *)r.targets + r0 * (x->index == SK_I64 ? 8 : 4);
+    const int64_t n = std::min(most, x->rows - r0);
+    hipLaunchKernelGGL((k_logp_grad<T, NV>), dim3((unsigned)(n * pieces)), dim3(256), 0, st, r, (int)pieces,
+                       (const float2 *)stats + r0, dlogp + r0, (T *)d + r0 * ldd, ldd);
+  }
 }
 
 void run_logp_grad(const sk_logits *x, const float *stats, const float *dlogp, void *d, int64_t ldd, hipStream_t st) {
-  const dim3 g((unsigned)x->rows), b(256);
   if (x->dtype == SK_F32)
-    hipLaunchKernelGGL((k_logp_grad<float>), g, b, 0, st, rows_of(x), (const float2 *)stats, dlogp, d, ldd);
+    run_logp_grad_t<float>(x, stats, dlogp, d, ldd, st);
   else
-    hipLaunchKernelGGL((k_logp_grad<bf16>), g, b, 0, st, rows_of(x), (const float2 *)stats, dlogp, d, ldd);
+    run_logp_grad_t<bf16>(x, stats, dlogp, d, ldd, st);
 }
 
 }  // namespace
@@ -289,11 +515,10 @@ int sketch_policy_loss(const sk_logits *x, const float *old_logp, const float *a
   const Rows r = rows_of(x);
   const Policy p{old_logp, advantages, weights, ref_logp, 1.0f - clip_low, 1.0f + clip_high, kl_coef};
   if (x->rows) {
-    const dim3 g((unsigned)x->rows), b(256);
     if (x->dtype == SK_F32)
-      hipLaunchKernelGGL((k_policy<float>), g, b, 0, st, r, p, logp, token_loss, dlogits, ld_out);
+      run_policy_t<float>(x, p, logp, token_loss, dlogits, ld_out, st);
     else
-      hipLaunchKernelGGL((k_policy<bf16>), g, b, 0, st, r, p, logp, token_loss, dlogits, ld_out);
+      run_policy_t<bf16>(x, p, logp, token_loss, dlogits, ld_out, st);
   }
   hipLaunchKernelGGL(k_policy_total, dim3(1), dim3(1024), 0, st, r, x->rows, weights, token_loss, loss);
   return train_launched();

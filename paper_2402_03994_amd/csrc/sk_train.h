@@ -57,12 +57,6 @@ __device__ __forceinline__ bf16 from_f32<bf16>(float f) {
   return bf16{(uint16_t)bf16_bits(f)};
 }
 
-template <typename Op, typename T>
-__device__ __forceinline__ T wave_all(T v, Op op) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = op(v, __shfl_xor(v, d, 64));
-  return v;
-}
 struct OpMax {
   __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
@@ -72,6 +66,29 @@ struct OpAdd {
     return a + b;
   }
 };
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float lane_of(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+// Reduction over a wave (all 64 lanes active): rotations within the rows of 16 lanes, then the four rows' results.
+template <typename Op>
+__device__ __forceinline__ float wave_all(float v, Op op) {
+  v = op(v, dpp<0x128>(v));
+  v = op(v, dpp<0x124>(v));
+  v = op(v, dpp<0x122>(v));
+  v = op(v, dpp<0x121>(v));
+  return op(op(lane_of(v, 0), lane_of(v, 16)), op(lane_of(v, 32), lane_of(v, 48)));
+}
+template <typename Op>
+__device__ __forceinline__ double wave_all(double v, Op op) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v = op(v, __shfl_xor(v, d, 64));
+  return v;
+}
 
 // Reduction over a workgroup of W waves, in a fixed order; every thread gets the result.  `lds` holds W entries and
 // is free again after the next barrier.
@@ -86,5 +103,35 @@ __device__ __forceinline__ T block_all(T v, Op op, T *lds) {
   for (int i = 1; i < W; ++i) r = op(r, lds[i]);
   return r;
 }
+
+// 16 bytes of elements, aligned to one element only: the loads and stores of gfx950 take any alignment.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename T>
+struct Vec {
+  static constexpr int N = 16 / sizeof(T);
+  struct __attribute__((packed, aligned(sizeof(T)))) Any {
+    u32x4 v;
+  };
+  static __device__ __forceinline__ u32x4 load(const T *p) { return ((const Any *)p)->v; }
+  static __device__ __forceinline__ void store(T *p, u32x4 v) { ((Any *)p)->v = v; }
+  static __device__ __forceinline__ float get(u32x4 v, int i) {
+    if (sizeof(T) == 4) return __uint_as_float(v[i]);
+    return __uint_as_float((i & 1) ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16);
+  }
+  static __device__ __forceinline__ u32x4 pack(const float *f) {
+    u32x4 v;
+    if (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[i]);
+    } else {
+      typedef float f32x2 __attribute__((ext_vector_type(2)));
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{f[2 * i], f[2 * i + 1]}, bf16x2));
+    }
+    return v;
+  }
+};
 
 }  // namespace sk
