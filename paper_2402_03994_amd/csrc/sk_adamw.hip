@@ -3,9 +3,10 @@
 //
 // The tensors are cut into chunks of 4096 elements, one workgroup each, by a
 // table made at creation, so that one launch covers up to 128 tensors (their
-// addresses travel in the kernel's arguments).  A thread owns four consecutive
-// elements at a time and 16 lanes a 64-element block, whose largest moment is
-// found within the lanes' row.
+// addresses travel in the kernel's arguments).  A thread owns eight consecutive
+// elements at a time (16-byte loads of bf16, one Philox block for its
+// parameters and two for its moments) and eight lanes a 64-element block, whose
+// largest moment they find among themselves.
 #include <cmath>
 #include <vector>
 
@@ -40,63 +41,82 @@ struct AdamStep {
   const float *scale;
 };
 
-// four consecutive elements from e on, `live` of them valid
-template <typename T>
-__device__ __forceinline__ void load4(const T *p, int64_t e, int live, float v[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = i < live ? to_f32(p[e + i]) : 0.0f;
-}
-template <typename T>
-__device__ __forceinline__ void store4(T *p, int64_t e, int live, const float v[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < live) p[e + i] = from_f32<T>(v[i]);
-}
+constexpr int kPer = 8;  // consecutive elements of a thread: a 64-element block is 8 lanes
 
-// the largest of the 16 lanes of a row
-__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+// the kPer elements from e on, `live` of them valid (the others 0)
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int64_t e, int live, float v[kPer]) {
+  if (live == kPer) {
+    constexpr int N = Vec<T>::N;
 #pragma unroll
-  for (int d = 8; d >= 1; d >>= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)v, d, 16);
-    v = v > o ? v : o;
+    for (int k = 0; k < kPer; k += N) {
+      const u32x4 r = Vec<T>::load(p + e + k);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[k + i] = Vec<T>::get(r, i);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = i < live ? to_f32(p[e + i]) : 0.0f;
   }
-  return v;
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int64_t e, int live, const float v[kPer]) {
+  if (live == kPer) {
+    constexpr int N = Vec<T>::N;
+#pragma unroll
+    for (int k = 0; k < kPer; k += N) Vec<T>::store(p + e + k, Vec<T>::pack(v + k));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i < live) p[e + i] = from_f32<T>(v[i]);
+  }
 }
 
-// Codes of four values (of a 64-element block spread over 16 lanes) and the block's exponent byte.  TOP: the largest
+// the largest among 8 neighbouring lanes: neighbours, pairs of a quad, the two quads
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+  return v > o ? v : o;
+}
+__device__ __forceinline__ uint32_t block_max(uint32_t v) {
+  v = max_dpp<0xB1>(v);   // quad_perm [1, 0, 3, 2]
+  v = max_dpp<0x4E>(v);   // quad_perm [2, 3, 0, 1]
+  return max_dpp<0x141>(v);  // row_half_mirror
+}
+
+// Codes of eight values (of a 64-element block spread over 8 lanes) and the block's exponent byte.  TOP: the largest
 // exponent field, 15 with a sign bit (m), 31 without (v).
 template <int TOP>
-__device__ __forceinline__ uint32_t encode4(const float x[4], const uint32_t dither[4], uint32_t &eb) {
+__device__ __forceinline__ uint2 encode8(const float x[kPer], const uint32_t dither[kPer], uint32_t &eb) {
   uint32_t big = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < kPer; ++i) {
     const uint32_t a = __float_as_uint(x[i]) & 0x7FFFFFFFu;
     big = big > a ? big : a;
   }
-  big = row_max(big);
-  if (big >= 0x7F800000u) {  // an infinity or NaN: the block stands for NaNs
-    eb = 255;
-    return 0;
-  }
+  big = block_max(big);
+  // an infinity or NaN: the block stands for NaNs; so it does where 2^E with E = 128 would be needed
   eb = (big + 0x0FFFFFu) >> 23;
-  // a carry to the infinities' exponent (values above 1.875 * 2^127) is left to 255 as well
-  if (eb == 255) return 0;
-  uint32_t out = 0;
+  if (eb >= 255) {
+    eb = 255;
+    return make_uint2(0, 0);
+  }
+  uint32_t out[2] = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < kPer; ++i) {
     const uint32_t y = __float_as_uint(ldexpf(fabsf(x[i]), TOP - (int)eb));
     uint32_t c = (y + ((dither[i] << 4) | 8u)) >> 20;
     if (TOP == 15) c |= (__float_as_uint(x[i]) >> 24) & 0x80u;
-    out |= c << (8 * i);
+    out[i >> 2] |= c << (8 * (i & 3));
   }
-  return out;
+  return make_uint2(out[0], out[1]);
 }
 
 template <int TOP>
-__device__ __forceinline__ void decode4(uint32_t codes, uint32_t eb, float x[4]) {
+__device__ __forceinline__ void decode8(uint2 codes, uint32_t eb, float x[kPer]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t c = (codes >> (8 * i)) & 0xFFu;
+  for (int i = 0; i < kPer; ++i) {
+    const uint32_t c = ((i < 4 ? codes.x : codes.y) >> (8 * (i & 3))) & 0xFFu;
     float y = ldexpf(__uint_as_float((TOP == 15 ? c & 0x7Fu : c) << 20), (int)eb - TOP);
     if (TOP == 15) y = __uint_as_float(__float_as_uint(y) | ((c & 0x80u) << 24));
     x[i] = eb == 255 ? NAN : y;
@@ -118,26 +138,27 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
   const G *g = (const G *)ptrs.g[slot];
   float *master = MASTER ? ptrs.master[slot] : nullptr;
   const float shrink = s.lr_wd * t.decay;
-  for (int it = 0; it < kAdamChunk / 1024; ++it) {
-    const int64_t e = ck.e0 + it * 1024 + 4 * threadIdx.x;
-    if (e >= ((t.n + 63) & ~63ll)) break;  // whole blocks, so whole rows of lanes
-    const int live = t.n - e < 4 ? (t.n - e > 0 ? (int)(t.n - e) : 0) : 4;
-    float gv[4], pv[4], m[4], v[4];
-    load4(g, e, live, gv);
+#pragma unroll
+  for (int it = 0; it < kAdamChunk / (256 * kPer); ++it) {
+    const int64_t e = ck.e0 + it * 256 * kPer + kPer * threadIdx.x;
+    if (e >= ((t.n + 63) & ~63ll)) break;  // whole blocks, so whole groups of 8 lanes
+    const int live = t.n - e < kPer ? (t.n - e > 0 ? (int)(t.n - e) : 0) : kPer;
+    float gv[kPer], pv[kPer], m[kPer], v[kPer];
+    load8(g, e, live, gv);
     if (MASTER)
-      load4(master, e, live, pv);
+      load8((const float *)master, e, live, pv);
     else
-      load4((const P *)p, e, live, pv);
+      load8((const P *)p, e, live, pv);
     const int64_t at = t.at + e;
     if (STATE == SK_ADAMW_F32) {
-      *(float4 *)m = *(const float4 *)((const float *)mp + at);
-      *(float4 *)v = *(const float4 *)((const float *)vp + at);
+      load8((const float *)mp, at, kPer, m);
+      load8((const float *)vp, at, kPer, v);
     } else {
-      decode4<15>(*(const uint32_t *)((const uint8_t *)mp + at), mexp[at >> 6], m);
-      decode4<31>(*(const uint32_t *)((const uint8_t *)vp + at), vexp[at >> 6], v);
+      decode8<15>(*(const uint2 *)((const uint8_t *)mp + at), mexp[at >> 6], m);
+      decode8<31>(*(const uint2 *)((const uint8_t *)vp + at), vexp[at >> 6], v);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kPer; ++i) {
       const float gi = gv[i] * scale;
       const float ma = m[i] * s.b1, mb = gi * s.c1;
       m[i] = ma + mb;
@@ -148,39 +169,37 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
       const float change = s.rate * (m[i] / (sqrtf(v[i]) * s.root + s.eps));
       pv[i] -= shrink * pv[i] + change;
     }
+    const uint64_t step = (uint64_t)s.step << 32;
     if (STATE == SK_ADAMW_F32) {
-      *(float4 *)((float *)mp + at) = *(const float4 *)m;
-      *(float4 *)((float *)vp + at) = *(const float4 *)v;
+      store8((float *)mp, at, kPer, m);
+      store8((float *)vp, at, kPer, v);
     } else {
-      const W4 w = philox((uint64_t)(uint32_t)(e >> 2) | ((uint64_t)s.step << 32), (uint32_t)ck.tensor, ST_ADAMW,
-                          s.key);
-      uint32_t dm[4], dv[4], eb;
+      uint32_t dm[kPer], dv[kPer], eb;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        dm[i] = w.w[i] >> 16;
-        dv[i] = w.w[i] & 0xFFFFu;
+      for (int q = 0; q < 2; ++q) {
+        const W4 w = philox((uint64_t)((uint32_t)(e >> 2) + q) | step, (uint32_t)ck.tensor, ST_ADAMW, s.key);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          dm[4 * q + i] = w.w[i] >> 16;
+          dv[4 * q + i] = w.w[i] & 0xFFFFu;
+        }
       }
-      const uint32_t cm = encode4<15>(m, dm, eb);
-      *(uint32_t *)((uint8_t *)mp + at) = cm;
-      if ((threadIdx.x & 15) == 0) mexp[at >> 6] = (uint8_t)eb;
-      const uint32_t cv = encode4<31>(v, dv, eb);
-      *(uint32_t *)((uint8_t *)vp + at) = cv;
-      if ((threadIdx.x & 15) == 0) vexp[at >> 6] = (uint8_t)eb;
+      *(uint2 *)((uint8_t *)mp + at) = encode8<15>(m, dm, eb);
+      if ((threadIdx.x & 7) == 0) mexp[at >> 6] = (uint8_t)eb;
+      *(uint2 *)((uint8_t *)vp + at) = encode8<31>(v, dv, eb);
+      if ((threadIdx.x & 7) == 0) vexp[at >> 6] = (uint8_t)eb;
     }
-    if (MASTER) store4(master, e, live, pv);
+    if (MASTER) store8(master, e, live, pv);
     if (sizeof(P) == 2 && !MASTER) {
-      const W4 w = philox((uint64_t)(uint32_t)(e >> 3) | ((uint64_t)s.step << 32), (uint32_t)ck.tensor, ST_ADAMW_P,
-                          s.key);
-      const bool hi = (e >> 2) & 1;
+      const W4 w = philox((uint64_t)(uint32_t)(e >> 3) | step, (uint32_t)ck.tensor, ST_ADAMW_P, s.key);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t word = i < 2 ? (hi ? w.w[2] : w.w[0]) : (hi ? w.w[3] : w.w[1]);
-        const uint32_t u = (i & 1) ? word >> 16 : word & 0xFFFFu;
+      for (int i = 0; i < kPer; ++i) {
+        const uint32_t u = (i & 1) ? w.w[i >> 1] >> 16 : w.w[i >> 1] & 0xFFFFu;
         const uint32_t b = __float_as_uint(pv[i]);
         if ((b & 0x7FFFFFFFu) < 0x7F800000u) pv[i] = __uint_as_float((b + u) & 0xFFFF0000u);
       }
     }
-    store4(p, e, live, pv);
+    store8(p, e, live, pv);
   }
 }
 
@@ -193,13 +212,14 @@ __global__ __launch_bounds__(256) void k_adamw_norm(const AdamTensor *__restrict
   const AdamTensor t = tensors[ck.tensor];
   const G *g = (const G *)ptrs.g[ck.tensor - first];
   double s = 0.0;
-  for (int it = 0; it < kAdamChunk / 1024; ++it) {
-    const int64_t e = ck.e0 + it * 1024 + 4 * threadIdx.x;
-    const int live = t.n - e < 4 ? (t.n - e > 0 ? (int)(t.n - e) : 0) : 4;
-    float gv[4];
-    load4(g, e, live, gv);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s += (double)gv[i] * gv[i];
+  for (int it = 0; it < kAdamChunk / (256 * kPer); ++it) {
+    const int64_t e = ck.e0 + it * 256 * kPer + kPer * threadIdx.x;
+    const int live = t.n - e < kPer ? (t.n - e > 0 ? (int)(t.n - e) : 0) : kPer;
+    float gv[kPer];
+    load8(g, e, live, gv);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) s += (double)gv[i] * gv[i];
   }
   s = block_all<4>(s, OpAdd(), lds);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -221,18 +241,17 @@ __global__ __launch_bounds__(1024) void k_adamw_scale(const double *__restrict__
   }
 }
 
-__global__ __launch_bounds__(256) void k_adamw_moments(int64_t groups, const uint32_t *__restrict__ m,
-                                                       const uint8_t *__restrict__ mexp,
-                                                       const uint32_t *__restrict__ v,
-                                                       const uint8_t *__restrict__ vexp, float4 *__restrict__ mo,
-                                                       float4 *__restrict__ vo) {
+__global__ __launch_bounds__(256) void k_adamw_moments(int64_t groups, const uint2 *__restrict__ m,
+                                                       const uint8_t *__restrict__ mexp, const uint2 *__restrict__ v,
+                                                       const uint8_t *__restrict__ vexp, float *__restrict__ mo,
+                                                       float *__restrict__ vo) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= groups) return;
-  float x[4];
-  decode4<15>(m[i], mexp[i >> 4], x);
-  mo[i] = make_float4(x[0], x[1], x[2], x[3]);
-  decode4<31>(v[i], vexp[i >> 4], x);
-  vo[i] = make_float4(x[0], x[1], x[2], x[3]);
+  float x[kPer], y[kPer];
+  decode8<15>(m[i], mexp[i >> 3], x);
+  decode8<31>(v[i], vexp[i >> 3], y);
+  store8(mo, i * kPer, kPer, x);
+  store8(vo, i * kPer, kPer, y);
 }
 
 }  // namespace
@@ -409,9 +428,9 @@ int sketch_adamw_moments(sk_adamw *h, const uint8_t *m, const uint8_t *m_exp, co
   if (!h || !m || !m_exp || !v || !v_exp || !m_out || !v_out) return train_fail(SK_EINVAL, "NULL argument");
   if (h->state != SK_ADAMW_8BIT) return train_fail(SK_EINVAL, "the moments of this handle are fp32");
   TrainGuard guard(h->device);
-  const int64_t groups = h->elems / 4;
+  const int64_t groups = h->elems / kPer;
   hipLaunchKernelGGL(k_adamw_moments, dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, (hipStream_t)stream, groups,
-                     (const uint32_t *)m, m_exp, (const uint32_t *)v, v_exp, (float4 *)m_out, (float4 *)v_out);
+                     (const uint2 *)m, m_exp, (const uint2 *)v, v_exp, m_out, v_out);
   return train_launched();
 }
 
