@@ -42,8 +42,24 @@ __device__ __forceinline__ float logp_of(float xt, Stats s, float scale) {
   return s.z == 0.0f ? -INFINITY : (xt - s.m) * scale - logf(s.z);
 }
 
-// The part of a row that a thread of THREADS holds: up to NV vectors of 16 bytes, THREADS vectors apart, from vector
-// v0 on, and (one tile only) one of the vocab % N entries after the last whole vector.  What is beyond the row is -inf.
+// A row cut at 16-byte boundaries: `head` entries before the first one, nv vectors, `rem` entries after the last.
+// Odd vocabularies put rows of bf16 at any even address, where 16-byte accesses across the boundaries cost a fifth of
+// the bandwidth (50257 columns: 5.2 TB/s read as they lie, 6.3 TB/s cut).
+struct Cut {
+  int head, nv, rem;
+};
+template <typename T>
+__device__ __forceinline__ Cut cut_of(const T *x, int vocab) {
+  constexpr int N = Vec<T>::N;
+  int head = (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T);
+  head = head < vocab ? head : vocab;
+  const int nv = (vocab - head) / N;
+  return Cut{head, nv, vocab - head - nv * N};
+}
+
+// The part of a row that a thread of THREADS holds: up to NV vectors, THREADS vectors apart, from vector v0 on, and
+// (with the first tile) one of the entries outside the vectors: thread i < 8 the head's, thread 8 + i the last ones.
+// What is beyond the row is -inf.
 template <typename T, int THREADS, int NV>
 struct Tile {
   static constexpr int N = Vec<T>::N;
@@ -51,16 +67,28 @@ struct Tile {
   u32x4 raw[NV];
   float rest;
 
-  __device__ __forceinline__ void load(const T *x, int vocab, int v0, int tid) {
-    const int nv = vocab / N;
+  // where the thread's single entry lies, -1 if it has none
+  static __device__ __forceinline__ int single(Cut q, int v0, int tid) {
+    if (v0 == 0 && tid < q.head) return tid;
+    if (v0 == 0 && tid >= 8 && tid < 8 + q.rem) return q.head + q.nv * N + tid - 8;
+    return -1;
+  }
+  // the thread that holds entry j, within the tiles of v0
+  static __device__ __forceinline__ int owner(Cut q, int j) {
+    if (j < q.head) return j;
+    const int i = (j - q.head) / N;
+    return i < q.nv ? i % THREADS : 8 + j - q.head - q.nv * N;
+  }
+  __device__ __forceinline__ void load(const T *x, Cut q, int v0, int tid) {
+    const T *a = x + q.head;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int i = v0 + k * THREADS + tid;
       raw[k] = u32x4{kNone, kNone, kNone, kNone};
-      if (i < nv) raw[k] = Vec<T>::load(x + (int64_t)i * N);
+      if (i < q.nv) raw[k] = Vec<T>::load(a + (int64_t)i * N);
     }
-    const int j = nv * N + tid;
-    rest = v0 == 0 && j < vocab ? to_f32(x[j]) : -INFINITY;
+    const int j = single(q, v0, tid);
+    rest = j >= 0 ? to_f32(x[j]) : -INFINITY;
   }
   // The vectors stay packed between two uses: without this the compiler carries the unpacked bf16 values along, twice
   // the registers.
@@ -90,22 +118,32 @@ struct Tile {
     return z;
   }
   // w exp(scale (x - m)) to the row d
-  __device__ __forceinline__ void store(T *d, int vocab, int v0, int tid, float m, float k2, float w) const {
-    const int nv = vocab / N;
+  __device__ __forceinline__ void store(T *d, Cut q, int v0, int tid, float m, float k2, float w) const {
+    T *a = d + q.head;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int i = v0 + k * THREADS + tid;
-      if (i < nv) {
+      if (i < q.nv) {
         float f[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) f[e] = w * __builtin_amdgcn_exp2f((Vec<T>::get(raw[k], e) - m) * k2);
-        Vec<T>::store(d + (int64_t)i * N, Vec<T>::pack(f));
+        Vec<T>::store(a + (int64_t)i * N, Vec<T>::pack(f));
       }
     }
-    const int j = nv * N + tid;
-    if (v0 == 0 && j < vocab) d[j] = from_f32<T>(w * __builtin_amdgcn_exp2f((rest - m) * k2));
+    const int j = single(q, v0, tid);
+    if (j >= 0) d[j] = from_f32<T>(w * __builtin_amdgcn_exp2f((rest - m) * k2));
   }
 };
+
+// zeros to vectors v0 + tid, v0 + tid + THREADS, .. below v1 of a row and (with its first ones) to what lies outside them
+template <typename T, int THREADS>
+__device__ __forceinline__ void row_zero(T *d, int vocab, int v0, int v1, int tid) {
+  const Cut q = cut_of(d, vocab);
+  v1 = v1 < q.nv ? v1 : q.nv;
+  for (int i = v0 + tid; i < v1; i += THREADS) Vec<T>::store(d + q.head + (int64_t)i * Vec<T>::N, u32x4{0, 0, 0, 0});
+  const int j = Tile<T, THREADS, 1>::single(q, v0, tid);
+  if (j >= 0) d[j] = from_f32<T>(0.0f);
+}
 
 // exp(scale (x - m)) of what a thread has summed under its own largest entry, moved to the common m
 __device__ __forceinline__ float moved(Stats s, float m, float k2) {
@@ -146,38 +184,35 @@ __device__ __forceinline__ Stats thread_stats(TileT &t, float k2) {
 template <typename T, int THREADS, int NV, bool RESIDENT>
 __device__ __forceinline__ void row_grad(const T *x, T *d, int vocab, float scale, Stats s, int target, float xt, float c,
                                          Tile<T, THREADS, NV> &t, int tid) {
-  constexpr int N = Vec<T>::N;
-  const int nv = vocab / N;
   if (c == 0.0f || s.z == 0.0f) {
-    for (int i = tid; i < nv; i += THREADS) Vec<T>::store(d + (int64_t)i * N, u32x4{0, 0, 0, 0});
-    if (nv * N + tid < vocab) d[nv * N + tid] = from_f32<T>(0.0f);
+    row_zero<T, THREADS>(d, vocab, 0, INT32_MAX, tid);
     return;
   }
+  const Cut q = cut_of(x, vocab);
   const float k2 = scale * kLog2e, cs = c * scale, w = -cs / s.z;
   if (RESIDENT) {
     t.stay();
-    t.store(d, vocab, 0, tid, s.m, k2, w);
+    t.store(d, q, 0, tid, s.m, k2, w);
   } else {
-    for (int v0 = 0; v0 < nv || v0 == 0; v0 += THREADS * NV) {
-      t.load(x, vocab, v0, tid);
-      t.store(d, vocab, v0, tid, s.m, k2, w);
+    for (int v0 = 0; v0 < q.nv || v0 == 0; v0 += THREADS * NV) {
+      t.load(x, q, v0, tid);
+      t.store(d, q, v0, tid, s.m, k2, w);
     }
   }
   // the target's entry, again by the thread that has just stored it
-  const int i = target / N;
-  if (tid == (i < nv ? i % THREADS : target - nv * N))
+  if (tid == Tile<T, THREADS, NV>::owner(q, target))
     d[target] = from_f32<T>(cs * (1.0f - __builtin_amdgcn_exp2f((xt - s.m) * k2) / s.z));
 }
 
 template <typename T, int THREADS, int NV, bool RESIDENT>
 __device__ __forceinline__ Stats row_stats(const T *x, int vocab, float k2, Tile<T, THREADS, NV> &t, int tid,
                                            float (*lds)[16]) {
-  t.load(x, vocab, 0, tid);
+  const Cut q = cut_of(x, vocab);
+  t.load(x, q, 0, tid);
   Stats s = thread_stats(t, k2);
   if (!RESIDENT) {
-    const int nv = vocab / Vec<T>::N;
-    for (int v0 = THREADS * NV; v0 < nv; v0 += THREADS * NV) {
-      t.load(x, vocab, v0, tid);
+    for (int v0 = THREADS * NV; v0 < q.nv; v0 += THREADS * NV) {
+      t.load(x, q, v0, tid);
       const Stats o = thread_stats(t, k2);
       const float m = fmaxf(s.m, o.m);
       s = Stats{m, moved(s, m, k2) + moved(o, m, k2)};
@@ -270,34 +305,31 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_policy(Rows r
 }
 
 // The gradient from known (m, z): nothing of a row has to be held, so a row is cut into pieces of 256 x NV vectors, one
-// workgroup each.
+// workgroup each.  The last rows come first: they are what the kernel that found (m, z) has left in the cache.
 template <typename T, int NV>
-__global__ __launch_bounds__(256) void k_logp_grad(Rows r, int pieces, const float2 *__restrict__ stats,
+__global__ __launch_bounds__(256) void k_logp_grad(Rows r, int64_t rows, int pieces, const float2 *__restrict__ stats,
                                                    const float *__restrict__ dlogp, void *dl, int64_t ldd) {
-  constexpr int N = Vec<T>::N;
-  const int64_t t = blockIdx.x / (unsigned)pieces;
-  const int piece = blockIdx.x % (unsigned)pieces, tid = threadIdx.x;
-  const int target = target_at(r, t), vocab = r.vocab, nv = vocab / N;
+  typedef Tile<T, 256, NV> TileT;
+  const int64_t t = rows - 1 - blockIdx.x / (unsigned)pieces;
+  const int v0 = (int)(blockIdx.x % (unsigned)pieces) * 256 * NV, tid = threadIdx.x;
+  const int target = target_at(r, t), vocab = r.vocab;
   const T *x = (const T *)r.x + t * r.ld;
   T *d = (T *)dl + t * ldd;
   const float c = target >= 0 ? dlogp[t] : 0.0f;
   const float2 s = stats[t];
-  const int v0 = piece * 256 * NV;
   if (c == 0.0f || s.y == 0.0f) {
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-      if (v0 + k * 256 + tid < nv) Vec<T>::store(d + (int64_t)(v0 + k * 256 + tid) * N, u32x4{0, 0, 0, 0});
-    if (v0 == 0 && nv * N + tid < vocab) d[nv * N + tid] = from_f32<T>(0.0f);
+    row_zero<T, 256>(d, vocab, v0, v0 + 256 * NV, tid);
     return;
   }
   const float k2 = r.scale * kLog2e, cs = c * r.scale;
-  const int i = target / N;
-  const bool mine = i < nv ? (i >= v0 && i < v0 + 256 * NV && tid == (i - v0) % 256)
-                           : (v0 == 0 && tid == target - nv * N);
+  const Cut q = cut_of(x, vocab);
+  const int i = (target - q.head) / TileT::N;  // the target's vector; outside them the first piece's
+  const bool here = target >= q.head && i < q.nv ? i >= v0 && i < v0 + 256 * NV : v0 == 0;
+  const bool mine = here && tid == TileT::owner(q, target);
   const float xt = mine ? to_f32(x[target]) : 0.0f;  // read before the thread's stores, for the gradient in place
-  Tile<T, 256, NV> tile;
-  tile.load(x, vocab, v0, tid);
-  tile.store(d, vocab, v0, tid, s.x, k2, -cs / s.y);
+  TileT tile;
+  tile.load(x, q, v0, tid);
+  tile.store(d, q, v0, tid, s.x, k2, -cs / s.y);
   if (mine) d[target] = from_f32<T>(cs * (1.0f - __builtin_amdgcn_exp2f((xt - s.x) * k2) / s.y));
 }
 
@@ -462,7 +494,7 @@ void run_logp_grad_t(const sk_logits *x, const float *stats, const float *dlogp,
     r.x = (const T *)r.x + r0 * r.ld;
     r.targets = (const char *)r.targets + r0 * (x->index == SK_I64 ? 8 : 4);
     const int64_t n = std::min(most, x->rows - r0);
-    hipLaunchKernelGGL((k_logp_grad<T, NV>), dim3((unsigned)(n * pieces)), dim3(256), 0, st, r, (int)pieces,
+    hipLaunchKernelGGL((k_logp_grad<T, NV>), dim3((unsigned)(n * pieces)), dim3(256), 0, st, r, n, (int)pieces,
                        (const float2 *)stats + r0, dlogp + r0, (T *)d + r0 * ldd, ldd);
   }
 }

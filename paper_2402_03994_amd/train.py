@@ -141,9 +141,14 @@ def _logits(logits: torch.Tensor, targets: torch.Tensor, scale: float) -> _lib.L
 
 
 def _dlogits(logits: torch.Tensor, out: Optional[torch.Tensor]):
-    """The gradient's tensor (contiguous if it is new) and its row stride."""
+    """The gradient's tensor and its row stride.  A new one keeps the row stride of logits that are padded by up to 64
+    columns, so that rows of both start at the same place of 16 bytes."""
     if out is None:
-        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device), logits.shape[1]
+        n, vocab = logits.shape
+        ld = logits.stride(0) if n > 1 else vocab
+        if vocab < ld <= vocab + 64:
+            return torch.empty((n, ld), dtype=logits.dtype, device=logits.device)[:, :vocab], ld
+        return torch.empty((n, vocab), dtype=logits.dtype, device=logits.device), vocab
     if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device:
         raise ValueError("out must have the shape, type and device of the logits")
     return out, _rows(out, "out")
