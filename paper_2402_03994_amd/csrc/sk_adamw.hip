@@ -85,7 +85,7 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v) {
 }
 
 // Codes of eight values (of a 64-element block spread over 8 lanes) and the block's exponent byte.  TOP: the largest
-// exponent field, 15 with a sign bit (m), 31 without (v).
+// exponent field, 15 with a sign bit (m), 31 without (v); dither: what is added below the codes.
 template <int TOP>
 __device__ __forceinline__ uint2 encode8(const float x[kPer], const uint32_t dither[kPer], uint32_t &eb) {
   uint32_t big = 0;
@@ -101,26 +101,63 @@ __device__ __forceinline__ uint2 encode8(const float x[kPer], const uint32_t dit
     eb = 255;
     return make_uint2(0, 0);
   }
-  uint32_t out[2] = {0, 0};
+  uint32_t top[kPer];  // the codes in the highest byte
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const uint32_t y = __float_as_uint(ldexpf(fabsf(x[i]), TOP - (int)eb));
-    uint32_t c = (y + ((dither[i] << 4) | 8u)) >> 20;
-    if (TOP == 15) c |= (__float_as_uint(x[i]) >> 24) & 0x80u;
-    out[i >> 2] |= c << (8 * (i & 3));
+    top[i] = (y + dither[i]) << 4;
+    if (TOP == 15) top[i] = (top[i] & 0x7FFFFFFFu) | (__float_as_uint(x[i]) & 0x80000000u);
+  }
+  uint32_t out[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {  // v_perm_b32: bytes 0 .. 3 of the second operand, 4 .. 7 of the first
+    const uint32_t lo = __builtin_amdgcn_perm(top[4 * i + 1], top[4 * i], 0x0C0C0703u);
+    const uint32_t hi = __builtin_amdgcn_perm(top[4 * i + 3], top[4 * i + 2], 0x07030C0Cu);
+    out[i] = lo | hi;
   }
   return make_uint2(out[0], out[1]);
 }
 
+// What eight codes stand for.  The block's 2^E comes in two factors (2^(127 - TOP) times a code is exact, and E may
+// reach beyond either side of what one factor holds); the second is NaN for exponent byte 255.
 template <int TOP>
 __device__ __forceinline__ void decode8(uint2 codes, uint32_t eb, float x[kPer]) {
+  const float unit = __uint_as_float((254u - TOP) << 23);
+  const float block = __uint_as_float(eb == 255 ? 0x7FC00000u : eb == 0 ? 0x00400000u : eb << 23);
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const uint32_t c = ((i < 4 ? codes.x : codes.y) >> (8 * (i & 3))) & 0xFFu;
-    float y = ldexpf(__uint_as_float((TOP == 15 ? c & 0x7Fu : c) << 20), (int)eb - TOP);
-    if (TOP == 15) y = __uint_as_float(__float_as_uint(y) | ((c & 0x80u) << 24));
-    x[i] = eb == 255 ? NAN : y;
+    const uint32_t w = i < 4 ? codes.x : codes.y;
+    const int at = 8 * (i & 3);
+    uint32_t y;
+    if (TOP == 15)  // sign, then seven bits from bit 20
+      y = (uint32_t)((int32_t)(w << (24 - at)) >> 4) & 0x87F00000u;
+    else
+      y = (at <= 20 ? w << (20 - at) : w >> (at - 20)) & 0x0FF00000u;
+    x[i] = __uint_as_float(y) * unit * block;
   }
+}
+
+// A Philox4x32-10 block as philox() gives it, its exclusive-ors of three in one instruction.
+__device__ __forceinline__ W4 philox_adam(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, Key key) {
+  uint32_t k0 = key.k0, k1 = key.k1;
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+    c0 = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c1, k0, 0x96);
+    c2 = __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c3, k1, 0x96);
+    c1 = (uint32_t)p1;
+    c3 = (uint32_t)p0;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return W4{{c0, c1, c2, c3}};
+}
+
+// m / (sqrt(v) root + eps).  The hardware's square root and reciprocal (one unit in the last place each, nothing for
+// inputs below 2^-126) serve where eps is large beside 2^-63; an eps as small takes the correctly rounded ones.
+__device__ __forceinline__ float ratio(float m, float v, float root, float eps, bool tiny_eps) {
+  if (tiny_eps) return m / (sqrtf(v) * root + eps);
+  return m * __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_sqrtf(v), root, eps));
 }
 
 template <typename P, typename G, int STATE, bool MASTER>
@@ -165,11 +202,12 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
       const float gg = gi * gi;
       const float va = v[i] * s.b2, vb = gg * s.c2;
       v[i] = va + vb;
-      // the change is formed first, so that the parameter is rounded once
-      const float change = s.rate * (m[i] / (sqrtf(v[i]) * s.root + s.eps));
-      pv[i] -= shrink * pv[i] + change;
     }
-    const uint64_t step = (uint64_t)s.step << 32;
+    // the change is formed first, so that the parameter is rounded once
+    const bool tiny_eps = s.eps < 1e-12f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      pv[i] -= __builtin_fmaf(s.rate, ratio(m[i], v[i], s.root, s.eps, tiny_eps), shrink * pv[i]);
     if (STATE == SK_ADAMW_F32) {
       store8((float *)mp, at, kPer, m);
       store8((float *)vp, at, kPer, v);
@@ -177,11 +215,11 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
       uint32_t dm[kPer], dv[kPer], eb;
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const W4 w = philox((uint64_t)((uint32_t)(e >> 2) + q) | step, (uint32_t)ck.tensor, ST_ADAMW, s.key);
+        const W4 w = philox_adam((uint32_t)(e >> 2) + q, s.step, (uint32_t)ck.tensor, ST_ADAMW, s.key);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          dm[4 * q + i] = w.w[i] >> 16;
-          dv[4 * q + i] = w.w[i] & 0xFFFFu;
+        for (int i = 0; i < 4; ++i) {  // 16 u + 8
+          dm[4 * q + i] = ((w.w[i] >> 12) & 0xFFFF0u) | 8u;
+          dv[4 * q + i] = ((w.w[i] << 4) & 0xFFFF0u) | 8u;
         }
       }
       *(uint2 *)((uint8_t *)mp + at) = encode8<15>(m, dm, eb);
@@ -191,12 +229,12 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
     }
     if (MASTER) store8(master, e, live, pv);
     if (sizeof(P) == 2 && !MASTER) {
-      const W4 w = philox((uint64_t)(uint32_t)(e >> 3) | step, (uint32_t)ck.tensor, ST_ADAMW_P, s.key);
+      // an infinity has nothing below its 16 bits, and NaNs of arithmetic are quiet: neither is changed by u
+      const W4 w = philox_adam((uint32_t)(e >> 3), s.step, (uint32_t)ck.tensor, ST_ADAMW_P, s.key);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const uint32_t u = (i & 1) ? w.w[i >> 1] >> 16 : w.w[i >> 1] & 0xFFFFu;
-        const uint32_t b = __float_as_uint(pv[i]);
-        if ((b & 0x7FFFFFFFu) < 0x7F800000u) pv[i] = __uint_as_float((b + u) & 0xFFFF0000u);
+        pv[i] = __uint_as_float((__float_as_uint(pv[i]) + u) & 0xFFFF0000u);
       }
     }
     store8(p, e, live, pv);
@@ -277,23 +315,22 @@ void free_adamw(sk_adamw *h) {
   delete h;
 }
 
+// MASTER goes with bf16 parameters alone
 template <typename P, typename G>
 void launch_adamw(int state, bool master, dim3 grid, hipStream_t st, const AdamTensor *t, const AdamChunk *c, int first,
                   const AdamPtrs &ptrs, const AdamStep &s, const sk_adamw_step *a) {
 #define SK_ADAMW(STATE, MASTER)                                                                                 \
   hipLaunchKernelGGL((k_adamw<P, G, STATE, MASTER>), grid, dim3(256), 0, st, t, c, first, ptrs, s, a->m, a->v, \
                      a->m_exp, a->v_exp)
-  if (state == SK_ADAMW_F32) {
-    if (master)
-      SK_ADAMW(SK_ADAMW_F32, true);
-    else
-      SK_ADAMW(SK_ADAMW_F32, false);
-  } else {
-    if (master)
-      SK_ADAMW(SK_ADAMW_8BIT, true);
-    else
-      SK_ADAMW(SK_ADAMW_8BIT, false);
+  if constexpr (sizeof(P) == 2) {
+    if (master && state == SK_ADAMW_F32) SK_ADAMW(SK_ADAMW_F32, true);
+    if (master && state != SK_ADAMW_F32) SK_ADAMW(SK_ADAMW_8BIT, true);
+    if (master) return;
   }
+  if (state == SK_ADAMW_F32)
+    SK_ADAMW(SK_ADAMW_F32, false);
+  else
+    SK_ADAMW(SK_ADAMW_8BIT, false);
 #undef SK_ADAMW
 }
 
