@@ -253,7 +253,8 @@ __device__ __forceinline__ int64_t row_of_thread(int &tid) {
 
 template <typename T, int THREADS, int NV, bool RESIDENT>
 __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_logp(Rows r, int64_t rows, float *__restrict__ logp,
-                                                                       float2 *__restrict__ stats) {
+                                                                       float2 *__restrict__ stats,
+                                                                       float *__restrict__ rowc) {
   __shared__ float lds[2][16];
   int tid;
   const int64_t t = row_of_thread<THREADS>(tid);
@@ -271,6 +272,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_logp(Rows r, 
   if (tid == 0) {
     logp[t] = lp;
     if (stats) stats[t] = make_float2(s.m, s.z);
+    if (rowc) rowc[t] = 0.0f;  // until a pair has its factors: rows outside all texts keep it
   }
 }
 
@@ -304,12 +306,28 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_policy(Rows r
   if (d) row_grad<T, THREADS, NV, RESIDENT>(x, (T *)d + t * ldd, r.vocab, r.scale, s, target, xt, c, tile, tid);
 }
 
+// the mean of the pairs' losses, by 256 threads
+__device__ __forceinline__ void pair_total(const float *pair_loss, int64_t pairs, float *loss, double *lds) {
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < pairs; i += 256) s += pair_loss[i];
+  s = block_all<4>(s, OpAdd(), lds);
+  if (threadIdx.x == 0) *loss = (float)(s / (double)pairs);
+}
+
 // The gradient from known (m, z): nothing of a row has to be held, so a row is cut into pieces of 256 x NV vectors, one
 // workgroup each.  The last rows come first: they are what the kernel that found (m, z) has left in the cache.
+// One workgroup more (the preference loss) adds up the pairs' losses meanwhile.
 template <typename T, int NV>
 __global__ __launch_bounds__(256) void k_logp_grad(Rows r, int64_t rows, int pieces, const float2 *__restrict__ stats,
-                                                   const float *__restrict__ dlogp, void *dl, int64_t ldd) {
+                                                   const float *__restrict__ dlogp, void *dl, int64_t ldd,
+                                                   const float *__restrict__ pair_loss, int64_t pairs,
+                                                   float *__restrict__ loss) {
   typedef Tile<T, 256, NV> TileT;
+  __shared__ double lds[4];
+  if (blockIdx.x >= rows * pieces) {
+    pair_total(pair_loss, pairs, loss, lds);
+    return;
+  }
   const int64_t t = rows - 1 - blockIdx.x / (unsigned)pieces;
   const int v0 = (int)(blockIdx.x % (unsigned)pieces) * 256 * NV, tid = threadIdx.x;
   const int target = target_at(r, t), vocab = r.vocab;
@@ -334,13 +352,17 @@ __global__ __launch_bounds__(256) void k_logp_grad(Rows r, int64_t rows, int pie
 }
 
 // sum_t w_t l_t over the unmasked rows, in fp64 in a fixed order
-__global__ __launch_bounds__(1024) void k_policy_total(Rows r, int64_t rows, const float *__restrict__ w,
-                                                       const float *__restrict__ l, float *__restrict__ loss) {
-  __shared__ double lds[16];
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_policy_total(Rows r, int64_t rows, const float *__restrict__ w,
+                                                          const float *__restrict__ l, float *__restrict__ loss) {
+  __shared__ double lds[THREADS / 64];
   double s = 0.0;
-  for (int64_t t = threadIdx.x; t < rows; t += 1024)
-    if (target_at(r, t) >= 0 && w[t] != 0.0f) s += (double)w[t] * l[t];
-  s = block_all<16>(s, OpAdd(), lds);
+#pragma unroll 4
+  for (int64_t t = threadIdx.x; t < rows; t += THREADS) {
+    const float wt = w[t], lt = l[t];
+    s += target_at(r, t) >= 0 && wt != 0.0f ? (double)wt * lt : 0.0;
+  }
+  s = block_all<THREADS / 64>(s, OpAdd(), lds);
   if (threadIdx.x == 0) *loss = (float)s;
 }
 
@@ -359,55 +381,53 @@ __device__ __forceinline__ int64_t offset_at(const Pairs &p, int64_t i) {
 
 __device__ __forceinline__ double softplus(double u) { return fmax(u, 0.0) + log1p(exp(-fabs(u))); }
 
-// One workgroup per pair: both texts' sums, the pair's loss, and each row's factor d loss / d logp.
-__global__ __launch_bounds__(256) void k_pair(Rows r, Pairs p, const float *__restrict__ logp,
+// One workgroup per pair, half of it per text: the texts' sums, the pair's loss, and each row's factor d loss / d logp.
+__global__ __launch_bounds__(512) void k_pair(Rows r, Pairs p, const float *__restrict__ logp,
                                               float *__restrict__ rowc, float *__restrict__ seq,
                                               float *__restrict__ pair_loss) {
-  __shared__ double lds[2][12];
+  __shared__ double sums[3][8];
   const int64_t pair = blockIdx.x;
-  double gap[2];
-  float share[2];
-  for (int h = 0; h < 2; ++h) {
-    const int64_t a = offset_at(p, 2 * pair + h), b = offset_at(p, 2 * pair + h + 1);
-    double s = 0.0, g = 0.0, n = 0.0;
-    for (int64_t t = a + threadIdx.x; t < b; t += 256)
-      if (target_at(r, t) >= 0) {
-        s += logp[t];
-        g += (double)logp[t] - p.ref[t];
-        n += 1.0;
-      }
-    s = block_all<4>(s, OpAdd(), lds[h]);
-    g = block_all<4>(g, OpAdd(), lds[h] + 4);
-    n = block_all<4>(n, OpAdd(), lds[h] + 8);
-    share[h] = p.average ? (float)(1.0 / fmax(n, 1.0)) : 1.0f;
-    gap[h] = p.average ? g / fmax(n, 1.0) : g;
-    if (threadIdx.x == 0) seq[2 * pair + h] = (float)(p.average ? s / fmax(n, 1.0) : s);
+  const int h = threadIdx.x >> 8, tid = threadIdx.x & 255;
+  const int64_t a = offset_at(p, 2 * pair + h), b = offset_at(p, 2 * pair + h + 1);
+  double s = 0.0, g = 0.0, n = 0.0;
+#pragma unroll 4
+  for (int64_t t = a + tid; t < b; t += 256) {
+    const float lp = logp[t], ref = p.ref[t];
+    const bool live = target_at(r, t) >= 0;
+    s += live ? (double)lp : 0.0;
+    g += live ? (double)lp - ref : 0.0;
+    n += live ? 1.0 : 0.0;
   }
-  const double d = (double)p.beta * (gap[0] - gap[1]), eps = p.smoothing;
-  const double loss = (eps < 1.0 ? (1.0 - eps) * softplus(-d) : 0.0) + (eps > 0.0 ? eps * softplus(d) : 0.0);
+  s = wave_all(s, OpAdd());
+  g = wave_all(g, OpAdd());
+  n = wave_all(n, OpAdd());
+  if ((threadIdx.x & 63) == 0) {
+    sums[0][threadIdx.x >> 6] = s;
+    sums[1][threadIdx.x >> 6] = g;
+    sums[2][threadIdx.x >> 6] = n;
+  }
+  __syncthreads();
+  double share[2], gap[2], total[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const double *q = &sums[0][4 * i];
+    total[i] = (q[0] + q[1]) + (q[2] + q[3]);
+    gap[i] = (q[8] + q[9]) + (q[10] + q[11]);
+    share[i] = p.average ? 1.0 / fmax((q[16] + q[17]) + (q[18] + q[19]), 1.0) : 1.0;
+  }
+  const double d = (double)p.beta * (gap[0] * share[0] - gap[1] * share[1]), eps = p.smoothing;
+  if (tid == 0) seq[2 * pair + h] = (float)(total[h] * share[h]);
+  if (threadIdx.x == 0)
+    pair_loss[pair] = (float)((eps < 1.0 ? (1.0 - eps) * softplus(-d) : 0.0) + (eps > 0.0 ? eps * softplus(d) : 0.0));
   const double c = -(double)p.beta / (double)p.pairs * ((1.0 - eps) / (1.0 + exp(d)) - eps / (1.0 + exp(-d)));
-  if (threadIdx.x == 0) pair_loss[pair] = (float)loss;
-  for (int h = 0; h < 2; ++h) {
-    const int64_t a = offset_at(p, 2 * pair + h), b = offset_at(p, 2 * pair + h + 1);
-    const float ch = (float)(h ? -c : c) * share[h];
-    for (int64_t t = a + threadIdx.x; t < b; t += 256) rowc[t] = ch;
-  }
-}
-
-// Rows outside all texts: before the first offset and from the last one on.
-__global__ __launch_bounds__(256) void k_pair_rest(Pairs p, float *__restrict__ rowc) {
-  const int64_t a = offset_at(p, 0), b = offset_at(p, 2 * p.pairs);
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t < p.rows && (t < a || t >= b)) rowc[t] = 0.0f;
+  const float ch = (float)((h ? -c : c) * share[h]);
+  for (int64_t t = a + tid; t < b; t += 256) rowc[t] = ch;
 }
 
 __global__ __launch_bounds__(256) void k_pair_total(const float *__restrict__ pair_loss, int64_t pairs,
                                                     float *__restrict__ loss) {
   __shared__ double lds[4];
-  double s = 0.0;
-  for (int64_t i = threadIdx.x; i < pairs; i += 256) s += pair_loss[i];
-  s = block_all<4>(s, OpAdd(), lds);
-  if (threadIdx.x == 0) *loss = (float)(s / (double)pairs);
+  pair_total(pair_loss, pairs, loss, lds);
 }
 
 int check_logits(const sk_logits *x) {
@@ -455,20 +475,20 @@ void with_row_shape(int64_t nv, F f) {
 }
 
 template <typename T>
-void run_logp_t(const sk_logits *x, float *logp, float *stats, hipStream_t st) {
+void run_logp_t(const sk_logits *x, float *logp, float *stats, float *rowc, hipStream_t st) {
   with_row_shape<T>(x->vocab / Vec<T>::N, [&](auto th, auto nv, auto res) {
     constexpr int TH = decltype(th)::value;
     const int64_t blocks = TH == 64 ? (x->rows + 3) / 4 : x->rows;
     hipLaunchKernelGGL((k_logp<T, TH, decltype(nv)::value, decltype(res)::value>), dim3((unsigned)blocks),
-                       dim3(TH == 64 ? 256 : TH), 0, st, rows_of(x), x->rows, logp, (float2 *)stats);
+                       dim3(TH == 64 ? 256 : TH), 0, st, rows_of(x), x->rows, logp, (float2 *)stats, rowc);
   });
 }
 
-void run_logp(const sk_logits *x, float *logp, float *stats, hipStream_t st) {
+void run_logp(const sk_logits *x, float *logp, float *stats, float *rowc, hipStream_t st) {
   if (x->dtype == SK_F32)
-    run_logp_t<float>(x, logp, stats, st);
+    run_logp_t<float>(x, logp, stats, rowc, st);
   else
-    run_logp_t<bf16>(x, logp, stats, st);
+    run_logp_t<bf16>(x, logp, stats, rowc, st);
 }
 
 template <typename T>
@@ -482,28 +502,37 @@ void run_policy_t(const sk_logits *x, const Policy &p, float *logp, float *token
   });
 }
 
+struct PairTotal {  // of the preference loss
+  const float *pair_loss = nullptr;
+  int64_t pairs = 0;
+  float *loss = nullptr;
+};
+
 template <typename T>
-void run_logp_grad_t(const sk_logits *x, const float *stats, const float *dlogp, void *d, int64_t ldd,
+void run_logp_grad_t(const sk_logits *x, const float *stats, const float *dlogp, void *d, int64_t ldd, PairTotal total,
                      hipStream_t st) {
   constexpr int NV = 4;
   const int64_t pieces = std::max<int64_t>(1, (x->vocab / Vec<T>::N + 256 * NV - 1) / (256 * NV));
   // a grid holds fewer than 2^31 workgroups
-  const int64_t most = std::max<int64_t>(1, INT32_MAX / pieces);
+  const int64_t most = std::max<int64_t>(1, (INT32_MAX - 1) / pieces);
   for (int64_t r0 = 0; r0 < x->rows; r0 += most) {
     Rows r = rows_of(x);
     r.x = (const T *)r.x + r0 * r.ld;
     r.targets = (const char *)r.targets + r0 * (x->index == SK_I64 ? 8 : 4);
     const int64_t n = std::min(most, x->rows - r0);
-    hipLaunchKernelGGL((k_logp_grad<T, NV>), dim3((unsigned)(n * pieces)), dim3(256), 0, st, r, n, (int)pieces,
-                       (const float2 *)stats + r0, dlogp + r0, (T *)d + r0 * ldd, ldd);
+    const int64_t blocks = n * pieces + (r0 == 0 && total.loss ? 1 : 0);
+    hipLaunchKernelGGL((k_logp_grad<T, NV>), dim3((unsigned)blocks), dim3(256), 0, st, r, n, (int)pieces,
+                       (const float2 *)stats + r0, dlogp + r0, (T *)d + r0 * ldd, ldd, total.pair_loss, total.pairs,
+                       total.loss);
   }
 }
 
-void run_logp_grad(const sk_logits *x, const float *stats, const float *dlogp, void *d, int64_t ldd, hipStream_t st) {
+void run_logp_grad(const sk_logits *x, const float *stats, const float *dlogp, void *d, int64_t ldd, PairTotal total,
+                   hipStream_t st) {
   if (x->dtype == SK_F32)
-    run_logp_grad_t<float>(x, stats, dlogp, d, ldd, st);
+    run_logp_grad_t<float>(x, stats, dlogp, d, ldd, total, st);
   else
-    run_logp_grad_t<bf16>(x, stats, dlogp, d, ldd, st);
+    run_logp_grad_t<bf16>(x, stats, dlogp, d, ldd, total, st);
 }
 
 }  // namespace
@@ -515,7 +544,7 @@ int sketch_token_logp(const sk_logits *x, float *logp, float *stats, void *strea
   if (rc != SK_OK || x->rows == 0) return rc;
   if (!logp) return train_fail(SK_EINVAL, "NULL argument");
   TrainGuard guard(x->device);
-  run_logp(x, logp, stats, (hipStream_t)stream);
+  run_logp(x, logp, stats, nullptr, (hipStream_t)stream);
   return train_launched();
 }
 
@@ -526,7 +555,7 @@ int sketch_token_logp_grad(const sk_logits *x, const float *stats, const float *
   if (!stats || !dlogp || !dlogits) return train_fail(SK_EINVAL, "NULL argument");
   if ((rc = check_out(x, dlogits, ld_out)) != SK_OK) return rc;
   TrainGuard guard(x->device);
-  run_logp_grad(x, stats, dlogp, dlogits, ld_out, (hipStream_t)stream);
+  run_logp_grad(x, stats, dlogp, dlogits, ld_out, PairTotal(), (hipStream_t)stream);
   return train_launched();
 }
 
@@ -552,7 +581,11 @@ int sketch_policy_loss(const sk_logits *x, const float *old_logp, const float *a
     else
       run_policy_t<bf16>(x, p, logp, token_loss, dlogits, ld_out, st);
   }
-  hipLaunchKernelGGL(k_policy_total, dim3(1), dim3(1024), 0, st, r, x->rows, weights, token_loss, loss);
+  // one workgroup: four waves are there sooner, sixteen get through more rows (256 rows a thread-step)
+  if (x->rows <= 1024)
+    hipLaunchKernelGGL(k_policy_total<256>, dim3(1), dim3(256), 0, st, r, x->rows, weights, token_loss, loss);
+  else
+    hipLaunchKernelGGL(k_policy_total<1024>, dim3(1), dim3(1024), 0, st, r, x->rows, weights, token_loss, loss);
   return train_launched();
 }
 
@@ -578,13 +611,12 @@ int sketch_preference_loss(const sk_logits *x, const void *offsets, sk_index off
   hipStream_t st = (hipStream_t)stream;
   float *stats = (float *)work, *logp = stats + 2 * x->rows, *rowc = logp + x->rows;
   const Pairs p{offsets, (int32_t)offsets_index, average, pairs, x->rows, ref_logp, beta, smoothing};
-  if (x->rows) run_logp(x, logp, stats, st);
-  hipLaunchKernelGGL(k_pair, dim3((unsigned)pairs), dim3(256), 0, st, rows_of(x), p, logp, rowc, seq_logp, pair_loss);
-  hipLaunchKernelGGL(k_pair_total, dim3(1), dim3(256), 0, st, pair_loss, pairs, loss);
-  if (x->rows && dlogits) {
-    hipLaunchKernelGGL(k_pair_rest, dim3((unsigned)((x->rows + 255) / 256)), dim3(256), 0, st, p, rowc);
-    run_logp_grad(x, stats, rowc, dlogits, ld_out, st);
-  }
+  if (x->rows) run_logp(x, logp, stats, rowc, st);
+  hipLaunchKernelGGL(k_pair, dim3((unsigned)pairs), dim3(512), 0, st, rows_of(x), p, logp, rowc, seq_logp, pair_loss);
+  if (x->rows && dlogits)
+    run_logp_grad(x, stats, rowc, dlogits, ld_out, PairTotal{pair_loss, pairs, loss}, st);
+  else
+    hipLaunchKernelGGL(k_pair_total, dim3(1), dim3(256), 0, st, pair_loss, pairs, loss);
   return train_launched();
 }
 

@@ -18,7 +18,7 @@ _DT = {torch.float32: _lib.SK_F32, torch.bfloat16: _lib.SK_BF16}
 
 
 def _stream_ptr(device: torch.device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)  # current_stream(device).cuda_stream, 2 us sooner
 
 
 class Sketch:
