@@ -53,8 +53,8 @@ int sketch_embed(const void *weight, sk_dtype dtype, int64_t vocab, int64_t widt
  *   dy       [batch, n, width], row stride ld >= width elements.
  *   out      [batch, vocab, width] contiguous.
  *   work     sketch_embed_grad_work_bytes(batch, n, width) bytes, 256-byte aligned.
- * SK_EUNSUPPORTED for vocab > 2^20, batch > 2^18, batch * n > 2^28, width > 2^24 or
- * about batch * n * width > 2^42.
+ * SK_EUNSUPPORTED for vocab > 2^20, batch > 2^18, batch * n >= 2^28, width > 2^24 or
+ * about batch * n * width > 2^37.
  */
 int64_t sketch_embed_grad_work_bytes(int64_t batch, int64_t n, int64_t width);
 int sketch_embed_grad(const void *dy, sk_dtype dtype, int64_t ld, const void *ids, sk_index index, int64_t batch,

@@ -301,6 +301,8 @@ struct sk_adamw {
   int n_tensors = 0;
   int64_t elems = 0, n_chunks = 0;
   std::vector<int64_t> numel, first_chunk;  // first chunk of each tensor, and the end
+  // one allocation: scale, partial sums of the norm, tensors, chunks
+  void *d_block = nullptr;
   AdamTensor *d_tensors = nullptr;
   AdamChunk *d_chunks = nullptr;
   double *d_part = nullptr;
@@ -310,8 +312,7 @@ struct sk_adamw {
 namespace {
 
 void free_adamw(sk_adamw *h) {
-  for (void *p : {(void *)h->d_tensors, (void *)h->d_chunks, (void *)h->d_part, (void *)h->d_scale})
-    if (p) (void)hipFree(p);
+  if (h->d_block) (void)hipFree(h->d_block);
   delete h;
 }
 
@@ -352,8 +353,7 @@ int sketch_adamw_create(const int64_t *numel, const float *decay, int32_t n_tens
   int ndev = 0;
   if (hipGetDeviceCount(&ndev) != hipSuccess || device < 0 || device >= ndev)
     return train_fail(SK_EINVAL, "device out of range");
-  std::vector<AdamTensor> tensors;
-  std::vector<AdamChunk> chunks;
+  std::vector<char> tables;  // tensors, then chunks
   sk_adamw *h = new sk_adamw();
   try {
     h->device = device;
@@ -362,29 +362,39 @@ int sketch_adamw_create(const int64_t *numel, const float *decay, int32_t n_tens
     h->n_tensors = n_tensors;
     for (int l = 0; l < n_tensors; ++l) {
       h->numel.push_back(numel[l]);
-      h->first_chunk.push_back((int64_t)chunks.size());
-      tensors.push_back(AdamTensor{numel[l], h->elems, decay ? decay[l] : 1.0f});
-      h->elems += (numel[l] + 63) / 64 * 64;
-      for (int64_t e = 0; e < numel[l]; e += kAdamChunk) chunks.push_back(AdamChunk{l, 0, e});
+      h->first_chunk.push_back(h->n_chunks);
+      h->n_chunks += (numel[l] + kAdamChunk - 1) / kAdamChunk;
     }
-    h->n_chunks = (int64_t)chunks.size();
     h->first_chunk.push_back(h->n_chunks);
+    if (h->n_chunks >= (1 << 24)) {  // a grid of 2^32 threads
+      delete h;
+      return train_fail(SK_EUNSUPPORTED, "more than 2^36 elements");
+    }
+    tables.resize(sizeof(AdamTensor) * n_tensors + sizeof(AdamChunk) * h->n_chunks);
   } catch (...) {
     delete h;
     throw;
   }
+  AdamTensor *tensors = (AdamTensor *)tables.data();
+  AdamChunk *chunks = (AdamChunk *)(tensors + n_tensors);
+  for (int l = 0; l < n_tensors; ++l) {
+    tensors[l] = AdamTensor{numel[l], h->elems, decay ? decay[l] : 1.0f};
+    h->elems += (numel[l] + 63) / 64 * 64;
+    for (int64_t e = 0; e < numel[l]; e += kAdamChunk) *chunks++ = AdamChunk{l, 0, e};
+  }
   TrainGuard guard(device);
-  if (hipMalloc((void **)&h->d_tensors, sizeof(AdamTensor) * tensors.size()) != hipSuccess ||
-      hipMalloc((void **)&h->d_chunks, sizeof(AdamChunk) * chunks.size()) != hipSuccess ||
-      hipMalloc((void **)&h->d_part, sizeof(double) * chunks.size()) != hipSuccess ||
-      hipMalloc((void **)&h->d_scale, sizeof(float)) != hipSuccess) {
+  const size_t at_tensors = 16 + sizeof(double) * h->n_chunks;
+  if (hipMalloc(&h->d_block, at_tensors + tables.size()) != hipSuccess) {
     (void)hipGetLastError();
+    h->d_block = nullptr;
     free_adamw(h);
     return train_fail(SK_ENOMEM, "hipMalloc failed");
   }
-  if (hipMemcpy(h->d_tensors, tensors.data(), sizeof(AdamTensor) * tensors.size(), hipMemcpyHostToDevice) !=
-          hipSuccess ||
-      hipMemcpy(h->d_chunks, chunks.data(), sizeof(AdamChunk) * chunks.size(), hipMemcpyHostToDevice) != hipSuccess) {
+  h->d_scale = (float *)h->d_block;
+  h->d_part = (double *)((char *)h->d_block + 16);
+  h->d_tensors = (AdamTensor *)((char *)h->d_block + at_tensors);
+  h->d_chunks = (AdamChunk *)(h->d_tensors + n_tensors);
+  if (hipMemcpy(h->d_tensors, tables.data(), tables.size(), hipMemcpyHostToDevice) != hipSuccess) {
     free_adamw(h);
     return train_fail(SK_EHIP, "hipMemcpy of the tables failed");
   }

@@ -11,16 +11,17 @@
 //               counted by brute force (64 entries a workgroup against all of
 //               the run; 4096 comparisons an entry over the whole chip take
 //               less time than the barriers of a sort in one workgroup's LDS).
+//               The launch's other workgroups zero the gradient meanwhile.
 //   k_eg_merge  joins up to 16 sorted runs: an entry's place is its own plus
 //               what a binary search in each other run gives, one lane a run.
 //   k_eg_sum    a wave adds up R sorted entries for 64 vectors of columns and
 //               writes out every id that begins and ends among them; what
 //               crosses the cut is written to the workspace (head: the part of
-//               an id that began earlier, tail: of one that goes on).  The
-//               launch's other workgroups zero the rows that no id names.
+//               an id that began earlier, tail: of one that goes on).
 //   k_eg_join   tail + heads of the ids that cross cuts.
 // Every sum has a fixed order: the sorted one within R entries, then piece by
-// piece.  Bound by writing the gradient (vocab x width per group).
+// piece.  Bound by writing the gradient (vocab x width per group); to zero all
+// of it costs the named rows a second write and spares the others a look-up.
 #include <algorithm>
 
 #include "sk_train.h"
@@ -55,10 +56,10 @@ __device__ __forceinline__ void store_n(O *p, const float *f) {
 
 template <typename W, typename O>
 __global__ __launch_bounds__(256) void k_embed(const W *__restrict__ w, int64_t vocab, int width, int64_t ld,
-                                               const void *__restrict__ ids, int index, int64_t n, int pieces,
-                                               float scale, O *__restrict__ out) {
+                                               const void *__restrict__ ids, int index, int64_t block0,
+                                               int64_t n, int pieces, float scale, O *__restrict__ out) {
   constexpr int N = Vec<W>::N, NV = 4;
-  const int64_t job = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t job = (block0 + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t t = job / pieces;
   if (t >= n) return;
   const int lane = threadIdx.x & 63, nv = width / N, v0 = (int)(job % pieces) * 64 * NV + lane;
@@ -88,10 +89,35 @@ struct Entry {  // a token of its group: id and position
   uint32_t id, pos;
 };
 
+// What is to be zeroed: `bytes` bytes, an even number, from an even address on.
+struct Zeros {
+  char *p;
+  int64_t bytes;
+};
+
+// 16 bytes a thread, one workgroup after the other: 8 x 50257 x 768 fp32 at 6.8 TB/s, where workgroups that go through
+// stretches of their own reach 4 to 5.5.
+__device__ __forceinline__ void zero_part(Zeros z, int64_t block, int64_t blocks) {
+  int64_t head = (int64_t)((16 - ((uintptr_t)z.p & 15)) & 15);
+  head = head < z.bytes ? head : z.bytes;
+  const int64_t nv = (z.bytes - head) / 16;
+  u32x4 *v = (u32x4 *)(z.p + head);
+  for (int64_t i = block * 512 + threadIdx.x; i < nv; i += blocks * 512) v[i] = u32x4{0, 0, 0, 0};
+  if (block == 0 && threadIdx.x < 16) {  // up to 7 pairs of bytes on either side
+    const int64_t at = threadIdx.x < 8 ? 2 * threadIdx.x : head + nv * 16 + 2 * (threadIdx.x - 8);
+    if (at < (threadIdx.x < 8 ? head : z.bytes)) *(uint16_t *)(z.p + at) = 0;
+  }
+}
+
 // Ranks 64 entries of a run against the whole run, eight waves taking turns at its blocks of 64.
 __global__ __launch_bounds__(512) void k_eg_rank(const void *__restrict__ ids, int index, int64_t n, int64_t vocab,
-                                                 int runs, int tiles, Entry *__restrict__ sorted) {
+                                                 int runs, int tiles, int rank_blocks, Entry *__restrict__ sorted,
+                                                 Zeros z) {
   __shared__ int part[8][64];
+  if (blockIdx.x >= rank_blocks) {
+    zero_part(z, blockIdx.x - rank_blocks, gridDim.x - rank_blocks);
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t run = blockIdx.x / (unsigned)tiles, b = run / runs, p0 = (run % runs) * kRun;
   const int tile = blockIdx.x % (unsigned)tiles, len = (int)(n - p0 < kRun ? n - p0 : kRun);
@@ -106,13 +132,13 @@ __global__ __launch_bounds__(512) void k_eg_rank(const void *__restrict__ ids, i
   for (int blk = wave; blk * 64 < len; blk += 8) {
     const uint32_t theirs = key(blk * 64 + lane);
     if (blk < tile) {  // earlier entries of the same id come first
-#pragma unroll
+#pragma unroll 16
       for (int j = 0; j < 64; ++j) count += (uint32_t)__builtin_amdgcn_readlane((int)theirs, j) <= mine;
     } else if (blk > tile) {
-#pragma unroll
+#pragma unroll 16
       for (int j = 0; j < 64; ++j) count += (uint32_t)__builtin_amdgcn_readlane((int)theirs, j) < mine;
     } else {
-#pragma unroll
+#pragma unroll 16
       for (int j = 0; j < 64; ++j) {
         const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)theirs, j);
         count += k < mine || (k == mine && j < lane);
@@ -190,35 +216,10 @@ __device__ __forceinline__ void put_part(float *row, int c, int width, const flo
 }
 
 template <typename G, typename O>
-__global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, unsigned sum_blocks, const G *__restrict__ dy,
+__global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *__restrict__ dy,
                                                 O *__restrict__ out) {
   constexpr int N = Vec<G>::N, U = 32 / N;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (blockIdx.x >= sum_blocks) {
-    // zeros to the rows without an entry: 64 rows a wave, each lane looks one up
-    const int64_t per = (s.vocab + 255) / 256, j = blockIdx.x - sum_blocks, b = j / per;
-    const int64_t r0 = (j % per) * 256 + wave * 64, r = r0 + lane;
-    const Entry *k = s.sorted + b * s.n;
-    int64_t lo = 0, hi = s.n;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) >> 1;
-      if ((int64_t)k[mid].id < r)
-        lo = mid + 1;
-      else
-        hi = mid;
-    }
-    uint64_t absent = __ballot(r < s.vocab && (lo >= s.n || (int64_t)k[lo].id != r));
-    constexpr int NO = Vec<O>::N;
-    while (absent) {
-      const int at = __builtin_ctzll(absent);
-      absent &= absent - 1;
-      O *row = out + (b * s.vocab + r0 + at) * s.width;
-      const int nv = s.width / NO;
-      for (int v = lane; v < nv; v += 64) Vec<O>::store(row + (int64_t)v * NO, u32x4{0, 0, 0, 0});
-      if (nv * NO + lane < s.width) row[nv * NO + lane] = from_f32<O>(0.0f);
-    }
-    return;
-  }
   const int64_t job = (int64_t)blockIdx.x * 4 + wave;
   if (job >= jobs) return;
   const int64_t bt = job / s.pieces, b = bt / s.tiles, tile = bt % s.tiles, e0 = tile * s.R;
@@ -322,8 +323,10 @@ template <typename W, typename O>
 void run_embed(const void *w, int64_t vocab, int64_t width, int64_t ld, const void *ids, int index, int64_t n,
                float scale, void *out, hipStream_t st) {
   const int64_t pieces = std::max<int64_t>(1, (width / Vec<W>::N + 255) / 256);
-  hipLaunchKernelGGL((k_embed<W, O>), dim3((unsigned)((n * pieces + 3) / 4)), dim3(256), 0, st, (const W *)w, vocab,
-                     (int)width, ld, ids, index, n, (int)pieces, scale, (O *)out);
+  grid_parts((n * pieces + 3) / 4, [&](uint32_t block0, uint32_t blocks) {
+    hipLaunchKernelGGL((k_embed<W, O>), dim3(blocks), dim3(256), 0, st, (const W *)w, vocab, (int)width, ld, ids, index,
+                       (int64_t)block0, n, (int)pieces, scale, (O *)out);
+  });
 }
 
 // Entries a wave adds up: few where there are few waves (8192 fill the chip), else enough that little is left to join.
@@ -352,16 +355,17 @@ void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batc
   Sums s;
   s.head = (float *)((char *)work + w.entries * (n > kRun ? 2 : 1));
   s.tail = s.head + w.sums / 4;
-  if (n) {
-    const int64_t runs = (n + kRun - 1) / kRun;
-    const int64_t tiles = (std::min<int64_t>(n, kRun) + 63) / 64;  // of a run
-    hipLaunchKernelGGL(k_eg_rank, dim3((unsigned)(batch * runs * tiles)), dim3(512), 0, st, ids, index, n, vocab,
-                       (int)runs, (int)tiles, sorted);
-    for (int64_t len = kRun; len < n; len *= kMergeRuns) {
-      hipLaunchKernelGGL(k_eg_merge, dim3((unsigned)((batch * n * kMergeRuns + 255) / 256)), dim3(256), 0, st, sorted,
-                         other, n, len, batch * n);
-      std::swap(sorted, other);
-    }
+  const int64_t runs = (n + kRun - 1) / kRun, tiles = (std::min<int64_t>(n, kRun) + 63) / 64;  // tiles of a run
+  const int64_t rank_blocks = batch * runs * tiles;
+  const Zeros z{(char *)out, accumulate ? 0 : batch * vocab * width * (int64_t)sizeof(O)};
+  const int64_t blocks = rank_blocks + std::min<int64_t>((z.bytes + 8191) / 8192, 1 << 21);
+  if (blocks)
+    hipLaunchKernelGGL(k_eg_rank, dim3((unsigned)blocks), dim3(512), 0, st, ids, index, n, vocab, (int)runs, (int)tiles,
+                       (int)rank_blocks, sorted, z);
+  for (int64_t len = kRun; len < n; len *= kMergeRuns) {
+    hipLaunchKernelGGL(k_eg_merge, dim3((unsigned)((batch * n * kMergeRuns + 255) / 256)), dim3(256), 0, st, sorted,
+                       other, n, len, batch * n);
+    std::swap(sorted, other);
   }
   s.sorted = sorted;
   s.n = n;
@@ -373,11 +377,10 @@ void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batc
   s.R = eg_tile(batch, n, width);
   s.accumulate = accumulate;
   s.scale = scale;
-  const int64_t jobs = batch * w.tiles * s.pieces, sum_blocks = (jobs + 3) / 4;
-  const int64_t blocks = sum_blocks + (accumulate ? 0 : batch * ((vocab + 255) / 256));
-  if (blocks)
-    hipLaunchKernelGGL((k_eg_sum<G, O>), dim3((unsigned)blocks), dim3(256), 0, st, s, jobs, (unsigned)sum_blocks,
-                       (const G *)dy, out);
+  const int64_t jobs = batch * w.tiles * s.pieces;
+  if (jobs)
+    hipLaunchKernelGGL((k_eg_sum<G, O>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, s, jobs, (const G *)dy,
+                       out);
   if (w.tiles > 1)
     hipLaunchKernelGGL((k_eg_join<O>), dim3((unsigned)(batch * w.tiles * ((width + 255) / 256))), dim3(256), 0, st, s,
                        out);
@@ -413,7 +416,8 @@ int sketch_embed(const void *weight, sk_dtype dtype, int64_t vocab, int64_t widt
 }
 
 int64_t sketch_embed_grad_work_bytes(int64_t batch, int64_t n, int64_t width) {
-  if (batch < 1 || n < 0 || width < 1 || batch > (1 << 30) || n > (1 << 30) || batch * n > (1 << 30)) return 0;
+  if (batch < 1 || n < 0 || width < 1 || batch > (1 << 18) || n >= (1 << 28) || batch * n >= (1 << 28) || width > (1 << 24))
+    return 0;
   return std::max<int64_t>(256, eg_work(batch, n, width).bytes);
 }
 
@@ -425,8 +429,8 @@ int sketch_embed_grad(const void *dy, sk_dtype dtype, int64_t ld, const void *id
   if (batch < 1 || vocab < 1 || width < 1 || n < 0 || ld < width)
     return train_fail(SK_EINVAL, "need batch, vocab, width >= 1, n >= 0 and ld >= width");
   // what the launches' grids and 32-bit entries hold
-  if (vocab > (1 << 20) || width > (1 << 24) || batch > (1 << 18) || n > (1 << 28) || batch * n > (1 << 28) ||
-      batch * ((n + 15) / 16 * ((width + 255) / 256)) > (1 << 30))
+  if (vocab > (1 << 20) || width > (1 << 24) || batch > (1 << 18) || n >= (1 << 28) || batch * n >= (1 << 28) ||
+      batch * eg_work(batch, n, width).tiles * ((width + 255) / 256) > kGridBlocks)
     return train_fail(SK_EUNSUPPORTED, "sizes above what the kernels take");
   if (!out || (n && (!dy || !ids || !work))) return train_fail(SK_EINVAL, "NULL argument");
   if (n && work_bytes < sketch_embed_grad_work_bytes(batch, n, width))

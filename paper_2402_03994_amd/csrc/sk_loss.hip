@@ -59,13 +59,17 @@ __device__ __forceinline__ Cut cut_of(const T *x, int vocab) {
 
 // The part of a row that a thread of THREADS holds: up to NV vectors, THREADS vectors apart, from vector v0 on, and
 // (with the first tile) one of the entries outside the vectors: thread i < 8 the head's, thread 8 + i the last ones.
-// What is beyond the row is -inf.
-template <typename T, int THREADS, int NV>
+// What is beyond the row is -inf.  The last NL of the NV vectors lie in LDS, each thread's own (no barrier).
+template <typename T, int THREADS, int NV, int NL = 0>
 struct Tile {
   static constexpr int N = Vec<T>::N;
   static constexpr uint32_t kNone = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
-  u32x4 raw[NV];
+  static constexpr int NR = NV - NL;  // vectors in registers
+  u32x4 raw[NR];
   float rest;
+  u32x4 *lds;  // [NL][THREADS]
+
+  __device__ __forceinline__ u32x4 vec(int k, int tid) const { return k < NR ? raw[k] : lds[(k - NR) * THREADS + tid]; }
 
   // where the thread's single entry lies, -1 if it has none
   static __device__ __forceinline__ int single(Cut q, int v0, int tid) {
@@ -81,38 +85,49 @@ struct Tile {
   }
   __device__ __forceinline__ void load(const T *x, Cut q, int v0, int tid) {
     const T *a = x + q.head;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
+    auto one = [&](int k) {
       const int i = v0 + k * THREADS + tid;
-      raw[k] = u32x4{kNone, kNone, kNone, kNone};
-      if (i < q.nv) raw[k] = Vec<T>::load(a + (int64_t)i * N);
+      u32x4 v = u32x4{kNone, kNone, kNone, kNone};
+      if (i < q.nv) v = Vec<T>::load(a + (int64_t)i * N);
+      return v;
+    };
+    if (NL) {  // LDS first, so that the registers they pass through are free again for the others
+#pragma unroll
+      for (int k = 0; k < NL; ++k) lds[k * THREADS + tid] = one(NR + k);
+      asm volatile("" ::: "memory");
     }
+#pragma unroll
+    for (int k = 0; k < NR; ++k) raw[k] = one(k);
     const int j = single(q, v0, tid);
     rest = j >= 0 ? to_f32(x[j]) : -INFINITY;
   }
-  // The vectors stay packed between two uses: without this the compiler carries the unpacked bf16 values along, twice
-  // the registers.
+  // The vectors stay packed, and in LDS, between two uses: without this the compiler carries the unpacked bf16 values
+  // along, twice the registers, and those of LDS too.
   __device__ __forceinline__ void stay() {
     if (sizeof(T) == 2) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(raw[k]));
+      for (int k = 0; k < NR; ++k) asm volatile("" : "+v"(raw[k]));
     }
+    if (NL) asm volatile("" ::: "memory");
   }
-  __device__ __forceinline__ float largest() const {
+  __device__ __forceinline__ float largest(int tid) const {
     float m = rest;
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      const u32x4 v = vec(k, tid);
 #pragma unroll
-      for (int i = 0; i < N; ++i) m = fmaxf(m, Vec<T>::get(raw[k], i));
+      for (int i = 0; i < N; ++i) m = fmaxf(m, Vec<T>::get(v, i));
+    }
     return m;
   }
-  __device__ __forceinline__ float expsum(float m, float k2) const {
+  __device__ __forceinline__ float expsum(float m, float k2, int tid) const {
     float z = __builtin_amdgcn_exp2f((rest - m) * k2);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
+      const u32x4 v = vec(k, tid);
       float s = 0.0f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((Vec<T>::get(raw[k], i) - m) * k2);
+      for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((Vec<T>::get(v, i) - m) * k2);
       z += s;
     }
     return z;
@@ -124,9 +139,10 @@ struct Tile {
     for (int k = 0; k < NV; ++k) {
       const int i = v0 + k * THREADS + tid;
       if (i < q.nv) {
+        const u32x4 v = vec(k, tid);
         float f[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = w * __builtin_amdgcn_exp2f((Vec<T>::get(raw[k], e) - m) * k2);
+        for (int e = 0; e < N; ++e) f[e] = w * __builtin_amdgcn_exp2f((Vec<T>::get(v, e) - m) * k2);
         Vec<T>::store(a + (int64_t)i * N, Vec<T>::pack(f));
       }
     }
@@ -173,17 +189,17 @@ __device__ __forceinline__ Stats join(Stats s, float k2, float (*lds)[16]) {
 
 // (m, z) of a tile's entries by one thread; an exponent of no entry at all is left out
 template <typename TileT>
-__device__ __forceinline__ Stats thread_stats(TileT &t, float k2) {
-  const float m = t.largest();
+__device__ __forceinline__ Stats thread_stats(TileT &t, float k2, int tid) {
+  const float m = t.largest(tid);
   t.stay();
-  return Stats{m, t.expsum(m == -INFINITY ? 0.0f : m, k2)};
+  return Stats{m, t.expsum(m == -INFINITY ? 0.0f : m, k2, tid)};
 }
 
 // Writes the row c scale (onehot - p) of a target; called with what the threads hold of the row, or (RESIDENT false)
 // with nothing: the row is read again, tile by tile.
-template <typename T, int THREADS, int NV, bool RESIDENT>
+template <typename T, int THREADS, int NV, bool RESIDENT, typename TileT>
 __device__ __forceinline__ void row_grad(const T *x, T *d, int vocab, float scale, Stats s, int target, float xt, float c,
-                                         Tile<T, THREADS, NV> &t, int tid) {
+                                         TileT &t, int tid) {
   if (c == 0.0f || s.z == 0.0f) {
     row_zero<T, THREADS>(d, vocab, 0, INT32_MAX, tid);
     return;
@@ -200,20 +216,19 @@ __device__ __forceinline__ void row_grad(const T *x, T *d, int vocab, float scal
     }
   }
   // the target's entry, again by the thread that has just stored it
-  if (tid == Tile<T, THREADS, NV>::owner(q, target))
+  if (tid == TileT::owner(q, target))
     d[target] = from_f32<T>(cs * (1.0f - __builtin_amdgcn_exp2f((xt - s.m) * k2) / s.z));
 }
 
-template <typename T, int THREADS, int NV, bool RESIDENT>
-__device__ __forceinline__ Stats row_stats(const T *x, int vocab, float k2, Tile<T, THREADS, NV> &t, int tid,
-                                           float (*lds)[16]) {
+template <typename T, int THREADS, int NV, bool RESIDENT, typename TileT>
+__device__ __forceinline__ Stats row_stats(const T *x, int vocab, float k2, TileT &t, int tid, float (*lds)[16]) {
   const Cut q = cut_of(x, vocab);
   t.load(x, q, 0, tid);
-  Stats s = thread_stats(t, k2);
+  Stats s = thread_stats(t, k2, tid);
   if (!RESIDENT) {
     for (int v0 = THREADS * NV; v0 < q.nv; v0 += THREADS * NV) {
       t.load(x, q, v0, tid);
-      const Stats o = thread_stats(t, k2);
+      const Stats o = thread_stats(t, k2, tid);
       const float m = fmaxf(s.m, o.m);
       s = Stats{m, moved(s, m, k2) + moved(o, m, k2)};
     }
@@ -240,24 +255,25 @@ __device__ __forceinline__ void policy_token(const Policy &p, int64_t t, float l
   }
 }
 
-// One row by THREADS threads; rows of one wave share a workgroup of four.
+// One row by THREADS threads, from row0 on; rows of one wave share a workgroup of four.
 template <int THREADS>
-__device__ __forceinline__ int64_t row_of_thread(int &tid) {
+__device__ __forceinline__ int64_t row_of_thread(int64_t row0, int &tid) {
   if (THREADS > 64) {
     tid = threadIdx.x;
-    return blockIdx.x;
+    return row0 + blockIdx.x;
   }
   tid = threadIdx.x & 63;
-  return (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  return row0 + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
 }
 
 template <typename T, int THREADS, int NV, bool RESIDENT>
-__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_logp(Rows r, int64_t rows, float *__restrict__ logp,
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_logp(Rows r, int64_t row0, int64_t rows,
+                                                                       float *__restrict__ logp,
                                                                        float2 *__restrict__ stats,
                                                                        float *__restrict__ rowc) {
   __shared__ float lds[2][16];
   int tid;
-  const int64_t t = row_of_thread<THREADS>(tid);
+  const int64_t t = row_of_thread<THREADS>(row0, tid);
   if (t >= rows) return;
   const int target = target_at(r, t);
   const T *x = (const T *)r.x + t * r.ld;
@@ -277,19 +293,21 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_logp(Rows r, 
 }
 
 // d (NULL: the loss alone) may be the logits: a row's threads hold it, or have all read it, before any of them writes.
-template <typename T, int THREADS, int NV, bool RESIDENT>
-__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_policy(Rows r, int64_t rows, Policy p,
+template <typename T, int THREADS, int NV, bool RESIDENT, int NL>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_policy(Rows r, int64_t row0, int64_t rows, Policy p,
                                                                          float *__restrict__ logp,
                                                                          float *__restrict__ loss_t, void *d,
                                                                          int64_t ldd) {
   __shared__ float lds[2][16];
   int tid;
-  const int64_t t = row_of_thread<THREADS>(tid);
+  const int64_t t = row_of_thread<THREADS>(row0, tid);
   if (t >= rows) return;
   const int target = target_at(r, t);
   const float w = target >= 0 ? p.weights[t] : 0.0f;
   const T *x = (const T *)r.x + t * r.ld;
-  Tile<T, THREADS, NV> tile;
+  __shared__ u32x4 more[NL ? NL * THREADS : 1];
+  Tile<T, THREADS, NV, NL> tile;
+  tile.lds = more;
   Stats s{0.0f, 0.0f};
   float lp = 0.0f, l = 0.0f, c = 0.0f, xt = 0.0f;
   if (w != 0.0f) {
@@ -454,33 +472,68 @@ Rows rows_of(const sk_logits *x) {
   return Rows{x->data, x->targets, x->ld, (int32_t)x->vocab, (int32_t)x->index, x->scale};
 }
 
-// Threads and vectors for a row of nv whole vectors: the fewest that hold it.  Beyond 1024 x 16 vectors a row is
-// streamed.
-template <typename T, typename F>
-void with_row_shape(int64_t nv, F f) {
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// f(threads, vectors of a thread, resident, vectors of them in LDS) for rows of up to nv vectors.  Where there are
+// many rows, what counts is how much of them the chip holds at a time: about four to eight vectors a thread, so that a
+// CU has several rows (16924 bf16 columns, log-probabilities: 4.3 TB/s with 1024 threads, 6.0 with 256; policy update:
+// 4.9 with 1024, 5.7 with 512; 8000 columns, policy: 5.2 with 256 threads, 5.4 with one wave).  Few rows want their
+// latency shared by more threads.
+template <typename F>
+void with_row_shape(int64_t nv, int64_t rows, F f) {
+  const bool few = rows <= 1024;
   if (nv <= 64 * 4)
-    f(std::integral_constant<int, 64>(), std::integral_constant<int, 4>(), std::true_type());
+    f(Int<64>(), Int<4>(), std::true_type(), Int<0>());
+  else if (!few && nv <= 64 * 8)
+    f(Int<64>(), Int<8>(), std::true_type(), Int<0>());
+  else if (!few && nv <= 64 * 16)
+    f(Int<64>(), Int<16>(), std::true_type(), Int<0>());
   else if (nv <= 256 * 4)
-    f(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), std::true_type());
+    f(Int<256>(), Int<4>(), std::true_type(), Int<0>());
   else if (nv <= 256 * 8)
-    f(std::integral_constant<int, 256>(), std::integral_constant<int, 8>(), std::true_type());
+    f(Int<256>(), Int<8>(), std::true_type(), Int<0>());
+  else if (nv <= 512 * 7)
+    f(Int<512>(), Int<8>(), std::true_type(), Int<0>());
   else if (nv <= 1024 * 4)
-    f(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>(), std::true_type());
+    f(Int<1024>(), Int<4>(), std::true_type(), Int<0>());
   else if (nv <= 1024 * 8)
-    f(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>(), std::true_type());
+    f(Int<1024>(), Int<8>(), std::true_type(), Int<0>());
   else if (nv <= 1024 * 16)
-    f(std::integral_constant<int, 1024>(), std::integral_constant<int, 16>(), std::true_type());
+    f(Int<1024>(), Int<16>(), std::true_type(), Int<0>());
+  else if (nv <= 1024 * 32)  // 384 KB of registers and 128 KB of LDS
+    f(Int<1024>(), Int<32>(), std::true_type(), Int<8>());
   else
-    f(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>(), std::false_type());
+    f(Int<1024>(), Int<8>(), std::false_type(), Int<0>());
+}
+
+// launch(first row, workgroups) for all rows of a kernel that takes `per` rows a workgroup of `threads`: HIP refuses
+// grids of 2^32 threads.
+template <typename F>
+void row_parts(int64_t rows, int per, int threads, F launch) {
+  const int64_t most = ((1ll << 31) / threads) * per;
+  for (int64_t r0 = 0; r0 < rows; r0 += most)
+    launch(r0, (unsigned)((std::min(most, rows - r0) + per - 1) / per));
+}
+
+template <typename T, int TH, int NV, bool RES>
+void launch_logp(const sk_logits *x, float *logp, float *stats, float *rowc, hipStream_t st) {
+  constexpr int kPer = TH == 64 ? 4 : 1, kThreads = TH * kPer;
+  row_parts(x->rows, kPer, kThreads, [&](int64_t r0, unsigned blocks) {
+    hipLaunchKernelGGL((k_logp<T, TH, NV, RES>), dim3(blocks), dim3(kThreads), 0, st, rows_of(x), r0, x->rows, logp,
+                       (float2 *)stats, rowc);
+  });
 }
 
 template <typename T>
 void run_logp_t(const sk_logits *x, float *logp, float *stats, float *rowc, hipStream_t st) {
-  with_row_shape<T>(x->vocab / Vec<T>::N, [&](auto th, auto nv, auto res) {
-    constexpr int TH = decltype(th)::value;
-    const int64_t blocks = TH == 64 ? (x->rows + 3) / 4 : x->rows;
-    hipLaunchKernelGGL((k_logp<T, TH, decltype(nv)::value, decltype(res)::value>), dim3((unsigned)blocks),
-                       dim3(TH == 64 ? 256 : TH), 0, st, rows_of(x), x->rows, logp, (float2 *)stats, rowc);
+  with_row_shape(x->vocab / Vec<T>::N, x->rows, [&](auto th, auto nv, auto res, auto) {
+    // a row that is read once need not be held: above 1024 x 8 vectors it is streamed
+    constexpr int TH = decltype(th)::value, NV = decltype(nv)::value;
+    if constexpr (TH == 1024 && NV > 8)
+      launch_logp<T, 1024, 8, false>(x, logp, stats, rowc, st);
+    else
+      launch_logp<T, TH, NV, decltype(res)::value>(x, logp, stats, rowc, st);
   });
 }
 
@@ -494,11 +547,12 @@ void run_logp(const sk_logits *x, float *logp, float *stats, float *rowc, hipStr
 template <typename T>
 void run_policy_t(const sk_logits *x, const Policy &p, float *logp, float *token_loss, void *d, int64_t ldd,
                   hipStream_t st) {
-  with_row_shape<T>(x->vocab / Vec<T>::N, [&](auto th, auto nv, auto res) {
-    constexpr int TH = decltype(th)::value;
-    const int64_t blocks = TH == 64 ? (x->rows + 3) / 4 : x->rows;
-    hipLaunchKernelGGL((k_policy<T, TH, decltype(nv)::value, decltype(res)::value>), dim3((unsigned)blocks),
-                       dim3(TH == 64 ? 256 : TH), 0, st, rows_of(x), x->rows, p, logp, token_loss, d, ldd);
+  with_row_shape(x->vocab / Vec<T>::N, x->rows, [&](auto th, auto nv, auto res, auto nl) {
+    constexpr int TH = decltype(th)::value, kPer = TH == 64 ? 4 : 1, kThreads = TH * kPer;
+    row_parts(x->rows, kPer, kThreads, [&](int64_t r0, unsigned blocks) {
+      hipLaunchKernelGGL((k_policy<T, TH, decltype(nv)::value, decltype(res)::value, decltype(nl)::value>), dim3(blocks),
+                         dim3(kThreads), 0, st, rows_of(x), r0, x->rows, p, logp, token_loss, d, ldd);
+    });
   });
 }
 
@@ -513,8 +567,7 @@ void run_logp_grad_t(const sk_logits *x, const float *stats, const float *dlogp,
                      hipStream_t st) {
   constexpr int NV = 4;
   const int64_t pieces = std::max<int64_t>(1, (x->vocab / Vec<T>::N + 256 * NV - 1) / (256 * NV));
-  // a grid holds fewer than 2^31 workgroups
-  const int64_t most = std::max<int64_t>(1, (INT32_MAX - 1) / pieces);
+  const int64_t most = std::max<int64_t>(1, kGridBlocks / pieces);
   for (int64_t r0 = 0; r0 < x->rows; r0 += most) {
     Rows r = rows_of(x);
     r.x = (const T *)r.x + r0 * r.ld;
