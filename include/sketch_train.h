@@ -47,7 +47,7 @@ int sketch_embed(const void *weight, sk_dtype dtype, int64_t vocab, int64_t widt
  * Gradient of the lookup: for each of `batch` groups of n tokens
  *   out[v] (+)= scale * sum over t with ids[t] = v of dy[t]
  * with the sum in fp32 in an order that the ids alone set (that of t in pieces of
- * 16 or 64 tokens, then the pieces), rounded once to out_dtype; ids outside [0, vocab) add nothing.
+ * 16, 32 or 64 tokens, then the pieces), rounded once to out_dtype; ids outside [0, vocab) add nothing.
  * batch > 1 gives one gradient per example.  Rows that no id names are zeroed
  * (accumulate = 0) or kept (accumulate = 1).
  *   dy       [batch, n, width], row stride ld >= width elements.

@@ -39,7 +39,22 @@ struct AdamStep {
   uint32_t step;
   Key key;
   const float *scale;
+  // a list of up to kFewChunks chunks: its norm's partial sums are added up here
+  const double *part;
+  int64_t n_part;
+  float max_norm;
+  float *norm;
 };
+
+constexpr int64_t kFewChunks = 256;
+
+// The scale of the gradients from the sum of their squares: NaN where the norm is not finite, so that the step changes
+// nothing.
+__device__ __forceinline__ float clip_scale(double sum, float gs, float max_norm, float *norm) {
+  const float nm = (float)(fabs((double)gs) * sqrt(sum));
+  if (norm) *norm = nm;
+  return nm < INFINITY ? gs * fminf(1.0f, max_norm / (nm + 1e-6f)) : NAN;
+}
 
 constexpr int kPer = 8;  // consecutive elements of a thread: a 64-element block is 8 lanes
 
@@ -166,7 +181,12 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
                                                AdamStep s, void *__restrict__ mp, void *__restrict__ vp,
                                                uint8_t *__restrict__ mexp, uint8_t *__restrict__ vexp) {
 #pragma clang fp contract(off)
-  const float scale = s.scale ? *s.scale : 1.0f;
+  float scale = s.scale ? *s.scale : 1.0f;
+  if (s.part) {  // in the order of the chunks, by every workgroup: one launch and one wait less than k_adamw_scale
+    __shared__ double lds[4];
+    const double sum = block_all<4>(threadIdx.x < s.n_part ? s.part[threadIdx.x] : 0.0, OpAdd(), lds);
+    scale = clip_scale(sum, scale, s.max_norm, blockIdx.x == 0 && first == 0 && threadIdx.x == 0 ? s.norm : nullptr);
+  }
   if (!(fabsf(scale) < INFINITY)) return;
   const AdamChunk ck = chunks[blockIdx.x];
   const AdamTensor t = tensors[ck.tensor];
@@ -263,7 +283,6 @@ __global__ __launch_bounds__(256) void k_adamw_norm(const AdamTensor *__restrict
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-// The norm and the scale of the gradients: NaN where the norm is not finite, so that the step changes nothing.
 __global__ __launch_bounds__(1024) void k_adamw_scale(const double *__restrict__ part, int64_t n,
                                                       const float *__restrict__ grad_scale, float max_norm,
                                                       float *__restrict__ norm, float *__restrict__ scale) {
@@ -271,12 +290,7 @@ __global__ __launch_bounds__(1024) void k_adamw_scale(const double *__restrict__
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < n; i += 1024) s += part[i];
   s = block_all<16>(s, OpAdd(), lds);
-  if (threadIdx.x == 0) {
-    const float gs = grad_scale ? *grad_scale : 1.0f;
-    const float nm = (float)(fabs((double)gs) * sqrt(s));
-    if (norm) *norm = nm;
-    *scale = nm < INFINITY ? gs * fminf(1.0f, max_norm / (nm + 1e-6f)) : NAN;
-  }
+  if (threadIdx.x == 0) *scale = clip_scale(s, grad_scale ? *grad_scale : 1.0f, max_norm, norm);
 }
 
 __global__ __launch_bounds__(256) void k_adamw_moments(int64_t groups, const uint2 *__restrict__ m,
@@ -435,8 +449,13 @@ int sketch_adamw_apply(sk_adamw *h, const sk_adamw_step *a, void *const *params,
   s.eps = (float)a->eps;
   s.step = (uint32_t)a->step;
   s.key = h->key;
-  s.scale = a->max_norm > 0.0 ? h->d_scale : a->grad_scale;
-  for (int pass = a->max_norm > 0.0 ? 0 : 1; pass < 2; ++pass) {
+  const bool clip = a->max_norm > 0.0, few = h->n_chunks <= kFewChunks;
+  s.scale = clip && !few ? h->d_scale : a->grad_scale;
+  s.part = clip && few ? h->d_part : nullptr;
+  s.n_part = h->n_chunks;
+  s.max_norm = (float)a->max_norm;
+  s.norm = a->norm;
+  for (int pass = clip ? 0 : 1; pass < 2; ++pass) {
     for (int l0 = 0; l0 < h->n_tensors; l0 += kAdamPtrs) {
       const int l1 = std::min(l0 + kAdamPtrs, h->n_tensors);
       AdamPtrs ptrs;
@@ -463,7 +482,7 @@ int sketch_adamw_apply(sk_adamw *h, const sk_adamw_step *a, void *const *params,
         launch_adamw<bf16, bf16>(h->state, masters != nullptr, grid, st, h->d_tensors, ck, l0, ptrs, s, a);
       }
     }
-    if (pass == 0)
+    if (pass == 0 && !few)
       hipLaunchKernelGGL(k_adamw_scale, dim3(1), dim3(1024), 0, st, h->d_part, h->n_chunks, a->grad_scale,
                          (float)a->max_norm, a->norm, h->d_scale);
   }

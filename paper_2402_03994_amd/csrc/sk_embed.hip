@@ -9,8 +9,9 @@
 //   k_eg_rank   sorts each run of up to 4096 tokens of a group by (id,
 //               position): an entry's place is how many entries are smaller,
 //               counted by brute force (64 entries a workgroup against all of
-//               the run; 4096 comparisons an entry over the whole chip take
-//               less time than the barriers of a sort in one workgroup's LDS).
+//               the run, 64 comparisons an instruction: their mask's bits are
+//               counted in the scalar unit), which takes the whole chip less
+//               time than a sort's barriers take one workgroup.
 //               The launch's other workgroups zero the gradient meanwhile.
 //   k_eg_merge  joins up to 16 sorted runs: an entry's place is its own plus
 //               what a binary search in each other run gives, one lane a run.
@@ -23,6 +24,7 @@
 // piece.  Bound by writing the gradient (vocab x width per group); to zero all
 // of it costs the named rows a second write and spares the others a look-up.
 #include <algorithm>
+#include <type_traits>
 
 #include "sk_train.h"
 
@@ -30,7 +32,8 @@ using namespace sk;
 
 namespace {
 
-constexpr uint32_t kNoId = 0xFFFFFFFFu;  // of a masked token: sorts to the end
+constexpr int kNoId = 0x7FFFFFFE;    // of a masked token: sorts to the end
+constexpr int kBeyond = 0x7FFFFFFF;  // beyond a run: above whatever is compared with it
 constexpr int kRun = 4096;               // tokens ranked by brute force
 constexpr int kMergeRuns = 16;
 
@@ -86,7 +89,8 @@ __global__ __launch_bounds__(256) void k_embed(const W *__restrict__ w, int64_t 
 }
 
 struct Entry {  // a token of its group: id and position
-  uint32_t id, pos;
+  int id;
+  uint32_t pos;
 };
 
 // What is to be zeroed: `bytes` bytes, an even number, from an even address on.
@@ -114,7 +118,8 @@ __global__ __launch_bounds__(512) void k_eg_rank(const void *__restrict__ ids, i
                                                  int runs, int tiles, int rank_blocks, Entry *__restrict__ sorted,
                                                  Zeros z) {
   __shared__ int part[8][64];
-  if (blockIdx.x >= rank_blocks) {
+  // those that rank come first: dealt out among those that zero they take longer (65536 tokens: 41 us, 48 to 60)
+  if (blockIdx.x >= (unsigned)rank_blocks) {
     zero_part(z, blockIdx.x - rank_blocks, gridDim.x - rank_blocks);
     return;
   }
@@ -122,36 +127,54 @@ __global__ __launch_bounds__(512) void k_eg_rank(const void *__restrict__ ids, i
   const int64_t run = blockIdx.x / (unsigned)tiles, b = run / runs, p0 = (run % runs) * kRun;
   const int tile = blockIdx.x % (unsigned)tiles, len = (int)(n - p0 < kRun ? n - p0 : kRun);
   if (tile * 64 >= len) return;
-  auto key = [&](int i) -> uint32_t {
-    if (i >= len) return kNoId;
+  auto key = [&](int i) -> int {
+    if (i >= len) return kBeyond;
     const int64_t v = id_at(ids, index, b * n + p0 + i);
-    return v >= 0 && v < vocab ? (uint32_t)v : kNoId;
+    return v >= 0 && v < vocab ? (int)v : kNoId;
   };
-  const uint32_t mine = key(tile * 64 + lane);
+  const int mine = key(tile * 64 + lane);
+  // The wave's share of the run: blocks wave, wave + 8, ..  Entries of earlier blocks count where they are not above an
+  // entry (one less is below it), so that entries of one id stay in order.
+  constexpr int kBlocks = kRun / 64 / 8;
+  const int blocks = (len + 63) / 64, own = wave == tile % 8;
+  int theirs[kBlocks];
+#pragma unroll
+  for (int k = 0; k < kBlocks; ++k) {
+    const int blk = wave + 8 * k;
+    theirs[k] = kBeyond;
+    if (blk < blocks && blk != tile) theirs[k] = key(blk * 64 + lane) - (blk < tile);
+  }
   int count = 0;
-  for (int blk = wave; blk * 64 < len; blk += 8) {
-    const uint32_t theirs = key(blk * 64 + lane);
-    if (blk < tile) {  // earlier entries of the same id come first
-#pragma unroll 16
-      for (int j = 0; j < 64; ++j) count += (uint32_t)__builtin_amdgcn_readlane((int)theirs, j) <= mine;
-    } else if (blk > tile) {
-#pragma unroll 16
-      for (int j = 0; j < 64; ++j) count += (uint32_t)__builtin_amdgcn_readlane((int)theirs, j) < mine;
-    } else {
-#pragma unroll 16
-      for (int j = 0; j < 64; ++j) {
-        const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)theirs, j);
-        count += k < mine || (k == mine && j < lane);
-      }
+  auto rank = [&](auto some) {
+#pragma unroll 8
+    for (int i = 0; i < 64; ++i) {
+      const int m = __builtin_amdgcn_readlane(mine, i);
+      int c = 0;
+#pragma unroll
+      for (int k = 0; k < decltype(some)::value; ++k) c += __builtin_popcountll(__ballot(theirs[k] < m));
+      count = lane == i ? c : count;
+    }
+  };
+  if (blocks <= 8)
+    rank(std::integral_constant<int, 1>());
+  else if (blocks <= 24)
+    rank(std::integral_constant<int, 3>());
+  else
+    rank(std::integral_constant<int, kBlocks>());
+  if (own) {  // the tile against itself
+#pragma unroll 8
+    for (int j = 0; j < 64; ++j) {
+      const int k = __builtin_amdgcn_readlane(mine, j);
+      count += k < mine || (k == mine && j < lane);
     }
   }
   part[wave][lane] = count;
   __syncthreads();
   if (wave == 0 && tile * 64 + lane < len) {
-    int rank = 0;
+    int place = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rank += part[i][lane];
-    sorted[b * n + p0 + rank] = Entry{mine, (uint32_t)(p0 + tile * 64 + lane)};
+    for (int i = 0; i < 8; ++i) place += part[i][lane];
+    sorted[b * n + p0 + place] = Entry{mine, (uint32_t)(p0 + tile * 64 + lane)};
   }
 }
 
@@ -173,7 +196,7 @@ __global__ __launch_bounds__(256) void k_eg_merge(const Entry *__restrict__ in, 
   const Entry *run = in + b * n + r0;
   while (lo < hi) {
     const int64_t mid = (lo + hi) >> 1;
-    const uint32_t k = run[mid].id;
+    const int k = run[mid].id;
     if (r < own ? k <= mine.id : k < mine.id)
       lo = mid + 1;
     else
@@ -218,7 +241,7 @@ __device__ __forceinline__ void put_part(float *row, int c, int width, const flo
 template <typename G, typename O>
 __global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *__restrict__ dy,
                                                 O *__restrict__ out) {
-  constexpr int N = Vec<G>::N, U = 32 / N;
+  constexpr int N = Vec<G>::N, U = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t job = (int64_t)blockIdx.x * 4 + wave;
   if (job >= jobs) return;
@@ -227,9 +250,9 @@ __global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *_
   const Entry *k = s.sorted + b * s.n;
   Entry e{kNoId, 0};
   if (lane < s.R && e0 + lane < s.n) e = k[e0 + lane];
-  const uint32_t before = e0 > 0 ? k[e0 - 1].id : kNoId, after = e0 + s.R < s.n ? k[e0 + s.R].id : kNoId;
+  const int before = e0 > 0 ? k[e0 - 1].id : kNoId, after = e0 + s.R < s.n ? k[e0 + s.R].id : kNoId;
   float acc[N];
-  uint32_t cur = kNoId;
+  int cur = kNoId;
   bool began = true;
   O *const o = out + b * s.vocab * s.width;
   auto flush = [&](bool ends) {
@@ -243,7 +266,7 @@ __global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *_
     float x[U][N];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)e.id, i0 + u);
+      const int id = __builtin_amdgcn_readlane(e.id, i0 + u);
       const uint32_t pos = (uint32_t)__builtin_amdgcn_readlane((int)e.pos, i0 + u);
       if (id == kNoId) continue;  // the rest of the tile is empty
       const G *row = dy + (b * s.n + pos) * s.ld;
@@ -258,7 +281,7 @@ __global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *_
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)e.id, i0 + u);
+      const int id = __builtin_amdgcn_readlane(e.id, i0 + u);
       if (id == kNoId) continue;
       if (id != cur) {
         flush(true);
@@ -284,7 +307,7 @@ __global__ __launch_bounds__(256) void k_eg_join(Sums s, O *__restrict__ out) {
   const int64_t bt = blockIdx.x / (unsigned)pieces, b = bt / s.tiles, tile = bt % s.tiles, e1 = (tile + 1) * s.R;
   if (e1 >= s.n) return;
   const Entry *k = s.sorted + b * s.n;
-  const uint32_t id = k[e1 - 1].id;
+  const int id = k[e1 - 1].id;
   if (id == kNoId || k[e1].id != id) return;
   if (k[e1 - s.R].id == id && e1 > s.R && k[e1 - s.R - 1].id == id) return;  // began earlier
   int64_t heads = 0;
@@ -305,8 +328,20 @@ __global__ __launch_bounds__(256) void k_eg_join(Sums s, O *__restrict__ out) {
       if (c + i < s.width) acc[i] += row[c + i];
   };
   if (wave == 0) add(s.tail + bt * s.width);
-#pragma unroll 4
-  for (int64_t h = wave; h < heads; h += 4) add(s.head + (bt + 1 + h) * s.width);
+  const float *head = s.head + (bt + 1) * s.width;
+  int64_t h = wave;
+  for (; h + 28 < heads; h += 32) {  // eight loads at a time: a frequent id has hundreds of heads
+    float x[8][N];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[u][i] = c + i < s.width ? head[(h + 4 * u) * s.width + c + i] : 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) acc[i] += x[u][i];
+  }
+  for (; h < heads; h += 4) add(head + h * s.width);
   if (wave)
 #pragma unroll
     for (int i = 0; i < N; ++i) part[wave - 1][lane * N + i] = acc[i];
@@ -329,9 +364,10 @@ void run_embed(const void *w, int64_t vocab, int64_t width, int64_t ld, const vo
   });
 }
 
-// Entries a wave adds up: few where there are few waves (8192 fill the chip), else enough that little is left to join.
+// Entries a wave adds up: few while there are few waves (8192 fill the chip), else enough that little is left to join.
 int eg_tile(int64_t batch, int64_t n, int64_t width) {
-  return batch * n * ((width + 255) / 256) > 8192 * 16 ? 64 : 16;
+  const int64_t work = batch * n * ((width + 511) / 512);
+  return work <= 16384 * 16 ? 16 : work <= 16384 * 32 ? 32 : 64;
 }
 
 struct EgWork {

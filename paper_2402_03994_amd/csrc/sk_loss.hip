@@ -132,7 +132,8 @@ struct Tile {
     }
     return z;
   }
-  // w exp(scale (x - m)) to the row d
+  // w exp(scale (x - m)) to the row d, past the caches: the logits stay in them for the gradient pass (4096 x 50257 bf16
+  // read twice and written once: 169 us with ordinary stores, 153 us)
   __device__ __forceinline__ void store(T *d, Cut q, int v0, int tid, float m, float k2, float w) const {
     T *a = d + q.head;
 #pragma unroll
@@ -143,7 +144,7 @@ struct Tile {
         float f[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) f[e] = w * __builtin_amdgcn_exp2f((Vec<T>::get(v, e) - m) * k2);
-        Vec<T>::store(a + (int64_t)i * N, Vec<T>::pack(f));
+        Vec<T>::stream(a + (int64_t)i * N, Vec<T>::pack(f));
       }
     }
     const int j = single(q, v0, tid);
@@ -156,7 +157,7 @@ template <typename T, int THREADS>
 __device__ __forceinline__ void row_zero(T *d, int vocab, int v0, int v1, int tid) {
   const Cut q = cut_of(d, vocab);
   v1 = v1 < q.nv ? v1 : q.nv;
-  for (int i = v0 + tid; i < v1; i += THREADS) Vec<T>::store(d + q.head + (int64_t)i * Vec<T>::N, u32x4{0, 0, 0, 0});
+  for (int i = v0 + tid; i < v1; i += THREADS) Vec<T>::stream(d + q.head + (int64_t)i * Vec<T>::N, u32x4{0, 0, 0, 0});
   const int j = Tile<T, THREADS, 1>::single(q, v0, tid);
   if (j >= 0) d[j] = from_f32<T>(0.0f);
 }
@@ -565,7 +566,7 @@ struct PairTotal {  // of the preference loss
 template <typename T>
 void run_logp_grad_t(const sk_logits *x, const float *stats, const float *dlogp, void *d, int64_t ldd, PairTotal total,
                      hipStream_t st) {
-  constexpr int NV = 4;
+  constexpr int NV = 2;  // 16384 x 50257 bf16 rows, 40% masked, both passes: 642 us with 2, 649 with 4, 692 with 8
   const int64_t pieces = std::max<int64_t>(1, (x->vocab / Vec<T>::N + 256 * NV - 1) / (256 * NV));
   const int64_t most = std::max<int64_t>(1, kGridBlocks / pieces);
   for (int64_t r0 = 0; r0 < x->rows; r0 += most) {

@@ -106,6 +106,8 @@ __device__ __forceinline__ T block_all(T v, Op op, T *lds) {
 
 // 16 bytes of elements, aligned to one element only: the loads and stores of gfx950 take any alignment.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 template <typename T>
 struct Vec {
   static constexpr int N = 16 / sizeof(T);
@@ -114,6 +116,13 @@ struct Vec {
   };
   static __device__ __forceinline__ u32x4 load(const T *p) { return ((const Any *)p)->v; }
   static __device__ __forceinline__ void store(T *p, u32x4 v) { ((Any *)p)->v = v; }
+  // past the caches: for what is not read again soon, so that something else stays there
+  static __device__ __forceinline__ void stream(T *p, u32x4 v) {
+    if (sizeof(T) == 4)
+      __builtin_nontemporal_store(v, (u32x4_at4 *)p);
+    else
+      __builtin_nontemporal_store(v, (u32x4_at2 *)p);
+  }
   static __device__ __forceinline__ float get(u32x4 v, int i) {
     if (sizeof(T) == 4) return __uint_as_float(v[i]);
     return __uint_as_float((i & 1) ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16);
