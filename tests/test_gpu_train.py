@@ -594,3 +594,68 @@ def test_binding_refuses(dev):
         fw.policy_loss(x, t, v, v, v, kl_coef=0.1)
     with pytest.raises(fw.SketchError):
         fw.token_logp(x, t, scale=0.0)
+
+
+def test_adamw_norm_of_many_chunks(dev):
+    """Lists of more than 256 chunks have their norm added up by a kernel of its own."""
+    import paper_2402_03994_amd as fw
+    sizes = [3_000_001, 70, 1_500_000]
+    opt = fw.AdamW(sizes)
+    g = [torch.randn(n, device=dev) * 0.01 for n in sizes]
+    p = [torch.zeros(n, device=dev) for n in sizes]
+    want = np.sqrt(sum((host(t) ** 2).sum() for t in g))
+    norm = opt.step(p, g, 1, lr=0.1, betas=(0.5, 0.5), eps=1e-3, weight_decay=0.0, max_norm=2.0)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    s = np.float32(2.0) / (np.float32(float(norm)) + np.float32(1e-6))
+    for n, at, t in zip(sizes, (0, 3_000_064, 3_000_192), g):
+        m, v = O.adamw_moments(np.zeros(n, np.float32), np.zeros(n, np.float32), t.cpu().numpy(), 0.5, 0.5, s)
+        assert np.array_equal(opt.m[at:at + n].cpu().numpy(), m) and np.array_equal(opt.v[at:at + n].cpu().numpy(), v)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-8])
+def test_adamw_small_second_moments(dev, eps):
+    """Second moments down to the smallest fp32 numbers, with and without an eps that hides them."""
+    import paper_2402_03994_amd as fw
+    n = 4000
+    opt = fw.AdamW([n])
+    g = torch.logspace(-24, 3, n, device=dev)  # squares from 0 to 1e6
+    g[n // 2:] *= -1
+    p = torch.zeros(n, device=dev)
+    opt.step([p], [g], 1, lr=1.0, betas=(0.9, 0.999), eps=eps, weight_decay=0.0)
+    m, v = opt.m[:n].cpu().numpy(), opt.v[:n].cpu().numpy()
+    ref = O.adamw_param(np.zeros(n), m, v, 1, 1.0, 0.9, 0.999, eps, 0.0)
+    got = host(p)
+    big = ~np.isfinite(ref) | (np.abs(ref) > 1e30)  # v = 0: m / eps
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    # beta powers in fp32 and a few roundings of the ratio
+    assert (np.abs(got - ref)[~big] <= 2.0 ** -20 * np.abs(ref)[~big]).all()
+    assert np.array_equal(np.sign(got[big]), np.sign(ref[big]))
+
+
+def test_embed_grad_of_many_runs(dev):
+    """More than 16 sorted runs: two rounds of merges."""
+    import paper_2402_03994_amd as fw
+    r = np.random.default_rng(8)
+    n, vocab = 70001, 90000
+    ids = np.minimum((vocab + 1.0) ** r.random(n) - 1, vocab - 1).astype(np.int64)
+    ids[:300] = -1
+    dy = r.standard_normal((n, 3)).astype(np.float32)
+    got = host(fw.embed_grad(torch.from_numpy(dy).to(dev), torch.from_numpy(ids).to(dev), vocab))
+    ref, size = O.embed_grad(dy, ids, vocab, 1.0)
+    runs = np.bincount(ids[ids >= 0], minlength=vocab)[:, None]
+    assert (np.abs(got - ref) <= (runs + 3) * 2.0 ** -24 * size).all()
+
+
+def test_example_trains(dev):
+    """The operators and the sketch together: both losses fall, sketched gradients keep their angles."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "subspace_preference.py")
+    spec = importlib.util.spec_from_file_location("subspace_preference", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    pref, pol, err = ex.main(40)
+    assert abs(pref[0] - np.log(2)) < 1e-6  # no difference from the reference yet
+    assert pref[-1] < 0.5 * pref[0]
+    assert pol[-1] < pol[0]
+    assert err < 6 / np.sqrt(ex.D)  # a cosine of two sketched vectors is off by about 1 / sqrt(D)
