@@ -208,13 +208,16 @@ __global__ __launch_bounds__(256) void k_eg_merge(const Entry *__restrict__ in, 
   if (r == 0) out[b * n + g0 + rank] = mine;
 }
 
-// the N columns from c on of a row of sums to out or (accumulate) onto it
-template <typename O, int N>
+// the N columns from c on of a row of sums to out or (accumulate) onto it; WHOLE: all of them are in the row
+template <typename O, int N, bool WHOLE>
 __device__ __forceinline__ void put(O *row, int c, int width, const float *acc, float scale, int accumulate) {
-  if (c + N <= width) {
+  if (WHOLE || c + N <= width) {
     float f[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = scale * acc[i] + (accumulate ? to_f32(row[c + i]) : 0.0f);
+    for (int i = 0; i < N; ++i) f[i] = scale * acc[i];
+    if (accumulate)
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i] += to_f32(row[c + i]);
     store_n<O, N>(row + c, f);
   } else {
 #pragma unroll
@@ -222,6 +225,7 @@ __device__ __forceinline__ void put(O *row, int c, int width, const float *acc, 
       if (c + i < width) row[c + i] = from_f32<O>(scale * acc[i] + (accumulate ? to_f32(row[c + i]) : 0.0f));
   }
 }
+
 // Few tokens, in one launch: a workgroup owns `rows` rows of a group's gradient, lists the tokens that name them, in
 // order, and writes every row, the named ones as the sum of their tokens and the others as zeros.
 constexpr int kFewTokens = 512;
@@ -302,7 +306,7 @@ __global__ __launch_bounds__(256) void k_eg_few(const G *__restrict__ dy, int64_
             for (int i = 0; i < N; ++i) acc[i] += x[u][i];
       }
     }
-    if ((named || !accumulate) && c < width) put<O, N>(o, c, width, acc, scale, accumulate);
+    if ((named || !accumulate) && c < width) put<O, N, false>(o, c, width, acc, scale, accumulate);
   }
 }
 
@@ -315,22 +319,20 @@ struct Sums {
   float *head, *tail;  // [batch, tiles, width]
 };
 
-template <int N>
-__device__ __forceinline__ void put_part(float *row, int c, int width, const float *acc) {
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (c + i < width) row[c + i] = acc[i];
-}
-
-template <typename G, typename O>
+// WHOLE: every lane has a whole vector of columns; the last lane's of a width that is no multiple of one begin earlier,
+// so that a few columns are added up and written twice, with the same values (65536 x 767 bf16: 71 us with the last
+// columns one by one).  That is not for accumulation, where the second of two waves would add to the first one's sum.
+template <typename G, typename O, bool WHOLE>
 __global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *__restrict__ dy,
                                                 O *__restrict__ out) {
-  constexpr int N = Vec<G>::N, U = 4;
+  constexpr int N = Vec<G>::N, U = WHOLE ? 16 : 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t job = (int64_t)blockIdx.x * 4 + wave;
   if (job >= jobs) return;
   const int64_t bt = job / s.pieces, b = bt / s.tiles, tile = bt % s.tiles, e0 = tile * s.R;
-  const int c = (int)(job % s.pieces) * 64 * N + lane * N;
+  int c = (int)(job % s.pieces) * 64 * N + lane * N;
+  const bool idle = c >= s.width;
+  if (WHOLE && c + N > s.width) c = s.width - N;
   const Entry *k = s.sorted + b * s.n;
   Entry e{kNoId, 0};
   if (lane < s.R && e0 + lane < s.n) e = k[e0 + lane];
@@ -340,27 +342,39 @@ __global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *_
   bool began = true;
   O *const o = out + b * s.vocab * s.width;
   auto flush = [&](bool ends) {
-    if (cur == kNoId) return;
-    if (began && ends)
-      put<O, N>(o + (int64_t)cur * s.width, c, s.width, acc, s.scale, s.accumulate);
-    else
-      put_part<N>((began ? s.tail : s.head) + bt * s.width, c, s.width, acc);
+    if (cur == kNoId || idle) return;
+    if (began && ends) {
+      put<O, N, WHOLE>(o + (int64_t)cur * s.width, c, s.width, acc, s.scale, s.accumulate);
+    } else {
+      float *part = (began ? s.tail : s.head) + bt * s.width + c;
+      if (WHOLE) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) Vec<float>::store(part + i, Vec<float>::pack(acc + i));
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (c + i < s.width) part[i] = acc[i];
+      }
+    }
   };
   for (int i0 = 0; i0 < s.R; i0 += U) {
-    float x[U][N];
+    u32x4 x[U];
+    float y[WHOLE ? 1 : U][N];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int id = __builtin_amdgcn_readlane(e.id, i0 + u);
       const uint32_t pos = (uint32_t)__builtin_amdgcn_readlane((int)e.pos, i0 + u);
       if (id == kNoId) continue;  // the rest of the tile is empty
       const G *row = dy + (b * s.n + pos) * s.ld;
-      if (c + N <= s.width) {
+      if (WHOLE) {
+        if (!idle) x[u] = Vec<G>::load(row + c);
+      } else if (c + N <= s.width) {
         const u32x4 v = Vec<G>::load(row + c);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[u][i] = Vec<G>::get(v, i);
+        for (int i = 0; i < N; ++i) y[u][i] = Vec<G>::get(v, i);
       } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[u][i] = c + i < s.width ? to_f32(row[c + i]) : 0.0f;
+        for (int i = 0; i < N; ++i) y[u][i] = c + i < s.width ? to_f32(row[c + i]) : 0.0f;
       }
     }
 #pragma unroll
@@ -375,7 +389,7 @@ __global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *_
         for (int i = 0; i < N; ++i) acc[i] = 0.0f;
       }
 #pragma unroll
-      for (int i = 0; i < N; ++i) acc[i] += x[u][i];
+      for (int i = 0; i < N; ++i) acc[i] += WHOLE ? Vec<G>::get(x[u], i) : y[WHOLE ? 0 : u][i];
     }
   }
   flush(after != cur);
@@ -391,9 +405,9 @@ __global__ __launch_bounds__(256) void k_eg_join(Sums s, O *__restrict__ out) {
   const int64_t bt = blockIdx.x / (unsigned)pieces, b = bt / s.tiles, tile = bt % s.tiles, e1 = (tile + 1) * s.R;
   if (e1 >= s.n) return;
   const Entry *k = s.sorted + b * s.n;
-  const int id = k[e1 - 1].id;
-  if (id == kNoId || k[e1].id != id) return;
-  if (k[e1 - s.R].id == id && e1 > s.R && k[e1 - s.R - 1].id == id) return;  // began earlier
+  // all at once: most workgroups only wait for these
+  const int id = k[e1 - 1].id, next = k[e1].id, first = k[e1 - s.R].id, before = e1 > s.R ? k[e1 - s.R - 1].id : kNoId;
+  if (id == kNoId || next != id || (first == id && before == id)) return;  // ends here, or began earlier
   int64_t heads = 0;
   for (;;) {
     const int64_t at = e1 + (heads + lane) * s.R;
@@ -435,7 +449,7 @@ __global__ __launch_bounds__(256) void k_eg_join(Sums s, O *__restrict__ out) {
   for (int w = 0; w < 3; ++w)
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] += part[w][lane * N + i];
-  if (c < s.width) put<O, N>(out + (b * s.vocab + id) * s.width, c, s.width, acc, s.scale, s.accumulate);
+  if (c < s.width) put<O, N, false>(out + (b * s.vocab + id) * s.width, c, s.width, acc, s.scale, s.accumulate);
 }
 
 template <typename W, typename O>
@@ -510,9 +524,11 @@ void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batc
   s.accumulate = accumulate;
   s.scale = scale;
   const int64_t jobs = batch * w.tiles * s.pieces;
-  if (jobs)
-    hipLaunchKernelGGL((k_eg_sum<G, O>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, s, jobs, (const G *)dy,
-                       out);
+  const dim3 sum_blocks((unsigned)((jobs + 3) / 4));
+  if (jobs && (width % Vec<G>::N == 0 || (!accumulate && width >= Vec<G>::N)))
+    hipLaunchKernelGGL((k_eg_sum<G, O, true>), sum_blocks, dim3(256), 0, st, s, jobs, (const G *)dy, out);
+  else if (jobs)
+    hipLaunchKernelGGL((k_eg_sum<G, O, false>), sum_blocks, dim3(256), 0, st, s, jobs, (const G *)dy, out);
   if (w.tiles > 1)
     hipLaunchKernelGGL((k_eg_join<O>), dim3((unsigned)(batch * w.tiles * ((width + 255) / 256))), dim3(256), 0, st, s,
                        out);
