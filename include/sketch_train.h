@@ -135,7 +135,7 @@ int sketch_preference_loss(const sk_logits *x, const void *offsets, sk_index off
                            int64_t work_bytes, void *stream);
 
 /*
- * AdamW over a list of parameter tensors, one launch for up to 128 of them:
+ * AdamW over a list of parameter tensors, one launch for up to 160 of them:
  *   g = g s;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
  *   p = p (1 - lr wd_l) - lr / (1 - b1^step) m / (sqrt(v / (1 - b2^step)) + eps)
  * in fp32, each product and sum of the two moments rounded by itself, so that

@@ -2,7 +2,7 @@
 // or in 8 bits (C ABI of include/sketch_train.h).
 //
 // The tensors are cut into chunks of 4096 elements, one workgroup each, by a
-// table made at creation, so that one launch covers up to 128 tensors (their
+// table made at creation, so that one launch covers up to 160 tensors (their
 // addresses travel in the kernel's arguments).  A thread owns eight consecutive
 // elements at a time (16-byte loads of bf16, one Philox block for its
 // parameters and two for its moments) and eight lanes a 64-element block, whose
@@ -17,7 +17,7 @@ using namespace sk;
 namespace {
 
 constexpr int kAdamChunk = 4096;
-constexpr int kAdamPtrs = 128;  // tensors per launch
+constexpr int kAdamPtrs = 160;  // tensors per launch: 3840 bytes of the 4 KB that arguments may take
 constexpr uint32_t ST_ADAMW = SK_STREAM_ADAMW, ST_ADAMW_P = SK_STREAM_ADAMW_P;
 
 struct AdamTensor {

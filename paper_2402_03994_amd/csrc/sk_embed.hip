@@ -43,12 +43,12 @@ __device__ __forceinline__ int64_t id_at(const void *ids, int index, int64_t t) 
 
 // N elements from floats, at an address aligned to one element
 template <typename O, int N>
-__device__ __forceinline__ void store_n(O *p, const float *f) {
+__device__ __forceinline__ void store_n(O *p, const float *f, bool past = false) {
   if (sizeof(O) == 4) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) Vec<O>::store(p + i, Vec<O>::pack(f + i));
+    for (int i = 0; i < N; i += 4) Vec<O>::store(p + i, Vec<O>::pack(f + i), past);
   } else if (N == 8) {
-    Vec<O>::store(p, Vec<O>::pack(f));
+    Vec<O>::store(p, Vec<O>::pack(f), past);
   } else {  // four bf16
     struct __attribute__((packed, aligned(2))) Half {
       uint32_t a, b;
@@ -60,7 +60,7 @@ __device__ __forceinline__ void store_n(O *p, const float *f) {
 template <typename W, typename O>
 __global__ __launch_bounds__(256) void k_embed(const W *__restrict__ w, int64_t vocab, int width, int64_t ld,
                                                const void *__restrict__ ids, int index, int64_t block0,
-                                               int64_t n, int pieces, float scale, O *__restrict__ out) {
+                                               int64_t n, int pieces, float scale, bool past, O *__restrict__ out) {
   constexpr int N = Vec<W>::N, NV = 4;
   const int64_t job = (block0 + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t t = job / pieces;
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void k_embed(const W *__restrict__ w, int64_t 
       float f[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) f[i] = scale * Vec<W>::get(raw[k], i);
-      store_n<O, N>(o + (int64_t)(v0 + 64 * k) * N, f);
+      store_n<O, N>(o + (int64_t)(v0 + 64 * k) * N, f, past);
     }
   const int c = nv * N + lane;  // the width % N last columns, by the first piece
   if (v0 == lane && c < width) o[c] = from_f32<O>(live ? scale * to_f32(x[c]) : 0.0f);
@@ -323,14 +323,15 @@ struct Sums {
 // so that a few columns are added up and written twice, with the same values (65536 x 767 bf16: 71 us with the last
 // columns one by one).  That is not for accumulation, where the second of two waves would add to the first one's sum.
 template <typename G, typename O, bool WHOLE>
-__global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *__restrict__ dy,
+__global__ __launch_bounds__(256) void k_eg_sum(Sums s, uint32_t jobs, const G *__restrict__ dy,
                                                 O *__restrict__ out) {
   constexpr int N = Vec<G>::N, U = WHOLE ? 16 : 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t job = (int64_t)blockIdx.x * 4 + wave;
+  const uint32_t job = blockIdx.x * 4 + wave;
   if (job >= jobs) return;
-  const int64_t bt = job / s.pieces, b = bt / s.tiles, tile = bt % s.tiles, e0 = tile * s.R;
-  int c = (int)(job % s.pieces) * 64 * N + lane * N;
+  const uint32_t bt = job / (uint32_t)s.pieces, b = bt / (uint32_t)s.tiles, tile = bt % (uint32_t)s.tiles;
+  const int64_t e0 = (int64_t)tile * s.R;
+  int c = (int)(job % (uint32_t)s.pieces) * 64 * N + lane * N;
   const bool idle = c >= s.width;
   if (WHOLE && c + N > s.width) c = s.width - N;
   const Entry *k = s.sorted + b * s.n;
@@ -346,7 +347,7 @@ __global__ __launch_bounds__(256) void k_eg_sum(Sums s, int64_t jobs, const G *_
     if (began && ends) {
       put<O, N, WHOLE>(o + (int64_t)cur * s.width, c, s.width, acc, s.scale, s.accumulate);
     } else {
-      float *part = (began ? s.tail : s.head) + bt * s.width + c;
+      float *part = (began ? s.tail : s.head) + (int64_t)bt * s.width + c;
       if (WHOLE) {
 #pragma unroll
         for (int i = 0; i < N; i += 4) Vec<float>::store(part + i, Vec<float>::pack(acc + i));
@@ -458,7 +459,7 @@ void run_embed(const void *w, int64_t vocab, int64_t width, int64_t ld, const vo
   const int64_t pieces = std::max<int64_t>(1, (width / Vec<W>::N + 255) / 256);
   grid_parts((n * pieces + 3) / 4, [&](uint32_t block0, uint32_t blocks) {
     hipLaunchKernelGGL((k_embed<W, O>), dim3(blocks), dim3(256), 0, st, (const W *)w, vocab, (int)width, ld, ids, index,
-                       (int64_t)block0, n, (int)pieces, scale, (O *)out);
+                       (int64_t)block0, n, (int)pieces, scale, n * width * (int64_t)sizeof(O) > kPastBytes, (O *)out);
   });
 }
 
@@ -526,9 +527,9 @@ void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batc
   const int64_t jobs = batch * w.tiles * s.pieces;
   const dim3 sum_blocks((unsigned)((jobs + 3) / 4));
   if (jobs && (width % Vec<G>::N == 0 || (!accumulate && width >= Vec<G>::N)))
-    hipLaunchKernelGGL((k_eg_sum<G, O, true>), sum_blocks, dim3(256), 0, st, s, jobs, (const G *)dy, out);
+    hipLaunchKernelGGL((k_eg_sum<G, O, true>), sum_blocks, dim3(256), 0, st, s, (uint32_t)jobs, (const G *)dy, out);
   else if (jobs)
-    hipLaunchKernelGGL((k_eg_sum<G, O, false>), sum_blocks, dim3(256), 0, st, s, jobs, (const G *)dy, out);
+    hipLaunchKernelGGL((k_eg_sum<G, O, false>), sum_blocks, dim3(256), 0, st, s, (uint32_t)jobs, (const G *)dy, out);
   if (w.tiles > 1)
     hipLaunchKernelGGL((k_eg_join<O>), dim3((unsigned)(batch * w.tiles * ((width + 255) / 256))), dim3(256), 0, st, s,
                        out);

@@ -25,6 +25,7 @@ struct Rows {
   int32_t vocab;
   int32_t index;
   float scale;
+  bool past;  // the gradient is stored past the caches
 };
 
 // the target of row t, -1 where it is masked
@@ -132,9 +133,9 @@ struct Tile {
     }
     return z;
   }
-  // w exp(scale (x - m)) to the row d, past the caches: the logits stay in them for the gradient pass (4096 x 50257 bf16
-  // read twice and written once: 169 us with ordinary stores, 153 us)
-  __device__ __forceinline__ void store(T *d, Cut q, int v0, int tid, float m, float k2, float w) const {
+  // w exp(scale (x - m)) to the row d, past the caches where that keeps the logits in them for the gradient pass (4096 x
+  // 50257 bf16 read twice and written once: 169 us with ordinary stores, 153 us)
+  __device__ __forceinline__ void store(T *d, Cut q, int v0, int tid, float m, float k2, float w, bool past) const {
     T *a = d + q.head;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -144,7 +145,7 @@ struct Tile {
         float f[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) f[e] = w * __builtin_amdgcn_exp2f((Vec<T>::get(v, e) - m) * k2);
-        Vec<T>::stream(a + (int64_t)i * N, Vec<T>::pack(f));
+        Vec<T>::store(a + (int64_t)i * N, Vec<T>::pack(f), past);
       }
     }
     const int j = single(q, v0, tid);
@@ -154,10 +155,10 @@ struct Tile {
 
 // zeros to vectors v0 + tid, v0 + tid + THREADS, .. below v1 of a row and (with its first ones) to what lies outside them
 template <typename T, int THREADS>
-__device__ __forceinline__ void row_zero(T *d, int vocab, int v0, int v1, int tid) {
+__device__ __forceinline__ void row_zero(T *d, int vocab, int v0, int v1, int tid, bool past) {
   const Cut q = cut_of(d, vocab);
   v1 = v1 < q.nv ? v1 : q.nv;
-  for (int i = v0 + tid; i < v1; i += THREADS) Vec<T>::stream(d + q.head + (int64_t)i * Vec<T>::N, u32x4{0, 0, 0, 0});
+  for (int i = v0 + tid; i < v1; i += THREADS) Vec<T>::store(d + q.head + (int64_t)i * Vec<T>::N, u32x4{0, 0, 0, 0}, past);
   const int j = Tile<T, THREADS, 1>::single(q, v0, tid);
   if (j >= 0) d[j] = from_f32<T>(0.0f);
 }
@@ -200,20 +201,20 @@ __device__ __forceinline__ Stats thread_stats(TileT &t, float k2, int tid) {
 // with nothing: the row is read again, tile by tile.
 template <typename T, int THREADS, int NV, bool RESIDENT, typename TileT>
 __device__ __forceinline__ void row_grad(const T *x, T *d, int vocab, float scale, Stats s, int target, float xt, float c,
-                                         TileT &t, int tid) {
+                                         bool past, TileT &t, int tid) {
   if (c == 0.0f || s.z == 0.0f) {
-    row_zero<T, THREADS>(d, vocab, 0, INT32_MAX, tid);
+    row_zero<T, THREADS>(d, vocab, 0, INT32_MAX, tid, past);
     return;
   }
   const Cut q = cut_of(x, vocab);
   const float k2 = scale * kLog2e, cs = c * scale, w = -cs / s.z;
   if (RESIDENT) {
     t.stay();
-    t.store(d, q, 0, tid, s.m, k2, w);
+    t.store(d, q, 0, tid, s.m, k2, w, past);
   } else {
     for (int v0 = 0; v0 < q.nv || v0 == 0; v0 += THREADS * NV) {
       t.load(x, q, v0, tid);
-      t.store(d, q, v0, tid, s.m, k2, w);
+      t.store(d, q, v0, tid, s.m, k2, w, past);
     }
   }
   // the target's entry, again by the thread that has just stored it
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_policy(Rows r
     logp[t] = lp;
     loss_t[t] = l;
   }
-  if (d) row_grad<T, THREADS, NV, RESIDENT>(x, (T *)d + t * ldd, r.vocab, r.scale, s, target, xt, c, tile, tid);
+  if (d) row_grad<T, THREADS, NV, RESIDENT>(x, (T *)d + t * ldd, r.vocab, r.scale, s, target, xt, c, r.past, tile, tid);
 }
 
 // the mean of the pairs' losses, by 256 threads
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(256) void k_logp_grad(Rows r, int64_t rows, int pie
   const float c = target >= 0 ? dlogp[t] : 0.0f;
   const float2 s = stats[t];
   if (c == 0.0f || s.y == 0.0f) {
-    row_zero<T, 256>(d, vocab, v0, v0 + 256 * NV, tid);
+    row_zero<T, 256>(d, vocab, v0, v0 + 256 * NV, tid, r.past);
     return;
   }
   const float k2 = r.scale * kLog2e, cs = c * r.scale;
@@ -366,7 +367,7 @@ __global__ __launch_bounds__(256) void k_logp_grad(Rows r, int64_t rows, int pie
   const float xt = mine ? to_f32(x[target]) : 0.0f;  // read before the thread's stores, for the gradient in place
   TileT tile;
   tile.load(x, q, v0, tid);
-  tile.store(d, q, v0, tid, s.x, k2, -cs / s.y);
+  tile.store(d, q, v0, tid, s.x, k2, -cs / s.y, r.past);
   if (mine) d[target] = from_f32<T>(cs * (1.0f - __builtin_amdgcn_exp2f((xt - s.x) * k2) / s.y));
 }
 
@@ -470,7 +471,8 @@ int check_out(const sk_logits *x, const void *dlogits, int64_t ld_out) {
 }
 
 Rows rows_of(const sk_logits *x) {
-  return Rows{x->data, x->targets, x->ld, (int32_t)x->vocab, (int32_t)x->index, x->scale};
+  const int64_t bytes = x->rows * x->vocab * (x->dtype == SK_F32 ? 4 : 2);
+  return Rows{x->data, x->targets, x->ld, (int32_t)x->vocab, (int32_t)x->index, x->scale, bytes > kPastBytes};
 }
 
 template <int V>

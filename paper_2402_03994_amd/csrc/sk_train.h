@@ -104,6 +104,10 @@ __device__ __forceinline__ T block_all(T v, Op op, T *lds) {
   return r;
 }
 
+// Outputs above this size are stored past the caches (32 MB of L2, 256 MB in front of the memory); what is smaller is
+// left there for the next kernel to read.
+constexpr int64_t kPastBytes = 64 << 20;
+
 // 16 bytes of elements, aligned to one element only: the loads and stores of gfx950 take any alignment.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
@@ -116,7 +120,16 @@ struct Vec {
   };
   static __device__ __forceinline__ u32x4 load(const T *p) { return ((const Any *)p)->v; }
   static __device__ __forceinline__ void store(T *p, u32x4 v) { ((Any *)p)->v = v; }
-  // past the caches: for what is not read again soon, so that something else stays there
+  // past the caches: for more than they hold, so that something else stays there
+  static __device__ __forceinline__ void store(T *p, u32x4 v, bool past) {
+    if (past) {
+      asm volatile("");  // or the compiler makes one ordinary store of the two
+      stream(p, v);
+      asm volatile("");
+    } else {
+      store(p, v);
+    }
+  }
   static __device__ __forceinline__ void stream(T *p, u32x4 v) {
     if (sizeof(T) == 4)
       __builtin_nontemporal_store(v, (u32x4_at4 *)p);

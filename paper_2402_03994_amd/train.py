@@ -236,7 +236,7 @@ def preference_loss(logits: torch.Tensor, targets: torch.Tensor, offsets: torch.
 
 
 class AdamW:
-    """AdamW over a list of parameter tensors, stepped in one launch for up to 128 of them.
+    """AdamW over a list of parameter tensors, stepped in one launch for up to 160 of them.
 
     shapes: per tensor its shape or element count.  state: "f32" or "8bit" moments (a byte an element and an exponent
     byte for each 64; rounded up or down at random from `seed`, step and place, so that two runs agree).  decay: a

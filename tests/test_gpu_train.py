@@ -659,3 +659,23 @@ def test_example_trains(dev):
     assert pref[-1] < 0.5 * pref[0]
     assert pol[-1] < pol[0]
     assert err < 6 / np.sqrt(ex.D)  # a cosine of two sketched vectors is off by about 1 / sqrt(D)
+
+
+def test_adamw_many_tensors(dev):
+    """More tensors than one launch takes, the norm over all of them."""
+    import paper_2402_03994_amd as fw
+    sizes = [1 + 37 * k % 611 for k in range(400)]
+    opt = fw.AdamW(sizes, decay=[k % 2 for k in range(400)])
+    g = [torch.randn(n, device=dev) for n in sizes]
+    p = [torch.randn(n, device=dev) for n in sizes]
+    before = np.concatenate([host(t) for t in p])
+    gh = np.concatenate([t.cpu().numpy() for t in g])
+    norm = opt.step(p, g, 1, lr=0.1, eps=1e-6, weight_decay=0.1, max_norm=1.0)
+    want = np.sqrt((gh.astype(np.float64) ** 2).sum())
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    s = np.float32(1.0) / (np.float32(float(norm)) + np.float32(1e-6))
+    m, v = O.adamw_moments(np.zeros_like(gh), np.zeros_like(gh), gh, 0.9, 0.999, s)
+    assert np.array_equal(unpadded(opt.m.cpu().numpy(), sizes), m) and np.array_equal(unpadded(opt.v.cpu().numpy(), sizes), v)
+    wd = np.concatenate([np.full(n, 0.1 * (k % 2)) for k, n in enumerate(sizes)])
+    ref = O.adamw_param(before, m, v, 1, 0.1, 0.9, 0.999, 1e-6, wd)
+    assert (np.abs(np.concatenate([host(t) for t in p]) - ref) <= 2.0 ** -20 * np.abs(ref - before) + 2.0 ** -23 * np.abs(before)).all()
