@@ -7,6 +7,13 @@
 // elements at a time (16-byte loads of bf16, one Philox block for its
 // parameters and two for its moments) and eight lanes a 64-element block, whose
 // largest moment they find among themselves.
+//
+// k_adamw with fp32 moments is bound by memory (28 bytes an element; fp32
+// parameters and gradients: 5.1 TB/s).  With 8-bit moments the random words, the
+// square root and the codes take about 85 operations an element of the 100 that
+// fit beside 10 bytes (bf16): GPT-2 small, 124 million elements, 230 us, 5.4
+// TB/s.  k_adamw_moments writes 8 bytes an element at 5.4 TB/s.  k_adamw_norm
+// reads the gradients once more; its fp64 sums cost nothing beside that.
 #include <cmath>
 #include <vector>
 

@@ -3,9 +3,11 @@
 //
 // Lookup: a wave copies up to 4 KB of a row (64 lanes x 4 vectors of 16
 // bytes), so that a row needs no more waves than its bytes ask for and one id
-// is read per wave; bound by memory.
+// is read per wave.  Bound by memory: 32768 rows of 4096 bf16, 268 MB out of
+// 98 MB of the table, 71 us; one row of 768 fp32 2 us, all of it latency.
 //
-// Gradient, in three or four launches, without atomics on floats:
+// Gradient, in three or four launches, without atomics on floats (and in one,
+// k_eg_few, for few tokens):
 //   k_eg_rank   sorts each run of up to 4096 tokens of a group by (id,
 //               position): an entry's place is how many entries are smaller,
 //               counted by brute force (64 entries a workgroup against all of
@@ -23,6 +25,8 @@
 // Every sum has a fixed order: the sorted one within R entries, then piece by
 // piece.  Bound by writing the gradient (vocab x width per group); to zero all
 // of it costs the named rows a second write and spares the others a look-up.
+// 8 examples of 1024 tokens, 50257 x 768 fp32 each: 183 us to rank and zero (6.8
+// TB/s), 20 us to sum, 6 us to join.
 #include <algorithm>
 #include <type_traits>
 

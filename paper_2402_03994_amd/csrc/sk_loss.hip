@@ -6,7 +6,25 @@
 // exp(scale (x_j - m)): log p_t = scale (x_t - m) - log z, and every gradient is
 // a number c of the row times scale (onehot - p).  The exponentials are at most
 // 1, so a row whose entries are all the type's lowest value is the uniform
-// distribution; a row of -inf alone has m taken as 0 and z = 0.
+// distribution; a row of -inf alone has m taken as 0 and z = 0.  Sums, statistics
+// and factors are fp32 (over positions and texts fp64); a gradient is rounded
+// once, to the type of the logits.
+//
+// Every kernel is bound by memory (a large copy reaches 4.9 TB/s on the card, a
+// fill 6.8, reading alone 6.3):
+//   k_logp       one read of the unmasked rows, by the threads of one workgroup
+//                (or one wave) that hold a row, or stream it, in registers.
+//                Each thread sums under its own maximum, so that one barrier
+//                joins both.  10682 x 50257 bf16: 175 to 183 us, 6 TB/s.
+//   k_policy     the same, then the token's loss and the row's gradient from
+//                the registers: one read, one write, no second launch over the
+//                logits.  8192 x 128256 bf16, 40% masked: 606 us, 5.5 TB/s.
+//   k_logp_grad  the gradient from known (m, z).  The preference loss needs it:
+//                a row's factor is known when its pair's rows have all been
+//                read.  16384 x 50257 bf16, 40% masked: 160 us of k_logp, 440
+//                us (6 TB/s), of a floor of 540 us for one read and one write.
+//   k_pair       a workgroup a pair, 4 to 7 us; k_policy_total one workgroup, 2
+//                to 5 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -479,19 +497,20 @@ template <int V>
 using Int = std::integral_constant<int, V>;
 
 // f(threads, vectors of a thread, resident, vectors of them in LDS) for rows of up to nv vectors.  Where there are
-// many rows, what counts is how much of them the chip holds at a time: about four to eight vectors a thread, so that a
-// CU has several rows (16924 bf16 columns, log-probabilities: 4.3 TB/s with 1024 threads, 6.0 with 256; policy update:
-// 4.9 with 1024, 5.7 with 512; 8000 columns, policy: 5.2 with 256 threads, 5.4 with one wave).  Few rows want their
-// latency shared by more threads.
+// many rows, what counts is how much of them the chip holds at a time: four to eight vectors a thread, so that a CU has
+// several rows (bf16 columns, log-probabilities and policy update: 4142 columns 4.2 and 5.3 TB/s with 256 threads, 5.2
+// and 5.6 with one wave; 16924 columns 4.3 and 4.9 with 1024 threads, 5.2 and 5.7 with 512).  Up to 512 rows leave
+// waves to spare, and a row is done sooner by four of them (4000 columns, 64 rows, policy: 3.8 us, 5.1 us by one; 1024
+// rows: 6.7 us, 5.9 us).
 template <typename F>
 void with_row_shape(int64_t nv, int64_t rows, F f) {
-  const bool few = rows <= 1024;
+  const bool few = rows <= 512;
   if (nv <= 64 * 4)
     f(Int<64>(), Int<4>(), std::true_type(), Int<0>());
   else if (!few && nv <= 64 * 8)
     f(Int<64>(), Int<8>(), std::true_type(), Int<0>());
-  else if (!few && nv <= 64 * 16)
-    f(Int<64>(), Int<16>(), std::true_type(), Int<0>());
+  else if (!few && nv <= 64 * 12)
+    f(Int<64>(), Int<12>(), std::true_type(), Int<0>());
   else if (nv <= 256 * 4)
     f(Int<256>(), Int<4>(), std::true_type(), Int<0>());
   else if (nv <= 256 * 8)
@@ -504,7 +523,7 @@ void with_row_shape(int64_t nv, int64_t rows, F f) {
     f(Int<1024>(), Int<8>(), std::true_type(), Int<0>());
   else if (nv <= 1024 * 16)
     f(Int<1024>(), Int<16>(), std::true_type(), Int<0>());
-  else if (nv <= 1024 * 32)  // 384 KB of registers and 128 KB of LDS
+  else if (nv <= 1024 * 32)  // 384 KB of registers and 128 KB of LDS (128256 fp32 columns: 5.5 TB/s, 3.7 read twice)
     f(Int<1024>(), Int<32>(), std::true_type(), Int<8>());
   else
     f(Int<1024>(), Int<8>(), std::false_type(), Int<0>());
@@ -637,7 +656,7 @@ int sketch_policy_loss(const sk_logits *x, const float *old_logp, const float *a
     else
       run_policy_t<bf16>(x, p, logp, token_loss, dlogits, ld_out, st);
   }
-  // one workgroup: four waves are there sooner, sixteen get through more rows (256 rows a thread-step)
+  // one workgroup: four waves are done sooner with few rows (61: 1.8 us), sixteen with many (8192: 4.8 us)
   if (x->rows <= 1024)
     hipLaunchKernelGGL(k_policy_total<256>, dim3(1), dim3(256), 0, st, r, x->rows, weights, token_loss, loss);
   else
