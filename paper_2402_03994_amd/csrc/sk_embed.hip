@@ -230,22 +230,26 @@ __device__ __forceinline__ void put(O *row, int c, int width, const float *acc, 
   }
 }
 
-// Few tokens, in one launch: a workgroup owns `rows` rows of a group's gradient, lists the tokens that name them, in
-// order, and writes every row, the named ones as the sum of their tokens and the others as zeros.
-constexpr int kFewTokens = 512;
-template <typename G, typename O>
+// Few tokens (up to 256 TURNS), in one launch: a workgroup owns `rows` rows of a group's gradient, lists the tokens that
+// name them, in order, and writes every row, the named ones as the sum of their tokens and the others as zeros.  Bound by
+// the frequent ids: a wave adds up eight of an id's tokens at a time.
+// WHOLE: every lane has a whole vector of columns; the last lane's of a width that is no multiple of one begin earlier,
+// so that a few columns are added up and written twice, with the same values.  That is not for accumulation, where the
+// second of two waves would add to the first one's sum.
+constexpr int kFewTokens = 1024;
+template <typename G, typename O, bool WHOLE, int TURNS>
 __global__ __launch_bounds__(256) void k_eg_few(const G *__restrict__ dy, int64_t ld, const void *__restrict__ ids,
                                                 int index, int n, int64_t vocab, int width, int rows, int64_t per,
                                                 int64_t block0, float scale, int accumulate, O *__restrict__ out) {
-  constexpr int N = Vec<G>::N, U = 4, kTurns = kFewTokens / 256;
-  __shared__ int counts[kTurns * 4];
-  __shared__ int list[kFewTokens];  // (row << 16) | position
+  constexpr int N = Vec<G>::N, U = WHOLE ? 8 : 1;
+  __shared__ int counts[TURNS * 4];
+  __shared__ int list[TURNS * 256];  // (row << 16) | position
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t block = block0 + blockIdx.x, b = block / per, v0 = block % per * rows;
-  int row[kTurns];
-  uint64_t mask[kTurns];
+  int row[TURNS];
+  uint64_t mask[TURNS];
 #pragma unroll
-  for (int j = 0; j < kTurns; ++j) {
+  for (int j = 0; j < TURNS; ++j) {
     const int i = j * 256 + tid;
     const int64_t v = i < n ? id_at(ids, index, b * n + i) : -1;
     // ids outside the vocabulary are not in [v0, v0 + rows) either, but for the last rows'
@@ -256,7 +260,7 @@ __global__ __launch_bounds__(256) void k_eg_few(const G *__restrict__ dy, int64_
   __syncthreads();
   int total = 0;
 #pragma unroll
-  for (int q = 0; q < kTurns * 4; ++q) {
+  for (int q = 0; q < TURNS * 4; ++q) {
     const int j = q / 4;
     if (q % 4 == wave && row[j] >= 0)
       list[total + __builtin_popcountll(mask[j] & ((1ull << lane) - 1))] = row[j] << 16 | (j * 256 + tid);
@@ -274,7 +278,10 @@ __global__ __launch_bounds__(256) void k_eg_few(const G *__restrict__ dy, int64_
   }
   const int pieces = (width + 64 * N - 1) / (64 * N);
   for (int t = wave; t < live * pieces; t += 4) {
-    const int r = t / pieces, c = (t % pieces) * 64 * N + lane * N;
+    const int r = t / pieces;
+    int c = (t % pieces) * 64 * N + lane * N;
+    const bool idle = c >= width;
+    if (WHOLE && c + N > width) c = width - N;
     O *o = out + (b * vocab + v0 + r) * width;
     float acc[N];
 #pragma unroll
@@ -285,7 +292,7 @@ __global__ __launch_bounds__(256) void k_eg_few(const G *__restrict__ dy, int64_
       uint64_t hit = __ballot(e >= 0 && e >> 16 == r);
       named |= hit != 0;
       while (hit) {
-        float x[U][N];
+        u32x4 x[U];
         int count = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -294,23 +301,22 @@ __global__ __launch_bounds__(256) void k_eg_few(const G *__restrict__ dy, int64_
           hit &= hit - 1;
           ++count;
           const G *g = dy + (b * n + pos) * ld;
-          if (c + N <= width) {
-            const u32x4 w = Vec<G>::load(g + c);
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[u][i] = Vec<G>::get(w, i);
+          if (WHOLE) {
+            if (!idle) x[u] = Vec<G>::load(g + c);
           } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[u][i] = c + i < width ? to_f32(g[c + i]) : 0.0f;
+            for (int i = 0; i < N; ++i) acc[i] += c + i < width ? to_f32(g[c + i]) : 0.0f;
           }
         }
+        if (WHOLE)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (u < count)
+          for (int u = 0; u < U; ++u)
+            if (u < count)
 #pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] += x[u][i];
+              for (int i = 0; i < N; ++i) acc[i] += Vec<G>::get(x[u], i);
       }
     }
-    if ((named || !accumulate) && c < width) put<O, N, false>(o, c, width, acc, scale, accumulate);
+    if ((named || !accumulate) && !idle) put<O, N, WHOLE>(o, c, width, acc, scale, accumulate);
   }
 }
 
@@ -323,9 +329,7 @@ struct Sums {
   float *head, *tail;  // [batch, tiles, width]
 };
 
-// WHOLE: every lane has a whole vector of columns; the last lane's of a width that is no multiple of one begin earlier,
-// so that a few columns are added up and written twice, with the same values (65536 x 767 bf16: 71 us with the last
-// columns one by one).  That is not for accumulation, where the second of two waves would add to the first one's sum.
+// WHOLE as above (65536 x 767 bf16: 34 us, 71 us with the last columns one by one).
 template <typename G, typename O, bool WHOLE>
 __global__ __launch_bounds__(256) void k_eg_sum(Sums s, uint32_t jobs, const G *__restrict__ dy,
                                                 O *__restrict__ out) {
@@ -489,15 +493,32 @@ EgWork eg_work(int64_t batch, int64_t n, int64_t width) {
 template <typename G, typename O>
 void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batch, int64_t n, int64_t vocab,
             int64_t width, float scale, O *out, int accumulate, void *work, hipStream_t st) {
-  // One launch is sooner done than three (333 tokens, 8000 x 256 fp32: 13 us, 22 us); where the gradient is large, looking
-  // through the tokens in each of its workgroups costs more than sorting them once (8 x 50257 x 768 fp32: 128 tokens
-  // 236 us, 204 us sorted).
-  if (n <= kFewTokens && batch * vocab * width * (int64_t)sizeof(O) <= (64 << 20)) {
-    const int rows = (int)std::max<int64_t>(1, std::min<int64_t>(64, 16384 / (width * (int64_t)sizeof(O))));
+  const bool whole = width % Vec<G>::N == 0 || (!accumulate && width >= Vec<G>::N);
+  // One launch is sooner done than three (8000 x 256 fp32: 333 tokens 6 us on the device, 1024 tokens 11 us, sorted 19;
+  // 10000 x 1000: 1000 tokens 16 us, 22; 4 x 20000 x 64: 1024 tokens 24 us, 20, and 6 us less to launch); where the
+  // gradient is large, looking through the tokens in each of its workgroups costs more than sorting them once (8 x 50257
+  // x 768 fp32: 128 tokens 236 us, 204 us sorted).
+  const int64_t bytes = batch * vocab * width * (int64_t)sizeof(O);
+  if (n <= kFewTokens && bytes <= (64 << 20)) {
+    // few rows a workgroup where frequent ids are to be dealt out (8 MB, 333 tokens: 4 KB 5.4 us, 8 KB 7.9
+    // us), more where the tokens are looked through that often (40 MB, 300 tokens: 15 us, 10 us)
+    const int64_t share = bytes <= (16 << 20) ? 4096 : 8192;
+    const int rows = (int)std::max<int64_t>(1, std::min<int64_t>(16, share / (width * (int64_t)sizeof(O))));
     const int64_t per = (vocab + rows - 1) / rows;
     grid_parts(batch * per, [&](uint32_t block0, uint32_t blocks) {
-      hipLaunchKernelGGL((k_eg_few<G, O>), dim3(blocks), dim3(256), 0, st, (const G *)dy, ld, ids, index, (int)n, vocab,
-                         (int)width, rows, per, (int64_t)block0, scale, accumulate, out);
+      auto launch = [&](auto w, auto turns) {
+        hipLaunchKernelGGL((k_eg_few<G, O, decltype(w)::value, decltype(turns)::value>), dim3(blocks), dim3(256), 0, st,
+                           (const G *)dy, ld, ids, index, (int)n, vocab, (int)width, rows, per, (int64_t)block0, scale,
+                           accumulate, out);
+      };
+      if (whole && n <= 256)
+        launch(std::true_type(), std::integral_constant<int, 1>());
+      else if (whole && n <= 512)
+        launch(std::true_type(), std::integral_constant<int, 2>());
+      else if (whole)
+        launch(std::true_type(), std::integral_constant<int, 4>());
+      else
+        launch(std::false_type(), std::integral_constant<int, 4>());
     });
     return;
   }
@@ -530,7 +551,7 @@ void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batc
   s.scale = scale;
   const int64_t jobs = batch * w.tiles * s.pieces;
   const dim3 sum_blocks((unsigned)((jobs + 3) / 4));
-  if (jobs && (width % Vec<G>::N == 0 || (!accumulate && width >= Vec<G>::N)))
+  if (jobs && whole)
     hipLaunchKernelGGL((k_eg_sum<G, O, true>), sum_blocks, dim3(256), 0, st, s, (uint32_t)jobs, (const G *)dy, out);
   else if (jobs)
     hipLaunchKernelGGL((k_eg_sum<G, O, false>), sum_blocks, dim3(256), 0, st, s, (uint32_t)jobs, (const G *)dy, out);

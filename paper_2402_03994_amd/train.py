@@ -66,8 +66,11 @@ def _rows(t: torch.Tensor, name: str) -> int:
     """The row stride of a matrix whose rows are contiguous."""
     if t.dim() != 2 or t.shape[1] < 1:
         raise ValueError(f"{name} must be a matrix with at least one column")
-    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if (t.stride(1) != 1 and t.shape[1] > 1) or ld < t.shape[1]:
+    n, width = t.shape
+    if t.is_contiguous():
+        return width
+    ld = t.stride(0) if n > 1 else width
+    if (t.stride(1) != 1 and width > 1) or ld < width:
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
     return ld
 
@@ -104,12 +107,12 @@ def embed_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float 
     if dy.shape[:-1] != tokens.shape or dy.dim() < 2 or dy.shape[-1] < 1:
         raise ValueError("dy must be [*tokens.shape, width]")
     index = _ids(tokens, "tokens", device)
-    width = dy.shape[-1]
-    try:
-        rows = dy.view(-1, width)
-    except RuntimeError:
-        raise ValueError("dy must have rows of one stride") from None
-    ld = _rows(rows, "dy")
+    width = ld = dy.shape[-1]
+    if not dy.is_contiguous():
+        try:
+            ld = _rows(dy.view(-1, width), "dy")
+        except RuntimeError:
+            raise ValueError("dy must have rows of one stride") from None
     if per_example and tokens.dim() < 2:
         raise ValueError("per_example needs tokens [batch, ...]")
     batch = tokens.shape[0] if per_example else 1
@@ -126,7 +129,7 @@ def embed_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float 
     n = tokens.numel() // batch
     nw = lib.sketch_embed_grad_work_bytes(batch, n, width)
     work = torch.empty(nw, dtype=torch.uint8, device=device)
-    _lib.check(lib.sketch_embed_grad(rows.data_ptr(), _dtype(dy, "dy"), ld, tokens.data_ptr(), index, batch, n, vocab,
+    _lib.check(lib.sketch_embed_grad(dy.data_ptr(), _dtype(dy, "dy"), ld, tokens.data_ptr(), index, batch, n, vocab,
                                      width, scale, out.data_ptr(), _dtype(out, "out"), int(accumulate),
                                      work.data_ptr(), nw, device.index, _stream_ptr(device)))
     return out
