@@ -500,8 +500,8 @@ void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batc
   // x 768 fp32: 128 tokens 236 us, 204 us sorted).
   const int64_t bytes = batch * vocab * width * (int64_t)sizeof(O);
   if (n <= kFewTokens && bytes <= (64 << 20)) {
-    // few rows a workgroup where frequent ids are to be dealt out (8 MB, 333 tokens: 4 KB 5.4 us, 8 KB 7.9
-    // us), more where the tokens are looked through that often (40 MB, 300 tokens: 15 us, 10 us)
+    // few rows a workgroup where frequent ids are to be dealt out (8 MB, 333 tokens: 4 KB 5.4 us, 8 KB 7.9 us), more where
+    // many workgroups look through the tokens (40 MB, 300 tokens: 15 us, 10 us)
     const int64_t share = bytes <= (16 << 20) ? 4096 : 8192;
     const int rows = (int)std::max<int64_t>(1, std::min<int64_t>(16, share / (width * (int64_t)sizeof(O))));
     const int64_t per = (vocab + rows - 1) / rows;
@@ -604,7 +604,7 @@ int sketch_embed_grad(const void *dy, sk_dtype dtype, int64_t ld, const void *id
     return train_fail(SK_EINVAL, "need batch, vocab, width >= 1, n >= 0 and ld >= width");
   // what the launches' grids and 32-bit entries hold
   if (vocab > (1 << 20) || width > (1 << 24) || batch > (1 << 18) || n >= (1 << 28) || batch * n >= (1 << 28) ||
-      batch * eg_work(batch, n, width).tiles * ((width + 255) / 256) > kGridBlocks)
+      batch * vocab > (1ll << 40) / width || batch * eg_work(batch, n, width).tiles * ((width + 255) / 256) > kGridBlocks)
     return train_fail(SK_EUNSUPPORTED, "sizes above what the kernels take");
   if (!out || (n && (!dy || !ids || !work))) return train_fail(SK_EINVAL, "NULL argument");
   if (n && work_bytes < sketch_embed_grad_work_bytes(batch, n, width))

@@ -269,9 +269,9 @@ __device__ __forceinline__ void policy_token(const Policy &p, int64_t t, float l
   l = free <= held || free != free ? -free : -held;
   d = free <= held || free != free ? -free : 0.0f;
   if (p.kl != 0.0f) {
-    const float u = p.ref[t] - logp, e = expf(u);
-    l += p.kl * (e - u - 1.0f);
-    d += p.kl * (1.0f - e);
+    const float u = p.ref[t] - logp, e = expm1f(u);  // near the reference e^u - 1 would have lost what u is
+    l += p.kl * (e - u);
+    d -= p.kl * e;
   }
 }
 
@@ -674,7 +674,7 @@ int sketch_preference_loss(const sk_logits *x, const void *offsets, sk_index off
   if (rc != SK_OK) return rc;
   if (offsets_index != SK_I32 && offsets_index != SK_I64) return train_fail(SK_EDTYPE, "unknown index type");
   if (pairs < 1) return train_fail(SK_EINVAL, "need at least one pair");
-  if (pairs > INT32_MAX) return train_fail(SK_EUNSUPPORTED, "more than 2^31 - 1 pairs");
+  if (pairs > (1 << 22)) return train_fail(SK_EUNSUPPORTED, "more than 2^22 pairs");  // a grid below 2^32 threads
   if (!std::isfinite(beta)) return train_fail(SK_EINVAL, "beta must be finite");
   if (!(smoothing >= 0.0f && smoothing <= 1.0f)) return train_fail(SK_EINVAL, "smoothing must be in [0, 1]");
   if (!offsets || !loss || !seq_logp || !pair_loss) return train_fail(SK_EINVAL, "NULL argument");

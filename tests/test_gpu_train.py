@@ -679,3 +679,20 @@ def test_adamw_many_tensors(dev):
     wd = np.concatenate([np.full(n, 0.1 * (k % 2)) for k, n in enumerate(sizes)])
     ref = O.adamw_param(before, m, v, 1, 0.1, 0.9, 0.999, 1e-6, wd)
     assert (np.abs(np.concatenate([host(t) for t in p]) - ref) <= 2.0 ** -20 * np.abs(ref - before) + 2.0 ** -23 * np.abs(before)).all()
+
+
+def test_policy_divergence_near_the_reference(dev):
+    """u = ref - logp down to 1e-6: the divergence e^u - 1 - u and its derivative e^u - 1 do not lose what u is."""
+    import paper_2402_03994_amd as fw
+    n, vocab = 64, 300
+    x, t = torch.randn(n, vocab, device=dev), torch.randint(0, vocab, (n,), device=dev)
+    lp = fw.token_logp(x, t)[0]
+    ref = lp + torch.logspace(-6, 0, n, device=dev) * torch.where(torch.arange(n, device=dev) % 2 == 0, 1.0, -1.0)
+    zero, one = torch.zeros(n, device=dev), torch.ones(n, device=dev)
+    r = fw.policy_loss(x, t, lp, zero, one, ref_logp=ref, kl_coef=1.0)
+    assert torch.equal(r.logp, lp)
+    u = host(ref) - host(lp)  # exact in fp32
+    # expm1 is off by a unit of its last place or two, and the difference is rounded once
+    assert (np.abs(host(r.token_loss) - (np.expm1(u) - u)) <= 2.0 ** -21 * np.abs(np.expm1(u))).all()
+    d = O.token_logp_grad(host(x), t.cpu().numpy(), -np.expm1(u), 1.0)
+    assert (np.abs(host(r.dlogits) - d) <= (2.0 ** -20 + 2 * err_logp(10.0, vocab)) * np.abs(np.expm1(u))[:, None]).all()
