@@ -696,3 +696,45 @@ def test_policy_divergence_near_the_reference(dev):
     assert (np.abs(host(r.token_loss) - (np.expm1(u) - u)) <= 2.0 ** -21 * np.abs(np.expm1(u))).all()
     d = O.token_logp_grad(host(x), t.cpu().numpy(), -np.expm1(u), 1.0)
     assert (np.abs(host(r.dlogits) - d) <= (2.0 ** -20 + 2 * err_logp(10.0, vocab)) * np.abs(np.expm1(u))[:, None]).all()
+
+
+@pytest.mark.parametrize("vocab", [2, 65, 3000, 50257, 140003])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_logits_of_any_size(dev, vocab, dt):
+    """Rows around values so large that the product with the scale loses the difference, with ties and with entries
+    far below, and scales at both ends of the type."""
+    import paper_2402_03994_amd as fw
+    g = torch.Generator().manual_seed(vocab)
+    bases = [1e9, -1e9, 3e8, 4.5e8, -4.5e8, 1e20, -1e20, 3e38, -3e38, 0.0, 7.0]
+    rows = len(bases)
+    t = torch.randint(0, vocab, (rows,), generator=g)
+    c = torch.randn(rows, generator=g)
+    for scale in (1.0, 1e-35, 1e35):
+        x = torch.tensor(bases)[:, None].repeat(1, vocab).to(dt)
+        far = torch.rand(rows, vocab, generator=g) < 0.25
+        x = torch.where(far, (torch.tensor(bases)[:, None] - 2 * torch.tensor(bases)[:, None].abs().clamp(max=1e38) * 0.1
+                              - 1.0).to(dt), x)
+        x[:, : vocab // 2] = torch.where(torch.tensor(bases)[:, None] < 1e37, torch.tensor(-3e38).to(dt), x[:, : vocab // 2])
+        if scale < 1.0:
+            x = x.clamp(min=0.0)  # differences of finite logits stay finite
+        s = float(np.float32(scale))
+        xd, td = odd(x, dev, 1, 1), t.to(dev)
+        logp, stats = fw.token_logp(xd, td, scale=scale)
+        A = exponent_sizes(x, s)
+        with np.errstate(all="ignore"):
+            want = O.token_logp(x.double().numpy(), t.numpy(), s)
+        big = np.abs(want) > 3e38  # beyond fp32
+        assert (host(logp)[big] < -3e38).all()
+        check_logp(np.where(big, 0.0, host(logp)), np.where(big, 0.0, want), A, vocab, x, s)
+        ref = O.token_logp_grad(x.double().numpy(), t.numpy(), c.double().numpy(), s)
+        p = O.softmax_rows(x.double().numpy(), s)[0]
+        d = fw.token_logp_grad(xd, td, stats, c.to(dev), scale=scale)
+        check_grad(host(d), ref, c.double().numpy(), p, A, vocab, s, dt)
+        if scale == 1.0:
+            ok = np.abs(want) < 80.0  # where the ratio to the old policy is of any use
+            w = torch.from_numpy(np.where(ok, c.numpy(), 0.0).astype(np.float32)).to(dev)
+            r = fw.policy_loss(xd, td, logp, torch.ones(rows, device=dev), w)
+            assert np.array_equal(host(r.logp)[ok], host(logp)[ok])
+            cw = -np.where(ok, c.double().numpy(), 0.0)
+            ref = O.token_logp_grad(x.double().numpy(), t.numpy(), cw, s)
+            check_grad(host(r.dlogits), ref, cw, p, A, vocab, s, dt)
