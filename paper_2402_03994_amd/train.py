@@ -8,6 +8,7 @@ loss: a model continues with logits.backward(dlogits).
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import operator
 from typing import NamedTuple, Optional, Sequence
@@ -311,7 +312,8 @@ class AdamW:
                 set(map(T.get_device, tensors)) != {self.device.index} or not all(map(T.is_contiguous, tensors)):
             raise ValueError(f"{name}: contiguous {dt} tensors on {self.device} with these counts are needed: "
                              f"{self.numels[:8]}{'..' if len(self.numels) > 8 else ''}")
-        return (ctypes.c_void_p * len(tensors))(*map(T.data_ptr, tensors)), dt
+        at = array.array("Q", list(map(T.data_ptr, tensors)))  # two thirds of the time of filling the ctypes array itself
+        return (ctypes.c_void_p * len(tensors)).from_buffer(at), dt
 
     def step(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], step: int, lr: float,
              betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
