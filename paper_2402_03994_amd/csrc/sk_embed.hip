@@ -117,19 +117,21 @@ __device__ __forceinline__ void zero_part(Zeros z, int64_t block, int64_t blocks
   }
 }
 
-// Ranks 64 entries of a run against the whole run, eight waves taking turns at its blocks of 64.
+// Ranks 64 entries of a run against the whole run, eight waves taking turns at its blocks of 64: workgroup block0 +
+// blockIdx.x of rank_blocks that rank and zero_blocks that zero.
 __global__ __launch_bounds__(512) void k_eg_rank(const void *__restrict__ ids, int index, int64_t n, int64_t vocab,
-                                                 int runs, int tiles, int rank_blocks, Entry *__restrict__ sorted,
-                                                 Zeros z) {
+                                                 int runs, int tiles, uint32_t block0, uint32_t rank_blocks,
+                                                 uint32_t zero_blocks, Entry *__restrict__ sorted, Zeros z) {
   __shared__ int part[8][64];
+  const uint32_t block = block0 + blockIdx.x;
   // those that rank come first: dealt out among those that zero they take longer (65536 tokens: 41 us, 48 to 60)
-  if (blockIdx.x >= (unsigned)rank_blocks) {
-    zero_part(z, blockIdx.x - rank_blocks, gridDim.x - rank_blocks);
+  if (block >= rank_blocks) {
+    zero_part(z, block - rank_blocks, zero_blocks);
     return;
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t run = blockIdx.x / (unsigned)tiles, b = run / runs, p0 = (run % runs) * kRun;
-  const int tile = blockIdx.x % (unsigned)tiles, len = (int)(n - p0 < kRun ? n - p0 : kRun);
+  const int64_t run = block / (unsigned)tiles, b = run / runs, p0 = (run % runs) * kRun;
+  const int tile = block % (unsigned)tiles, len = (int)(n - p0 < kRun ? n - p0 : kRun);
   if (tile * 64 >= len) return;
   auto key = [&](int i) -> int {
     if (i >= len) return kBeyond;
@@ -184,8 +186,8 @@ __global__ __launch_bounds__(512) void k_eg_rank(const void *__restrict__ ids, i
 
 // Sorted runs of `len` entries, 16 at a time: 16 lanes an entry.
 __global__ __launch_bounds__(256) void k_eg_merge(const Entry *__restrict__ in, Entry *__restrict__ out, int64_t n,
-                                                  int64_t len, int64_t total) {
-  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kMergeRuns;
+                                                  int64_t len, int64_t total, uint32_t block0) {
+  const int64_t e = ((int64_t)(block0 + blockIdx.x) * 256 + threadIdx.x) / kMergeRuns;
   const int r = threadIdx.x % kMergeRuns;
   if (e >= total) return;  // all 16 lanes of an entry
   const int64_t b = e / n, i = e % n, g0 = i / (len * kMergeRuns) * (len * kMergeRuns);
@@ -490,9 +492,11 @@ EgWork eg_work(int64_t batch, int64_t n, int64_t width) {
   return w;
 }
 
+// Returns at the first launch that fails: the kernels after it would take what the workspace happens to hold for
+// positions and ids.
 template <typename G, typename O>
-void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batch, int64_t n, int64_t vocab,
-            int64_t width, float scale, O *out, int accumulate, void *work, hipStream_t st) {
+int run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batch, int64_t n, int64_t vocab,
+           int64_t width, float scale, O *out, int accumulate, void *work, hipStream_t st) {
   const bool whole = width % Vec<G>::N == 0 || (!accumulate && width >= Vec<G>::N);
   // One launch is sooner done than three (8000 x 256 fp32: 333 tokens 6 us on the device, 1024 tokens 11 us, sorted 19;
   // 10000 x 1000: 1000 tokens 16 us, 22; 4 x 20000 x 64: 1024 tokens 24 us, 20, and 6 us less to launch); where the
@@ -520,7 +524,7 @@ void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batc
       else
         launch(std::false_type(), std::integral_constant<int, 4>());
     });
-    return;
+    return train_launched();
   }
   const EgWork w = eg_work(batch, n, width);
   Entry *sorted = (Entry *)work, *other = (Entry *)((char *)work + w.entries);
@@ -528,17 +532,25 @@ void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batc
   s.head = (float *)((char *)work + w.entries * (n > kRun ? 2 : 1));
   s.tail = s.head + w.sums / 4;
   const int64_t runs = (n + kRun - 1) / kRun, tiles = (std::min<int64_t>(n, kRun) + 63) / 64;  // tiles of a run
+  // up to 2^23 workgroups that rank (a run of few tokens takes as many as the longest) and 2^21 that zero: more than one
+  // launch of 512 threads each may hold
   const int64_t rank_blocks = batch * runs * tiles;
   const Zeros z{(char *)out, accumulate ? 0 : batch * vocab * width * (int64_t)sizeof(O)};
-  const int64_t blocks = rank_blocks + std::min<int64_t>((z.bytes + 8191) / 8192, 1 << 21);
-  if (blocks)
-    hipLaunchKernelGGL(k_eg_rank, dim3((unsigned)blocks), dim3(512), 0, st, ids, index, n, vocab, (int)runs, (int)tiles,
-                       (int)rank_blocks, sorted, z);
-  for (int64_t len = kRun; len < n; len *= kMergeRuns) {
-    hipLaunchKernelGGL(k_eg_merge, dim3((unsigned)((batch * n * kMergeRuns + 255) / 256)), dim3(256), 0, st, sorted,
-                       other, n, len, batch * n);
+  const int64_t zero_blocks = std::min<int64_t>((z.bytes + 8191) / 8192, 1 << 21);
+  constexpr int64_t kMost = kGridBlocks / 2;
+  for (int64_t b = 0; b < rank_blocks + zero_blocks; b += kMost)
+    hipLaunchKernelGGL(k_eg_rank, dim3((unsigned)std::min(kMost, rank_blocks + zero_blocks - b)), dim3(512), 0, st, ids,
+                       index, n, vocab, (int)runs, (int)tiles, (uint32_t)b, (uint32_t)rank_blocks, (uint32_t)zero_blocks,
+                       sorted, z);
+  int rc = train_launched();
+  for (int64_t len = kRun; rc == SK_OK && len < n; len *= kMergeRuns) {
+    grid_parts((batch * n * kMergeRuns + 255) / 256, [&](uint32_t block0, uint32_t blocks) {
+      hipLaunchKernelGGL(k_eg_merge, dim3(blocks), dim3(256), 0, st, sorted, other, n, len, batch * n, block0);
+    });
     std::swap(sorted, other);
+    rc = train_launched();
   }
+  if (rc != SK_OK) return rc;
   s.sorted = sorted;
   s.n = n;
   s.vocab = vocab;
@@ -555,9 +567,9 @@ void run_eg(const void *dy, int64_t ld, const void *ids, int index, int64_t batc
     hipLaunchKernelGGL((k_eg_sum<G, O, true>), sum_blocks, dim3(256), 0, st, s, (uint32_t)jobs, (const G *)dy, out);
   else if (jobs)
     hipLaunchKernelGGL((k_eg_sum<G, O, false>), sum_blocks, dim3(256), 0, st, s, (uint32_t)jobs, (const G *)dy, out);
-  if (w.tiles > 1)
-    hipLaunchKernelGGL((k_eg_join<O>), dim3((unsigned)(batch * w.tiles * ((width + 255) / 256))), dim3(256), 0, st, s,
-                       out);
+  if ((rc = train_launched()) != SK_OK || w.tiles <= 1) return rc;
+  hipLaunchKernelGGL((k_eg_join<O>), dim3((unsigned)(batch * w.tiles * ((width + 255) / 256))), dim3(256), 0, st, s, out);
+  return train_launched();
 }
 
 bool dtype_ok(int d) { return d == SK_F32 || d == SK_BF16; }
@@ -612,14 +624,12 @@ int sketch_embed_grad(const void *dy, sk_dtype dtype, int64_t ld, const void *id
   TrainGuard guard(device);
   hipStream_t st = (hipStream_t)stream;
   if (dtype == SK_F32 && out_dtype == SK_F32)
-    run_eg<float>(dy, ld, ids, index, batch, n, vocab, width, scale, (float *)out, accumulate, work, st);
-  else if (dtype == SK_F32)
-    run_eg<float>(dy, ld, ids, index, batch, n, vocab, width, scale, (bf16 *)out, accumulate, work, st);
-  else if (out_dtype == SK_F32)
-    run_eg<bf16>(dy, ld, ids, index, batch, n, vocab, width, scale, (float *)out, accumulate, work, st);
-  else
-    run_eg<bf16>(dy, ld, ids, index, batch, n, vocab, width, scale, (bf16 *)out, accumulate, work, st);
-  return train_launched();
+    return run_eg<float>(dy, ld, ids, index, batch, n, vocab, width, scale, (float *)out, accumulate, work, st);
+  if (dtype == SK_F32)
+    return run_eg<float>(dy, ld, ids, index, batch, n, vocab, width, scale, (bf16 *)out, accumulate, work, st);
+  if (out_dtype == SK_F32)
+    return run_eg<bf16>(dy, ld, ids, index, batch, n, vocab, width, scale, (float *)out, accumulate, work, st);
+  return run_eg<bf16>(dy, ld, ids, index, batch, n, vocab, width, scale, (bf16 *)out, accumulate, work, st);
 }
 
 }  // extern "C"

@@ -738,3 +738,22 @@ def test_logits_of_any_size(dev, vocab, dt):
             cw = -np.where(ok, c.double().numpy(), 0.0)
             ref = O.token_logp_grad(x.double().numpy(), t.numpy(), cw, s)
             check_grad(host(r.dlogits), ref, cw, p, A, vocab, s, dt)
+
+
+@pytest.mark.parametrize("batch,n,vocab", [(65_000, 4_100, 2_200), (1, (1 << 28) - 8, 1 << 20)])
+def test_embed_grad_of_more_than_one_grid(dev, batch, n, vocab):
+    """What the ranking (8.4 million workgroups of 512 threads here) and the merging (2^28 entries, 16 threads each) need
+    is more than a launch of 2^32 threads takes.  Whole numbers: every sum is exact."""
+    import paper_2402_03994_amd as fw
+    if batch > 1:
+        blocks = batch * 2 * 64 + batch * vocab * 4 // 8192
+        assert blocks * 512 >= 1 << 32
+    else:
+        assert -(-batch * n * 16 // 256) * 256 >= 1 << 32
+    g = torch.Generator(device=dev).manual_seed(n)
+    ids = torch.randint(0, vocab, (batch, n), generator=g, device=dev, dtype=torch.int32)
+    dy = torch.randint(-2, 3, (batch, n, 1), generator=g, device=dev, dtype=torch.int8).to(BF16)
+    got = fw.embed_grad(dy, ids, vocab, per_example=True)
+    key = (ids + torch.arange(batch, device=dev)[:, None] * vocab).view(-1)
+    ref = torch.zeros(batch * vocab, device=dev).index_add_(0, key, dy.view(-1).float())
+    assert torch.equal(got.view(-1), ref)
