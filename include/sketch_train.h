@@ -163,7 +163,8 @@ int sketch_preference_loss(const sk_logits *x, const void *offsets, sk_index off
  *     and stands for NaNs.
  * Parameters in bf16 without a master copy are rounded the same way: the 16
  * bits that are cut off get u added, half (i mod 2) of word (i / 2 mod 4) of
- * the block with counter (i / 8, step, l, SK_STREAM_ADAMW_P).
+ * the block with counter (i / 8, step, l, SK_STREAM_ADAMW_P).  To a NaN nothing is
+ * added.
  */
 #define SK_STREAM_ADAMW 11
 #define SK_STREAM_ADAMW_P 12

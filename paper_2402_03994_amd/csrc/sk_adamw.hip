@@ -256,11 +256,15 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
     }
     if (MASTER) store8(master, e, live, pv);
     if (sizeof(P) == 2 && !MASTER) {
-      // an infinity has nothing below its 16 bits, and NaNs of arithmetic are quiet: neither is changed by u
+      // An infinity has nothing below its 16 bits and stays one.  A NaN may have all of its bits set, where u would carry
+      // into the sign and beyond: eight values that hold one (four comparisons of two) are rounded apart.
       const W4 w = philox_adam((uint32_t)(e >> 3), s.step, (uint32_t)ck.tensor, ST_ADAMW_P, s.key);
+      const bool nan = __builtin_isunordered(pv[0], pv[1]) || __builtin_isunordered(pv[2], pv[3]) ||
+                       __builtin_isunordered(pv[4], pv[5]) || __builtin_isunordered(pv[6], pv[7]);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const uint32_t u = (i & 1) ? w.w[i >> 1] >> 16 : w.w[i >> 1] & 0xFFFFu;
+        uint32_t u = (i & 1) ? w.w[i >> 1] >> 16 : w.w[i >> 1] & 0xFFFFu;
+        if (__builtin_expect(nan, 0)) u = pv[i] != pv[i] ? 0 : u;
         pv[i] = __uint_as_float((__float_as_uint(pv[i]) + u) & 0xFFFF0000u);
       }
     }

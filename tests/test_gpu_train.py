@@ -757,3 +757,26 @@ def test_embed_grad_of_more_than_one_grid(dev, batch, n, vocab):
     key = (ids + torch.arange(batch, device=dev)[:, None] * vocab).view(-1)
     ref = torch.zeros(batch * vocab, device=dev).index_add_(0, key, dy.view(-1).float())
     assert torch.equal(got.view(-1), ref)
+
+
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+@pytest.mark.parametrize("bits", [0x7FFFFFFF, -1, 0x7FC00000, 0x7F80FFFF])
+def test_adamw_random_rounding_keeps_nan(dev, state, bits):
+    """A NaN whose bits are all ones has no room for a random addend: bf16 parameters must not come out as zeros."""
+    import paper_2402_03994_amd as fw
+    n = 4096 + 77
+    opt = fw.AdamW([n], state=state, seed=5)
+    p = torch.full((n,), 0.5, dtype=BF16, device=dev)
+    g = torch.ones(n, device=dev)
+    bad = torch.arange(n, device=dev) % 97 == 3
+    g.view(torch.int32)[bad] = bits
+    opt.step([p], [g], 1, lr=0.125)
+    assert torch.isnan(p[bad]).all()
+    assert torch.isfinite(p[~bad]).all()
+    if state == "f32":  # the same NaN from a moment
+        q = torch.full((n,), 0.5, dtype=BF16, device=dev)
+        opt.m.zero_()
+        opt.v.zero_()
+        opt.m[:n].view(torch.int32)[bad] = bits
+        opt.step([q], [torch.ones(n, device=dev)], 1, lr=0.125)
+        assert torch.isnan(q[bad]).all() and torch.isfinite(q[~bad]).all()
