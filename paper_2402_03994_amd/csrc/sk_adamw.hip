@@ -175,10 +175,13 @@ __device__ __forceinline__ W4 philox_adam(uint32_t c0, uint32_t c1, uint32_t c2,
   return W4{{c0, c1, c2, c3}};
 }
 
-// m / (sqrt(v) root + eps).  The hardware's square root and reciprocal (one unit in the last place each, nothing for
-// inputs below 2^-126) serve where eps is large beside 2^-63; an eps as small takes the correctly rounded ones.
+// m / (sqrt(v) root + eps), square root and quotient rounded correctly where the parameter is held in 32 bits (EXACT).
+// Where it is about to be rounded at random to 8 bits, the hardware's square root and reciprocal serve (one unit in the
+// last of 24 each, nothing for inputs below 2^-126), with an eps that is large beside 2^-63.  124 million elements, moments
+// in 32 bits: 583 us exact and 588 us by the hardware's; in 8 bits, fp32 parameters and bf16 gradients: 314 us, 299 us.
+template <bool EXACT>
 __device__ __forceinline__ float ratio(float m, float v, float root, float eps, bool tiny_eps) {
-  if (tiny_eps) return m / (sqrtf(v) * root + eps);
+  if (EXACT || tiny_eps) return m / __builtin_fmaf(sqrtf(v), root, eps);
   return m * __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_sqrtf(v), root, eps));
 }
 
@@ -234,7 +237,7 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
     const bool tiny_eps = s.eps < 1e-12f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      pv[i] -= __builtin_fmaf(s.rate, ratio(m[i], v[i], s.root, s.eps, tiny_eps), shrink * pv[i]);
+      pv[i] -= __builtin_fmaf(s.rate, ratio<sizeof(P) == 4 || MASTER>(m[i], v[i], s.root, s.eps, tiny_eps), shrink * pv[i]);
     if (STATE == SK_ADAMW_F32) {
       store8((float *)mp, at, kPer, m);
       store8((float *)vp, at, kPer, v);

@@ -780,3 +780,22 @@ def test_adamw_random_rounding_keeps_nan(dev, state, bits):
         opt.m[:n].view(torch.int32)[bad] = bits
         opt.step([q], [torch.ones(n, device=dev)], 1, lr=0.125)
         assert torch.isnan(q[bad]).all() and torch.isfinite(q[~bad]).all()
+
+
+@pytest.mark.parametrize("state,master", [("f32", False), ("8bit", False), ("f32", True), ("8bit", True)])
+def test_adamw_quotient_is_rounded_correctly(dev, state, master):
+    """A first step from zero parameters with b1 = b2 = 0 and lr = 1 leaves p = -g / (sqrt(g^2) + eps): the square root,
+    the sum and the quotient round once each, 3 times 2^-24."""
+    import paper_2402_03994_amd as fw
+    n = 1 << 20
+    gen = torch.Generator().manual_seed(3)
+    g = torch.exp(8 * torch.randn(n, generator=gen)).clamp(2.0 ** -20, 2.0 ** 20)
+    opt = fw.AdamW([n], state=state)
+    p = torch.zeros(n, dtype=BF16 if master else F32, device=dev)
+    mast = torch.zeros(n, device=dev) if master else None
+    eps = 2.0 ** -6
+    opt.step([p], [g.to(dev)], 1, lr=1.0, betas=(0.0, 0.0), eps=eps, weight_decay=0.0, masters=[mast] if master else None)
+    v = (g * g).double().numpy()
+    ref = -g.double().numpy() / (np.sqrt(v) + eps)
+    got = host(mast if master else p)
+    assert (np.abs(got - ref) <= 3 * 2.0 ** -24 * 1.000001 * np.abs(ref)).all()
