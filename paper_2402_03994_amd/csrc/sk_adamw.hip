@@ -177,8 +177,9 @@ __device__ __forceinline__ W4 philox_adam(uint32_t c0, uint32_t c1, uint32_t c2,
 
 // m / (sqrt(v) root + eps), square root and quotient rounded correctly where the parameter is held in 32 bits (EXACT).
 // Where it is about to be rounded at random to 8 bits, the hardware's square root and reciprocal serve (one unit in the
-// last of 24 each, nothing for inputs below 2^-126), with an eps that is large beside 2^-63.  124 million elements, moments
-// in 32 bits: 583 us exact and 588 us by the hardware's; in 8 bits, fp32 parameters and bf16 gradients: 314 us, 299 us.
+// last of 24 each, nothing for inputs below 2^-126), with an eps beside which root 2^-63 is nothing.  124 million
+// elements, moments in 32 bits: 583 us exact and 588 us by the hardware's; in 8 bits, fp32 parameters and bf16
+// gradients: 314 us, 299 us.
 template <bool EXACT>
 __device__ __forceinline__ float ratio(float m, float v, float root, float eps, bool tiny_eps) {
   if (EXACT || tiny_eps) return m / __builtin_fmaf(sqrtf(v), root, eps);
@@ -234,7 +235,7 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
       v[i] = va + vb;
     }
     // the change is formed first, so that the parameter is rounded once
-    const bool tiny_eps = s.eps < 1e-12f;
+    const bool tiny_eps = s.eps < s.root * 0x1p-39f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
       pv[i] -= __builtin_fmaf(s.rate, ratio<sizeof(P) == 4 || MASTER>(m[i], v[i], s.root, s.eps, tiny_eps), shrink * pv[i]);

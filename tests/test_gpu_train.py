@@ -799,3 +799,19 @@ def test_adamw_quotient_is_rounded_correctly(dev, state, master):
     ref = -g.double().numpy() / (np.sqrt(v) + eps)
     got = host(mast if master else p)
     assert (np.abs(got - ref) <= 3 * 2.0 ** -24 * 1.000001 * np.abs(ref)).all()
+
+
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+def test_adamw_small_second_moments_under_a_large_correction(dev, state):
+    """b2 next to 1 makes the bias correction 1 / sqrt(1 - b2^t) large, and v far below 2^-126 counts beside eps."""
+    import paper_2402_03994_amd as fw
+    n = 512
+    opt = fw.AdamW([n], state=state)
+    p, g = torch.zeros(n, dtype=BF16, device=dev), torch.full((n,), 1e-13, device=dev)
+    b2 = 1 - 1e-14
+    opt.step([p], [g], 1, lr=1.0, betas=(0.0, b2), eps=1e-12, weight_decay=0.0)
+    m, v = O.adamw_moments(np.zeros(1, np.float32), np.zeros(1, np.float32), np.full(1, 1e-13, np.float32), 0.0, b2, 1.0)
+    assert 0 < v[0] < 2.0 ** -126
+    want = float(O.adamw_param(np.zeros(1), m, v, 1, 1.0, 0.0, b2, 1e-12, 0.0)[0])
+    assert abs(want + 1 / 11) < 1e-3
+    assert (np.abs(host(p) - want) <= 2.0 ** -7 * abs(want)).all()  # up or down to a neighbour in bf16
