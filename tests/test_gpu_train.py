@@ -815,3 +815,29 @@ def test_adamw_small_second_moments_under_a_large_correction(dev, state):
     want = float(O.adamw_param(np.zeros(1), m, v, 1, 1.0, 0.0, b2, 1e-12, 0.0)[0])
     assert abs(want + 1 / 11) < 1e-3
     assert (np.abs(host(p) - want) <= 2.0 ** -7 * abs(want)).all()  # up or down to a neighbour in bf16
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.7])
+@pytest.mark.parametrize("vocab,rows", [(300, 5), (2500, 600), (15013, 5), (140003, 3)])
+def test_small_entries_of_an_fp32_gradient(dev, vocab, rows, scale):
+    """Entries far below the largest keep fp32's precision.  x - m is exact here; an entry p_j rounds in the hardware's
+    exponential (2 halves of a unit), its correction, the factor c / z and the product with it, and z = 1.01 at most in
+    its last few additions (8): 13 times 2^-24."""
+    import paper_2402_03994_amd as fw
+    r = np.random.default_rng(vocab)
+    x = -r.integers(64 * 16, 64 * 80, (rows, vocab)) / 64.0
+    t = r.integers(0, vocab, rows)
+    x[np.arange(rows), t] = 0.0
+    s = float(np.float32(scale))
+    if s < 1:
+        x[x < 0] -= 8.0
+    xd, td = torch.from_numpy(x.astype(np.float32)).to(dev), torch.from_numpy(t).to(dev)
+    p = O.softmax_rows(x, s)[0]
+    other = np.arange(vocab)[None, :] != t[:, None]
+    one = torch.ones(rows, device=dev)
+    logp, stats = fw.token_logp(xd, td, scale=scale)
+    d = host(fw.token_logp_grad(xd, td, stats, one, scale=scale))
+    tol = 13 * 2.0 ** -24 * s * p
+    assert (np.abs(d + s * p) <= tol)[other].all()
+    d = host(fw.policy_loss(xd, td, logp, -one, one, scale=scale).dlogits)  # ratio 1: the factor is 1
+    assert (np.abs(d + s * p) <= tol)[other].all()
