@@ -4,7 +4,10 @@ Argument marshalling only: the embedding lookup and its gradient, the token
 log-probabilities, the policy and preference losses with their gradients and
 the AdamW step run in the HIP kernels of libsketch.so on torch's current
 stream.  The losses return the gradient with respect to the logits next to the
-loss: a model continues with logits.backward(dlogits).
+loss: a model continues with logits.backward(dlogits).  No call records itself for
+autograd (embed() of a weight that requires a gradient gives a tensor without one);
+what a call overwrites counts as modified in place, so that a graph that has saved
+it refuses its backward pass.
 """
 from __future__ import annotations
 
@@ -14,6 +17,7 @@ import operator
 from typing import NamedTuple, Optional, Sequence
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import _lib
 from .sketch import _DT, _stream_ptr
@@ -85,7 +89,8 @@ def embed(weight: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: O
     ld = _rows(weight, "weight")
     index = _ids(tokens, "tokens", device)
     shape = (*tokens.shape, weight.shape[1])
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(shape, dtype=out_dtype or weight.dtype, device=device)
     elif out.shape != shape or out.device != device or not out.is_contiguous() or \
             (out_dtype is not None and out.dtype != out_dtype):
@@ -93,6 +98,8 @@ def embed(weight: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: O
     _lib.check(_lib.load().sketch_embed(weight.data_ptr(), _dtype(weight, "weight"), weight.shape[0], weight.shape[1], ld,
                                         tokens.data_ptr(), index, tokens.numel(), scale, out.data_ptr(),
                                         _dtype(out, "out"), device.index, _stream_ptr(device)))
+    if given:
+        increment_version(out)
     return out
 
 
@@ -118,7 +125,8 @@ def embed_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float 
         raise ValueError("per_example needs tokens [batch, ...]")
     batch = tokens.shape[0] if per_example else 1
     shape = (batch, vocab, width) if per_example else (vocab, width)
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate:
             raise ValueError("accumulate needs out")
         out = torch.empty(shape, dtype=out_dtype, device=device)
@@ -133,6 +141,8 @@ def embed_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float 
     _lib.check(lib.sketch_embed_grad(dy.data_ptr(), _dtype(dy, "dy"), ld, tokens.data_ptr(), index, batch, n, vocab,
                                      width, scale, out.data_ptr(), _dtype(out, "out"), int(accumulate),
                                      work.data_ptr(), nw, device.index, _stream_ptr(device)))
+    if given:
+        increment_version(out)
     return out
 
 
@@ -182,10 +192,12 @@ def token_logp_grad(logits: torch.Tensor, targets: torch.Tensor, stats: torch.Te
     if stats.dtype != torch.float32 or stats.device != logits.device or stats.shape != (n, 2) or not stats.is_contiguous():
         raise ValueError(f"stats must be contiguous float32 [{n}, 2] on {logits.device}")
     dp = _vec(dlogp, n, logits.device, "dlogp")
-    out, ld = _dlogits(logits, out)
-    _lib.check(_lib.load().sketch_token_logp_grad(ctypes.byref(x), stats.data_ptr(), dp, out.data_ptr(), ld,
+    d, ld = _dlogits(logits, out)
+    _lib.check(_lib.load().sketch_token_logp_grad(ctypes.byref(x), stats.data_ptr(), dp, d.data_ptr(), ld,
                                                   _stream_ptr(logits.device)))
-    return out
+    if out is not None:
+        increment_version(out)
+    return d
 
 
 def policy_loss(logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor,
@@ -208,6 +220,8 @@ def policy_loss(logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.Ten
     _lib.check(_lib.load().sketch_policy_loss(ctypes.byref(x), *args, clip[0], clip[1], kl_coef, loss.data_ptr(),
                                               logp.data_ptr(), token_loss.data_ptr(),
                                               d.data_ptr() if grad else None, ld, _stream_ptr(device)))
+    if grad and out is not None:
+        increment_version(out)
     return PolicyLoss(loss, logp, token_loss, d)
 
 
@@ -236,6 +250,8 @@ def preference_loss(logits: torch.Tensor, targets: torch.Tensor, offsets: torch.
     _lib.check(lib.sketch_preference_loss(ctypes.byref(x), offsets.data_ptr(), index, pairs, ref, beta, label_smoothing,
                                           int(average), at, at + 4, at + 4 + 8 * pairs, d.data_ptr() if grad else None,
                                           ld, work.data_ptr(), nw, _stream_ptr(device)))
+    if grad and out is not None:
+        increment_version(out)
     return PreferenceLoss(small[0], small[1:1 + 2 * pairs], small[1 + 2 * pairs:], d)
 
 
@@ -344,6 +360,7 @@ class AdamW:
                            None if self.v_exp is None else self.v_exp.data_ptr())
         _lib.check(self.lib.sketch_adamw_apply(self._h, ctypes.byref(a), pp, _DT[pdt], gp, _DT[gdt], mp,
                                                _stream_ptr(self.device)))
+        increment_version(params if masters is None else [*params, *masters])
         return norm
 
     def moments(self):

@@ -841,3 +841,37 @@ def test_small_entries_of_an_fp32_gradient(dev, vocab, rows, scale):
     assert (np.abs(d + s * p) <= tol)[other].all()
     d = host(fw.policy_loss(xd, td, logp, -one, one, scale=scale).dlogits)  # ratio 1: the factor is 1
     assert (np.abs(d + s * p) <= tol)[other].all()
+
+
+def test_writes_in_place_are_seen_by_autograd(dev):
+    """A graph that has saved what a call overwrites refuses its backward pass, as after any in-place operation."""
+    import paper_2402_03994_amd as fw
+    w = torch.randn(40, 8, device=dev, requires_grad=True)
+    t = torch.randint(0, 8, (40,), device=dev)
+    v = torch.zeros(40, device=dev)
+    stats = fw.token_logp(w.detach(), t)[1]
+    offs = torch.tensor([0, 20, 40], device=dev)
+    opt = fw.AdamW([(40, 8)])
+
+    def masters():
+        p = torch.zeros(40, 8, dtype=BF16, device=dev, requires_grad=True)
+        y = p * p
+        opt.step([p], [torch.ones(40, 8, device=dev)], 1, lr=0.1, masters=[w.detach()])
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.sum().backward()
+
+    d = lambda: w.detach()  # noqa: E731  (shares the version of w)
+    for write in (lambda: opt.step([w], [torch.ones(40, 8, device=dev)], 1, lr=0.1), masters,
+                  lambda: fw.embed(torch.randn(9, 8, device=dev), t, out=d()),
+                  lambda: fw.embed_grad(torch.randn(5, 8, device=dev), t[:5], 40, out=d()),
+                  lambda: fw.token_logp_grad(d(), t, stats, v, out=d()),
+                  lambda: fw.policy_loss(d(), t, v, v, v, out=d()),
+                  lambda: fw.preference_loss(d(), t, offs, v, out=d())):
+        y = w * w
+        write()
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.sum().backward()
+    y = w * w  # what only reads changes nothing
+    fw.policy_loss(d(), t, v, v, v)
+    fw.embed(d(), t)
+    y.sum().backward()
