@@ -180,7 +180,9 @@ int sketch_adamw_create(const int64_t *numel, const float *decay, int32_t n_tens
  * a 64th of it). */
 int64_t sketch_adamw_state_elems(const sk_adamw *h);
 
-/* One step's numbers; the pointers are device memory of the handle's device. */
+/* One step's numbers; the pointers are device memory of the handle's device.
+ * lr weight_decay, lr / (1 - beta1^step) and eps must be finite in fp32, and an
+ * eps above 0 must not become 0 there (SK_EINVAL). */
 typedef struct {
   int64_t step;            /* 1, 2, .. < 2^32 */
   double lr, beta1, beta2, eps, weight_decay;

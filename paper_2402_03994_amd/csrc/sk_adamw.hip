@@ -449,10 +449,6 @@ int sketch_adamw_apply(sk_adamw *h, const sk_adamw_step *a, void *const *params,
   if (!std::isfinite(a->lr) || !std::isfinite(a->weight_decay) || !(a->eps >= 0.0) || !std::isfinite(a->eps))
     return train_fail(SK_EINVAL, "lr and weight_decay must be finite, eps finite and >= 0");
   if (!(a->max_norm >= 0.0)) return train_fail(SK_EINVAL, "max_norm must be >= 0");
-  for (int l = 0; l < h->n_tensors; ++l)
-    if (!params[l] || !grads[l] || (masters && !masters[l])) return train_fail(SK_EINVAL, "NULL tensor pointer");
-  TrainGuard guard(h->device);
-  hipStream_t st = (hipStream_t)stream;
   AdamStep s;
   s.b1 = (float)a->beta1;
   s.c1 = (float)(1.0 - a->beta1);
@@ -464,6 +460,12 @@ int sketch_adamw_apply(sk_adamw *h, const sk_adamw_step *a, void *const *params,
   s.eps = (float)a->eps;
   s.step = (uint32_t)a->step;
   s.key = h->key;
+  if (!std::isfinite(s.lr_wd) || !std::isfinite(s.rate) || !std::isfinite(s.eps) || (a->eps > 0.0 && s.eps == 0.0f))
+    return train_fail(SK_EINVAL, "lr, lr weight_decay, lr / (1 - beta1^step) or eps is outside fp32");
+  for (int l = 0; l < h->n_tensors; ++l)
+    if (!params[l] || !grads[l] || (masters && !masters[l])) return train_fail(SK_EINVAL, "NULL tensor pointer");
+  TrainGuard guard(h->device);
+  hipStream_t st = (hipStream_t)stream;
   const bool clip = a->max_norm > 0.0, few = h->n_chunks <= kFewChunks;
   s.scale = clip && !few ? h->d_scale : a->grad_scale;
   s.part = clip && few ? h->d_part : nullptr;

@@ -875,3 +875,17 @@ def test_writes_in_place_are_seen_by_autograd(dev):
     fw.policy_loss(d(), t, v, v, v)
     fw.embed(d(), t)
     y.sum().backward()
+
+
+def test_adamw_refuses_what_fp32_does_not_hold(dev):
+    """The step's numbers are fp32: an eps that becomes 0 would make 0 / 0 of a zero gradient, a rate that overflows NaN."""
+    import paper_2402_03994_amd as fw
+    opt, p, g = fw.AdamW([70]), [torch.ones(70, device=dev)], [torch.zeros(70, device=dev)]
+    for kw in (dict(eps=1e-50), dict(eps=1e39), dict(lr=1e39), dict(lr=1e20, weight_decay=1e20),
+               dict(lr=1e38, betas=(0.999, 0.999))):
+        with pytest.raises(fw.SketchError):
+            opt.step(p, g, 1, **{**dict(lr=0.1), **kw})
+    assert (p[0] == 1).all() and not opt.m.any()
+    for eps in (1e-39, 1e38):
+        opt.step(p, g, 1, lr=0.1, eps=eps, weight_decay=0.0, max_norm=float("inf"))
+        assert (p[0] == 1).all()
