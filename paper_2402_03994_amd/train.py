@@ -323,11 +323,15 @@ class AdamW:
     def _pointers(self, tensors, name, dtype=None):
         # one C-level pass per property: a list of 150 parameters is checked in a third of a loop's time
         T = torch.Tensor
-        dt = tensors[0].dtype if dtype is None and len(tensors) else dtype
-        if list(map(T.numel, tensors)) != self.numels or set(map(_get_dtype, tensors)) != {dt} or \
-                set(map(T.get_device, tensors)) != {self.device.index} or not all(map(T.is_contiguous, tensors)):
-            raise ValueError(f"{name}: contiguous {dt} tensors on {self.device} with these counts are needed: "
-                             f"{self.numels[:8]}{'..' if len(self.numels) > 8 else ''}")
+        try:
+            dt = tensors[0].dtype if dtype is None else dtype
+            same = list(map(T.numel, tensors)) == self.numels and set(map(_get_dtype, tensors)) == {dt} and \
+                set(map(T.get_device, tensors)) == {self.device.index} and all(map(T.is_contiguous, tensors))
+        except (TypeError, AttributeError, IndexError):  # not a list, or not of tensors
+            dt, same = dtype, False
+        if not same:
+            raise ValueError(f"{name}: contiguous {dt or 'float32 or bfloat16'} tensors on {self.device} with these counts are "
+                             f"needed: {self.numels[:8]}{'..' if len(self.numels) > 8 else ''}")
         at = array.array("Q", list(map(T.data_ptr, tensors)))  # two thirds of the time of filling the ctypes array itself
         return (ctypes.c_void_p * len(tensors)).from_buffer(at), dt
 
@@ -335,7 +339,8 @@ class AdamW:
              betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
              masters: Optional[Sequence[torch.Tensor]] = None, grad_scale: Optional[torch.Tensor] = None,
              max_norm: Optional[float] = None) -> Optional[torch.Tensor]:
-        """One step (1, 2, ..) on params (float32 or bfloat16, in place).
+        """One step (1, 2, ..) on params (float32 or bfloat16, in place), one type for all of them and one for all grads;
+        every tensor of the list takes part, so that each needs a gradient.
 
         masters: float32 copies of bfloat16 params that the step is taken on; without them bfloat16 params are rounded
         at random.  grad_scale: one float32 on the device that multiplies the gradients; a step where it is not finite

@@ -889,3 +889,15 @@ def test_adamw_refuses_what_fp32_does_not_hold(dev):
     for eps in (1e-39, 1e38):
         opt.step(p, g, 1, lr=0.1, eps=eps, weight_decay=0.0, max_norm=float("inf"))
         assert (p[0] == 1).all()
+
+
+def test_adamw_refuses_lists_of_other_things(dev):
+    import paper_2402_03994_amd as fw
+    opt, p, g = fw.AdamW([5, 7]), [torch.ones(5, device=dev), torch.ones(7, device=dev)], None
+    g = [torch.ones_like(t) for t in p]
+    for bad in ([g[0], None], [None, None], [], None, g[0], [g[0], 3.0], [g[0], g[1].cpu()], [g[0], g[1].bfloat16()]):
+        with pytest.raises(ValueError):
+            opt.step(p, bad, 1, lr=0.1)
+        with pytest.raises(ValueError):
+            opt.step(bad, g, 1, lr=0.1)
+    assert all((t == 1).all() for t in p)
