@@ -67,7 +67,8 @@ int sketch_embed_grad(const void *dy, sk_dtype dtype, int64_t ld, const void *id
  *   targets  [rows]; a target outside [0, vocab) masks its position: the row of
  *            logits is not read, its log-probability counts as 0 and its
  *            gradient is a row of zeros.
- *   scale    > 0: the softmax is that of scale * data (1 / temperature).
+ *   scale    in [2^-120, 2^127]: the softmax is that of scale * data
+ *            (1 / temperature).
  * vocab < 2^31.
  */
 typedef struct {

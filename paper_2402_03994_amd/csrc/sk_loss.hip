@@ -499,7 +499,9 @@ int check_logits(const sk_logits *x) {
   if (x->index != SK_I32 && x->index != SK_I64) return train_fail(SK_EDTYPE, "unknown index type");
   if (x->rows < 0 || x->vocab < 1 || x->ld < x->vocab)
     return train_fail(SK_EINVAL, "need rows >= 0, vocab >= 1 and ld >= vocab");
-  if (!(x->scale > 0.0f) || !std::isfinite(x->scale)) return train_fail(SK_EINVAL, "scale must be positive and finite");
+  // scale log2 e stays finite, and where x - m overflows, the exponent -2^128 scale of its exponential is one of 0
+  if (!(x->scale >= 0x1p-120f && x->scale <= 0x1p127f))
+    return train_fail(SK_EINVAL, "scale must be in [2^-120, 2^127]");
   if (x->rows > INT32_MAX || x->vocab > INT32_MAX)
     return train_fail(SK_EUNSUPPORTED, "more than 2^31 - 1 rows or columns");
   if (x->rows && (!x->data || !x->targets)) return train_fail(SK_EINVAL, "NULL argument");

@@ -114,3 +114,16 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
                  lambda: fw.preference_loss(x, t, torch.tensor([0, 1, 2]), v)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_losses_refuse_scales_that_fp32_products_do_not_hold():
+    """scale log2 e has to be finite, and a difference of finite logits that overflows has to be an exponential of 0."""
+    L = _lib.load()
+    for scale in (3e38, 1.8e38, 7e-37, 1e-39, 1e-45):
+        x = logits(scale=scale, rows=0)  # refused whatever the rows
+        assert L.sketch_token_logp(x, P, P, None) == -1, scale
+        assert L.sketch_token_logp_grad(x, P, P, P, 8, None) == -1
+        assert L.sketch_policy_loss(x, P, P, P, None, 0.2, 0.2, 0.0, P, P, P, P, 8, None) == -1
+        assert L.sketch_preference_loss(x, P, 1, 1, P, 0.1, 0.0, 0, P, P, P, P, 8, P, 1 << 40, None) == -1
+    for scale in (1.7e38, 1.0, 7.6e-37):
+        assert L.sketch_token_logp(logits(scale=scale, rows=0), P, P, None) == 0
