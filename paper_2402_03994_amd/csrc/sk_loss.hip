@@ -81,7 +81,10 @@ struct Stats {
 };
 
 __device__ __forceinline__ float logp_of(float xt, Stats s, float scale) {
-  return s.z == 0.0f ? -INFINITY : (xt - s.m) * scale - logf(s.z);
+  if (s.z == 0.0f) return -INFINITY;
+  float a = (xt - s.m) * scale;
+  if (a == -INFINITY) a = (0.5f * xt - 0.5f * s.m) * scale * 2.0f;  // the difference alone may have overflowed
+  return a - logf(s.z);
 }
 
 // A row cut at 16-byte boundaries: `head` entries before the first one, nv vectors, `rem` entries after the last.

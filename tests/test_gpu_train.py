@@ -901,3 +901,23 @@ def test_adamw_refuses_lists_of_other_things(dev):
         with pytest.raises(ValueError):
             opt.step(bad, g, 1, lr=0.1)
     assert all((t == 1).all() for t in p)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_targets_too_far_for_a_difference(dev, dt):
+    """x_t - m overflows while scale (x_t - m) does not."""
+    import paper_2402_03994_amd as fw
+    x = torch.full((3, 100), -3e38).to(dt)
+    x[:, 7] = 3e38
+    x[1] = -float("inf")
+    x[1, 7] = 3e38
+    t = torch.tensor([5, 5, 7])
+    for scale in (0.25, 2.0 ** -100, 2.0 ** -120):
+        logp, stats = fw.token_logp(x.to(dev), t.to(dev), scale=scale)
+        want = O.token_logp(x.double().numpy(), t.numpy(), scale)
+        assert np.isfinite(want[[0, 2]]).all() and want[1] == -np.inf
+        got = host(logp)
+        assert got[1] == -np.inf and (np.abs(got - want)[[0, 2]] <= 2.0 ** -22 * np.abs(want[[0, 2]])).all()
+        one = torch.ones(3, device=dev)
+        d = fw.policy_loss(x.to(dev), t.to(dev), logp.clamp(min=-3e38), one, one, scale=scale)
+        assert np.array_equal(host(d.logp), got)
