@@ -465,6 +465,7 @@ int sketch_adamw_apply(sk_adamw *h, const sk_adamw_step *a, void *const *params,
   for (int l = 0; l < h->n_tensors; ++l)
     if (!params[l] || !grads[l] || (masters && !masters[l])) return train_fail(SK_EINVAL, "NULL tensor pointer");
   TrainGuard guard(h->device);
+  if (!guard.ok) return train_no_device();
   hipStream_t st = (hipStream_t)stream;
   const bool clip = a->max_norm > 0.0, few = h->n_chunks <= kFewChunks;
   s.scale = clip && !few ? h->d_scale : a->grad_scale;
@@ -511,6 +512,7 @@ int sketch_adamw_moments(sk_adamw *h, const uint8_t *m, const uint8_t *m_exp, co
   if (!h || !m || !m_exp || !v || !v_exp || !m_out || !v_out) return train_fail(SK_EINVAL, "NULL argument");
   if (h->state != SK_ADAMW_8BIT) return train_fail(SK_EINVAL, "the moments of this handle are fp32");
   TrainGuard guard(h->device);
+  if (!guard.ok) return train_no_device();
   const int64_t groups = h->elems / kPer;
   hipLaunchKernelGGL(k_adamw_moments, dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, (hipStream_t)stream, groups,
                      (const uint2 *)m, m_exp, (const uint2 *)v, v_exp, m_out, v_out);

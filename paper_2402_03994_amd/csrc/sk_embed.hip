@@ -589,6 +589,7 @@ int sketch_embed(const void *weight, sk_dtype dtype, int64_t vocab, int64_t widt
   if (n == 0) return SK_OK;
   if (!weight || !ids || !out) return train_fail(SK_EINVAL, "NULL argument");
   TrainGuard guard(device);
+  if (!guard.ok) return train_no_device();
   hipStream_t st = (hipStream_t)stream;
   if (dtype == SK_F32 && out_dtype == SK_F32)
     run_embed<float, float>(weight, vocab, width, ld, ids, index, n, scale, out, st);
@@ -622,6 +623,7 @@ int sketch_embed_grad(const void *dy, sk_dtype dtype, int64_t ld, const void *id
   if (n && work_bytes < sketch_embed_grad_work_bytes(batch, n, width))
     return train_fail(SK_EINVAL, "work is smaller than sketch_embed_grad_work_bytes");
   TrainGuard guard(device);
+  if (!guard.ok) return train_no_device();
   hipStream_t st = (hipStream_t)stream;
   if (dtype == SK_F32 && out_dtype == SK_F32)
     return run_eg<float>(dy, ld, ids, index, batch, n, vocab, width, scale, (float *)out, accumulate, work, st);

@@ -649,6 +649,7 @@ int sketch_token_logp(const sk_logits *x, float *logp, float *stats, void *strea
   if (rc != SK_OK || x->rows == 0) return rc;
   if (!logp) return train_fail(SK_EINVAL, "NULL argument");
   TrainGuard guard(x->device);
+  if (!guard.ok) return train_no_device();
   run_logp(x, logp, stats, nullptr, (hipStream_t)stream);
   return train_launched();
 }
@@ -660,6 +661,7 @@ int sketch_token_logp_grad(const sk_logits *x, const float *stats, const float *
   if (!stats || !dlogp || !dlogits) return train_fail(SK_EINVAL, "NULL argument");
   if ((rc = check_out(x, dlogits, ld_out)) != SK_OK) return rc;
   TrainGuard guard(x->device);
+  if (!guard.ok) return train_no_device();
   run_logp_grad(x, stats, dlogp, dlogits, ld_out, PairTotal(), (hipStream_t)stream);
   return train_launched();
 }
@@ -677,6 +679,7 @@ int sketch_policy_loss(const sk_logits *x, const float *old_logp, const float *a
   if (x->rows && kl_coef != 0.0f && !ref_logp) return train_fail(SK_EINVAL, "kl_coef needs ref_logp");
   if ((rc = check_out(x, dlogits, ld_out)) != SK_OK) return rc;
   TrainGuard guard(x->device);
+  if (!guard.ok) return train_no_device();
   hipStream_t st = (hipStream_t)stream;
   const Rows r = rows_of(x);
   const Policy p{old_logp, advantages, weights, ref_logp, 1.0f - clip_low, 1.0f + clip_high, kl_coef};
@@ -713,6 +716,7 @@ int sketch_preference_loss(const sk_logits *x, const void *offsets, sk_index off
     return train_fail(SK_EINVAL, "work is smaller than sketch_preference_work_bytes");
   if ((rc = check_out(x, dlogits, ld_out)) != SK_OK) return rc;
   TrainGuard guard(x->device);
+  if (!guard.ok) return train_no_device();
   hipStream_t st = (hipStream_t)stream;
   float *stats = (float *)work, *logp = stats + 2 * x->rows, *rowc = logp + x->rows;
   const Pairs p{offsets, (int32_t)offsets_index, average, pairs, x->rows, ref_logp, beta, smoothing};

@@ -27,14 +27,17 @@ inline int train_launched() noexcept {
 
 struct TrainGuard {  // the caller's current device again on scope exit
   int prev = -1, dev;
+  bool ok;  // false: there is no device `dev`
   explicit TrainGuard(int d) : dev(d) {
     if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-    if (prev != dev) (void)hipSetDevice(dev);
+    ok = dev >= 0 && (prev == dev || hipSetDevice(dev) == hipSuccess);
+    if (!ok) (void)hipGetLastError();
   }
   ~TrainGuard() {
     if (prev >= 0 && prev != dev) (void)hipSetDevice(prev);
   }
 };
+inline int train_no_device() noexcept { return train_fail(SK_EINVAL, "device out of range"); }
 
 // Elements: float or bf16 (held as its 16 bits).
 struct bf16 {

@@ -127,3 +127,18 @@ def test_losses_refuse_scales_that_fp32_products_do_not_hold():
         assert L.sketch_preference_loss(x, P, 1, 1, P, 0.1, 0.0, 0, P, P, P, P, 8, P, 1 << 40, None) == -1
     for scale in (1.7e38, 1.0, 7.6e-37):
         assert L.sketch_token_logp(logits(scale=scale, rows=0), P, P, None) == 0
+
+
+@pytest.mark.parametrize("device", [-1, 99])
+def test_a_device_that_does_not_exist_is_refused(device):
+    """Nothing is queued on another device instead."""
+    L = _lib.load()
+    x = logits(device=device)
+    assert L.sketch_token_logp(x, P, P, None) == -1
+    assert L.sketch_token_logp_grad(x, P, P, P + 64, 8, None) == -1
+    assert L.sketch_policy_loss(x, P, P, P, None, 0.2, 0.2, 0.0, P, P, P, P + 64, 8, None) == -1
+    assert L.sketch_preference_loss(x, P, 1, 1, P, 0.1, 0.0, 0, P, P, P, P + 64, 8, P, 1 << 40, None) == -1
+    assert L.sketch_embed(P, 0, 4, 8, 8, P, 1, 3, 1.0, P, 0, device, None) == -1
+    nw = L.sketch_embed_grad_work_bytes(2, 3, 8)
+    assert L.sketch_embed_grad(P, 0, 8, P, 1, 2, 3, 4, 8, 1.0, P, 0, 0, P, nw, device, None) == -1
+    assert b"device" in L.sketch_last_error()
