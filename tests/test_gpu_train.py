@@ -921,3 +921,19 @@ def test_targets_too_far_for_a_difference(dev, dt):
         one = torch.ones(3, device=dev)
         d = fw.policy_loss(x.to(dev), t.to(dev), logp.clamp(min=-3e38), one, one, scale=scale)
         assert np.array_equal(host(d.logp), got)
+
+
+def test_stream_without_the_short_way(dev, monkeypatch):
+    """torch's own function for the raw stream is a shortcut: without it the public way gives the same stream."""
+    import paper_2402_03994_amd as fw
+    from paper_2402_03994_amd import sketch
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        want = sketch._stream_ptr(dev)
+        assert want == side.cuda_stream
+        monkeypatch.setattr(sketch, "_raw_stream", None)
+        assert sketch._stream_ptr(dev) == want
+        x = fw.embed(torch.ones(3, 4, device=dev), torch.tensor([0, 2], device=dev))
+    side.synchronize()
+    assert (x == 1).all()
+    assert sketch._stream_ptr(dev) == torch.cuda.current_stream(dev).cuda_stream
