@@ -937,3 +937,47 @@ def test_stream_without_the_short_way(dev, monkeypatch):
     side.synchronize()
     assert (x == 1).all()
     assert sketch._stream_ptr(dev) == torch.cuda.current_stream(dev).cuda_stream
+
+
+# a vocabulary and a number of rows for each shape that a row's threads take (vectors of 4 or 8 columns by the type), with
+# gradients on both sides of the size from which they are stored past the caches
+SHAPES = [(F32, 1500, 515), (F32, 2500, 1030), (F32, 6007, 27), (F32, 15013, 27), (F32, 30522, 27), (F32, 32000, 530),
+          (BF16, 3001, 515), (BF16, 5003, 1030), (BF16, 20011, 27), (BF16, 30522, 27), (BF16, 32000, 1061)]
+
+
+@pytest.mark.parametrize("dt,vocab,rows", SHAPES)
+def test_losses_of_every_row_shape(dev, dt, vocab, rows):
+    import paper_2402_03994_amd as fw
+    x, t = make_logits(rows, vocab, dt, vocab + rows)
+    t[[k for k in range(rows) if k % 9 in (4, 6)]] = -1  # logs of 0: looked at elsewhere
+    old, adv, w, ref = policy_inputs(x, t, vocab)
+    f = lambda v: v.double().numpy()  # noqa: E731
+    xh, th = f(x), t.numpy()
+    lo, kl = float(np.float32(0.2)), float(np.float32(0.2))
+    loss, logp, tok, dref = O.policy(xh, th, f(old), f(adv), f(w), f(ref), lo, lo, kl, 1.0)
+    live = (th >= 0) & (th < vocab) & (f(w) != 0)
+    A, p = exponent_sizes(x, 1.0), np.nan_to_num(O.softmax_rows(xh, 1.0)[0])
+    z = lambda v: np.where(live, v, 0.0)  # noqa: E731
+    e = err_logp(A.max(1), vocab) + (np.abs(logp) + 4) * 2.0 ** -22
+    size = z(np.abs(f(adv)) * np.exp(logp - f(old)) + kl * (2 + np.exp(f(ref) - logp)))
+    c = z(f(w)) * O.policy_tokens(z(logp), z(f(old)), z(f(adv)), z(f(ref)), lo, lo, kl)[1]
+    rel = (2 * err_logp(A, vocab) + 2 * err_logp(0.0, vocab)) * p
+    tol = np.abs(c)[:, None] * rel + (z(f(w)) * size * (e + 2.0 ** -22))[:, None] + (HALF[dt] + 2.0 ** -22) * np.abs(dref) + 1e-37
+    for lead, pad in ((0, 0), (1, 3)):
+        xd, args = odd(x, dev, lead, pad), [v.to(dev) for v in (t, old, adv, w)]
+        got = fw.policy_loss(xd, *args, ref_logp=ref.to(dev), kl_coef=0.2)
+        check_logp(host(got.logp), logp, A, vocab, x, 1.0)
+        assert (np.abs(host(got.token_loss) - tok) <= size * e + 2.0 ** -22 * size).all()
+        assert abs(float(got.loss) - loss) <= (z(f(w)) * (size * e + 2.0 ** -22 * size)).sum() + 2.0 ** -24 * abs(loss)
+        assert (np.abs(host(got.dlogits) - dref) <= tol).all()
+        lp, stats = fw.token_logp(xd, args[0])
+        check_logp(host(lp), O.token_logp(xh, th, 1.0), A, vocab, x, 1.0)
+        cd = torch.from_numpy(np.where(live, c, 0.0).astype(np.float32))
+        d = fw.token_logp_grad(xd, args[0], stats, cd.to(dev))
+        dlog = O.token_logp_grad(xh, th, f(cd), 1.0)
+        assert (np.abs(host(d) - dlog) <= np.abs(f(cd))[:, None] * rel + (HALF[dt] + 2.0 ** -22) * np.abs(dlog) + 1e-37).all()
+        keep = xd.clone()
+        assert torch.equal(fw.token_logp_grad(xd, args[0], stats, cd.to(dev), out=xd), d)  # in place
+        xd.copy_(keep)
+        again = fw.policy_loss(xd, *args, ref_logp=ref.to(dev), kl_coef=0.2, out=xd)
+        assert torch.equal(again.dlogits, got.dlogits) and torch.equal(again.loss, got.loss)
