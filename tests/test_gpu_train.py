@@ -981,3 +981,39 @@ def test_losses_of_every_row_shape(dev, dt, vocab, rows):
         xd.copy_(keep)
         again = fw.policy_loss(xd, *args, ref_logp=ref.to(dev), kl_coef=0.2, out=xd)
         assert torch.equal(again.dlogits, got.dlogits) and torch.equal(again.loss, got.loss)
+
+
+@pytest.mark.parametrize("n,vocab,width,dt", [(300_001, 5000, 3, F32), (600_001, 5000, 3, BF16), (140_001, 300, 515, BF16),
+                                              (280_001, 300, 515, F32), (600_001, 7, 8, BF16)])
+def test_embed_grad_in_larger_tiles(dev, n, vocab, width, dt):
+    """Long batches are added up 32 and 64 tokens at a time.  The entries are small whole numbers, so that every sum is
+    exact in fp32, whatever its order."""
+    import paper_2402_03994_amd as fw
+    g = torch.Generator(device=dev).manual_seed(n)
+    ids = ((vocab + 1.0) ** torch.rand(n, generator=g, device=dev, dtype=torch.float64) - 1).long().clamp_(0, vocab - 1)
+    ids[torch.rand(n, generator=g, device=dev) < 0.3] = vocab // 2  # an id that crosses thousands of tiles
+    ids[torch.rand(n, generator=g, device=dev) < 0.05] = -1
+    ids[-70:] = vocab
+    dy = torch.randint(-3, 4, (n, width), generator=g, device=dev).to(dt)
+    live = (ids >= 0) & (ids < vocab)
+    ref = torch.zeros(vocab, width, dtype=torch.float64, device=dev).index_add_(0, ids[live], dy[live].double())
+    assert torch.equal(fw.embed_grad(dy, ids, vocab, scale=0.5).double(), 0.5 * ref)
+    out = torch.randint(-3, 4, (vocab, width), generator=g, device=dev).float()
+    want = 0.5 * ref + out
+    assert torch.equal(fw.embed_grad(dy, ids.int(), vocab, scale=0.5, out=out, accumulate=True).double(), want)
+
+
+@pytest.mark.parametrize("odt", [F32, BF16])
+@pytest.mark.parametrize("lead", range(1, 9))
+def test_embed_grad_zeroes_its_own_memory_alone(dev, odt, lead):
+    """An output at any address, between entries that are somebody else's."""
+    import paper_2402_03994_amd as fw
+    n, vocab, width = 1100, 301, 7
+    buf = torch.full((lead + vocab * width + 9,), 5.0, dtype=odt, device=dev)
+    out = buf[lead:lead + vocab * width].view(vocab, width)
+    ids = torch.arange(n, device=dev) % 50 * 3
+    got = fw.embed_grad(torch.ones(n, width, device=dev), ids, vocab, out=out)
+    assert got.data_ptr() == out.data_ptr()
+    ref = torch.zeros(vocab, device=dev).index_add_(0, ids, torch.ones(n, device=dev))
+    assert torch.equal(out.float(), ref[:, None].expand(vocab, width))
+    assert (buf[:lead] == 5).all() and (buf[lead + vocab * width:] == 5).all()
