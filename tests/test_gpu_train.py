@@ -1017,3 +1017,58 @@ def test_embed_grad_zeroes_its_own_memory_alone(dev, odt, lead):
     ref = torch.zeros(vocab, device=dev).index_add_(0, ids, torch.ones(n, device=dev))
     assert torch.equal(out.float(), ref[:, None].expand(vocab, width))
     assert (buf[:lead] == 5).all() and (buf[lead + vocab * width:] == 5).all()
+
+
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+@pytest.mark.parametrize("pdt,gdt,master", [(F32, F32, False), (F32, BF16, False), (BF16, BF16, False), (BF16, F32, True),
+                                            (BF16, BF16, True), (BF16, F32, False)])
+def test_adamw_of_two_launches(dev, state, pdt, gdt, master):
+    """180 tensors of 234 chunks: two launches that each form the norm, with every kind of state and parameter."""
+    assert len(SIZES) * 18 > 160 and sum((n + 4095) // 4096 for n in SIZES) * 18 <= 256
+    two_launches(dev, state, pdt, gdt, master, SIZES * 18)
+
+
+def two_launches(dev, state, pdt, gdt, master, sizes):
+    import paper_2402_03994_amd as fw
+    total, seed = sum(sizes), 2 ** 40 + 5
+    r = np.random.default_rng(12)
+    decay = [float(k % 3 > 0) for k in range(len(sizes))]
+    split = lambda t: list(torch.split(t, sizes))  # noqa: E731
+    p0 = torch.from_numpy(r.standard_normal(total).astype(np.float32))
+    buf = p0.to(pdt).to(dev)
+    mast = p0.to(dev) if master else None
+    hp = p0.double().numpy() if master else host(buf)
+    opt = fw.AdamW(sizes, state=state, decay=decay, seed=seed)
+    m, v = np.zeros(total, np.float32), np.zeros(total, np.float32)
+    wd = np.concatenate([np.full(n, 0.1 * d) for n, d in zip(sizes, decay)])
+    words = lambda k, step: np.concatenate([O.adamw_words(n, step, l, seed)[k] for l, n in enumerate(sizes)])  # noqa: E731
+    for step in (1, 2):
+        g = torch.from_numpy((r.standard_normal(total) * 0.01).astype(np.float32)).to(gdt)
+        norm = float(opt.step(split(buf), split(g.to(dev)), step, lr=0.01, betas=(0.9, 0.99), eps=1e-6, weight_decay=0.1,
+                              masters=split(mast) if master else None, max_norm=0.5))
+        gh = g.float().numpy()
+        want = np.sqrt((gh.astype(np.float64) ** 2).sum())
+        assert want > 0.5 and abs(norm - want) <= 2.0 ** -23 * want
+        s = min(np.float32(1.0), np.float32(0.5) / (np.float32(norm) + np.float32(1e-6)))
+        m, v = O.adamw_moments(m, v, gh, 0.9, 0.99, s)
+        ref = O.adamw_param(hp, m, v, step, 0.01, 0.9, 0.99, 1e-6, wd)
+        tol = 2.0 ** -20 * np.abs(ref - hp) + 2.0 ** -23 * np.abs(hp)
+        if state == "8bit":
+            for x, k, top, code, exp in ((m, 0, 15, opt.m, opt.m_exp), (v, 1, 31, opt.v, opt.v_exp)):
+                u = padded(words(k, step).astype(np.int64), sizes).reshape(-1, 64)
+                c, e = O.encode8(padded(x, sizes).reshape(-1, 64), top, u)
+                assert np.array_equal(exp.cpu().numpy(), e) and np.array_equal(code.cpu().numpy().reshape(-1, 64), c)
+                x[:] = unpadded(O.decode8(c, e, top).reshape(-1), sizes)
+        else:
+            assert np.array_equal(unpadded(opt.m.cpu().numpy(), sizes), m)
+            assert np.array_equal(unpadded(opt.v.cpu().numpy(), sizes), v)
+        if pdt == BF16 and not master:
+            u = words(2, step)
+            a, b = (np.abs(((((ref + k * np.sign(ref) * tol).astype(np.float32).view(np.uint32).astype(np.int64) + u) >> 16 << 16)
+                            .astype(np.uint32)).view(np.float32).astype(np.float64)) for k in (-1, 1))
+            hp = host(buf)
+            assert (((a <= np.abs(hp)) & (np.abs(hp) <= b)) | (np.abs(ref) < 1e-6)).all()
+        else:
+            hp = host(mast if master else buf)
+            assert (np.abs(hp - ref) <= tol).all()
+            assert not master or torch.equal(buf, mast.to(BF16))
