@@ -531,7 +531,9 @@ using Int = std::integral_constant<int, V>;
 // several rows (bf16 columns, log-probabilities and policy update: 4142 columns 4.2 and 5.3 TB/s with 256 threads, 5.2
 // and 5.6 with one wave; 16924 columns 4.3 and 4.9 with 1024 threads, 5.2 and 5.7 with 512).  Up to 512 rows leave
 // waves to spare, and a row is done sooner by four of them (4000 columns, 64 rows, policy: 3.8 us, 5.1 us by one; 1024
-// rows: 6.7 us, 5.9 us).
+// rows: 6.7 us, 5.9 us).  Six of eight vectors a thread are the most that 512 threads take: 8192 rows, policy update with
+// 512 threads of 8 and 1024 of 4, bf16 95 and 118 us (2100 vectors), 154 and 153 (3100), 172 and 167 (3584), 218 and 200
+// (4090); fp32 91 and 102, 151 and 142, 168 and 157, 216 and 189.
 template <typename F>
 void with_row_shape(int64_t nv, int64_t rows, F f) {
   const bool few = rows <= 512;
@@ -545,7 +547,7 @@ void with_row_shape(int64_t nv, int64_t rows, F f) {
     f(Int<256>(), Int<4>(), std::true_type(), Int<0>());
   else if (nv <= 256 * 8)
     f(Int<256>(), Int<8>(), std::true_type(), Int<0>());
-  else if (nv <= 512 * 7)
+  else if (nv <= 512 * 6)
     f(Int<512>(), Int<8>(), std::true_type(), Int<0>());
   else if (nv <= 1024 * 4)
     f(Int<1024>(), Int<4>(), std::true_type(), Int<0>());
