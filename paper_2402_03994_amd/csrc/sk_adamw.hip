@@ -159,22 +159,6 @@ __device__ __forceinline__ void decode8(uint2 codes, uint32_t eb, float x[kPer])
   }
 }
 
-// A Philox4x32-10 block as philox() gives it, its exclusive-ors of three in one instruction.
-__device__ __forceinline__ W4 philox_adam(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, Key key) {
-  uint32_t k0 = key.k0, k1 = key.k1;
-#pragma unroll
-  for (int r = 0; r < 10; ++r) {
-    const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
-    c0 = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c1, k0, 0x96);
-    c2 = __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c3, k1, 0x96);
-    c1 = (uint32_t)p1;
-    c3 = (uint32_t)p0;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
-  }
-  return W4{{c0, c1, c2, c3}};
-}
-
 // m / (sqrt(v) root + eps), square root and quotient rounded correctly where the parameter is held in 32 bits (EXACT).
 // Where it is about to be rounded at random to 8 bits, the hardware's square root and reciprocal serve (one unit in the
 // last of 24 each, nothing for inputs below 2^-126), with an eps beside which root 2^-63 is nothing.  124 million
@@ -246,7 +230,7 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
       uint32_t dm[kPer], dv[kPer], eb;
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const W4 w = philox_adam((uint32_t)(e >> 2) + q, s.step, (uint32_t)ck.tensor, ST_ADAMW, s.key);
+        const W4 w = philox_at<true>((uint32_t)(e >> 2) + q, s.step, (uint32_t)ck.tensor, ST_ADAMW, s.key);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {  // 16 u + 8
           dm[4 * q + i] = ((w.w[i] >> 12) & 0xFFFF0u) | 8u;
@@ -262,7 +246,7 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamTensor *__restrict__ te
     if (sizeof(P) == 2 && !MASTER) {
       // An infinity has nothing below its 16 bits and stays one.  A NaN may have all of its bits set, where u would carry
       // into the sign and beyond: eight values that hold one (four comparisons of two) are rounded apart.
-      const W4 w = philox_adam((uint32_t)(e >> 3), s.step, (uint32_t)ck.tensor, ST_ADAMW_P, s.key);
+      const W4 w = philox_at<true>((uint32_t)(e >> 3), s.step, (uint32_t)ck.tensor, ST_ADAMW_P, s.key);
       const bool nan = __builtin_isunordered(pv[0], pv[1]) || __builtin_isunordered(pv[2], pv[3]) ||
                        __builtin_isunordered(pv[4], pv[5]) || __builtin_isunordered(pv[6], pv[7]);
 #pragma unroll

@@ -47,15 +47,25 @@ struct W4 {
   uint32_t w[4];
 };
 
-SK_HD W4 philox(uint64_t ctr, uint32_t layer, uint32_t stream, Key key) {
-  uint32_t c0 = (uint32_t)ctr, c1 = (uint32_t)(ctr >> 32), c2 = layer, c3 = stream;
+// One block at the counter (c0, c1, c2, c3).  XOR3: device code in which the exclusive-ors of three are one instruction
+// each, for a kernel that the vector units bound (AdamW with 8-bit moments draws three blocks for eight elements).
+template <bool XOR3 = false>
+SK_HD W4 philox_at(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, Key key) {
   uint32_t k0 = key.k0, k1 = key.k1;
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t p0 = (uint64_t)0xD2511F53u * c0;
     const uint64_t p1 = (uint64_t)0xCD9E8D57u * c2;
-    const uint32_t n0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
-    const uint32_t n2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+    uint32_t n0, n2;
+    if constexpr (XOR3) {
+#if defined(__HIP_DEVICE_COMPILE__)
+      n0 = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c1, k0, 0x96);
+      n2 = __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c3, k1, 0x96);
+#endif
+    } else {
+      n0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+      n2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+    }
     c1 = (uint32_t)p1;
     c3 = (uint32_t)p0;
     c0 = n0;
@@ -69,6 +79,10 @@ SK_HD W4 philox(uint64_t ctr, uint32_t layer, uint32_t stream, Key key) {
   o.w[2] = c2;
   o.w[3] = c3;
   return o;
+}
+
+SK_HD W4 philox(uint64_t ctr, uint32_t layer, uint32_t stream, Key key) {
+  return philox_at((uint32_t)ctr, (uint32_t)(ctr >> 32), layer, stream, key);
 }
 
 SK_HD uint32_t pick(const W4 &w, uint32_t i) {
