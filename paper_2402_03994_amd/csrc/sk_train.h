@@ -108,12 +108,8 @@ __device__ __forceinline__ T block_all(T v, Op op, T *lds) {
 }
 
 // Outputs above this size are stored past the caches (32 MB of L2, 256 MB in front of the memory); what is smaller is
-// left there for the kernel that reads it next.  The call alone is done sooner past the caches from 64 MB on, the call and
-// a reader of its output later: policy update in bf16 and one pass over its gradient of 80 MB 83 us past the caches, 74 us
-// through them, of 120 MB 110 and 95, of 160 MB 145 and 128, of 240 MB 220 and 216; log-probabilities, their gradient
-// and a product with it of 80 MB 156 and 153, of 120 MB 204 and 198, of 160 MB 225 and 229, of 240 MB 307 and 320; lookup
-// and one pass over 98 MB 88 and 74, over 246 MB 210 and 219.
-constexpr int64_t kPastBytes = 128 << 20;
+// left there for the next kernel to read.
+constexpr int64_t kPastBytes = 64 << 20;
 
 // 16 bytes of elements, aligned to one element only: the loads and stores of gfx950 take any alignment.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
