@@ -1072,3 +1072,36 @@ def two_launches(dev, state, pdt, gdt, master, sizes):
             hp = host(mast if master else buf)
             assert (np.abs(hp - ref) <= tol).all()
             assert not master or torch.equal(buf, mast.to(BF16))
+
+
+@pytest.mark.parametrize("dt,vocab,rows", [(F32, 1501, 25000), (BF16, 5003, 15000), (F32, 50257, 700), (BF16, 50257, 1400),
+                                           (BF16, 32000, 2300)])
+def test_large_outputs_are_those_of_their_thirds(dev, dt, vocab, rows):
+    """Gradients and lookups that are stored past the caches, in place too, against calls whose outputs are not."""
+    import paper_2402_03994_amd as fw
+    g = torch.Generator(device=dev).manual_seed(rows)
+    x = torch.randn(rows, vocab, generator=g, device=dev).mul_(2).to(dt)
+    t = torch.randint(-1, vocab, (rows,), generator=g, device=dev)
+    old, adv, w = (torch.randn(rows, generator=g, device=dev) for _ in range(3))
+    third = -(-rows // 3)
+    assert third * vocab * x.element_size() < 64 << 20 < x.numel() * x.element_size()
+    lp, stats = fw.token_logp(x, t)
+    old = lp - 0.1 * old
+    parts = [slice(k, min(k + third, rows)) for k in range(0, rows, third)]
+    for scale in (1.0, 0.5):
+        whole = fw.policy_loss(x, t, old, adv, w, scale=scale).dlogits
+        for s in parts:
+            assert torch.equal(whole[s], fw.policy_loss(x[s], t[s], old[s], adv[s], w[s], scale=scale).dlogits)
+    d = fw.token_logp_grad(x, t, stats, w)
+    for s in parts:
+        assert torch.equal(d[s], fw.token_logp_grad(x[s], t[s], stats[s], w[s]))
+    ids = torch.randint(-1, rows, (rows,), generator=g, device=dev)
+    e = fw.embed(x, ids, scale=0.7)
+    for s in parts:
+        assert torch.equal(e[s], fw.embed(x, ids[s], scale=0.7))
+    y = x.clone()
+    fw.token_logp_grad(y, t, stats, w, out=y)
+    assert torch.equal(y, d)
+    y.copy_(x)
+    fw.policy_loss(y, t, old, adv, w, scale=0.5, out=y)
+    assert torch.equal(y, whole)
