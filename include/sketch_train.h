@@ -46,8 +46,12 @@ int sketch_embed(const void *weight, sk_dtype dtype, int64_t vocab, int64_t widt
 /*
  * Gradient of the lookup: for each of `batch` groups of n tokens
  *   out[v] (+)= scale * sum over t with ids[t] = v of dy[t]
- * with the sum in fp32 in an order that the ids alone set (that of t in pieces of
- * 16, 32 or 64 tokens, then the pieces), rounded once to out_dtype; ids outside [0, vocab) add nothing.
+ * with the sum in fp32, rounded once to out_dtype; ids outside [0, vocab) add
+ * nothing.  The order of a sum is set by the ids, the sizes and the types: that of
+ * t for up to 1024 tokens a group and 64 MB of out; else that of t in pieces of
+ * the sorted tokens (16, 32 or 64, by batch * n * width), then the pieces, every
+ * fourth of them in a sum of its own.  The same call gives the same bits; the
+ * gradient of one text may differ in its last bits with the batch it is part of.
  * batch > 1 gives one gradient per example.  Rows that no id names are zeroed
  * (accumulate = 0) or kept (accumulate = 1).
  *   dy       [batch, n, width], row stride ld >= width elements.
@@ -162,6 +166,11 @@ int sketch_preference_loss(const sk_logits *x, const void *offsets, sk_index off
  *     (i / 4, step, l, SK_STREAM_ADAMW) under the key of `seed`, for element i
  *     of tensor l.  A block that holds an infinity or NaN has exponent byte 255
  *     and stands for NaNs.
+ * step, lr and the other numbers of a call are taken when it is made: a captured
+ * graph repeats that very step, its bias corrections and its random words, at
+ * every replay.  A replay stands for training only where that is meant; a step of
+ * its own number is a call of its own.
+ *
  * Parameters in bf16 without a master copy are rounded the same way: the 16
  * bits that are cut off get u added, half (i mod 2) of word (i / 2 mod 4) of
  * the block with counter (i / 8, step, l, SK_STREAM_ADAMW_P).  To a NaN nothing is

@@ -18,11 +18,11 @@
 //                joins both.  10682 x 50257 bf16: 175 to 183 us, 6 TB/s.
 //   k_policy     the same, then the token's loss and the row's gradient from
 //                the registers: one read, one write, no second launch over the
-//                logits.  8192 x 128256 bf16, 40% masked: 606 us, 5.5 TB/s.
+//                logits.  8192 x 128256 bf16, 40% masked: 603 us, 5.6 TB/s.
 //   k_logp_grad  the gradient from known (m, z).  The preference loss needs it:
 //                a row's factor is known when its pair's rows have all been
-//                read.  16384 x 50257 bf16, 40% masked: 170 us of k_logp, 440
-//                us (6 TB/s), of a floor of 540 us for one read and one write.
+//                read.  16384 x 50257 bf16, 40% masked: 179 us of k_logp, 447
+//                us (5.9 TB/s), of a floor of 540 us for one read and one write.
 //   k_pair       a workgroup a pair, 4 to 7 us; k_policy_total one workgroup, 2
 //                to 5 us.
 #include <algorithm>

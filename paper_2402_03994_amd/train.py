@@ -110,7 +110,7 @@ def embed_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float 
 
     dy [*tokens.shape, width].  per_example: one gradient [vocab, width] for each entry of tokens' first axis, so that
     out [batch, vocab, width], viewed as [batch, vocab * width], is what Sketch.apply takes; else out [vocab, width].
-    accumulate adds to `out`.  Sums are kept in fp32 and do not depend on the order of execution."""
+    accumulate adds to `out`.  Sums are kept in fp32, in an order that the ids, the sizes and the types set."""
     device = _on_gpu(dy, "dy")
     if dy.shape[:-1] != tokens.shape or dy.dim() < 2 or dy.shape[-1] < 1:
         raise ValueError("dy must be [*tokens.shape, width]")
@@ -186,7 +186,8 @@ def token_logp(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1.0):
 
 def token_logp_grad(logits: torch.Tensor, targets: torch.Tensor, stats: torch.Tensor, dlogp: torch.Tensor,
                     scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """The gradient of sum(dlogp * logp) with respect to the logits, in their type.  out may be the logits."""
+    """The gradient of sum(dlogp * logp) with respect to the logits, in their type.  out may be the logits; a new tensor
+    has the row stride of logits that are padded by up to 64 columns (and is not contiguous then)."""
     x = _logits(logits, targets, scale)
     n = logits.shape[0]
     if stats.dtype != torch.float32 or stats.device != logits.device or stats.shape != (n, 2) or not stats.is_contiguous():
@@ -207,7 +208,8 @@ def policy_loss(logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.Ten
     r = exp(logp - old_logp), u = ref_logp - logp, and its gradient with respect to the logits.
 
     Rows with a masked target or weight 0 are not read.  The weights set the mean that is meant (over tokens:
-    mask / mask.sum(); over texts: mask / (texts * length)).  out (where grad) may be the logits."""
+    mask / mask.sum(); over texts: mask / (texts * length)).  out (where grad) may be the logits; a new dlogits has their
+    row stride, as token_logp_grad's."""
     x = _logits(logits, targets, scale)
     device, n = logits.device, logits.shape[0]
     args = [_vec(t, n, device, name) for t, name in ((old_logp, "old_logp"), (advantages, "advantages"),
@@ -233,7 +235,8 @@ def preference_loss(logits: torch.Tensor, targets: torch.Tensor, offsets: torch.
     respect to the logits.
 
     ref_logp [T]: the reference model's token_logp.  average: texts by their mean instead of their sum.  Masked
-    targets (prompts, padding) count nothing.  out (where grad) may be the logits."""
+    targets (prompts, padding) count nothing.  out (where grad) may be the logits; a new dlogits has their row stride, as
+    token_logp_grad's."""
     x = _logits(logits, targets, scale)
     device, n = logits.device, logits.shape[0]
     index = _ids(offsets, "offsets", device)
@@ -262,7 +265,11 @@ class AdamW:
     byte for each 64; rounded up or down at random from `seed`, step and place, so that two runs agree).  decay: a
     factor of weight_decay per tensor (0 for biases and norms).
     m, v (and m_exp, v_exp with "8bit") are the state: each tensor's elements, padded to a multiple of 64, in list
-    order."""
+    order.
+    A list has one type: a model of two takes a handle for each, and clips by a norm of each, or by a common one that its
+    program forms and passes in grad_scale.
+    The numbers of a step are taken when it is called: a captured graph repeats that very step, random words included, at
+    every replay, and is no way to go on training."""
 
     def __init__(self, shapes: Sequence, state: str = "f32", decay: Optional[Sequence[float]] = None, seed: int = 0,
                  device=None):
