@@ -334,7 +334,7 @@ class AdamW:
             dt = tensors[0].dtype if dtype is None else dtype
             same = list(map(T.numel, tensors)) == self.numels and set(map(_get_dtype, tensors)) == {dt} and \
                 set(map(T.get_device, tensors)) == {self.device.index} and all(map(T.is_contiguous, tensors))
-        except (TypeError, AttributeError, IndexError):  # not a list, or not of tensors
+        except (TypeError, AttributeError, LookupError):  # not a list, or not of tensors
             dt, same = dtype, False
         if not same:
             raise ValueError(f"{name}: contiguous {dt or 'float32 or bfloat16'} tensors on {self.device} with these counts are "
