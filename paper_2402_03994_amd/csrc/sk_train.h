@@ -25,10 +25,13 @@ inline int train_launched() noexcept {
   return e == hipSuccess ? SK_OK : train_fail(SK_EHIP, hipGetErrorString(e));
 }
 
-struct TrainGuard {  // the caller's current device again on scope exit
+// The call's device, and the caller's current one again on scope exit.  An error that an earlier call to the runtime has
+// left is dropped: train_launched() would report it as this call's.
+struct TrainGuard {
   int prev = -1, dev;
   bool ok;  // false: there is no device `dev`
   explicit TrainGuard(int d) : dev(d) {
+    (void)hipGetLastError();
     if (hipGetDevice(&prev) != hipSuccess) prev = -1;
     ok = dev >= 0 && (prev == dev || hipSetDevice(dev) == hipSuccess);
     if (!ok) (void)hipGetLastError();

@@ -1105,3 +1105,20 @@ def test_large_outputs_are_those_of_their_thirds(dev, dt, vocab, rows):
     y.copy_(x)
     fw.policy_loss(y, t, old, adv, w, scale=0.5, out=y)
     assert torch.equal(y, whole)
+
+
+def test_errors_of_earlier_calls_are_not_reported(dev):
+    """What an unrelated call to the runtime has left as its last error is none of the next operator's."""
+    import ctypes
+
+    import paper_2402_03994_amd as fw
+    with open("/proc/self/maps") as maps:
+        path = next(line.split()[-1] for line in maps if "libamdhip64.so" in line)
+    hip = ctypes.CDLL(path)
+    w, t = torch.randn(8, 4, device=dev), torch.tensor([1, 7, 3], device=dev)
+    opt, g = fw.AdamW([(8, 4)]), torch.ones(8, 4, device=dev)
+    want, low = w[t].clone(), t % 4
+    for call in (lambda: torch.equal(fw.embed(w, t), want), lambda: fw.embed_grad(want, t, 8).abs().sum() > 0,
+                 lambda: torch.isfinite(fw.token_logp(w[:3], low)[0]).all(), lambda: opt.step([w], [g], 1, lr=0.1) is None):
+        assert hip.hipSetDevice(99) != 0  # refused by the runtime, nothing is queued
+        assert call()
