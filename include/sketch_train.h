@@ -140,6 +140,62 @@ int sketch_preference_loss(const sk_logits *x, const void *offsets, sk_index off
                            int64_t work_bytes, void *stream);
 
 /*
+ * Hidden states of `rows` positions, the output matrix that turns them into
+ * logits x_t = weight hidden_t, and their targets.  The logits are formed in
+ * pieces and never kept.
+ *   hidden   [rows, width], row stride ld_hidden >= width elements.
+ *   weight   [vocab, width], row stride ld_weight >= width elements.
+ *   targets, scale  as in sk_logits; of a masked position the hidden state is
+ *            not read either.
+ * dtype is that of hidden and weight.  SK_EUNSUPPORTED for rows > 2^20, vocab > 2^22
+ * or width > 2^16.
+ */
+typedef struct {
+  const void *hidden;
+  const void *weight;
+  const void *targets;
+  int64_t rows, vocab, width, ld_hidden, ld_weight;
+  float scale;
+  sk_dtype dtype;
+  sk_index index;
+  int32_t device;
+} sk_linear;
+
+/*
+ * logp[t] = log softmax(scale x_t)[targets[t]] (fp32) and stats [rows, 2] fp32
+ * (NULL if not wanted), as sketch_token_logp gives them for these logits.  bf16
+ * products and the sums are exact to fp32; of fp32 inputs each product is taken
+ * from two numbers of 11 bits an operand (22 bits; what lies below 2^-38 of the
+ * largest entry of weight, or of the row of hidden, is lost), so that infinities
+ * and NaNs in them give NaNs.
+ *   work     sketch_linear_logp_work_bytes(x) bytes (0 if x is refused), 256-byte
+ *            aligned.
+ */
+int64_t sketch_linear_logp_work_bytes(const sk_linear *x);
+int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work, int64_t work_bytes, void *stream);
+
+/*
+ * The gradient of sum_t dlogp[t] logp[t] from the stats of sketch_linear_logp:
+ * with g_t = scale dlogp[t] (onehot(targets[t]) - softmax(scale x_t)),
+ *   dhidden[t] = sum_v g_tv weight[v]        (the type of hidden; masked rows get
+ *                zeros, row stride ld_dhidden; NULL if not wanted)
+ *   dweight[b][v] (+)= sum over the rows t of example b of g_tv hidden[t]
+ *                [batch, vocab, width] contiguous, NULL if not wanted: rows are
+ *                `batch` examples of rows / batch each, batch > 1 gives one gradient
+ *                per example.  Of fp32 weights it is fp32, of bf16 weights either.
+ * Sums are fp32 and rounded once.  bf16 inputs have g rounded to bf16 before the
+ * products, whatever the type of dweight.  Rows with dlogp = 0 are masked.  Outputs
+ * may not overlap inputs.
+ *   work     sketch_linear_logp_grad_work_bytes(x, batch, dhidden wanted, dweight
+ *            wanted) bytes (0 if refused), 256-byte aligned.
+ * SK_EUNSUPPORTED for batch > 2^14.
+ */
+int64_t sketch_linear_logp_grad_work_bytes(const sk_linear *x, int64_t batch, int32_t dhidden, int32_t dweight);
+int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stats, const float *dlogp, void *dhidden,
+                            int64_t ld_dhidden, void *dweight, sk_dtype dweight_dtype, int32_t accumulate, void *work,
+                            int64_t work_bytes, void *stream);
+
+/*
  * AdamW over a list of parameter tensors, one launch for up to 160 of them:
  *   g = g s;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
  *   p = p (1 - lr wd_l) - lr / (1 - b1^step) m / (sqrt(v / (1 - b2^step)) + eps)

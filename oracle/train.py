@@ -167,3 +167,29 @@ def adamw_words(n, step, layer, seed):
     w = philox(i // 4, step, layer, 11, seed)[i, i % 4]
     p = philox(i // 8, step, layer, 12, seed)[i, (i // 2) % 4]
     return w >> 16, w & 0xFFFF, np.where(i % 2, p >> 16, p & 0xFFFF)
+
+
+def linear_logp(hidden, weight, targets, scale):
+    """log softmax(scale hidden weight^T)[targets] by rows."""
+    t = np.asarray(targets)
+    live = (t >= 0) & (t < len(weight))
+    out = np.zeros(len(t))
+    if live.any():
+        x = np.asarray(hidden, dtype=np.float64)[live] @ np.asarray(weight, dtype=np.float64).T
+        out[live] = softmax_rows(x, scale)[1][np.arange(live.sum()), t[live]]
+    return out
+
+
+def linear_logp_grad(hidden, weight, targets, dlogp, scale, batch=1):
+    """(dhidden [T, width], dweight [batch, vocab, width], g [T, vocab] at the logits, p [T, vocab])."""
+    t, c = np.asarray(targets), np.asarray(dlogp, dtype=np.float64)
+    W = np.asarray(weight, dtype=np.float64)
+    live = (t >= 0) & (t < len(W))
+    live &= np.where(live, c, 0.0) != 0
+    h = np.where(live[:, None], np.asarray(hidden, dtype=np.float64), 0.0)
+    x = h @ W.T
+    g = token_logp_grad(x, np.where(live, t, -1), c, scale)
+    p = np.where(live[:, None], softmax_rows(x, scale)[0], 0.0)
+    n = len(t) // batch
+    dw = np.stack([g[b * n:b * n + n].T @ h[b * n:b * n + n] for b in range(batch)])
+    return g @ W, dw, g, p

@@ -21,7 +21,8 @@ EXPORTS = ("sketch_create", "sketch_apply", "sketch_apply_noalloc", "sketch_appl
            "sketch_arnoldi_work_floats", "sketch_arnoldi_step", "sketch_arnoldi", "sk_hvp_profile",
            "sk_hvp_profile_read", "sketch_id_search_work_floats", "sketch_id_search", "sketch_embed", "sketch_embed_grad",
            "sketch_embed_grad_work_bytes", "sketch_token_logp", "sketch_token_logp_grad", "sketch_policy_loss",
-           "sketch_preference_work_bytes", "sketch_preference_loss", "sketch_adamw_create",
+           "sketch_preference_work_bytes", "sketch_preference_loss", "sketch_linear_logp_work_bytes",
+           "sketch_linear_logp", "sketch_linear_logp_grad_work_bytes", "sketch_linear_logp_grad", "sketch_adamw_create",
            "sketch_adamw_state_elems", "sketch_adamw_apply", "sketch_adamw_moments", "sketch_adamw_destroy")
 HVP_PROF_CLASSES = ["hvp_dots", "hvp_combine", "arnoldi_orth"]
 HVP_MAX_RANK = 32
@@ -49,6 +50,13 @@ class Info(ctypes.Structure):
 class Logits(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("targets", ctypes.c_void_p), ("rows", ctypes.c_int64),
                 ("vocab", ctypes.c_int64), ("ld", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("dtype", ctypes.c_int), ("index", ctypes.c_int), ("device", ctypes.c_int32)]
+
+
+class Linear(ctypes.Structure):
+    _fields_ = [("hidden", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("targets", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("ld_hidden", ctypes.c_int64), ("ld_weight", ctypes.c_int64), ("scale", ctypes.c_float),
                 ("dtype", ctypes.c_int), ("index", ctypes.c_int), ("device", ctypes.c_int32)]
 
 
@@ -120,7 +128,7 @@ def load() -> ctypes.CDLL:
     L.sketch_id_search.argtypes = [P, P, ctypes.POINTER(P), i64, f32, f32, i32, i32, P, P, P,
                                    ctypes.POINTER(IdResult), P]
     L.sketch_id_search.restype = ctypes.c_int
-    LP, SP = ctypes.POINTER(Logits), ctypes.POINTER(AdamWStep)
+    LP, SP, XP = ctypes.POINTER(Logits), ctypes.POINTER(AdamWStep), ctypes.POINTER(Linear)
     for name, restype, args in (
             ("sketch_embed", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, ctypes.c_int, i64, f32, P, ctypes.c_int,
                                             i32, P]),
@@ -133,6 +141,10 @@ def load() -> ctypes.CDLL:
             ("sketch_preference_work_bytes", i64, [i64]),
             ("sketch_preference_loss", ctypes.c_int, [LP, P, ctypes.c_int, i64, P, f32, f32, i32, P, P, P, P, i64, P,
                                                       i64, P]),
+            ("sketch_linear_logp_work_bytes", i64, [XP]),
+            ("sketch_linear_logp", ctypes.c_int, [XP, P, P, P, i64, P]),
+            ("sketch_linear_logp_grad_work_bytes", i64, [XP, i64, i32, i32]),
+            ("sketch_linear_logp_grad", ctypes.c_int, [XP, i64, P, P, P, i64, P, ctypes.c_int, i32, P, i64, P]),
             ("sketch_adamw_create", ctypes.c_int, [P, P, i32, ctypes.c_int, u64, i32, ctypes.POINTER(P)]),
             ("sketch_adamw_state_elems", i64, [P]),
             ("sketch_adamw_apply", ctypes.c_int, [P, SP, ctypes.POINTER(P), ctypes.c_int, ctypes.POINTER(P),

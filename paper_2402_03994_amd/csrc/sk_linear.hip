@@ -1,0 +1,1049 @@
+// sk_linear.hip -- log-probabilities of tokens from hidden states and the output
+// matrix, with both gradients, over pieces of the vocabulary (C ABI of
+// include/sketch_train.h).
+//
+// Logits x = H W^T are formed tile by tile in the matrix cores' accumulators and
+// never kept.  Forward: each tile leaves its (m, z) (largest logit, sum of
+// exp(scale (x - m))) per token, k_join joins them.  Gradient: the logits of a
+// piece of the vocabulary are formed again, become
+// G = dlogp scale (onehot - p) in the tile's epilogue, and the piece adds G W to
+// dH and gives its rows G^T H of dW:
+//   8 n V d operations for n tokens, of which 2 n V d are the second forming.
+// Rows whose target is masked are left out of everything: k_live lists the live
+// ones, each example's padded with empty rows to a multiple of 64 so that a step
+// of the products' K lies in one example.
+//
+// All three products are one kernel core, C[m][n] = sum_k A[m][k] B[n][k] with
+// K contiguous in both (Core below); H^T and W^T of a piece are written once for
+// it.  16-bit operands, fp32 sums.  bf16 inputs are used as they are and G is
+// rounded to bf16, once, like any entry of a bf16 gradient.  fp32 inputs are
+// split, x = hi + lo in two fp16 numbers (22 bits) under a power of two that
+// brings the largest to 2^13, and each product is the three hi lo, lo hi, hi hi:
+// the matrix cores' fp32 rate is a sixteenth of their fp16 rate.  What lo cannot
+// hold is below 2^-38 of the largest entry of its operand (for H: of the row).
+#include <algorithm>
+#include <climits>
+#include <type_traits>
+
+#include "sk_train.h"
+
+using namespace sk;
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kStep = 64;   // K a stage
+constexpr int kTop = 13;    // split operands lie below 2^(kTop + 1)
+constexpr int kTileM = 128; // vocabulary rows that one entry of the forward's partial statistics covers
+
+// What the kernels of a call share in its workspace.
+struct Meta {
+  int np;     // listed rows
+  int wbits;  // bits of the largest finite |W|
+  int ec;     // exponent bound of dlogp scale H
+};
+
+// A listed row in the gradient: logits are acc * f, G = live ? one [v = target] + w exp(scale (x - m)) : 0.
+struct RowPrm {
+  float m, w, one, f;
+};
+
+__device__ __forceinline__ int exponent_of(uint32_t bits) { return (int)((bits >> 23) & 255) - 127; }
+__device__ __forceinline__ int exponent_of(float x) { return exponent_of(__float_as_uint(x)); }
+
+// hi (low half) and lo of x, |x| < 2^15
+__device__ __forceinline__ uint32_t split(float x) {
+  const _Float16 h = (_Float16)x;
+  const float r = x - (float)h;
+  const _Float16 l = (_Float16)(r == r ? r : 0.0f);  // of an infinity hi is all
+  return (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
+}
+// plane p of two split numbers, or two bf16, side by side
+template <bool F16>
+__device__ __forceinline__ uint32_t two(float a, float b, int p) {
+  if (!F16) return bf16_bits(a) | bf16_bits(b) << 16;
+  return __builtin_amdgcn_perm(split(b), split(a), p ? 0x07060302 : 0x05040100);
+}
+
+// N elements of a row from column k on, zeros past the width
+template <int N, typename T>
+__device__ __forceinline__ void row_part(const T *row, int k, int width, float *f) {
+  if (k + N <= width) {
+#pragma unroll
+    for (int i = 0; i < N; i += Vec<T>::N) {
+      const u32x4 v = Vec<T>::load(row + k + i);
+#pragma unroll
+      for (int e = 0; e < Vec<T>::N; ++e) f[i + e] = Vec<T>::get(v, e);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = k + i < width ? to_f32(row[k + i]) : 0.0f;
+  }
+}
+
+// --- the list of rows ---------------------------------------------------------------------------------------
+struct Live {
+  const void *targets;
+  const float *dlogp;  // NULL: forward
+  int32_t index, vocab, n, batch;
+  int *list, *pos, *tgt, *seg, *cnt;
+  Meta *meta;
+  float *logp;
+  float2 *stats;
+};
+
+__device__ __forceinline__ int wave_scan(int v, int lane) {  // inclusive
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(v, d, 64);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+
+// One workgroup: counts of 64 rows each, their sums within the examples, the examples' starts, the list.
+__global__ __launch_bounds__(1024) void k_live(Live a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = (a.n + 63) / 64;
+  const int64_t chunks = (int64_t)per * a.batch;
+  auto target = [&](int64_t c, int64_t &t) {
+    const int i = (int)(c % per) * 64 + lane;
+    t = c / per * a.n + i;
+    if (i >= a.n) {
+      t = -1;
+      return -1;
+    }
+    const int64_t v = a.index == SK_I64 ? ((const int64_t *)a.targets)[t] : ((const int32_t *)a.targets)[t];
+    if (v < 0 || v >= a.vocab || (a.dlogp && a.dlogp[t] == 0.0f)) return -1;
+    return (int)v;
+  };
+  for (int64_t c = wave; c < chunks; c += 16) {
+    int64_t t;
+    const uint64_t live = __ballot(target(c, t) >= 0);
+    if (lane == 0) a.cnt[c] = __popcll(live);
+  }
+  __syncthreads();
+  for (int b = wave; b < a.batch; b += 16) {
+    int sum = 0;
+    for (int i = 0; i < per; i += 64) {
+      int *p = a.cnt + (int64_t)b * per + i + lane;
+      const int v = i + lane < per ? *p : 0, s = wave_scan(v, lane);
+      if (i + lane < per) *p = sum + s - v;
+      sum += __shfl(s, 63, 64);
+    }
+    if (lane == 0) a.seg[b + 1] = sum;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    int sum = 0;
+    for (int b = 0; b < a.batch; b += 64) {
+      const int v = b + lane < a.batch ? (a.seg[b + 1 + lane] + kStep - 1) / kStep * kStep : 0;
+      const int s = wave_scan(v, lane) + sum;
+      if (b + lane < a.batch) a.seg[b + 1 + lane] = s;
+      sum = __shfl(s, 63, 64);
+    }
+    if (lane == 0) {
+      a.seg[0] = 0;
+      *a.meta = Meta{sum, 0, INT_MIN / 2};
+    }
+  }
+  __syncthreads();
+  for (int64_t c = wave; c < chunks; c += 16) {
+    int64_t t;
+    const int v = target(c, t), b = (int)(c / per);
+    const uint64_t live = __ballot(v >= 0);
+    const int at = a.seg[b] + a.cnt[c];
+    if (v >= 0) {
+      const int p = at + __popcll(live & ((1ull << lane) - 1));
+      a.list[p] = (int)t;
+      a.tgt[p] = v;
+      a.pos[t] = p;
+    } else if (t >= 0) {
+      a.pos[t] = -1;
+      if (a.logp) {
+        a.logp[t] = 0.0f;
+        if (a.stats) a.stats[t] = float2{0.0f, 0.0f};
+      }
+    }
+    if (c % per == per - 1)
+      for (int p = at + __popcll(live) + lane; p < a.seg[b + 1]; p += 64) a.list[p] = a.tgt[p] = -1;
+  }
+}
+
+// --- operands -----------------------------------------------------------------------------------------------
+struct Gather {
+  const void *hidden;
+  int64_t ld;
+  int width, kp;
+  const int *list;
+  Meta *meta;
+  uint16_t *hc;
+  int64_t plane;
+  int *eh;
+  // gradient only
+  const float2 *stats;
+  const float *dlogp;
+  float scale;
+  RowPrm *prm;
+  float *rowf, *cs;
+};
+
+// Rows of H in list order, zeros to a width of kp; a wave a row.  fp32: the row's exponent, its split, and what the
+// gradient needs to know of it.
+template <typename T>
+__global__ __launch_bounds__(256) void k_gather(Gather a) {
+  const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (n >= a.meta->np) return;
+  const int t = a.list[n];
+  const T *row = (const T *)a.hidden + (int64_t)(t < 0 ? 0 : t) * a.ld;
+  const int width = t < 0 ? 0 : a.width;
+  uint16_t *hc = a.hc + (int64_t)n * a.kp;
+  int e = 0;
+  if (sizeof(T) == 4) {
+    float big = 0.0f;
+    for (int k = lane * 8; k < width; k += 512) {
+      float f[8];
+      row_part<8>(row, k, width, f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.0f);
+    }
+    e = exponent_of(wave_all(big, OpMax()));
+    if (lane == 0) a.eh[n] = e;
+  }
+  for (int k = lane * 8; k < a.kp; k += 512) {
+    float f[8];
+    row_part<8>(row, k, width, f);
+    if (sizeof(T) == 4) {
+      u32x4 h, l;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = ldexpf(f[i], kTop - e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[i] = two<true>(f[2 * i], f[2 * i + 1], 0);
+        l[i] = two<true>(f[2 * i], f[2 * i + 1], 1);
+      }
+      *(u32x4 *)(hc + k) = h;
+      *(u32x4 *)(hc + a.plane + k) = l;
+    } else {
+      *(u32x4 *)(hc + k) = Vec<bf16>::pack(f);
+    }
+  }
+  if (!a.prm || lane != 0) return;
+  RowPrm p{0.0f, 0.0f, 0.0f, 1.0f};
+  float c = 0.0f;
+  if (t >= 0) {
+    const float2 s = a.stats[t];
+    if (s.y != 0.0f) {
+      c = a.dlogp[t] * a.scale;
+      p.m = s.x;
+      p.one = sizeof(T) == 4 ? (float)(1 << kTop) : c;
+      p.w = -p.one / s.y;
+    }
+  }
+  if (sizeof(T) == 4) {
+    const int ew = exponent_of((uint32_t)a.meta->wbits);
+    p.f = ldexpf(1.0f, e + ew - 2 * kTop);
+    a.rowf[n] = ldexpf(c, ew - 2 * kTop);
+    a.cs[n] = c;
+    if (c != 0.0f) atomicMax(&a.meta->ec, e + exponent_of(c) + 1);
+  }
+  a.prm[n] = p;
+}
+
+// The largest finite |W|, over all rows.
+__global__ __launch_bounds__(256) void k_absmax(const float *w, int64_t ld, int rows, int width, Meta *meta) {
+  float big = 0.0f;
+  const int lane = threadIdx.x & 63;
+  for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4)
+    for (int k = lane * 4; k < width; k += 256) {
+      float f[4];
+      row_part<4>(w + (int64_t)r * ld, k, width, f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) big = fmaxf(big, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.0f);
+    }
+  big = wave_all(big, OpMax());
+  if (lane == 0) atomicMax(&meta->wbits, (int)__float_as_uint(big));
+}
+
+struct Prep {
+  const void *src;
+  int64_t ld;
+  int rows, width;  // what there is; zeros beyond
+  const Meta *meta;
+  // H^T: rows in list order, with their factors (fp32)
+  const int *list, *eh;
+  const float *cs;
+  uint16_t *copy;  // [rows][kp], NULL if not wanted
+  int64_t cplane;
+  int kp;
+  uint16_t *tr;  // [width][tld], NULL if not wanted
+  int64_t tplane;
+  int64_t tld;
+};
+
+// 64 rows by 64 columns through LDS: the padded copy of the rows and the transpose.
+template <typename T, bool LIST>
+__global__ __launch_bounds__(256) void k_prep(Prep a) {
+  constexpr int P = sizeof(T) == 4 ? 2 : 1;
+  __shared__ uint32_t lds[P][64][33];  // pairs of columns
+  const int r0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
+  if (LIST && r0 >= a.meta->np) return;
+  {
+    const int r = r0 + (threadIdx.x >> 2), k = k0 + (threadIdx.x & 3) * 16;
+    int64_t at = r < a.rows ? r : -1;
+    float scale = 1.0f;
+    int e = 0;
+    if (LIST) {
+      at = a.list[r];  // np is a multiple of 64
+      if (P == 2) {
+        e = a.eh[r];
+        scale = ldexpf(a.cs[r], e - a.meta->ec);
+      }
+    } else if (P == 2) {
+      e = exponent_of((uint32_t)a.meta->wbits);
+    }
+    float f[16];
+    row_part<16>((const T *)a.src + (at < 0 ? 0 : at) * a.ld, k, at < 0 ? 0 : a.width, f);
+    uint32_t h[P][8];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (P == 2) f[i] = ldexpf(f[i], kTop - e) * (at < 0 ? 0.0f : scale);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[p][i] = two<P == 2>(f[2 * i], f[2 * i + 1], p);
+      if (a.copy) {
+        u32x4 *c = (u32x4 *)(a.copy + p * a.cplane + (int64_t)r * a.kp + k);
+        c[0] = u32x4{h[p][0], h[p][1], h[p][2], h[p][3]};
+        c[1] = u32x4{h[p][4], h[p][5], h[p][6], h[p][7]};
+      }
+      if (a.tr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lds[p][threadIdx.x >> 2][(threadIdx.x & 3) * 8 + i] = h[p][i];
+      }
+    }
+  }
+  if (!a.tr) return;
+  __syncthreads();
+  const int k = threadIdx.x >> 2, r = (threadIdx.x & 3) * 16;
+  if (k0 + k >= a.width) return;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    uint32_t h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      h[i] = __builtin_amdgcn_perm(lds[p][r + 2 * i + 1][k >> 1], lds[p][r + 2 * i][k >> 1], k & 1 ? 0x07060302 : 0x05040100);
+    u32x4 *c = (u32x4 *)(a.tr + p * a.tplane + (int64_t)(k0 + k) * a.tld + r0 + r);
+    c[0] = u32x4{h[0], h[1], h[2], h[3]};
+    c[1] = u32x4{h[4], h[5], h[6], h[7]};
+  }
+}
+
+// --- the product --------------------------------------------------------------------------------------------
+// Rows of an operand: up to two planes of 16-bit numbers, K contiguous.
+struct Operand {
+  const uint16_t *p[2];
+  int64_t ld;  // elements
+};
+
+// A BM x BN tile by WM x WN waves, each (BM / WM) x (BN / WN) in 32 x 32 accumulators of v_mfma_f32_32x32x16.  Stages of
+// 64 of K go straight from memory to LDS, 16 bytes a lane, two stages deep: the loads of the next one are issued
+// behind the barrier that frees its buffer and have the products of a whole stage (2048 cycles of a CU's matrix cores
+// for 256 x 256) to arrive.  A row of a stage is 128 bytes, its eight 16-byte chunks exchanged by (row / 2) & 7, so that
+// the 32 rows that a wave reads at a time lie in different banks (exchanged by row & 7: 8192^3 bf16 957 us, 887 us so).
+// 8192^3: 256 x 256 1240 TFLOP/s, 128 x 128 (two workgroups a CU) 1108; the library's 1290.
+template <int BM_, int BN_, int WM_, int WN_>
+struct Tiling {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM * WN, TH = NW * 64;
+  static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  static constexpr int LDS = 2 * (BM + BN) * kStep * 2;
+};
+using Big = Tiling<256, 256, 2, 4>;
+using Small = Tiling<128, 128, 2, 2>;
+
+#if defined(__HIP_DEVICE_COMPILE__)
+template <typename C, bool F16>
+struct Core {
+  f32x16 acc[C::TM][C::TN];
+  int lane, wave, wm, wn, fr, fk;
+
+  __device__ __forceinline__ Core() {
+    lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wm = wave % C::WM;
+    wn = wave / C::WM;
+    fr = lane & 31;
+    fk = lane >> 5;
+  }
+  // the tile's row of accumulator entry (i, e) of this lane, and its column of (j)
+  __device__ __forceinline__ int row(int i, int e) const { return wm * (C::BM / C::WM) + i * 32 + (e >> 2) * 8 + fk * 4 + (e & 3); }
+  __device__ __forceinline__ int col(int j) const { return wn * (C::BN / C::WN) + j * 32 + fr; }
+
+  // acc = sum over `steps` stages from a and b on; rows from ra (rb) on repeat the last one
+  __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int ra, int rb, int steps) {
+    constexpr int LA = C::BM / (C::NW * 8), LB = C::BN / (C::NW * 8), STAGE = (C::BM + C::BN) * kStep * 2;
+    // lane l fetches chunk l % 8 of row l / 8 of its wave's eight rows
+    const int lrow = lane >> 3, src = (lane & 7);
+    int offa[LA], offb[LB];
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+      const int r = (i * C::NW + wave) * 8 + lrow;
+      offa[i] = min(r, ra - 1) * (int)(a.ld * 2) + (src ^ ((r >> 1) & 7)) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < LB; ++i) {
+      const int r = (i * C::NW + wave) * 8 + lrow;
+      offb[i] = min(r, rb - 1) * (int)(b.ld * 2) + (src ^ ((r >> 1) & 7)) * 16;
+    }
+    typedef __attribute__((address_space(3))) void *lds_ptr;
+    int part = 0, k = 0;  // of the next stage to load; parts: hi lo, lo hi, hi hi
+    auto load = [&](int st) {
+      const auto ma = __builtin_amdgcn_make_buffer_rsrc((void *)a.p[F16 && part == 1], 0, 0xFFFFFFFF, 0x00020000);
+      const auto mb = __builtin_amdgcn_make_buffer_rsrc((void *)b.p[F16 && part == 0], 0, 0xFFFFFFFF, 0x00020000);
+      char *to = lds + st * STAGE + wave * 1024;
+#pragma unroll
+      for (int i = 0; i < LA; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ma, (lds_ptr)(to + i * C::NW * 1024), 16, offa[i], k * (kStep * 2), 0, 0);
+#pragma unroll
+      for (int i = 0; i < LB; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(mb, (lds_ptr)(to + C::BM * kStep * 2 + i * C::NW * 1024), 16, offb[i],
+                                                 k * (kStep * 2), 0, 0);
+      if (++k == steps) {
+        k = 0;
+        ++part;
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    const int all = steps * (F16 ? 3 : 1);
+    if (all > 0) load(0);
+    for (int s = 0; s < all; ++s) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (s + 1 < all) load((s + 1) & 1);
+      const char *la = lds + (s & 1) * STAGE + wm * (C::BM / C::WM) * kStep * 2;
+      const char *lb = lds + (s & 1) * STAGE + (C::BM + wn * (C::BN / C::WN)) * kStep * 2;
+#pragma unroll
+      for (int ks = 0; ks < kStep / 16; ++ks) {
+        const int at = ((ks * 2 + fk) ^ ((fr >> 1) & 7)) * 16 + fr * kStep * 2;
+        u32x4 fa[C::TM], fb[C::TN];
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) fa[i] = *(const u32x4 *)(la + i * 32 * kStep * 2 + at);
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) fb[j] = *(const u32x4 *)(lb + j * 32 * kStep * 2 + at);
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+          for (int j = 0; j < C::TN; ++j) {
+            if (F16)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa[i]), __builtin_bit_cast(f16x8, fb[j]),
+                                                                 acc[i][j], 0, 0, 0);
+            else
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]),
+                                                                  __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
+          }
+      }
+    }
+  }
+};
+#endif
+
+__device__ __forceinline__ Operand at_row(Operand a, int64_t row, int64_t k = 0) {
+  a.p[0] += row * a.ld + k;
+  a.p[1] += row * a.ld + k;
+  return a;
+}
+
+// Tile number b of mt x nt: workgroups go to the eight XCDs in turn, and each XCD takes a run of tiles, in groups of
+// eight of m, so that its L2 holds the rows that its CUs share.
+__device__ __forceinline__ void tile_of(int b, int mt, int nt, int &tm, int &tn) {
+  const int total = mt * nt, q = total / 8, r = total % 8, x = b & 7;
+  b = x * q + (x < r ? x : r) + (b >> 3);
+  const int per = 8 * nt, g = b / per, gm = min(8, mt - g * 8);
+  tm = g * 8 + (b - g * per) % gm;
+  tn = (b - g * per) / gm;
+}
+
+struct Logit {
+  Operand w, h;
+  int v0, valid, kp;  // the piece: its first row of the vocabulary and how many there are
+  const Meta *meta;
+  const int *tgt, *eh;
+  float scale;
+  // forward
+  float2 *part;  // [vocabulary / 128][tcap]
+  float *xt;
+  int64_t tcap;
+  // gradient
+  const RowPrm *prm;
+  uint16_t *g, *gt;  // [tcap][piece], [piece][tcap]
+  int64_t gplane, piece;
+};
+
+template <typename C, bool F16, bool GRAD>
+__global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  const int np = a.meta->np, mt = (a.valid + C::BM - 1) / C::BM, nt = (np + C::BN - 1) / C::BN;
+  if ((int)blockIdx.x >= mt * nt) return;
+  int tm, tn;
+  tile_of(blockIdx.x, mt, nt, tm, tn);
+  const int m0 = tm * C::BM, n0 = tn * C::BN;
+  Core<C, F16> c;
+  c.run(lds, at_row(a.w, m0), at_row(a.h, n0), a.valid - m0, np - n0, a.kp / kStep);
+  const bool whole = m0 + C::BM <= a.valid;
+#pragma unroll
+  for (int j = 0; j < C::TN; ++j) {
+    const int n = n0 + c.col(j);
+    const bool in = n < np;
+    if (GRAD) {
+      const RowPrm p = in ? a.prm[n] : RowPrm{0.0f, 0.0f, 0.0f, 0.0f};
+      const int tv = in ? a.tgt[n] - a.v0 - m0 : -1;
+      const Power pw = power_of(a.scale);
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          float g[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int m = c.row(i, e + q);
+            float x = c.acc[i][j][e + q];
+            if (F16) x *= p.f;
+            g[q] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
+            if (m == tv) g[q] += p.one;
+            if (p.one == 0.0f || m0 + m >= a.valid) g[q] = 0.0f;
+          }
+          if (!in) continue;
+          const int64_t m = m0 + c.row(i, e);
+#pragma unroll
+          for (int plane = 0; plane < (F16 ? 2 : 1); ++plane) {
+            const uint32_t lo = two<F16>(g[0], g[1], plane), hi = two<F16>(g[2], g[3], plane);
+            *(u32x2 *)(a.g + plane * a.gplane + n * a.piece + m) = u32x2{lo, hi};
+            uint16_t *gt = a.gt + plane * a.gplane + m * a.tcap + n;
+            gt[0] = (uint16_t)lo;
+            gt[a.tcap] = (uint16_t)(lo >> 16);
+            gt[2 * a.tcap] = (uint16_t)hi;
+            gt[3 * a.tcap] = (uint16_t)(hi >> 16);
+          }
+        }
+    } else {
+      const float f = F16 && in ? ldexpf(1.0f, a.eh[n] + exponent_of((uint32_t)a.meta->wbits) - 2 * kTop) : 1.0f;
+      const float k2 = power_of(a.scale).k;
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float x = c.acc[i][j][e];
+          if (F16) x *= f;
+          if (!whole && m0 + c.row(i, e) >= a.valid) x = -INFINITY;
+          c.acc[i][j][e] = x;
+          m = fmaxf(m, x);
+        }
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      const float base = m == -INFINITY ? 0.0f : m;
+      float z = 0.0f;
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i) {
+        float s = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((c.acc[i][j][e] - base) * k2);
+        z += s;
+      }
+      z += __shfl_xor(z, 32, 64);
+      if (in) {
+        const int64_t unit = (a.v0 + m0) / (C::BM / C::WM) + c.wm;
+        if (c.fk == 0) a.part[unit * a.tcap + n] = float2{m, z};
+        const int tv = a.tgt[n] - a.v0 - m0 - c.wm * (C::BM / C::WM);
+        if (tv >= 0 && tv < C::BM / C::WM) {
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (c.row(i, e) - c.wm * (C::BM / C::WM) == tv) a.xt[n] = c.acc[i][j][e];
+        }
+      }
+    }
+  }
+#endif
+}
+
+// (m, z) of the listed rows from the units' and their log-probabilities; 64 rows a workgroup, whose waves share the units.
+__global__ __launch_bounds__(1024) void k_join(const Meta *meta, const int *list, const float2 *part, const float *xt,
+                                               int64_t tcap, int units, float scale, float *logp, float2 *stats) {
+  __shared__ float2 lds[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
+  if ((int)blockIdx.x * 64 >= meta->np) return;
+  const float k2 = power_of(scale).k;
+  auto join = [&](float2 a, float2 b) {
+    const float m = fmaxf(a.x, b.x), base = m == -INFINITY ? 0.0f : m;
+    // a sum of nothing is left out: its exponent may be a NaN
+    return float2{m, (a.y == 0.0f ? 0.0f : a.y * __builtin_amdgcn_exp2f((a.x - base) * k2)) +
+                         (b.y == 0.0f ? 0.0f : b.y * __builtin_amdgcn_exp2f((b.x - base) * k2))};
+  };
+  float2 s{-INFINITY, 0.0f};
+  for (int u = wave; u < units; u += 16) s = join(s, part[u * tcap + n]);
+  lds[wave][lane] = s;
+  __syncthreads();
+  if (wave) return;
+  for (int w = 1; w < 16; ++w) s = join(s, lds[w][lane]);
+  const int t = list[n];
+  if (t < 0) return;
+  if (s.x == -INFINITY) s.x = 0.0f;
+  logp[t] = logp_of(xt[n], Stats{s.x, s.y}, scale);
+  if (stats) stats[t] = s;
+}
+
+struct DHidden {
+  Operand wt, g;
+  int width, steps, per, splits;  // stages of the piece, of a split
+  bool first;
+  const Meta *meta;
+  const float *rowf;
+  float *acc;  // [splits][tcap][kp]
+  int64_t tcap;
+  int kp;
+};
+
+// acc[split] (+)= G W of the piece; accumulator rows are features, so that a lane has four of a token
+template <typename C, bool F16>
+__global__ __launch_bounds__(C::TH, 2) void k_dhidden(DHidden a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  const int np = a.meta->np, mt = (a.width + C::BM - 1) / C::BM, nt = (np + C::BN - 1) / C::BN;
+  const int tiles = mt * nt;
+  if ((int)blockIdx.x >= tiles * a.splits) return;
+  const int s = blockIdx.x / tiles;
+  int tm, tn;
+  tile_of(blockIdx.x - s * tiles, mt, nt, tm, tn);
+  const int m0 = tm * C::BM, n0 = tn * C::BN, k0 = s * a.per;
+  Core<C, F16> c;
+  c.run(lds, at_row(a.wt, m0, (int64_t)k0 * kStep), at_row(a.g, n0, (int64_t)k0 * kStep), a.width - m0, np - n0,
+        max(0, min(a.per, a.steps - k0)));
+#pragma unroll
+  for (int j = 0; j < C::TN; ++j) {
+    const int n = n0 + c.col(j);
+    if (n >= np) continue;
+    const float f = F16 ? a.rowf[n] : 1.0f;
+    float *to = a.acc + (s * a.tcap + n) * a.kp + m0;
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int m = c.row(i, e);
+        if (m0 + m >= a.kp) continue;
+        f32x4 v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = F16 ? c.acc[i][j][e + q] * f : c.acc[i][j][e + q];
+        if (!a.first) v += *(f32x4 *)(to + m);
+        *(f32x4 *)(to + m) = v;
+      }
+  }
+#endif
+}
+
+// dH: the splits' sums in order; zeros for masked rows
+template <typename T>
+__global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float *acc, int64_t tcap, int kp, int splits, int rows,
+                                                     int width, T *out, int64_t ld) {
+  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (t >= rows) return;
+  const int p = pos[t];
+  T *o = out + t * ld;
+  for (int k = lane * 8; k < width; k += 512) {
+    float f[8] = {};
+    if (p >= 0) {
+      const float *a = acc + (int64_t)p * kp + k;
+      for (int s = 0; s < splits; ++s, a += tcap * kp) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+          const f32x4 v = *(const f32x4 *)(a + i);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) f[i + q] += v[q];
+        }
+      }
+    }
+    if (k + 8 <= width) {
+#pragma unroll
+      for (int i = 0; i < 8; i += Vec<T>::N) Vec<T>::store(o + k + i, Vec<T>::pack(f + i));
+    } else {
+      for (int i = 0; k + i < width; ++i) o[k + i] = from_f32<T>(f[i]);
+    }
+  }
+}
+
+struct DWeight {
+  Operand ht, gt;
+  int width, valid;
+  int b0, batch;  // examples of this launch
+  const int *seg;
+  const Meta *meta;
+  void *out;       // rows from the piece's first on
+  int64_t vocab;   // rows from example to example
+  bool accumulate;
+};
+
+// dW rows of the piece, per example; accumulator rows are features, so that a lane has four of a row of dW
+template <typename C, bool F16, typename TO>
+__global__ __launch_bounds__(C::TH, 2) void k_dweight(DWeight a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
+  const int mt = (a.width + C::BM - 1) / C::BM, nt = (a.valid + C::BN - 1) / C::BN, tiles = mt * nt;
+  const int bi = blockIdx.x / tiles, b = a.b0 + bi;
+  int tm, tn;
+  tile_of(blockIdx.x - bi * tiles, mt, nt, tm, tn);
+  const int m0 = tm * C::BM, n0 = tn * C::BN, k0 = a.seg[b], k1 = a.seg[b + 1];
+  Core<C, F16> c;
+  c.run(lds, at_row(a.ht, m0, k0), at_row(a.gt, n0, k0), a.width - m0, a.valid - n0, (k1 - k0) / kStep);
+  const float f = F16 && k1 > k0 ? ldexpf(1.0f, max(a.meta->ec, -300) - 2 * kTop) : 1.0f;
+  TO *out = (TO *)a.out + b * a.vocab * a.width;
+#pragma unroll
+  for (int j = 0; j < C::TN; ++j) {
+    const int n = n0 + c.col(j);
+    if (n >= a.valid) continue;
+    TO *to = out + (int64_t)n * a.width + m0;
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int m = c.row(i, e);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (m0 + m + q >= a.width) break;
+          float v = F16 ? c.acc[i][j][e + q] * f : c.acc[i][j][e + q];
+          if (a.accumulate) v += to_f32(to[m + q]);
+          to[m + q] = from_f32<TO>(v);
+        }
+      }
+  }
+#endif
+}
+
+// --- host ---------------------------------------------------------------------------------------------------
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// How a call is cut, and where its parts lie in the workspace.
+struct Plan {
+  bool f16, copy, big;
+  int64_t batch, n, tcap, kp, piece, units, splits, planes;
+  int64_t list, pos, tgt, seg, cnt, meta, hc, eh, part, xt, prm, rowf, cs, ht, wc, wt, g, gt, acc, bytes;
+};
+
+Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
+  Plan p{};
+  p.f16 = x->dtype == SK_F32;
+  p.planes = p.f16 ? 2 : 1;
+  p.batch = batch;
+  p.n = x->rows / batch;
+  p.tcap = up(batch * up(p.n, kStep), 256);
+  p.tcap = std::max<int64_t>(p.tcap, 256);
+  p.kp = up(x->width, kStep);
+  // rows that 16-byte loads in whole stages read as they lie
+  p.copy = p.f16 || x->width % kStep || x->ld_weight % 8 || (uintptr_t)x->weight % 16 || x->ld_weight > (1 << 20);
+  // a piece: G and its transpose within 256 MB, a copy of W within 256 MB
+  int64_t most = x->vocab;
+  if (grad) most = std::min(most, ((int64_t)1 << 26) / (p.tcap * p.planes));
+  if (grad || p.copy) most = std::min(most, ((int64_t)1 << 27) / (p.kp * p.planes));
+  most = std::max<int64_t>(most / 256 * 256, 256);
+  const int64_t pieces = (x->vocab + most - 1) / most;
+  p.piece = up((x->vocab + pieces - 1) / pieces, 256);
+  p.units = (x->vocab + kTileM - 1) / kTileM + 1;
+  p.big = false;
+  p.splits = 1;
+  if (grad) {
+    const int64_t tiles = (up(x->width, 128) / 128) * (up(x->rows, 128) / 128);
+    p.splits = std::max<int64_t>(1, std::min(512 / std::max<int64_t>(tiles, 1), p.piece / 512));
+  }
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t r = at;
+    at += up(bytes, 256);
+    return r;
+  };
+  p.list = take(4 * p.tcap);
+  p.pos = take(4 * x->rows);
+  p.tgt = take(4 * p.tcap);
+  p.seg = take(4 * (batch + 1));
+  p.cnt = take(4 * batch * ((p.n + 63) / 64));
+  p.meta = take(sizeof(Meta));
+  p.hc = take(2 * p.planes * p.tcap * p.kp);
+  p.eh = take(4 * p.tcap);
+  if (p.copy) p.wc = take(2 * p.planes * p.piece * p.kp);
+  if (!grad) {
+    p.part = take(8 * p.units * p.tcap);
+    p.xt = take(4 * p.tcap);
+  } else {
+    p.prm = take(sizeof(RowPrm) * p.tcap);
+    p.rowf = take(4 * p.tcap);
+    p.cs = take(4 * p.tcap);
+    if (dweight) p.ht = take(2 * p.planes * p.tcap * p.kp);
+    if (dhidden) p.wt = take(2 * p.planes * p.piece * p.kp);
+    p.g = take(2 * p.planes * p.tcap * p.piece);
+    p.gt = take(2 * p.planes * p.tcap * p.piece);
+    if (dhidden) p.acc = take(4 * p.splits * p.tcap * p.kp);
+  }
+  p.bytes = at;
+  return p;
+}
+
+int check_linear(const sk_linear *x) {
+  if (!x) return train_fail(SK_EINVAL, "NULL argument");
+  if (x->dtype != SK_F32 && x->dtype != SK_BF16) return train_fail(SK_EDTYPE, "unknown dtype");
+  if (x->index != SK_I32 && x->index != SK_I64) return train_fail(SK_EDTYPE, "unknown index type");
+  if (x->rows < 0 || x->vocab < 1 || x->width < 1 || x->ld_hidden < x->width || x->ld_weight < x->width)
+    return train_fail(SK_EINVAL, "need rows >= 0, vocab >= 1, width >= 1 and row strides >= width");
+  if (!(x->scale >= 0x1p-120f && x->scale <= 0x1p127f))
+    return train_fail(SK_EINVAL, "scale must be in [2^-120, 2^127]");
+  if (x->rows > (1 << 20) || x->vocab > (1 << 22) || x->width > (1 << 16))
+    return train_fail(SK_EUNSUPPORTED, "more than 2^20 rows, 2^22 entries of the vocabulary or 2^16 features");
+  if (!x->weight || (x->rows && (!x->hidden || !x->targets))) return train_fail(SK_EINVAL, "NULL argument");
+  return SK_OK;
+}
+int check_batch(const sk_linear *x, int64_t batch) {
+  if (batch < 1 || x->rows % batch) return train_fail(SK_EINVAL, "rows must be a multiple of batch >= 1");
+  if (batch > (1 << 14)) return train_fail(SK_EUNSUPPORTED, "more than 2^14 examples");
+  return SK_OK;
+}
+
+template <typename T>
+T *ptr(void *work, int64_t at) {
+  return (T *)((char *)work + at);
+}
+
+Operand planes_of(uint16_t *p, int64_t plane, int64_t ld) { return Operand{{p, p + plane}, ld}; }
+
+// list, |W|, rows of H: what both directions begin with
+void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *stats_in, float *logp, float *stats, void *work,
+           hipStream_t st) {
+  Meta *meta = ptr<Meta>(work, p.meta);
+  int *list = ptr<int>(work, p.list);
+  hipLaunchKernelGGL(k_live, dim3(1), dim3(1024), 0, st,
+                     Live{x->targets, dlogp, (int32_t)x->index, (int32_t)x->vocab, (int32_t)p.n, (int32_t)p.batch, list,
+                          ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<int>(work, p.seg), ptr<int>(work, p.cnt), meta, logp,
+                          (float2 *)stats});
+  if (p.f16)
+    hipLaunchKernelGGL(k_absmax, dim3((unsigned)std::min<int64_t>(1024, (x->vocab + 3) / 4)), dim3(256), 0, st,
+                       (const float *)x->weight, x->ld_weight, (int)x->vocab, (int)x->width, meta);
+  const Gather g{x->hidden, x->ld_hidden, (int)x->width, (int)p.kp, list, meta, ptr<uint16_t>(work, p.hc), p.tcap * p.kp,
+                 ptr<int>(work, p.eh), (const float2 *)stats_in, dlogp, x->scale,
+                 dlogp ? ptr<RowPrm>(work, p.prm) : nullptr, ptr<float>(work, p.rowf), ptr<float>(work, p.cs)};
+  if (p.f16)
+    hipLaunchKernelGGL(k_gather<float>, dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, g);
+  else
+    hipLaunchKernelGGL(k_gather<bf16>, dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, g);
+}
+
+// W's rows from v0 on as an operand, and their transpose
+Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, bool transpose, void *work, hipStream_t st) {
+  const int e = p.f16 ? 4 : 2;
+  const void *src = (const char *)x->weight + v0 * x->ld_weight * e;
+  if (p.copy || transpose) {
+    Prep a{};
+    a.src = src;
+    a.ld = x->ld_weight;
+    a.rows = (int)valid;
+    a.width = (int)x->width;
+    a.meta = ptr<Meta>(work, p.meta);
+    if (p.copy) a.copy = ptr<uint16_t>(work, p.wc);
+    a.cplane = a.tplane = p.piece * p.kp;
+    a.kp = (int)p.kp;
+    if (transpose) a.tr = ptr<uint16_t>(work, p.wt);
+    a.tld = p.piece;
+    const dim3 grid((unsigned)(up(valid, 64) / 64), (unsigned)(p.kp / 64));
+    if (p.f16)
+      hipLaunchKernelGGL((k_prep<float, false>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_prep<bf16, false>), grid, dim3(256), 0, st, a);
+  }
+  if (p.copy) return planes_of(ptr<uint16_t>(work, p.wc), p.piece * p.kp, p.kp);
+  return Operand{{(const uint16_t *)src, (const uint16_t *)src}, x->ld_weight};
+}
+
+Logit logit_of(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, Operand w, void *work) {
+  Logit a{};
+  a.w = w;
+  a.h = planes_of(ptr<uint16_t>(work, p.hc), p.tcap * p.kp, p.kp);
+  a.v0 = (int)v0;
+  a.valid = (int)valid;
+  a.kp = (int)p.kp;
+  a.meta = ptr<Meta>(work, p.meta);
+  a.tgt = ptr<int>(work, p.tgt);
+  a.eh = ptr<int>(work, p.eh);
+  a.scale = x->scale;
+  a.tcap = p.tcap;
+  return a;
+}
+
+template <typename C, bool GRAD>
+void run_logits(const Plan &p, const Logit &a, int64_t rows, hipStream_t st) {
+  const unsigned blocks = (unsigned)(((a.valid + C::BM - 1) / C::BM) * ((rows + C::BN - 1) / C::BN));
+  if (p.f16)
+    hipLaunchKernelGGL((k_logits<C, true, GRAD>), dim3(blocks), dim3(C::TH), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_logits<C, false, GRAD>), dim3(blocks), dim3(C::TH), 0, st, a);
+}
+
+template <typename C>
+void run_dhidden(const Plan &p, const DHidden &a, hipStream_t st) {
+  const unsigned blocks = (unsigned)(((a.width + C::BM - 1) / C::BM) * (p.tcap / C::BN) * a.splits);
+  if (p.f16)
+    hipLaunchKernelGGL((k_dhidden<C, true>), dim3(blocks), dim3(C::TH), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_dhidden<C, false>), dim3(blocks), dim3(C::TH), 0, st, a);
+}
+
+template <typename C>
+void run_dweight(const Plan &p, DWeight a, sk_dtype odt, hipStream_t st) {
+  const int64_t tiles = (int64_t)((a.width + C::BM - 1) / C::BM) * ((a.valid + C::BN - 1) / C::BN);
+  const int64_t most = std::max<int64_t>(1, (1 << 22) / tiles);
+  for (int64_t b = 0; b < p.batch; b += most) {
+    a.b0 = (int)b;
+    a.batch = (int)std::min(most, p.batch - b);
+    const unsigned blocks = (unsigned)(tiles * a.batch);
+    if (p.f16)
+      hipLaunchKernelGGL((k_dweight<C, true, float>), dim3(blocks), dim3(C::TH), 0, st, a);
+    else if (odt == SK_F32)
+      hipLaunchKernelGGL((k_dweight<C, false, float>), dim3(blocks), dim3(C::TH), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_dweight<C, false, bf16>), dim3(blocks), dim3(C::TH), 0, st, a);
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t sketch_linear_logp_work_bytes(const sk_linear *x) {
+  if (check_linear(x) != SK_OK) return 0;
+  return plan_of(x, 1, false, false, false).bytes;
+}
+
+int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work, int64_t work_bytes, void *stream) {
+  int rc = check_linear(x);
+  if (rc != SK_OK || x->rows == 0) return rc;
+  if (!logp || !work) return train_fail(SK_EINVAL, "NULL argument");
+  const Plan p = plan_of(x, 1, false, false, false);
+  if (work_bytes < p.bytes) return train_fail(SK_EINVAL, "work is smaller than sketch_linear_logp_work_bytes");
+  TrainGuard guard(x->device);
+  if (!guard.ok) return train_no_device();
+  hipStream_t st = (hipStream_t)stream;
+  begin(x, p, nullptr, nullptr, logp, stats, work, st);
+  for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
+    const int64_t valid = std::min(p.piece, x->vocab - v0);
+    Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, false, work, st), work);
+    a.part = ptr<float2>(work, p.part);
+    a.xt = ptr<float>(work, p.xt);
+    run_logits<Big, false>(p, a, up(x->rows, kStep), st);
+  }
+  hipLaunchKernelGGL(k_join, dim3((unsigned)(p.tcap / 64)), dim3(1024), 0, st, ptr<Meta>(work, p.meta), ptr<int>(work, p.list),
+                     ptr<float2>(work, p.part), ptr<float>(work, p.xt), p.tcap, (int)up(x->vocab, 256) / kTileM, x->scale, logp,
+                     (float2 *)stats);
+  return train_launched();
+}
+
+int64_t sketch_linear_logp_grad_work_bytes(const sk_linear *x, int64_t batch, int32_t dhidden, int32_t dweight) {
+  if (check_linear(x) != SK_OK || check_batch(x, batch) != SK_OK) return 0;
+  return plan_of(x, batch, true, dhidden, dweight).bytes;
+}
+
+int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stats, const float *dlogp, void *dhidden,
+                            int64_t ld_dhidden, void *dweight, sk_dtype dweight_dtype, int32_t accumulate, void *work,
+                            int64_t work_bytes, void *stream) {
+  int rc = check_linear(x);
+  if (rc != SK_OK || (rc = check_batch(x, batch)) != SK_OK) return rc;
+  if (dweight_dtype != SK_F32 && dweight_dtype != SK_BF16) return train_fail(SK_EDTYPE, "unknown dtype");
+  if (x->dtype == SK_F32 && dweight_dtype != SK_F32) return train_fail(SK_EDTYPE, "dweight of fp32 weights is fp32");
+  if (!work || (x->rows && (!stats || !dlogp)) || (!dhidden && !dweight)) return train_fail(SK_EINVAL, "NULL argument");
+  if (dhidden && ld_dhidden < x->width) return train_fail(SK_EINVAL, "need ld_dhidden >= width");
+  const Plan p = plan_of(x, batch, true, dhidden != nullptr, dweight != nullptr);
+  if (work_bytes < p.bytes) return train_fail(SK_EINVAL, "work is smaller than sketch_linear_logp_grad_work_bytes");
+  TrainGuard guard(x->device);
+  if (!guard.ok) return train_no_device();
+  hipStream_t st = (hipStream_t)stream;
+  // k_live takes dlogp = NULL for the forward direction; without rows nothing is read from it
+  begin(x, p, dlogp ? dlogp : (const float *)work, stats, nullptr, nullptr, work, st);
+  Meta *meta = ptr<Meta>(work, p.meta);
+  const int64_t width = x->width;
+  if (dweight && x->rows) {
+    Prep a{};
+    a.src = x->hidden;
+    a.ld = x->ld_hidden;
+    a.width = (int)width;
+    a.meta = meta;
+    a.list = ptr<int>(work, p.list);
+    a.eh = ptr<int>(work, p.eh);
+    a.cs = ptr<float>(work, p.cs);
+    a.tr = ptr<uint16_t>(work, p.ht);
+    a.tplane = p.tcap * p.kp;
+    a.tld = p.tcap;
+    const dim3 grid((unsigned)(p.tcap / 64), (unsigned)(p.kp / 64));
+    if (p.f16)
+      hipLaunchKernelGGL((k_prep<float, true>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_prep<bf16, true>), grid, dim3(256), 0, st, a);
+  }
+  for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
+    const int64_t valid = std::min(p.piece, x->vocab - v0);
+    if (x->rows) {
+      Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, dhidden != nullptr, work, st), work);
+      a.prm = ptr<RowPrm>(work, p.prm);
+      a.g = ptr<uint16_t>(work, p.g);
+      a.gt = ptr<uint16_t>(work, p.gt);
+      a.gplane = p.tcap * p.piece;
+      a.piece = p.piece;
+      run_logits<Big, true>(p, a, p.tcap, st);
+    }
+    if (dhidden && x->rows) {
+      DHidden a{};
+      a.wt = planes_of(ptr<uint16_t>(work, p.wt), p.piece * p.kp, p.piece);
+      a.g = planes_of(ptr<uint16_t>(work, p.g), p.tcap * p.piece, p.piece);
+      a.width = (int)width;
+      a.steps = (int)(up(valid, kStep) / kStep);
+      a.splits = (int)p.splits;
+      a.per = (int)((a.steps + p.splits - 1) / p.splits);
+      a.first = v0 == 0;
+      a.meta = meta;
+      a.rowf = ptr<float>(work, p.rowf);
+      a.acc = ptr<float>(work, p.acc);
+      a.tcap = p.tcap;
+      a.kp = (int)p.kp;
+      run_dhidden<Small>(p, a, st);
+    }
+    if (dweight) {
+      DWeight a{};
+      a.ht = planes_of(ptr<uint16_t>(work, p.ht), p.tcap * p.kp, p.tcap);
+      a.gt = planes_of(ptr<uint16_t>(work, p.gt), p.tcap * p.piece, p.tcap);
+      a.width = (int)width;
+      a.valid = (int)valid;
+      a.seg = ptr<int>(work, p.seg);
+      a.meta = meta;
+      a.out = (char *)dweight + v0 * width * (dweight_dtype == SK_F32 ? 4 : 2);
+      a.vocab = x->vocab;
+      a.accumulate = accumulate != 0;
+      run_dweight<Small>(p, a, dweight_dtype, st);
+    }
+  }
+  if (dhidden && x->rows) {
+    const dim3 grid((unsigned)((x->rows + 3) / 4));
+    if (p.f16)
+      hipLaunchKernelGGL(k_dhidden_out<float>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.acc), p.tcap,
+                         (int)p.kp, (int)p.splits, (int)x->rows, (int)width, (float *)dhidden, ld_dhidden);
+    else
+      hipLaunchKernelGGL(k_dhidden_out<bf16>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.acc), p.tcap,
+                         (int)p.kp, (int)p.splits, (int)x->rows, (int)width, (bf16 *)dhidden, ld_dhidden);
+  }
+  return train_launched();
+}
+
+}  // extern "C"

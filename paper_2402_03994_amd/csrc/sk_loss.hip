@@ -34,31 +34,6 @@ using namespace sk;
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLog2eLow = 1.92596299113e-8f;  // log2 e - kLog2e
-
-// scale log2 e as a sum, for exp(scale d) = 2^(d (k + low))
-struct Power {
-  float k, low;
-};
-__device__ __forceinline__ Power power_of(float scale) {
-  const float k = scale * kLog2e;
-  return Power{k, __builtin_fmaf(scale, kLog2eLow, __builtin_fmaf(scale, kLog2e, -k))};
-}
-
-// exp(scale d) for an entry of a gradient of type T.  The hardware's exponential of the rounded product d k is off by
-// 5e-7 of its value at an exponent of -20 and 9e-7 at -40.  Beside bf16's 2^-8 that is nothing; fp32 entries get what the
-// product has lost as a factor 1 + r ln 2 (policy update of 4096 x 50257 fp32: 323 us, 317 us without).  The sums z need no
-// such care: exponentials count there by their size.
-template <typename T>
-__device__ __forceinline__ float entry_exp(float d, Power p) {
-  const float t = d * p.k, e = __builtin_amdgcn_exp2f(t);
-  if (sizeof(T) == 2) return e;
-  const float r = __builtin_fmaf(d, p.low, __builtin_fmaf(d, p.k, -t));
-  // d = -inf leaves a NaN in r, and a NaN in d one in e
-  return __builtin_fmaf(e, 0.69314718055994530942f * __builtin_amdgcn_fmed3f(r, -1.0f, 1.0f), e);
-}
-
 struct Rows {
   const void *x;
   const void *targets;
@@ -73,18 +48,6 @@ struct Rows {
 __device__ __forceinline__ int target_at(const Rows &r, int64_t t) {
   const int64_t v = r.index == SK_I64 ? ((const int64_t *)r.targets)[t] : ((const int32_t *)r.targets)[t];
   return v >= 0 && v < r.vocab ? (int)v : -1;
-}
-
-// A row's numbers: the largest entry m and z = sum_j exp(scale (x_j - m)).
-struct Stats {
-  float m, z;
-};
-
-__device__ __forceinline__ float logp_of(float xt, Stats s, float scale) {
-  if (s.z == 0.0f) return -INFINITY;
-  float a = (xt - s.m) * scale;
-  if (a == -INFINITY) a = (0.5f * xt - 0.5f * s.m) * scale * 2.0f;  // the difference alone may have overflowed
-  return a - logf(s.z);
 }
 
 // A row cut at 16-byte boundaries: `head` entries before the first one, nv vectors, `rem` entries after the last.

@@ -201,6 +201,93 @@ def token_logp_grad(logits: torch.Tensor, targets: torch.Tensor, stats: torch.Te
     return d
 
 
+def _linear(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, scale: float) -> _lib.Linear:
+    device = _on_gpu(hidden, "hidden")
+    if hidden.dim() < 2 or hidden.shape[:-1] != targets.shape or hidden.shape[-1] < 1:
+        raise ValueError("hidden must be [*targets.shape, width]")
+    width = ld = hidden.shape[-1]
+    if not hidden.is_contiguous():
+        try:
+            ld = _rows(hidden.view(-1, width), "hidden")
+        except RuntimeError:
+            raise ValueError("hidden must have rows of one stride") from None
+    index = _ids(targets, "targets", device)
+    if weight.device != device or weight.dtype != hidden.dtype or weight.dim() != 2 or weight.shape[1] != width:
+        raise ValueError(f"weight must be [vocab, {width}] of the type of hidden on {device}")
+    return _lib.Linear(hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), targets.numel(), weight.shape[0], width, ld,
+                       _rows(weight, "weight"), scale, _dtype(hidden, "hidden"), index, device.index)
+
+
+def linear_logp(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, scale: float = 1.0):
+    """token_logp(hidden @ weight.T, targets, scale) without the logits: (logp [*targets.shape], stats [*targets.shape, 2])
+    float32.
+
+    hidden [*targets.shape, width] and weight [vocab, width], float32 or bfloat16 alike, rows of one stride each; a target
+    outside [0, vocab) masks its position (logp 0, its hidden state is not read).  The logits live tile by tile in
+    registers; what a call needs beside its inputs is a few numbers for each position and 128 entries of the vocabulary,
+    and for float32 (or rows that 16-byte loads do not fit) a copy of a piece of the weight."""
+    x = _linear(hidden, weight, targets, scale)
+    device, lib = hidden.device, _lib.load()
+    logp = torch.empty(targets.shape, dtype=torch.float32, device=device)
+    stats = torch.empty((*targets.shape, 2), dtype=torch.float32, device=device)
+    nw = lib.sketch_linear_logp_work_bytes(ctypes.byref(x))
+    work = torch.empty(nw, dtype=torch.uint8, device=device)
+    _lib.check(lib.sketch_linear_logp(ctypes.byref(x), logp.data_ptr(), stats.data_ptr(), work.data_ptr(), nw,
+                                      _stream_ptr(device)))
+    return logp, stats
+
+
+def linear_logp_grad(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, stats: torch.Tensor,
+                     dlogp: torch.Tensor, scale: float = 1.0, per_example: bool = False, hidden_grad: bool = True,
+                     weight_grad: bool = True, out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                     accumulate: bool = False):
+    """(dhidden, dweight): the gradients of sum(dlogp * linear_logp(...)[0]) with respect to hidden, in its type, and to
+    weight (None for one that is not wanted).  Supervised cross entropy has dlogp = -weights.
+
+    stats: linear_logp's.  dlogp, float32, has the shape of targets.  per_example: one gradient [vocab, width] of the weight
+    for each entry of targets' first axis, so that dweight [batch, vocab, width], viewed as [batch, vocab * width], is what
+    Sketch.apply takes.  dweight has the weight's type; out_dtype (or an out of it) may be float32 for a bfloat16 weight.
+    accumulate adds to `out` (with tied weights embed_grad can add to it too).
+
+    The logits are formed again, a piece of the vocabulary at a time; the gradients at them are rounded to bfloat16 where the
+    inputs are.  Positions with a masked target or dlogp = 0 are not read and get zeros."""
+    x = _linear(hidden, weight, targets, scale)
+    device, lib = hidden.device, _lib.load()
+    if stats.dtype != torch.float32 or stats.device != device or stats.shape != (*targets.shape, 2) or \
+            not stats.is_contiguous():
+        raise ValueError(f"stats must be contiguous float32 {[*targets.shape, 2]} on {device}")
+    if dlogp.dtype != torch.float32 or dlogp.device != device or dlogp.shape != targets.shape or not dlogp.is_contiguous():
+        raise ValueError(f"dlogp must be contiguous float32 {list(targets.shape)} on {device}")
+    if per_example and targets.dim() < 2:
+        raise ValueError("per_example needs targets [batch, ...]")
+    batch = targets.shape[0] if per_example else 1
+    shape = (batch, *weight.shape) if per_example else tuple(weight.shape)
+    given = out is not None
+    if not weight_grad and (given or accumulate):
+        raise ValueError("out and accumulate are the weight's gradient's")
+    if not given:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        if weight_grad:
+            out = torch.empty(shape, dtype=out_dtype or weight.dtype, device=device)
+    elif out.shape != shape or out.device != device or not out.is_contiguous() or \
+            (out_dtype is not None and out.dtype != out_dtype):
+        raise ValueError(f"out must be contiguous {list(shape)} on {device}")
+    dhidden = torch.empty(hidden.shape, dtype=hidden.dtype, device=device) if hidden_grad else None
+    if batch == 0 or not (hidden_grad or weight_grad):
+        return dhidden, out
+    nw = lib.sketch_linear_logp_grad_work_bytes(ctypes.byref(x), batch, int(hidden_grad), int(weight_grad))
+    work = torch.empty(nw, dtype=torch.uint8, device=device)
+    _lib.check(lib.sketch_linear_logp_grad(ctypes.byref(x), batch, stats.data_ptr(), dlogp.data_ptr(),
+                                           dhidden.data_ptr() if hidden_grad else None, x.width,
+                                           out.data_ptr() if weight_grad else None,
+                                           _dtype(out, "out") if weight_grad else x.dtype, int(accumulate),
+                                           work.data_ptr(), nw, _stream_ptr(device)))
+    if given:
+        increment_version(out)
+    return dhidden, out
+
+
 def policy_loss(logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor,
                 weights: torch.Tensor, ref_logp: Optional[torch.Tensor] = None, clip=(0.2, 0.2), kl_coef: float = 0.0,
                 scale: float = 1.0, grad: bool = True, out: Optional[torch.Tensor] = None) -> PolicyLoss:

@@ -1,0 +1,244 @@
+"""GPU parity of the log-probabilities from hidden states and of their gradients with the fp64 definitions
+(oracle/train.py).
+
+Tolerances, all worked out from the arithmetic:
+* a logit is a sum of `width` products of size S = sum |h| |w|.  Products of bf16 are exact in fp32; of fp32 inputs each
+  operand is held to 2^-22 of itself or 2^-38 of its largest (three products): 2^-21 S + 2^-37 * width * max |h| max |w|.
+  The sum rounds once for each addition: X = (3 width + 8) 2^-24 S, at most.
+* log z: exponentials to (4 A + 4) 2^-24 for exponents of size A, then at most 32 additions in a row in a tile and
+  V / 2048 + 32 joins of tiles, three roundings each: E = (4 A + 3 V / 2048 + 140) 2^-24.  log p: twice scale X, and E.
+* g = scale dlogp (onehot - p): p to r = 2 (scale X + E) of itself, the target's 1 - p to p r + 2^-22 more; then
+  rounded to bf16 (2^-8 of itself), or held in two fp16 (2^-22 of itself or 2^-37 of scale dlogp).
+* a gradient's entry is a sum of n products: the errors of g times the other factor, 2^-22 of each product (fp32), n 2^-24
+  of their sizes, and the rounding of the output.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import train as O
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    assert torch.cuda.is_available(), "GPU tests need a ROCm device"
+    from paper_2402_03994_amd import _lib
+    _lib.load()
+    return torch.device("cuda", 0)
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def rows(t, dev, lead=0, pad=0):
+    """t on the device, starting `lead` elements into its storage, rows padded by `pad` entries of NaN."""
+    r, c = t.shape
+    buf = torch.full((lead + r * (c + pad),), float("nan"), dtype=t.dtype, device=dev)
+    v = buf[lead:].view(r, c + pad)[:, :c]
+    v.copy_(t)
+    return v
+
+
+def make(T, V, d, dt, seed, masked=True):
+    """Logits of a few units, one text's positions peaked; masked positions hold NaNs."""
+    g = torch.Generator().manual_seed(seed)
+    W = (torch.randn(V, d, generator=g) * (1.5 / d ** 0.5)).to(dt)
+    t = torch.randint(0, V, (T,), generator=g)
+    h = torch.randn(T, d, generator=g)
+    h[::3] += 4 * d ** 0.5 * torch.nn.functional.normalize(W[t[::3]].float(), dim=1)
+    if masked and T > 2:
+        dead = torch.rand(T, generator=g) < 0.3
+        t[dead] = torch.where(torch.rand(int(dead.sum()), generator=g) < 0.5, -100, V)
+        h[dead] = float("nan")
+    return h.to(dt), W, t, torch.randn(T, generator=g)
+
+
+def logit_error(h, W, dt):
+    """X [T, V] (zeros for NaN rows) and the logits."""
+    h = np.nan_to_num(h)
+    d = W.shape[1]
+    S = np.abs(h) @ np.abs(W).T
+    X = (3 * d + 8) * 2.0 ** -24 * S
+    if dt == F32:
+        X += 2.0 ** -21 * S + 2.0 ** -37 * d * np.abs(h).max(1, keepdims=True) * np.abs(W).max()
+    return X, h @ W.T
+
+
+def errors(h, W, dt, scale):
+    """(of log p: [T], relative of p: [T, V])"""
+    X, x = logit_error(h, W, dt)
+    A = np.abs(x - x.max(1, keepdims=True)) * scale
+    E = (4 * A + 3 * len(W) / 2048 + 140) * 2.0 ** -24
+    x_err = scale * X.max(1)
+    return 2 * x_err + E.max(1), 2 * (x_err[:, None] + E)
+
+
+def check(dev, T, V, d, dt, scale=1.0, batch=1, lead=0, pad=0, wlead=0, wpad=0, seed=None, index=torch.int64, odt=None,
+          accumulate=False):
+    import paper_2402_03994_amd as fw
+    h, W, t, c = make(T, V, d, dt, T + V + d if seed is None else seed)
+    hd, Wd, td, cd = rows(h, dev, lead, pad), rows(W, dev, wlead, wpad), t.to(dev).to(index), c.to(dev)
+    shape = (batch, T // batch) if batch > 1 else (T,)
+    hd = hd.unflatten(0, shape) if batch > 1 else hd
+    td, cd = td.view(shape), cd.view(shape)
+    logp, stats = fw.linear_logp(hd, Wd, td, scale=scale)
+    hn, Wn, tn, s = f64(h), f64(W), t.numpy(), float(np.float32(scale))
+    live = (tn >= 0) & (tn < V)
+    ref = O.linear_logp(hn, Wn, tn, s)
+    el, rp = errors(hn, Wn, dt, s)
+    got = f64(logp).reshape(-1)
+    assert not got[~live].any() and not f64(stats).reshape(-1, 2)[~live].any()
+    assert (np.abs(got - ref)[live] <= (el + 2.0 ** -23 * np.abs(ref))[live]).all()
+    odt = odt or dt
+    out = before = None
+    if accumulate:
+        out = torch.randn((batch, V, d) if batch > 1 else (V, d), generator=torch.Generator().manual_seed(3)).to(odt).to(dev)
+        before = f64(out).reshape(batch, V, d)
+    dh, dw = fw.linear_logp_grad(hd, Wd, td, stats, cd, scale=scale, per_example=batch > 1, out=out,
+                                 out_dtype=odt, accumulate=accumulate)
+    assert dh.dtype == dt and dh.shape == hd.shape and dw.dtype == odt
+    rh, rw, g, p = O.linear_logp_grad(hn, Wn, tn, f64(c), s, batch)
+    cs = np.where(live, np.abs(f64(c)), 0.0)[:, None] * s
+    eg = cs * p * rp
+    at = np.flatnonzero(live)
+    eg[at, tn[at]] += cs[at, 0] * 2.0 ** -22
+    eg += np.abs(g) * HALF[BF16] if dt == BF16 else np.abs(g) * 2.0 ** -22 + cs * 2.0 ** -37
+    ag, aW, ah = np.abs(g) + eg, np.abs(Wn), np.abs(np.nan_to_num(hn))
+    more = 0.0 if dt == BF16 else 2.0 ** -20
+    tol = eg @ aW + ((3 * V + 64) * 2.0 ** -24 + more) * (ag @ aW) + HALF[dt] * np.abs(rh) + 1e-37
+    err = np.abs(f64(dh).reshape(T, d) - rh)
+    assert (err <= tol).all(), (err / tol).max()
+    assert not f64(dh).reshape(T, d)[~live].any()
+    n = T // batch
+    for b in range(batch):
+        r = slice(b * n, b * n + n)
+        old = 0.0 if before is None else before[b]
+        tail = 0.0 if dt == BF16 else 2.0 ** -37 * n * (cs * ah).max()
+        want = rw[b] + old
+        tol = eg[r].T @ ah[r] + ((3 * n + 8) * 2.0 ** -24 + more) * (ag[r].T @ ah[r]) + tail + HALF[odt] * np.abs(want) \
+            + 2.0 ** -24 * np.abs(old) + 1e-37
+        err = np.abs(f64(dw).reshape(batch, V, d)[b] - want)
+        assert (err <= tol).all(), (b, (err / tol).max())
+    if not accumulate:
+        again = fw.linear_logp_grad(hd, Wd, td, stats, cd, scale=scale, per_example=batch > 1, out_dtype=odt)
+        assert torch.equal(again[0], dh) and torch.equal(again[1], dw)
+
+
+SHAPES = [(1, 1, 1), (2, 3, 5), (1, 300, 64), (16, 257, 40), (17, 1000, 250), (64, 128, 64), (70, 513, 128), (129, 256, 72),
+          (300, 700, 130), (257, 2000, 768), (1000, 1300, 96)]
+
+
+@pytest.mark.parametrize("T,V,d", SHAPES)
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear(dev, T, V, d, dt):
+    check(dev, T, V, d, dt)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("kw", [dict(lead=1, pad=3), dict(wlead=1, wpad=5), dict(lead=8, pad=8, wlead=8, wpad=64),
+                                dict(scale=0.7, index=torch.int32), dict(accumulate=True)])
+def test_linear_layouts(dev, dt, kw):
+    check(dev, 90, 600, 192, dt, **kw)
+    check(dev, 33, 210, 77, dt, **kw)
+
+
+def test_linear_fp32_gradient_of_bf16_weights(dev):
+    check(dev, 90, 600, 192, BF16, odt=F32)
+    check(dev, 90, 600, 192, BF16, odt=F32, accumulate=True)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("T,batch", [(6, 3), (130, 2), (128, 8), (700, 7), (1300, 20)])
+def test_linear_per_example(dev, dt, T, batch):
+    check(dev, T, 300, 65, dt, batch=batch)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_in_pieces(dev, dt):
+    """More than one piece of the vocabulary, against the same in fp64 on the device."""
+    import paper_2402_03994_amd as fw
+    T, V, d = 4200, 40000, 64
+    h, W, t, c = make(T, V, d, dt, 5)
+    hd, Wd, td, cd = (v.to(dev) for v in (h, W, t, c))
+    logp, stats = fw.linear_logp(hd, Wd, td)
+    dh, dw = fw.linear_logp_grad(hd, Wd, td, stats, cd)
+    live = ((td >= 0) & (td < V)).nonzero()[:, 0]
+    x = hd[live].double() @ Wd.double().T
+    ls = torch.log_softmax(x, 1)
+    one = td[live][:, None]
+    assert (logp[live].double() - ls.gather(1, one)[:, 0]).abs().max() < 2e-5  # 2 X of logits of size 30, E < 3e-5
+    g = ls.exp().neg_().scatter_add_(1, one, torch.ones_like(one, dtype=torch.float64)) * cd[live].double()[:, None]
+    # errors add up at random here: a part in 2^-8 (2^-20) of each term, over the norm
+    for got, want in ((dh[live], g @ Wd.double()), (dw, g.T @ hd[live].double())):
+        assert (got.double() - want).norm() <= (2.0 ** -8 if dt == BF16 else 2e-6) * want.norm()
+    dead = torch.ones(T, dtype=torch.bool, device=dev)
+    dead[live] = False
+    assert not dh[dead].any() and not logp[dead].any()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_masks(dev, dt):
+    """Nothing left to do, parts that are not wanted, rows of dlogp = 0."""
+    import paper_2402_03994_amd as fw
+    h, W, t, c = make(50, 90, 64, dt, 1)
+    hd, Wd, cd = h.to(dev), W.to(dev), c.to(dev)
+    none = torch.full((50,), -1, device=dev)
+    logp, stats = fw.linear_logp(hd, Wd, none)
+    assert not logp.any() and not stats.any()
+    old = torch.ones_like(Wd)
+    dh, dw = fw.linear_logp_grad(hd, Wd, none, stats, cd, out=old, accumulate=True)
+    assert not dh.any() and (dw == 1).all()
+    assert not fw.linear_logp_grad(hd, Wd, none, stats, cd)[1].any()
+    td = t.to(dev)
+    logp, stats = fw.linear_logp(hd, Wd, td)
+    both = fw.linear_logp_grad(hd, Wd, td, stats, cd)
+    assert torch.equal(fw.linear_logp_grad(hd, Wd, td, stats, cd, weight_grad=False)[0], both[0])
+    assert fw.linear_logp_grad(hd, Wd, td, stats, cd, weight_grad=False)[1] is None
+    assert torch.equal(fw.linear_logp_grad(hd, Wd, td, stats, cd, hidden_grad=False)[1], both[1])
+    zero = cd * (torch.arange(50, device=dev) % 2)
+    some = td.where(zero != 0, -1)
+    a, b = fw.linear_logp_grad(hd, Wd, td, stats, zero), fw.linear_logp_grad(hd, Wd, some, stats, cd)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    e = torch.empty(0, 64, dtype=dt, device=dev)
+    logp, stats = fw.linear_logp(e, Wd, none[:0])
+    assert logp.shape == (0,)
+    dh, dw = fw.linear_logp_grad(e, Wd, none[:0], stats, cd[:0])
+    assert dh.shape == (0, 64) and dw.shape == Wd.shape and not dw.any()
+
+
+def test_linear_agrees_with_given_logits(dev):
+    """The same statistics and log-probabilities as token_logp has for these logits, where they are exact in fp32."""
+    import paper_2402_03994_amd as fw
+    g = torch.Generator().manual_seed(2)
+    h = torch.randint(-8, 9, (40, 64), generator=g).float().to(dev)  # products and sums are whole numbers
+    W = (torch.randint(-8, 9, (333, 64), generator=g).float() / 64).to(dev)
+    t = torch.randint(-2, 335, (40,), generator=g).to(dev)
+    for dt in (F32, BF16):
+        lp, st = fw.linear_logp(h.to(dt), W.to(dt), t, scale=0.5)
+        rp, rs = fw.token_logp(h @ W.T, t, scale=0.5)
+        assert torch.equal(st[:, 0], rs[:, 0])
+        assert (lp - rp).abs().max() < 2e-6 * 20
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_gradient_against_differences(dev, dt):
+    """d/de of sum(dlogp logp) along directions of both inputs, by differences of the fp64 definition."""
+    import paper_2402_03994_amd as fw
+    h, W, t, c = make(40, 120, 64, dt, 9, masked=False)
+    t[5] = -1
+    _, stats = fw.linear_logp(h.to(dev), W.to(dev), t.to(dev))
+    dh, dw = fw.linear_logp_grad(h.to(dev), W.to(dev), t.to(dev), stats, c.to(dev))
+    r = np.random.default_rng(1)
+    uh, uw = r.standard_normal(h.shape), r.standard_normal(W.shape)
+    e = 1e-5
+    f = lambda k: (f64(c) * O.linear_logp(f64(h) + k * e * uh, f64(W) + k * e * uw, t.numpy(), 1.0)).sum()  # noqa: E731
+    want = (f(1) - f(-1)) / (2 * e)
+    got = (f64(dh) * uh).sum() + (f64(dw) * uw).sum()
+    size = np.sqrt((f64(dh) ** 2).sum() + (f64(dw) ** 2).sum())  # of a sum along random directions
+    assert abs(got - want) <= (2.0 ** -7 if dt == BF16 else 1e-5) * size * 4
