@@ -196,6 +196,50 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
                             int64_t work_bytes, void *stream);
 
 /*
+ * Dropout with a mask that is drawn again wherever it is needed:
+ *   out_i = residual_i + (u_i >= t ? x_i 65536 / (65536 - t) : 0),  t = floor(65536 p + 1/2)
+ * for element i = row * width + column of x, in fp32 and rounded once.  u_i is half
+ * (i mod 2) of word (i / 2 mod 4) of the Philox4x32-10 block with counter
+ * (i / 8, step, site, SK_STREAM_DROPOUT) under the key of `seed`: p counts in
+ * steps of 2^-16, and what is dropped may be anything.  The gradient with respect
+ * to x is the same call with dy in the place of x and without residual (that one's
+ * gradient is dy).
+ *   x, residual (NULL if none), out  [rows, width] of one type, row strides >= width
+ *   p        in [0, 1]; p that rounds to t = 65536 drops everything.
+ *   step_at  NULL, or one int64 in device memory whose low 32 bits stand for step
+ *            (a captured graph that is replayed draws a new mask when it changes)
+ *   step, site  in [0, 2^32)
+ * out may be x or residual (same row stride).  SK_EUNSUPPORTED for more than 2^35
+ * elements.
+ */
+#define SK_STREAM_DROPOUT 13
+int sketch_dropout(const void *x, sk_dtype dtype, int64_t rows, int64_t width, int64_t ld, const void *residual,
+                   int64_t ld_residual, void *out, int64_t ld_out, double p, uint64_t seed, int64_t step,
+                   const int64_t *step_at, int64_t site, int32_t device, void *stream);
+
+/*
+ * Balance loss of a router over E = `experts` from the logits of its tokens and the
+ * k ids it has chosen for each:
+ *   c_e = ids equal to e (counts),  n = tokens with an id in [0, E)
+ *   P_e = mean over those tokens of softmax(logits)_e (probs),  f_e = c_e / (n k)
+ *   loss = coef E sum_e f_e P_e  (coef where f or P is even)
+ *   dlogits_te = coef E / n p_te (f_e - sum_e' f_e' p_te')
+ * (c_e has no gradient).  A token without an id in [0, E) is masked: its logits are
+ * not read, its gradient is a row of zeros.  An id counts as often as it stands.
+ * With n = 0 everything is 0.  A row of -inf alone counts with probabilities 0.
+ *   logits   [tokens, E], row stride ld >= E;  ids [tokens, k] contiguous
+ *   loss, probs [E]  fp32;  counts [E] int64
+ *   dlogits  NULL, or the type of the logits, row stride ld_out; may be the logits
+ *            themselves (same ld)
+ *   work     sketch_balance_work_bytes(experts) bytes, 16-byte aligned
+ * SK_EUNSUPPORTED for experts > 2048, k > 1024 or 2^31 ids.
+ */
+int64_t sketch_balance_work_bytes(int64_t experts);
+int sketch_balance_loss(const void *logits, sk_dtype dtype, int64_t tokens, int64_t experts, int64_t ld, const void *ids,
+                        sk_index index, int64_t k, float coef, float *loss, int64_t *counts, float *probs, void *dlogits,
+                        int64_t ld_out, void *work, int64_t work_bytes, int32_t device, void *stream);
+
+/*
  * AdamW over a list of parameter tensors, one launch for up to 160 of them:
  *   g = g s;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
  *   p = p (1 - lr wd_l) - lr / (1 - b1^step) m / (sqrt(v / (1 - b2^step)) + eps)

@@ -193,3 +193,35 @@ def linear_logp_grad(hidden, weight, targets, dlogp, scale, batch=1):
     n = len(t) // batch
     dw = np.stack([g[b * n:b * n + n].T @ h[b * n:b * n + n] for b in range(batch)])
     return g @ W, dw, g, p
+
+
+# --- dropout and a router's balance loss ------------------------------------------------------------------
+def dropout_words(n, step, site, seed):
+    """The 16-bit random numbers of elements 0 .. n-1."""
+    i = np.arange(n)
+    w = philox(np.arange((n + 7) // 8), step, site, 13, seed)[i // 8, (i // 2) % 4]
+    return np.where(i % 2, w >> 16, w & 0xFFFF)
+
+
+def dropout(x, p, seed, step, site, residual=None):
+    """(out, kept), x and residual of any shape."""
+    x = np.asarray(x, dtype=np.float64)
+    t = int(np.floor(65536 * p + 0.5))
+    kept = (dropout_words(x.size, step, site, seed) >= t).reshape(x.shape)
+    out = np.where(kept, np.where(kept, x, 0.0) * (65536.0 / (65536 - t) if t < 65536 else 0.0), 0.0)
+    return (out if residual is None else out + np.asarray(residual, dtype=np.float64)), kept
+
+
+def balance_loss(x, ids, coef):
+    """(loss, counts, probs, dlogits)."""
+    ids = np.asarray(ids)
+    E = np.shape(x)[1]
+    valid = (ids >= 0) & (ids < E)
+    live = valid.any(1)
+    n = live.sum()
+    counts = np.bincount(ids[valid].astype(np.int64), minlength=E)
+    if n == 0:
+        return 0.0, counts, np.zeros(E), np.zeros(np.shape(x))
+    p = softmax_rows(np.where(live[:, None], np.asarray(x, dtype=np.float64), 0.0), 1.0)[0] * live[:, None]
+    f, probs = counts / (n * ids.shape[1]), p.sum(0) / n
+    return coef * E * (f * probs).sum(), counts, probs, coef * E / n * p * (f - (p @ f)[:, None])

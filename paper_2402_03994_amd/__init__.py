@@ -8,5 +8,6 @@ marshals torch tensors into that library.
 from .sketch import KINDS, Sketch  # noqa: F401
 from ._lib import SketchError  # noqa: F401
 from .hvp import SyntheticHessian, arnoldi, arnoldi_step, id_search, ritz_values, sketch_hvp  # noqa: F401
-from .train import (AdamW, PolicyLoss, PreferenceLoss, embed, embed_grad, linear_logp,  # noqa: F401
-                    linear_logp_grad, policy_loss, preference_loss, token_logp, token_logp_grad)
+from .train import (AdamW, BalanceLoss, PolicyLoss, PreferenceLoss, balance_loss, dropout, dropout_grad,  # noqa: F401
+                    embed, embed_grad, linear_logp, linear_logp_grad, policy_loss, preference_loss, token_logp,
+                    token_logp_grad)

@@ -22,7 +22,8 @@ EXPORTS = ("sketch_create", "sketch_apply", "sketch_apply_noalloc", "sketch_appl
            "sk_hvp_profile_read", "sketch_id_search_work_floats", "sketch_id_search", "sketch_embed", "sketch_embed_grad",
            "sketch_embed_grad_work_bytes", "sketch_token_logp", "sketch_token_logp_grad", "sketch_policy_loss",
            "sketch_preference_work_bytes", "sketch_preference_loss", "sketch_linear_logp_work_bytes",
-           "sketch_linear_logp", "sketch_linear_logp_grad_work_bytes", "sketch_linear_logp_grad", "sketch_adamw_create",
+           "sketch_linear_logp", "sketch_linear_logp_grad_work_bytes", "sketch_linear_logp_grad",
+           "sketch_dropout", "sketch_balance_work_bytes", "sketch_balance_loss", "sketch_adamw_create",
            "sketch_adamw_state_elems", "sketch_adamw_apply", "sketch_adamw_moments", "sketch_adamw_destroy")
 HVP_PROF_CLASSES = ["hvp_dots", "hvp_combine", "arnoldi_orth"]
 HVP_MAX_RANK = 32
@@ -145,6 +146,11 @@ def load() -> ctypes.CDLL:
             ("sketch_linear_logp", ctypes.c_int, [XP, P, P, P, i64, P]),
             ("sketch_linear_logp_grad_work_bytes", i64, [XP, i64, i32, i32]),
             ("sketch_linear_logp_grad", ctypes.c_int, [XP, i64, P, P, P, i64, P, ctypes.c_int, i32, P, i64, P]),
+            ("sketch_dropout", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, i64, P, i64, ctypes.c_double, u64, i64, P,
+                                              i64, i32, P]),
+            ("sketch_balance_work_bytes", i64, [i64]),
+            ("sketch_balance_loss", ctypes.c_int, [P, ctypes.c_int, i64, i64, i64, P, ctypes.c_int, i64, f32, P, P, P, P,
+                                                   i64, P, i64, i32, P]),
             ("sketch_adamw_create", ctypes.c_int, [P, P, i32, ctypes.c_int, u64, i32, ctypes.POINTER(P)]),
             ("sketch_adamw_state_elems", i64, [P]),
             ("sketch_adamw_apply", ctypes.c_int, [P, SP, ctypes.POINTER(P), ctypes.c_int, ctypes.POINTER(P),

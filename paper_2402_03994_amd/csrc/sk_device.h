@@ -56,7 +56,7 @@ SK_HD W4 philox_at(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, Key key) 
   for (int r = 0; r < 10; ++r) {
     const uint64_t p0 = (uint64_t)0xD2511F53u * c0;
     const uint64_t p1 = (uint64_t)0xCD9E8D57u * c2;
-    uint32_t n0, n2;
+    uint32_t n0 = 0, n2 = 0;
     if constexpr (XOR3) {
 #if defined(__HIP_DEVICE_COMPILE__)
       n0 = __builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c1, k0, 0x96);

@@ -43,6 +43,15 @@ class PreferenceLoss(NamedTuple):
     dlogits: Optional[torch.Tensor]
 
 
+class BalanceLoss(NamedTuple):
+    """loss (scalar float32), counts [experts] int64, probs [experts] float32 (mean probabilities), dlogits (None without
+    grad)."""
+    loss: torch.Tensor
+    counts: torch.Tensor
+    probs: torch.Tensor
+    dlogits: Optional[torch.Tensor]
+
+
 def _dtype(t: torch.Tensor, name: str) -> int:
     if t.dtype not in _DT:
         raise ValueError(f"{name} must be float32 or bfloat16")
@@ -286,6 +295,86 @@ def linear_logp_grad(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.
     if given:
         increment_version(out)
     return dhidden, out
+
+
+def dropout(x: torch.Tensor, p: float, seed: int, step, site: int = 0, residual: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """residual + x * mask / (1 - p), the mask drawn from (seed, step, site) and each element's place in x, never stored.
+
+    p counts in steps of 2^-16.  step: the training step, below 2^32, or one int64 on the device that holds it (a captured
+    graph that is replayed takes the step of each replay from there).  site: a number of its own for every place of a model
+    that drops.  residual and out have the shape and type of x (float32 or bfloat16); out may be x or residual."""
+    device = _on_gpu(x, "x")
+    dt = _dtype(x, "x")
+    for t, name in ((residual, "residual"), (out, "out")):
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype or t.device != device):
+            raise ValueError(f"{name} must have the shape, type and device of x")
+    step_at = None
+    if isinstance(step, torch.Tensor):
+        if step.dtype != torch.int64 or step.numel() != 1 or step.device != device:
+            raise ValueError(f"step must be a number or one int64 on {device}")
+        step, step_at = 0, step.data_ptr()
+    given = out is not None
+    if not given:
+        out = torch.empty(x.shape, dtype=x.dtype, device=device)
+    if x.numel() == 0:
+        return out
+    some = [t for t in (x, residual, out) if t is not None]
+    if all(t.is_contiguous() for t in some):
+        rows, width = 1, x.numel()
+        lds = [width] * len(some)
+    else:
+        rows, width = x.numel() // x.shape[-1], x.shape[-1]
+        lds = []
+        for t in some:
+            try:
+                lds.append(_rows(t.view(rows, width), "x, residual and out"))
+            except RuntimeError:
+                raise ValueError("x, residual and out must have rows of one stride") from None
+    _lib.check(_lib.load().sketch_dropout(x.data_ptr(), dt, rows, width, lds[0],
+                                          None if residual is None else residual.data_ptr(),
+                                          0 if residual is None else lds[1], out.data_ptr(), lds[-1], p,
+                                          int(seed) & 0xFFFFFFFFFFFFFFFF, int(step), step_at, int(site), device.index,
+                                          _stream_ptr(device)))
+    if given:
+        increment_version(out)
+    return out
+
+
+def dropout_grad(dy: torch.Tensor, p: float, seed: int, step, site: int = 0,
+                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of dropout(x, p, seed, step, site) with respect to x: dy * mask / (1 - p), the same mask (the residual's
+    gradient is dy).  out may be dy."""
+    return dropout(dy, p, seed, step, site, out=out)
+
+
+def balance_loss(logits: torch.Tensor, experts: torch.Tensor, coef: float = 1.0, grad: bool = True,
+                 out: Optional[torch.Tensor] = None) -> BalanceLoss:
+    """coef * E * sum_e f_e P_e over a router's E experts: P_e the tokens' mean softmax(logits)_e, f_e the share of e among
+    the ids they were sent to (counts, which carry no gradient), and its gradient with respect to the logits.
+
+    logits [T, E] (float32 or bfloat16, rows may have a stride); experts [T, k]: the ids of each token, those outside [0, E)
+    count nothing, and a token without another one is masked.  out (where grad) may be the logits; a new dlogits has their
+    row stride, as token_logp_grad's."""
+    device = _on_gpu(logits, "logits")
+    ld = _rows(logits, "logits")
+    index = _ids(experts, "experts", device)
+    n, E = logits.shape
+    if experts.dim() != 2 or experts.shape[0] != n or experts.shape[1] < 1:
+        raise ValueError("experts must be [T, k] for logits [T, E]")
+    small = torch.empty(1 + E, dtype=torch.float32, device=device)
+    counts = torch.empty(E, dtype=torch.int64, device=device)
+    d, ld_out = _dlogits(logits, out) if grad else (None, 0)
+    lib = _lib.load()
+    nw = lib.sketch_balance_work_bytes(E)
+    work = torch.empty(nw, dtype=torch.uint8, device=device)
+    _lib.check(lib.sketch_balance_loss(logits.data_ptr(), _dtype(logits, "logits"), n, E, ld, experts.data_ptr(), index,
+                                       experts.shape[1], coef, small.data_ptr(), counts.data_ptr(), small.data_ptr() + 4,
+                                       d.data_ptr() if grad else None, ld_out, work.data_ptr(), nw, device.index,
+                                       _stream_ptr(device)))
+    if grad and out is not None:
+        increment_version(out)
+    return BalanceLoss(small[0], counts, small[1:], d)
 
 
 def policy_loss(logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor,

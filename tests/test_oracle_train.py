@@ -101,3 +101,48 @@ def test_philox_words_match_the_c_oracle():
         c, k, want = row[:4], row[4:6], row[6:10]
         got = O.philox(np.array([c[0]]), c[1], c[2], c[3], k[0] | k[1] << 32)[0]
         assert [int(v) for v in got] == want
+
+
+@pytest.mark.parametrize("batch", [1, 3])
+def test_linear_gradients_against_differences(batch):
+    r = np.random.default_rng(3)
+    h, W, t, c = r.standard_normal((6, 4)), r.standard_normal((5, 4)), r.integers(0, 5, 6), r.standard_normal(6)
+    t[2] = -100
+    dh, dw, _, _ = O.linear_logp_grad(h, W, t, c, 0.7, batch)
+    assert np.abs(dh - numeric(lambda y: (c * O.linear_logp(y, W, t, 0.7)).sum(), h)).max() < TOL
+    for b in range(batch):
+        s = slice(b * 6 // batch, (b + 1) * 6 // batch)
+        assert np.abs(dw[b] - numeric(lambda y: (c[s] * O.linear_logp(h[s], y, t[s], 0.7)).sum(), W)).max() < TOL
+
+
+def test_linear_logp_is_token_logp_of_the_product():
+    r = np.random.default_rng(4)
+    h, W, t = r.standard_normal((6, 4)), r.standard_normal((5, 4)), np.array([0, 4, 5, -1, 2, 2])
+    assert np.allclose(O.linear_logp(h, W, t, 1.3), O.token_logp(h @ W.T, t, 1.3), atol=1e-14)
+
+
+def test_balance_gradient_against_differences():
+    """The counts are held: they are steps in the logits."""
+    r = np.random.default_rng(5)
+    x, ids = r.standard_normal((7, 5)), r.integers(-1, 6, (7, 2))
+    ids[3] = -1
+    loss, counts, probs, d = O.balance_loss(x, ids, 0.3)
+    assert np.abs(d - numeric(lambda y: O.balance_loss(y, ids, 0.3)[0], x)).max() < TOL
+    assert counts.sum() == ((ids >= 0) & (ids < 5)).sum() and abs(probs.sum() - 1) < 1e-12 and not d[3].any()
+
+
+def test_balance_loss_of_even_shares_is_its_coefficient():
+    ids = np.arange(12).reshape(6, 2) % 4
+    assert abs(O.balance_loss(np.zeros((6, 4)), ids, 0.7)[0] - 0.7) < 1e-15
+    assert O.balance_loss(np.zeros((2, 4)), -np.ones((2, 1), int), 0.7)[0] == 0
+
+
+def test_dropout_keeps_its_share_and_its_mean():
+    n, p = 1 << 18, 0.3
+    out, kept = O.dropout(np.ones(n), p, 5, 9, 2)
+    sd = np.sqrt(p * (1 - p) / n)
+    assert abs(kept.mean() - (1 - p)) < 5 * sd and abs(out.mean() - 1) < 5 * sd / (1 - p)
+    assert abs(np.corrcoef(kept[:-1], kept[1:])[0, 1]) < 5 / np.sqrt(n)
+    for other in ((5, 10, 2), (5, 9, 3), (6, 9, 2)):  # another step, site or seed: independent masks
+        assert abs(np.corrcoef(kept, O.dropout(np.ones(n), p, *other)[1])[0, 1]) < 5 / np.sqrt(n)
+    assert not O.dropout(np.full(9, np.nan), 1.0, 0, 0, 0)[0].any()

@@ -142,3 +142,99 @@ def test_a_device_that_does_not_exist_is_refused(device):
     nw = L.sketch_embed_grad_work_bytes(2, 3, 8)
     assert L.sketch_embed_grad(P, 0, 8, P, 1, 2, 3, 4, 8, 1.0, P, 0, 0, P, nw, device, None) == -1
     assert b"device" in L.sketch_last_error()
+
+
+def linear(**kw):
+    d = dict(hidden=P, weight=P, targets=P, rows=4, vocab=8, width=16, ld_hidden=16, ld_weight=16, scale=1.0, dtype=0, index=1,
+             device=0)
+    d.update(kw)
+    return ctypes.byref(_lib.Linear(*[d[k] for k, _ in _lib.Linear._fields_]))
+
+
+BAD_LINEAR = [(dict(dtype=2), -2), (dict(index=7), -2), (dict(rows=-1), -1), (dict(vocab=0), -1), (dict(width=0), -1),
+              (dict(ld_hidden=15), -1), (dict(ld_weight=15), -1), (dict(scale=0.0), -1), (dict(scale=float("nan")), -1),
+              (dict(scale=3e38), -1), (dict(rows=(1 << 20) + 1), -5), (dict(vocab=(1 << 22) + 1), -5),
+              (dict(width=(1 << 16) + 1, ld_hidden=1 << 17, ld_weight=1 << 17), -5), (dict(hidden=None), -1),
+              (dict(weight=None), -1), (dict(targets=None), -1)]
+
+
+@pytest.mark.parametrize("kw,code", BAD_LINEAR)
+def test_linear_refuses_bad_inputs(kw, code):
+    L = _lib.load()
+    x = linear(**kw)
+    assert L.sketch_linear_logp(x, P, P, P, 1 << 50, None) == code
+    assert L.sketch_linear_logp_grad(x, 1, P, P, P, 16, P, 0, 0, P, 1 << 50, None) == code
+    assert L.sketch_linear_logp_work_bytes(x) == 0 and L.sketch_linear_logp_grad_work_bytes(x, 1, 1, 1) == 0
+
+
+def test_linear_refuses_bad_arguments():
+    L = _lib.load()
+    x = linear()
+    nf, ng = L.sketch_linear_logp_work_bytes(x), L.sketch_linear_logp_grad_work_bytes(x, 2, 1, 1)
+    assert nf > 0 and ng > 0
+    assert L.sketch_linear_logp(None, P, P, P, nf, None) == -1
+    assert L.sketch_linear_logp(x, None, P, P, nf, None) == -1
+    assert L.sketch_linear_logp(x, P, P, None, nf, None) == -1
+    assert L.sketch_linear_logp(x, P, P, P, nf - 1, None) == -1
+    assert L.sketch_linear_logp(linear(rows=0, hidden=None, targets=None), None, None, None, 0, None) == 0
+
+    def grad(x=x, batch=2, stats=P, dlogp=P, dh=P, ld=16, dw=P, dt=0, work=P, nw=ng):
+        return L.sketch_linear_logp_grad(x, batch, stats, dlogp, dh, ld, dw, dt, 0, work, nw, None)
+
+    for kw, code in ((dict(batch=0), -1), (dict(batch=3), -1), (dict(stats=None), -1), (dict(dlogp=None), -1),
+                     (dict(dh=None, dw=None), -1), (dict(ld=15), -1), (dict(dt=2), -2), (dict(dt=1), -2),
+                     (dict(work=None), -1), (dict(nw=ng - 1), -1), (dict(x=linear(rows=1 << 15), batch=1 << 15), -5)):
+        assert grad(**kw) == code, kw
+
+
+def test_dropout_refuses_bad_arguments():
+    L = _lib.load()
+
+    def drop(x=P, dt=0, rows=2, width=8, ld=8, res=None, ldr=0, out=P, ldo=8, p=0.1, step=0, site=0, device=0):
+        return L.sketch_dropout(x, dt, rows, width, ld, res, ldr, out, ldo, p, 0, step, None, site, device, None)
+
+    for kw, code in ((dict(x=None), -1), (dict(out=None), -1), (dict(dt=2), -2), (dict(rows=-1), -1), (dict(width=0), -1),
+                     (dict(ld=7), -1), (dict(ldo=7), -1), (dict(res=P + 64, ldr=7), -1), (dict(p=-0.1), -1),
+                     (dict(p=1.1), -1), (dict(p=float("nan")), -1), (dict(step=-1), -1), (dict(step=1 << 32), -1),
+                     (dict(site=-1), -1), (dict(site=1 << 32), -1), (dict(ld=9), -1),
+                     (dict(res=P, ldr=9, x=P + 64), -1), (dict(rows=1 << 30, width=64, ld=64, ldo=64), -5),
+                     (dict(device=99), -1), (dict(device=-1), -1)):
+        assert drop(**kw) == code, kw
+    assert drop(rows=0, x=None, out=None) == 0
+
+
+def test_balance_refuses_bad_arguments():
+    L = _lib.load()
+
+    def balance(x=P, dt=0, tokens=2, experts=8, ld=8, ids=P, index=1, k=2, coef=1.0, loss=P, counts=P, probs=P, d=P, ldo=8,
+                work=P, nw=None, device=0):
+        nw = L.sketch_balance_work_bytes(experts) if nw is None else nw
+        return L.sketch_balance_loss(x, dt, tokens, experts, ld, ids, index, k, coef, loss, counts, probs, d, ldo, work, nw,
+                                     device, None)
+
+    for kw, code in ((dict(x=None), -1), (dict(ids=None), -1), (dict(dt=2), -2), (dict(index=2), -2), (dict(tokens=-1), -1),
+                     (dict(experts=0), -1), (dict(k=0), -1), (dict(ld=7), -1), (dict(ldo=7), -1),
+                     (dict(coef=float("inf")), -1), (dict(loss=None), -1), (dict(counts=None), -1), (dict(probs=None), -1),
+                     (dict(work=None), -1), (dict(nw=0), -1), (dict(ld=9), -1),
+                     (dict(experts=2049, ld=2049, ldo=2049), -5), (dict(k=1025), -5), (dict(tokens=1 << 31), -5),
+                     (dict(tokens=1 << 30, k=2), -5), (dict(device=99), -1), (dict(device=-1), -1)):
+        assert balance(**kw) == code, kw
+    assert L.sketch_balance_work_bytes(0) == 0
+
+
+def test_binding_refuses_host_tensors_of_the_later_operators():
+    x, t, v = torch.zeros(2, 8), torch.zeros(2, dtype=torch.int64), torch.zeros(2)
+    for call in (lambda: fw.linear_logp(x, x, t), lambda: fw.linear_logp_grad(x, x, t, torch.zeros(2, 2), v),
+                 lambda: fw.dropout(x, 0.1, 0, 0), lambda: fw.dropout_grad(x, 0.1, 0, 0),
+                 lambda: fw.balance_loss(x, t[:, None])):
+        with pytest.raises(ValueError):
+            call()
+
+
+@pytest.mark.parametrize("device", [-1, 99])
+def test_linear_refuses_a_device_that_does_not_exist(device):
+    L = _lib.load()
+    x = linear(device=device)
+    assert L.sketch_linear_logp(x, P, P, P, 1 << 50, None) == -1
+    assert L.sketch_linear_logp_grad(x, 1, P, P, P, 16, P, 0, 0, P, 1 << 50, None) == -1
+    assert b"device" in L.sketch_last_error()
