@@ -255,19 +255,29 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
   a.prm[n] = p;
 }
 
-// The largest finite |W|, over all rows.
+// The largest finite |W|, over all rows.  One atomic a workgroup, and only where it can change something: 50257 x 768 took
+// 68 us with one a wave, 40 us so (3.9 TB/s).
 __global__ __launch_bounds__(256) void k_absmax(const float *w, int64_t ld, int rows, int width, Meta *meta) {
+  __shared__ float lds[4];
   float big = 0.0f;
   const int lane = threadIdx.x & 63;
-  for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4)
-    for (int k = lane * 4; k < width; k += 256) {
-      float f[4];
-      row_part<4>(w + (int64_t)r * ld, k, width, f);
+  auto take = [&](const float *f) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) big = fmaxf(big, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.0f);
+    for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.0f);
+  };
+  for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
+    const float *row = w + (int64_t)r * ld;
+    for (int k = lane * 8; k < width; k += 1024) {
+      float f[8], g[8];
+      row_part<8>(row, k, width, f);
+      row_part<8>(row, k + 512, width, g);
+      take(f);
+      take(g);
     }
-  big = wave_all(big, OpMax());
-  if (lane == 0) atomicMax(&meta->wbits, (int)__float_as_uint(big));
+  }
+  big = block_all<4>(big, OpMax(), lds);
+  if (threadIdx.x == 0 && (int)__float_as_uint(big) > __hip_atomic_load(&meta->wbits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
+    atomicMax(&meta->wbits, (int)__float_as_uint(big));
 }
 
 struct Prep {
@@ -579,6 +589,125 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
 #endif
 }
 
+// --- few rows -----------------------------------------------------------------------------------------------
+constexpr int kFew = 16;        // rows up to which W goes straight from memory into the matrix cores, once
+constexpr int kFewUnit = 64;    // vocabulary rows of a workgroup
+
+__device__ __forceinline__ int target_of(const void *targets, int index, int64_t t, int vocab) {
+  const int64_t v = index == SK_I64 ? ((const int64_t *)targets)[t] : ((const int32_t *)targets)[t];
+  return v >= 0 && v < vocab ? (int)v : -1;
+}
+
+struct Few {
+  const void *hidden, *weight, *targets;
+  int64_t ld_hidden, ld_weight;
+  int rows, vocab, width, index;
+  float scale;
+  float2 *part;  // [kFew][units]
+  float *xt;     // [kFew]
+  int units;
+  float *logp;
+  float2 *stats;
+};
+
+// Logits of up to 16 rows by 16 entries of the vocabulary a wave.  Lane l holds row l % 16 of both operands; its eight
+// (fp32: four) columns from 8 (l / 16) on are one operand of v_mfma_f32_16x16x32_bf16 (element i of each lane one of
+// v_mfma_f32_16x16x4_f32, in which fp32 stays fp32).  Bound by reading W: SKINNY.
+template <typename T>
+__global__ __launch_bounds__(256) void k_few(Few a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int N = Vec<T>::N, K = 4 * N, U = 4;  // columns of a lane, of a step, steps whose loads are under way together
+  __shared__ float2 lds[4][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
+  const int v0 = blockIdx.x * kFewUnit + wave * 16, v = v0 + r;
+  const int target = r < a.rows ? target_of(a.targets, a.index, r, a.vocab) : -1;
+  const T *w = (const T *)a.weight + (int64_t)(v < a.vocab ? v : a.vocab - 1) * a.ld_weight;
+  const T *h = (const T *)a.hidden + (int64_t)(target >= 0 ? r : 0) * a.ld_hidden;
+  const int hw = target >= 0 ? a.width : 0;  // masked rows are not read
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int k0 = q * N; k0 - q * N < a.width; k0 += K * U) {
+    u32x4 fw[U], fh[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * K;
+      auto part = [&](const T *row, int width) {
+        if (k + N <= width) return Vec<T>::load(row + k);
+        float f[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = k + i < width ? to_f32(row[k + i]) : 0.0f;
+        return Vec<T>::pack(f);
+      };
+      fw[u] = part(w, a.width);
+      fh[u] = part(h, hw);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if constexpr (sizeof(T) == 2) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[u]), __builtin_bit_cast(bf16x8, fh[u]), acc, 0,
+                                                      0, 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fw[u][i]), __uint_as_float(fh[u][i]), acc, 0, 0, 0);
+      }
+    }
+  }
+  // this lane: entries v0 + 4 q + e of row r
+  const float k2 = power_of(a.scale).k;
+  float m = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int u = v0 + q * 4 + e;
+    if (u >= a.vocab) acc[e] = -INFINITY;
+    if (u == target) a.xt[r] = acc[e];
+    m = fmaxf(m, acc[e]);
+  }
+  m = fmaxf(m, __shfl_xor(m, 16, 64));
+  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  if (q == 0) lds[wave][r].x = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(lds[0][r].x, lds[1][r].x), fmaxf(lds[2][r].x, lds[3][r].x));
+  const float base = m == -INFINITY ? 0.0f : m;
+  float z = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) z += __builtin_amdgcn_exp2f((acc[e] - base) * k2);
+  z += __shfl_xor(z, 16, 64);
+  z += __shfl_xor(z, 32, 64);
+  if (q == 0) lds[wave][r].y = z;
+  __syncthreads();
+  if (threadIdx.x < (unsigned)a.rows)
+    a.part[threadIdx.x * (int64_t)a.units + blockIdx.x] = float2{m, lds[0][r].y + lds[1][r].y + lds[2][r].y + lds[3][r].y};
+#endif
+}
+
+// A workgroup a row: its (m, z) and log-probability from the units'.
+__global__ __launch_bounds__(512) void k_few_join(Few a) {
+  __shared__ float big[8];
+  __shared__ double sum[8];
+  const int t = blockIdx.x, target = target_of(a.targets, a.index, t, a.vocab);
+  Stats s{0.0f, 0.0f};
+  float lp = 0.0f;
+  if (target >= 0) {  // the same for all threads
+    const float2 *part = a.part + (int64_t)t * a.units;
+    const float k2 = power_of(a.scale).k;
+    float m = -INFINITY;
+    for (int u = threadIdx.x; u < a.units; u += 512) m = fmaxf(m, part[u].x);
+    m = block_all<8>(m, OpMax(), big);
+    if (m == -INFINITY) m = 0.0f;
+    double z = 0.0;
+    for (int u = threadIdx.x; u < a.units; u += 512) {
+      const float2 p = part[u];
+      if (p.y != 0.0f) z += (double)(p.y * __builtin_amdgcn_exp2f((p.x - m) * k2));
+    }
+    s = Stats{m, (float)block_all<8>(z, OpAdd(), sum)};
+    lp = logp_of(a.xt[t], s, a.scale);
+  }
+  if (threadIdx.x == 0) {
+    a.logp[t] = lp;
+    if (a.stats) a.stats[t] = float2{s.m, s.z};
+  }
+}
+
 // (m, z) of the listed rows from the units' and their log-probabilities; 64 rows a workgroup, whose waves share the units.
 __global__ __launch_bounds__(1024) void k_join(const Meta *meta, const int *list, const float2 *part, const float *xt,
                                                int64_t tcap, int units, float scale, float *logp, float2 *stats) {
@@ -755,7 +884,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   int64_t most = x->vocab;
   if (grad) most = std::min(most, ((int64_t)1 << 26) / (p.tcap * p.planes));
   if (grad || p.copy) most = std::min(most, ((int64_t)1 << 27) / (p.kp * p.planes));
-  most = std::max<int64_t>(most / 256 * 256, 256);
+  if (most < x->vocab) most = std::max<int64_t>(most / 256 * 256, 256);
   const int64_t pieces = (x->vocab + most - 1) / most;
   p.piece = up((x->vocab + pieces - 1) / pieces, 256);
   p.units = (x->vocab + kTileM - 1) / kTileM + 1;
@@ -833,7 +962,7 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
                           ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<int>(work, p.seg), ptr<int>(work, p.cnt), meta, logp,
                           (float2 *)stats});
   if (p.f16)
-    hipLaunchKernelGGL(k_absmax, dim3((unsigned)std::min<int64_t>(1024, (x->vocab + 3) / 4)), dim3(256), 0, st,
+    hipLaunchKernelGGL(k_absmax, dim3((unsigned)std::min<int64_t>(2048, (x->vocab + 3) / 4)), dim3(256), 0, st,
                        (const float *)x->weight, x->ld_weight, (int)x->vocab, (int)x->width, meta);
   const Gather g{x->hidden, x->ld_hidden, (int)x->width, (int)p.kp, list, meta, ptr<uint16_t>(work, p.hc), p.tcap * p.kp,
                  ptr<int>(work, p.eh), (const float2 *)stats_in, dlogp, x->scale,
@@ -938,6 +1067,17 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
   TrainGuard guard(x->device);
   if (!guard.ok) return train_no_device();
   hipStream_t st = (hipStream_t)stream;
+  if (x->rows <= kFew) {
+    const int units = (int)((x->vocab + kFewUnit - 1) / kFewUnit);
+    const Few a{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)x->width,
+                (int)x->index, x->scale, ptr<float2>(work, p.part), ptr<float>(work, p.xt), units, logp, (float2 *)stats};
+    if (p.f16)
+      hipLaunchKernelGGL(k_few<float>, dim3(units), dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL(k_few<bf16>, dim3(units), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_few_join, dim3((unsigned)x->rows), dim3(512), 0, st, a);
+    return train_launched();
+  }
   begin(x, p, nullptr, nullptr, logp, stats, work, st);
   for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
     const int64_t valid = std::min(p.piece, x->vocab - v0);
