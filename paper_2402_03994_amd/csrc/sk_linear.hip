@@ -39,7 +39,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStep = 64;   // K a stage
 constexpr int kTop = 13;    // split operands lie below 2^(kTop + 1)
-constexpr int kTileM = 128; // vocabulary rows that one entry of the forward's partial statistics covers
 
 // What the kernels of a call share in its workspace.
 struct Meta {
@@ -365,16 +364,22 @@ struct Operand {
 // 64 of K go straight from memory to LDS, 16 bytes a lane, two stages deep: the loads of the next one are issued
 // behind the barrier that frees its buffer and have the products of a whole stage (2048 cycles of a CU's matrix cores
 // for 256 x 256) to arrive.  A row of a stage is 128 bytes, its eight 16-byte chunks exchanged by (row / 2) & 7, so that
-// the 32 rows that a wave reads at a time lie in different banks (exchanged by row & 7: 8192^3 bf16 957 us, 887 us so).
-// 8192^3: 256 x 256 1240 TFLOP/s, 128 x 128 (two workgroups a CU) 1108; the library's 1290.
+// the 32 rows that a wave reads at a time lie in different banks (exchanged by row & 7: 8192^3 bf16, 256 x 256, 957 us, 887
+// us so).  Two workgroups share a CU, so that one's epilogue lies beside the other's products.  Alone (8192^3, and 16384 x
+// 2560 x 768, bf16): 128 x 192 1150 and 803 TFLOP/s, 128 x 128 1108 and 773, one 256 x 256 a CU 1240 and 729, the
+// library's 1290 and 817.  In the operators (4096 x 50257 x 768 and 8192 x 128256 x 4096): gradients 819 us and 15.5 ms with
+// 128 x 192, 891 us and 17.8 ms with 128 x 128, 1120 us and 15.9 ms with 256 x 256; log-probabilities 225 us and 4.47 ms,
+// 243 us and 5.0 ms, 226 us and 4.5 ms.  Up to 1024 rows the smaller tiles fill the chip better (gradients of 200 x 50257 x
+// 768: 134 us, 146 with the larger ones; 1000: 301 and 299).
 template <int BM_, int BN_, int WM_, int WN_>
 struct Tiling {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM * WN, TH = NW * 64;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   static constexpr int LDS = 2 * (BM + BN) * kStep * 2;
 };
-using Big = Tiling<256, 256, 2, 4>;
+using Large = Tiling<128, 192, 2, 2>;
 using Small = Tiling<128, 128, 2, 2>;
+constexpr int64_t kSmallRows = 1024;  // rows up to which the smaller tiles are taken
 
 #if defined(__HIP_DEVICE_COMPILE__)
 template <typename C, bool F16>
@@ -491,7 +496,7 @@ struct Logit {
   const int *tgt, *eh;
   float scale;
   // forward
-  float2 *part;  // [vocabulary / 128][tcap]
+  float2 *part;  // [vocabulary / 64][tcap]
   float *xt;
   int64_t tcap;
   // gradient
@@ -533,18 +538,8 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
             g[q] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
             if (m == tv) g[q] += p.one;
             if (p.one == 0.0f || m0 + m >= a.valid) g[q] = 0.0f;
-          }
-          if (!in) continue;
-          const int64_t m = m0 + c.row(i, e);
-#pragma unroll
-          for (int plane = 0; plane < (F16 ? 2 : 1); ++plane) {
-            const uint32_t lo = two<F16>(g[0], g[1], plane), hi = two<F16>(g[2], g[3], plane);
-            *(u32x2 *)(a.g + plane * a.gplane + n * a.piece + m) = u32x2{lo, hi};
-            uint16_t *gt = a.gt + plane * a.gplane + m * a.tcap + n;
-            gt[0] = (uint16_t)lo;
-            gt[a.tcap] = (uint16_t)(lo >> 16);
-            gt[2 * a.tcap] = (uint16_t)hi;
-            gt[3 * a.tcap] = (uint16_t)(hi >> 16);
+            // both halves of a split number, or the bf16's bits
+            c.acc[i][j][e + q] = __uint_as_float(F16 ? split(g[q]) : bf16_bits(g[q]));
           }
         }
     } else {
@@ -584,6 +579,45 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
               if (c.row(i, e) - c.wm * (C::BM / C::WM) == tv) a.xt[n] = c.acc[i][j][e];
         }
       }
+    }
+  }
+  if (!GRAD) return;
+  // G's rows leave through LDS, in whole lines (chunks of 16 bytes exchanged by the row, so that the lanes of a write meet
+  // different banks); its transpose's as they lie, 32 tokens a lane's row.
+#pragma unroll
+  for (int plane = 0; plane < (F16 ? 2 : 1); ++plane) {
+    constexpr int CH = C::BM / 8;
+    auto pair = [&](int i, int j, int e) {
+      return __builtin_amdgcn_perm(__float_as_uint(c.acc[i][j][e + 1]), __float_as_uint(c.acc[i][j][e]),
+                                   plane ? 0x07060302 : 0x05040100);
+    };
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+      const int n = c.col(j);
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const int m = c.row(i, e);
+          const u32x2 v{pair(i, j, e), pair(i, j, e + 2)};
+          *(u32x2 *)(lds + n * (C::BM * 2) + ((m >> 3) ^ (n & (CH - 1))) * 16 + (m & 4) * 2) = v;
+          if (n0 + n < np) {
+            uint16_t *gt = a.gt + plane * a.gplane + (int64_t)(m0 + m) * a.tcap + n0 + n;
+            gt[0] = (uint16_t)v[0];
+            gt[a.tcap] = (uint16_t)(v[0] >> 16);
+            gt[2 * a.tcap] = (uint16_t)v[1];
+            gt[3 * a.tcap] = (uint16_t)(v[1] >> 16);
+          }
+        }
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int k = threadIdx.x; k < C::BN * CH; k += C::TH) {
+      const int n = k / CH, m = k % CH;
+      if (n0 + n < np)
+        *(u32x4 *)(a.g + plane * a.gplane + (int64_t)(n0 + n) * a.piece + m0 + m * 8) =
+            *(const u32x4 *)(lds + n * (C::BM * 2) + (m ^ (n & (CH - 1))) * 16);
     }
   }
 #endif
@@ -734,57 +768,85 @@ __global__ __launch_bounds__(1024) void k_join(const Meta *meta, const int *list
   if (stats) stats[t] = s;
 }
 
-struct DHidden {
-  Operand wt, g;
-  int width, steps, per, splits;  // stages of the piece, of a split
-  bool first;
+// What a piece adds to dH, and its rows of dW.
+struct Back {
+  int width;
   const Meta *meta;
-  const float *rowf;
-  float *acc;  // [splits][tcap][kp]
+  const int *seg;
   int64_t tcap;
+  // dH: acc[split] (+)= G W^T^T
+  Operand g, wt;
+  int steps, per, splits;  // stages of the piece, of a split
+  int blocks;              // workgroups at most, a multiple of 8 (0: not wanted)
+  bool first;
+  float *acc;  // [splits][tcap][kp]
   int kp;
+  // dW
+  Operand gt, ht;
+  int valid, b0;  // rows of the piece, the launch's first example
+  void *out;      // rows from the piece's first on
+  int64_t vocab;  // rows from example to example
+  bool accumulate;
 };
 
-// acc[split] (+)= G W of the piece; accumulator rows are features, so that a lane has four of a token
-template <typename C, bool F16>
-__global__ __launch_bounds__(C::TH, 2) void k_dhidden(DHidden a) {
+// Both products of a piece in one launch: neither fills a whole number of rounds of the chip, and the longer ones (dH, K
+// is the piece) come first.  Accumulator rows are tokens (vocabulary entries), columns features, so that a store is 32
+// features of a row.
+template <typename C, bool F16, typename TO>
+__global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
-  const int np = a.meta->np, mt = (a.width + C::BM - 1) / C::BM, nt = (np + C::BN - 1) / C::BN;
-  const int tiles = mt * nt;
-  if ((int)blockIdx.x >= tiles * a.splits) return;
-  const int s = blockIdx.x / tiles;
+  const bool hidden = (int)blockIdx.x < a.blocks;
+  const int np = a.meta->np, rows = hidden ? np : a.valid, mt = (rows + C::BM - 1) / C::BM, nt = (a.width + C::BN - 1) / C::BN;
+  const int tiles = mt * nt, b = hidden ? blockIdx.x : blockIdx.x - a.blocks;
+  if (hidden && b >= tiles * a.splits) return;
+  const int part = b / tiles;  // split, or example
   int tm, tn;
-  tile_of(blockIdx.x - s * tiles, mt, nt, tm, tn);
-  const int m0 = tm * C::BM, n0 = tn * C::BN, k0 = s * a.per;
+  tile_of(b - part * tiles, mt, nt, tm, tn);
+  const int m0 = tm * C::BM, n0 = tn * C::BN;
+  const int k0 = hidden ? part * a.per * kStep : a.seg[a.b0 + part];
+  const int steps = hidden ? max(0, min(a.per, a.steps - part * a.per)) : (a.seg[a.b0 + part + 1] - k0) / kStep;
   Core<C, F16> c;
-  c.run(lds, at_row(a.wt, m0, (int64_t)k0 * kStep), at_row(a.g, n0, (int64_t)k0 * kStep), a.width - m0, np - n0,
-        max(0, min(a.per, a.steps - k0)));
+  c.run(lds, at_row(hidden ? a.g : a.gt, m0, k0), at_row(hidden ? a.wt : a.ht, n0, k0), rows - m0, a.width - n0, steps);
+  if (hidden) {
+    float *to = a.acc + (part * a.tcap + m0) * a.kp + n0;
 #pragma unroll
-  for (int j = 0; j < C::TN; ++j) {
-    const int n = n0 + c.col(j);
-    if (n >= np) continue;
-    const float f = F16 ? a.rowf[n] : 1.0f;
-    float *to = a.acc + (s * a.tcap + n) * a.kp + m0;
+    for (int j = 0; j < C::TN; ++j) {
+      if (n0 + c.col(j) >= a.kp) continue;
 #pragma unroll
-    for (int i = 0; i < C::TM; ++i)
+      for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int m = c.row(i, e);
-        if (m0 + m >= a.kp) continue;
-        f32x4 v;
+        for (int e = 0; e < 16; ++e) {
+          const int m = c.row(i, e);
+          if (m0 + m >= np) continue;
+          float *p = to + (int64_t)m * a.kp + c.col(j);
+          *p = a.first ? c.acc[i][j][e] : *p + c.acc[i][j][e];
+        }
+    }
+  } else {
+    const float f = F16 && steps ? ldexpf(1.0f, max(a.meta->ec, -300) - 2 * kTop) : 1.0f;
+    TO *to = (TO *)a.out + ((a.b0 + part) * a.vocab + m0) * a.width + n0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = F16 ? c.acc[i][j][e + q] * f : c.acc[i][j][e + q];
-        if (!a.first) v += *(f32x4 *)(to + m);
-        *(f32x4 *)(to + m) = v;
-      }
+    for (int j = 0; j < C::TN; ++j) {
+      if (n0 + c.col(j) >= a.width) continue;
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int m = c.row(i, e);
+          if (m0 + m >= a.valid) continue;
+          TO *p = to + (int64_t)m * a.width + c.col(j);
+          const float v = F16 ? c.acc[i][j][e] * f : c.acc[i][j][e];
+          *p = from_f32<TO>(a.accumulate ? v + to_f32(*p) : v);
+        }
+    }
   }
 #endif
 }
 
 // dH: the splits' sums in order; zeros for masked rows
 template <typename T>
-__global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float *acc, int64_t tcap, int kp, int splits, int rows,
+__global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float *rowf, const float *acc, int64_t tcap, int kp, int splits, int rows,
                                                      int width, T *out, int64_t ld) {
   const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (t >= rows) return;
@@ -802,6 +864,10 @@ __global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float
           for (int q = 0; q < 4; ++q) f[i + q] += v[q];
         }
       }
+      if (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= rowf[p];
+      }
     }
     if (k + 8 <= width) {
 #pragma unroll
@@ -812,59 +878,12 @@ __global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float
   }
 }
 
-struct DWeight {
-  Operand ht, gt;
-  int width, valid;
-  int b0, batch;  // examples of this launch
-  const int *seg;
-  const Meta *meta;
-  void *out;       // rows from the piece's first on
-  int64_t vocab;   // rows from example to example
-  bool accumulate;
-};
-
-// dW rows of the piece, per example; accumulator rows are features, so that a lane has four of a row of dW
-template <typename C, bool F16, typename TO>
-__global__ __launch_bounds__(C::TH, 2) void k_dweight(DWeight a) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
-  const int mt = (a.width + C::BM - 1) / C::BM, nt = (a.valid + C::BN - 1) / C::BN, tiles = mt * nt;
-  const int bi = blockIdx.x / tiles, b = a.b0 + bi;
-  int tm, tn;
-  tile_of(blockIdx.x - bi * tiles, mt, nt, tm, tn);
-  const int m0 = tm * C::BM, n0 = tn * C::BN, k0 = a.seg[b], k1 = a.seg[b + 1];
-  Core<C, F16> c;
-  c.run(lds, at_row(a.ht, m0, k0), at_row(a.gt, n0, k0), a.width - m0, a.valid - n0, (k1 - k0) / kStep);
-  const float f = F16 && k1 > k0 ? ldexpf(1.0f, max(a.meta->ec, -300) - 2 * kTop) : 1.0f;
-  TO *out = (TO *)a.out + b * a.vocab * a.width;
-#pragma unroll
-  for (int j = 0; j < C::TN; ++j) {
-    const int n = n0 + c.col(j);
-    if (n >= a.valid) continue;
-    TO *to = out + (int64_t)n * a.width + m0;
-#pragma unroll
-    for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int m = c.row(i, e);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (m0 + m + q >= a.width) break;
-          float v = F16 ? c.acc[i][j][e + q] * f : c.acc[i][j][e + q];
-          if (a.accumulate) v += to_f32(to[m + q]);
-          to[m + q] = from_f32<TO>(v);
-        }
-      }
-  }
-#endif
-}
-
 // --- host ---------------------------------------------------------------------------------------------------
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // How a call is cut, and where its parts lie in the workspace.
 struct Plan {
-  bool f16, copy, big;
+  bool f16, copy, large;
   int64_t batch, n, tcap, kp, piece, units, splits, planes;
   int64_t list, pos, tgt, seg, cnt, meta, hc, eh, part, xt, prm, rowf, cs, ht, wc, wt, g, gt, acc, bytes;
 };
@@ -880,19 +899,24 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.kp = up(x->width, kStep);
   // rows that 16-byte loads in whole stages read as they lie
   p.copy = p.f16 || x->width % kStep || x->ld_weight % 8 || (uintptr_t)x->weight % 16 || x->ld_weight > (1 << 20);
-  // a piece: G and its transpose within 256 MB, a copy of W within 256 MB
+  // a piece: G and its transpose in 512 MB (4096 x 50257 x 768 bf16 one launch more for each halving: 779, 819, 895 us with
+  // 1 GB, 512 and 256 MB), a copy of W in 256 MB
   int64_t most = x->vocab;
-  if (grad) most = std::min(most, ((int64_t)1 << 26) / (p.tcap * p.planes));
+  if (grad) most = std::min(most, ((int64_t)1 << 27) / (p.tcap * p.planes));
   if (grad || p.copy) most = std::min(most, ((int64_t)1 << 27) / (p.kp * p.planes));
   if (most < x->vocab) most = std::max<int64_t>(most / 256 * 256, 256);
   const int64_t pieces = (x->vocab + most - 1) / most;
   p.piece = up((x->vocab + pieces - 1) / pieces, 256);
-  p.units = (x->vocab + kTileM - 1) / kTileM + 1;
-  p.big = false;
+  p.units = up(x->vocab, 128) / 64;
+  p.large = x->rows > kSmallRows;
   p.splits = 1;
   if (grad) {
-    const int64_t tiles = (up(x->width, 128) / 128) * (up(x->rows, 128) / 128);
-    p.splits = std::max<int64_t>(1, std::min(512 / std::max<int64_t>(tiles, 1), p.piece / 512));
+    // dH has few tiles with all of the piece to sum up, dW many with the rows: a part of a dH tile takes half of what each
+    // of the chip's 512 places has to do in all (4096 x 50257 x 768 bf16: 1271, 902, 819, 868, 979 us with 1, 2, 4, 8, 16
+    // parts; 17 x 50257 x 768: 590, 203, 119, 123, 144 us with 1, 4, 16, 32, 64)
+    const int64_t bn = p.large ? Large::BN : Small::BN, nt = up(x->width, bn) / bn, steps = p.piece / kStep;
+    const int64_t all = up(p.tcap, 128) / 128 * nt * steps + batch * (p.piece / 128) * nt * (up(p.n, kStep) / kStep);
+    p.splits = std::max<int64_t>(1, std::min<int64_t>({(768 * steps + all / 2) / all, 32, steps / 4}));
   }
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -1015,38 +1039,44 @@ Logit logit_of(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, Ope
 }
 
 template <typename C, bool GRAD>
-void run_logits(const Plan &p, const Logit &a, int64_t rows, hipStream_t st) {
+void launch_logits(const Plan &p, const Logit &a, int64_t rows, hipStream_t st) {
   const unsigned blocks = (unsigned)(((a.valid + C::BM - 1) / C::BM) * ((rows + C::BN - 1) / C::BN));
   if (p.f16)
     hipLaunchKernelGGL((k_logits<C, true, GRAD>), dim3(blocks), dim3(C::TH), 0, st, a);
   else
     hipLaunchKernelGGL((k_logits<C, false, GRAD>), dim3(blocks), dim3(C::TH), 0, st, a);
 }
-
-template <typename C>
-void run_dhidden(const Plan &p, const DHidden &a, hipStream_t st) {
-  const unsigned blocks = (unsigned)(((a.width + C::BM - 1) / C::BM) * (p.tcap / C::BN) * a.splits);
-  if (p.f16)
-    hipLaunchKernelGGL((k_dhidden<C, true>), dim3(blocks), dim3(C::TH), 0, st, a);
+template <bool GRAD>
+void run_logits(const Plan &p, const Logit &a, int64_t rows, hipStream_t st) {
+  if (p.large)
+    launch_logits<Large, GRAD>(p, a, rows, st);
   else
-    hipLaunchKernelGGL((k_dhidden<C, false>), dim3(blocks), dim3(C::TH), 0, st, a);
+    launch_logits<Small, GRAD>(p, a, rows, st);
 }
 
 template <typename C>
-void run_dweight(const Plan &p, DWeight a, sk_dtype odt, hipStream_t st) {
-  const int64_t tiles = (int64_t)((a.width + C::BM - 1) / C::BM) * ((a.valid + C::BN - 1) / C::BN);
-  const int64_t most = std::max<int64_t>(1, (1 << 22) / tiles);
+void launch_back(const Plan &p, Back a, bool dhidden, bool dweight, sk_dtype odt, hipStream_t st) {
+  const int64_t nt = (a.width + C::BN - 1) / C::BN, tiles = (a.valid + C::BM - 1) / C::BM * nt;
+  a.blocks = dhidden ? (int)up((p.tcap + C::BM - 1) / C::BM * nt * a.splits, 8) : 0;
+  const int64_t most = std::max<int64_t>(1, (1 << 22) / tiles);  // examples of a launch: grids below 2^32 threads
   for (int64_t b = 0; b < p.batch; b += most) {
     a.b0 = (int)b;
-    a.batch = (int)std::min(most, p.batch - b);
-    const unsigned blocks = (unsigned)(tiles * a.batch);
+    const unsigned blocks = (unsigned)(a.blocks + (dweight ? tiles * std::min(most, p.batch - b) : 0));
     if (p.f16)
-      hipLaunchKernelGGL((k_dweight<C, true, float>), dim3(blocks), dim3(C::TH), 0, st, a);
+      hipLaunchKernelGGL((k_back<C, true, float>), dim3(blocks), dim3(C::TH), 0, st, a);
     else if (odt == SK_F32)
-      hipLaunchKernelGGL((k_dweight<C, false, float>), dim3(blocks), dim3(C::TH), 0, st, a);
+      hipLaunchKernelGGL((k_back<C, false, float>), dim3(blocks), dim3(C::TH), 0, st, a);
     else
-      hipLaunchKernelGGL((k_dweight<C, false, bf16>), dim3(blocks), dim3(C::TH), 0, st, a);
+      hipLaunchKernelGGL((k_back<C, false, bf16>), dim3(blocks), dim3(C::TH), 0, st, a);
+    a.blocks = 0;  // dH came with the first
+    if (!dweight) break;
   }
+}
+void run_back(const Plan &p, const Back &a, bool dhidden, bool dweight, sk_dtype odt, hipStream_t st) {
+  if (p.large)
+    launch_back<Large>(p, a, dhidden, dweight, odt, st);
+  else
+    launch_back<Small>(p, a, dhidden, dweight, odt, st);
 }
 
 }  // namespace
@@ -1084,10 +1114,10 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
     Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, false, work, st), work);
     a.part = ptr<float2>(work, p.part);
     a.xt = ptr<float>(work, p.xt);
-    run_logits<Big, false>(p, a, up(x->rows, kStep), st);
+    run_logits<false>(p, a, up(x->rows, kStep), st);
   }
   hipLaunchKernelGGL(k_join, dim3((unsigned)(p.tcap / 64)), dim3(1024), 0, st, ptr<Meta>(work, p.meta), ptr<int>(work, p.list),
-                     ptr<float2>(work, p.part), ptr<float>(work, p.xt), p.tcap, (int)up(x->vocab, 256) / kTileM, x->scale, logp,
+                     ptr<float2>(work, p.part), ptr<float>(work, p.xt), p.tcap, (int)p.units, x->scale, logp,
                      (float2 *)stats);
   return train_launched();
 }
@@ -1142,45 +1172,40 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
       a.gt = ptr<uint16_t>(work, p.gt);
       a.gplane = p.tcap * p.piece;
       a.piece = p.piece;
-      run_logits<Big, true>(p, a, p.tcap, st);
+      run_logits<true>(p, a, p.tcap, st);
     }
-    if (dhidden && x->rows) {
-      DHidden a{};
-      a.wt = planes_of(ptr<uint16_t>(work, p.wt), p.piece * p.kp, p.piece);
-      a.g = planes_of(ptr<uint16_t>(work, p.g), p.tcap * p.piece, p.piece);
-      a.width = (int)width;
-      a.steps = (int)(up(valid, kStep) / kStep);
-      a.splits = (int)p.splits;
-      a.per = (int)((a.steps + p.splits - 1) / p.splits);
-      a.first = v0 == 0;
-      a.meta = meta;
-      a.rowf = ptr<float>(work, p.rowf);
-      a.acc = ptr<float>(work, p.acc);
-      a.tcap = p.tcap;
-      a.kp = (int)p.kp;
-      run_dhidden<Small>(p, a, st);
-    }
-    if (dweight) {
-      DWeight a{};
-      a.ht = planes_of(ptr<uint16_t>(work, p.ht), p.tcap * p.kp, p.tcap);
-      a.gt = planes_of(ptr<uint16_t>(work, p.gt), p.tcap * p.piece, p.tcap);
-      a.width = (int)width;
-      a.valid = (int)valid;
-      a.seg = ptr<int>(work, p.seg);
-      a.meta = meta;
-      a.out = (char *)dweight + v0 * width * (dweight_dtype == SK_F32 ? 4 : 2);
-      a.vocab = x->vocab;
-      a.accumulate = accumulate != 0;
-      run_dweight<Small>(p, a, dweight_dtype, st);
-    }
+    Back a{};
+    a.width = (int)width;
+    a.meta = meta;
+    a.seg = ptr<int>(work, p.seg);
+    a.tcap = p.tcap;
+    a.g = planes_of(ptr<uint16_t>(work, p.g), p.tcap * p.piece, p.piece);
+    a.wt = planes_of(ptr<uint16_t>(work, p.wt), p.piece * p.kp, p.piece);
+    a.steps = (int)(up(valid, kStep) / kStep);
+    a.splits = (int)p.splits;
+    a.per = (int)((a.steps + p.splits - 1) / p.splits);
+    a.first = v0 == 0;
+    a.acc = ptr<float>(work, p.acc);
+    a.kp = (int)p.kp;
+    a.gt = planes_of(ptr<uint16_t>(work, p.gt), p.tcap * p.piece, p.tcap);
+    a.ht = planes_of(ptr<uint16_t>(work, p.ht), p.tcap * p.kp, p.tcap);
+    a.valid = (int)valid;
+    a.out = (char *)dweight + v0 * width * (dweight_dtype == SK_F32 ? 4 : 2);
+    a.vocab = x->vocab;
+    a.accumulate = accumulate != 0;
+    const bool dh = dhidden && x->rows;
+    if (!dh && !dweight) continue;
+    run_back(p, a, dh, dweight, dweight_dtype, st);
   }
   if (dhidden && x->rows) {
     const dim3 grid((unsigned)((x->rows + 3) / 4));
     if (p.f16)
-      hipLaunchKernelGGL(k_dhidden_out<float>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.acc), p.tcap,
+      hipLaunchKernelGGL(k_dhidden_out<float>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.rowf), ptr<float>(work, p.acc),
+                         p.tcap,
                          (int)p.kp, (int)p.splits, (int)x->rows, (int)width, (float *)dhidden, ld_dhidden);
     else
-      hipLaunchKernelGGL(k_dhidden_out<bf16>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.acc), p.tcap,
+      hipLaunchKernelGGL(k_dhidden_out<bf16>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.rowf), ptr<float>(work, p.acc),
+                         p.tcap,
                          (int)p.kp, (int)p.splits, (int)x->rows, (int)width, (bf16 *)dhidden, ld_dhidden);
   }
   return train_launched();
