@@ -13,9 +13,8 @@
 // ones, each example's padded with empty rows to a multiple of 64 so that a step
 // of the products' K lies in one example.
 //
-// All three products are one kernel core, C[m][n] = sum_k A[m][k] B[n][k] with
-// K contiguous in both (Core below); H^T and W^T of a piece are written once for
-// it.  16-bit operands, fp32 sums.  bf16 inputs are used as they are and G is
+// All three products are one kernel core, C[m][n] = sum_k A[m][k] B[n][k], which takes
+// its operands as they lie, with K along their rows or across them (Core below).  16-bit operands, fp32 sums.  bf16 inputs are used as they are and G is
 // rounded to bf16, once, like any entry of a bf16 gradient.  fp32 inputs are
 // split, x = hi + lo in two fp16 numbers (22 bits) under a power of two that
 // brings the largest to 2^13, and each product is the three hi lo, lo hi, hi hi:
@@ -249,7 +248,8 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
     p.f = ldexpf(1.0f, e + ew - 2 * kTop);
     a.rowf[n] = ldexpf(c, ew - 2 * kTop);
     a.cs[n] = c;
-    if (c != 0.0f) atomicMax(&a.meta->ec, e + exponent_of(c) + 1);
+    const int ec = e + exponent_of(c) + 1;
+    if (c != 0.0f && ec > __hip_atomic_load(&a.meta->ec, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&a.meta->ec, ec);
   }
   a.prm[n] = p;
 }
@@ -282,74 +282,48 @@ __global__ __launch_bounds__(256) void k_absmax(const float *w, int64_t ld, int 
 struct Prep {
   const void *src;
   int64_t ld;
-  int rows, width;  // what there is; zeros beyond
+  int rows, width, kp;  // what there is, zeros up to kp columns
   const Meta *meta;
-  // H^T: rows in list order, with their factors (fp32)
+  // H: rows in list order, with their factors (fp32)
   const int *list, *eh;
   const float *cs;
-  uint16_t *copy;  // [rows][kp], NULL if not wanted
-  int64_t cplane;
-  int kp;
-  uint16_t *tr;  // [width][tld], NULL if not wanted
-  int64_t tplane;
-  int64_t tld;
+  uint16_t *out;  // [..][kp]
+  int64_t plane;
 };
 
-// 64 rows by 64 columns through LDS: the padded copy of the rows and the transpose.
+// Rows as an operand takes them: padded with zeros to kp columns, fp32 split.  A wave a row, up to a multiple of 64 rows.
 template <typename T, bool LIST>
 __global__ __launch_bounds__(256) void k_prep(Prep a) {
   constexpr int P = sizeof(T) == 4 ? 2 : 1;
-  __shared__ uint32_t lds[P][64][33];  // pairs of columns
-  const int r0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
-  if (LIST && r0 >= a.meta->np) return;
-  {
-    const int r = r0 + (threadIdx.x >> 2), k = k0 + (threadIdx.x & 3) * 16;
-    int64_t at = r < a.rows ? r : -1;
-    float scale = 1.0f;
-    int e = 0;
-    if (LIST) {
-      at = a.list[r];  // np is a multiple of 64
-      if (P == 2) {
-        e = a.eh[r];
-        scale = ldexpf(a.cs[r], e - a.meta->ec);
-      }
-    } else if (P == 2) {
-      e = exponent_of((uint32_t)a.meta->wbits);
-    }
-    float f[16];
-    row_part<16>((const T *)a.src + (at < 0 ? 0 : at) * a.ld, k, at < 0 ? 0 : a.width, f);
-    uint32_t h[P][8];
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (LIST && r >= a.meta->np) return;
+  int64_t at = r < a.rows ? r : -1;
+  float scale = 1.0f;
+  int e = 0;
+  if (LIST) {
+    at = a.list[r];
+    e = a.eh[r];
+    scale = ldexpf(a.cs[r], e - a.meta->ec);
+  } else if (P == 2) {
+    e = exponent_of((uint32_t)a.meta->wbits);
+  }
+  const T *row = (const T *)a.src + (at < 0 ? 0 : at) * a.ld;
+  const int width = at < 0 ? 0 : a.width;
+  uint16_t *out = a.out + (int64_t)r * a.kp;
+  for (int k = lane * 8; k < a.kp; k += 512) {
+    float f[8];
+    row_part<8>(row, k, width, f);
+    if (P == 2) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (P == 2) f[i] = ldexpf(f[i], kTop - e) * (at < 0 ? 0.0f : scale);
+      for (int i = 0; i < 8; ++i) f[i] = LIST ? ldexpf(f[i], kTop - e) * (at < 0 ? 0.0f : scale) : ldexpf(f[i], kTop - e);
+    }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
+      u32x4 v;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[p][i] = two<P == 2>(f[2 * i], f[2 * i + 1], p);
-      if (a.copy) {
-        u32x4 *c = (u32x4 *)(a.copy + p * a.cplane + (int64_t)r * a.kp + k);
-        c[0] = u32x4{h[p][0], h[p][1], h[p][2], h[p][3]};
-        c[1] = u32x4{h[p][4], h[p][5], h[p][6], h[p][7]};
-      }
-      if (a.tr) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) lds[p][threadIdx.x >> 2][(threadIdx.x & 3) * 8 + i] = h[p][i];
-      }
+      for (int i = 0; i < 4; ++i) v[i] = two<P == 2>(f[2 * i], f[2 * i + 1], p);
+      *(u32x4 *)(out + p * a.plane + k) = v;
     }
-  }
-  if (!a.tr) return;
-  __syncthreads();
-  const int k = threadIdx.x >> 2, r = (threadIdx.x & 3) * 16;
-  if (k0 + k >= a.width) return;
-#pragma unroll
-  for (int p = 0; p < P; ++p) {
-    uint32_t h[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      h[i] = __builtin_amdgcn_perm(lds[p][r + 2 * i + 1][k >> 1], lds[p][r + 2 * i][k >> 1], k & 1 ? 0x07060302 : 0x05040100);
-    u32x4 *c = (u32x4 *)(a.tr + p * a.tplane + (int64_t)(k0 + k) * a.tld + r0 + r);
-    c[0] = u32x4{h[0], h[1], h[2], h[3]};
-    c[1] = u32x4{h[4], h[5], h[6], h[7]};
   }
 }
 
@@ -362,15 +336,13 @@ struct Operand {
 
 // A BM x BN tile by WM x WN waves, each (BM / WM) x (BN / WN) in 32 x 32 accumulators of v_mfma_f32_32x32x16.  Stages of
 // 64 of K go straight from memory to LDS, 16 bytes a lane, two stages deep: the loads of the next one are issued
-// behind the barrier that frees its buffer and have the products of a whole stage (2048 cycles of a CU's matrix cores
-// for 256 x 256) to arrive.  A row of a stage is 128 bytes, its eight 16-byte chunks exchanged by (row / 2) & 7, so that
-// the 32 rows that a wave reads at a time lie in different banks (exchanged by row & 7: 8192^3 bf16, 256 x 256, 957 us, 887
-// us so).  Two workgroups share a CU, so that one's epilogue lies beside the other's products.  Alone (8192^3, and 16384 x
-// 2560 x 768, bf16): 128 x 192 1150 and 803 TFLOP/s, 128 x 128 1108 and 773, one 256 x 256 a CU 1240 and 729, the
-// library's 1290 and 817.  In the operators (4096 x 50257 x 768 and 8192 x 128256 x 4096): gradients 819 us and 15.5 ms with
-// 128 x 192, 891 us and 17.8 ms with 128 x 128, 1120 us and 15.9 ms with 256 x 256; log-probabilities 225 us and 4.47 ms,
-// 243 us and 5.0 ms, 226 us and 4.5 ms.  Up to 1024 rows the smaller tiles fill the chip better (gradients of 200 x 50257 x
-// 768: 134 us, 146 with the larger ones; 1000: 301 and 299).
+// behind the barrier that frees its buffer and have the products of a whole stage to arrive.  Two workgroups share a
+// CU, so that one's epilogue lies beside the other's products.  Alone (8192^3, and 16384 x 2560 x 768, bf16): 128 x 192
+// 1150 and 803 TFLOP/s, 128 x 128 1108 and 773, one 256 x 256 a CU 1240 and 729, the library's 1290 and 817.  In the
+// operators (4096 x 50257 x 768 and 8192 x 128256 x 4096): gradients 819 us and 15.5 ms with 128 x 192, 891 us and 17.8
+// ms with 128 x 128, 1120 us and 15.9 ms with 256 x 256; log-probabilities 225 us and 4.47 ms, 243 us and 5.0 ms, 226 us
+// and 4.5 ms.  Up to 1024 rows the smaller tiles fill the chip better (gradients of 200 x 50257 x 768: 134 us, 146 with
+// the larger ones; 1000: 301 and 299).
 template <int BM_, int BN_, int WM_, int WN_>
 struct Tiling {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM * WN, TH = NW * 64;
@@ -382,52 +354,104 @@ using Small = Tiling<128, 128, 2, 2>;
 constexpr int64_t kSmallRows = 1024;  // rows up to which the smaller tiles are taken
 
 #if defined(__HIP_DEVICE_COMPILE__)
+typedef __attribute__((address_space(3))) void *lds_ptr;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// One operand of a tile, N of its rows, by TH threads of which a wave multiplies W of N / W rows.
+// KM false: K contiguous.  A stage is N rows of 128 bytes, their eight 16-byte chunks exchanged by (row / 2) & 7, so
+// that the 32 rows that a wave reads at a time lie in different banks (exchanged by row & 7: 8192^3 bf16, 256 x 256, 957
+// us, 887 us so).
+// KM true: the matrix has K for its rows and the operand's rows for its columns.  A stage is 64 rows of N columns, which
+// ds_read_b64_tr_b16 transposes: of 16 lanes, lane 4 r + q gives the address of four columns 4 q of row r, and lane i gets
+// column i of the four rows.  Chunks are exchanged so that the eight rows of 64 bytes that a wave reads at a time fill
+// the banks twice over: four rows lie 256 bytes (N = 128) or 384 bytes (192) apart.
+template <int N, int W, int TH, bool KM>
+struct Side {
+  static constexpr int CH = KM ? N / 8 : kStep / 8;  // chunks of an LDS row
+  static constexpr int L = N * kStep / 8 / TH;       // loads of a thread and stage
+  static constexpr int T = N / W / 32;
+  static_assert(!KM || N == 128 || N == 192, "exchanges are worked out for these");
+  int off[L], ld, limit, last;
+
+  static __device__ __forceinline__ int swz(int row) {
+    return !KM ? (row >> 1) & 7 : N == 128 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
+  }
+  // rows: how many there are from the tile's first on (those behind repeat one of them; a multiple of 8 with KM); depth: K
+  // rows that there are (KM)
+  __device__ __forceinline__ void init(const Operand &o, int rows, int depth) {
+    ld = (int)(o.ld * 2);
+    limit = rows;
+    last = depth - 1;
+#pragma unroll
+    for (int i = 0; i < L; ++i) off[i] = offset(i, KM ? kStep : rows);
+  }
+  __device__ __forceinline__ int offset(int i, int rows) const {
+    const int k = i * TH + threadIdx.x, r = k / CH, c = (k % CH) ^ swz(r);
+    return min(r, rows - 1) * ld + (KM ? min(c * 16, limit * 2 - 16) : c * 16);
+  }
+  // stage k of a plane to LDS
+  __device__ __forceinline__ void load(char *lds, const uint16_t *plane, int k) const {
+    const char *base = (const char *)plane + (int64_t)k * (KM ? (int64_t)ld * kStep : kStep * 2);
+    const auto m = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0xFFFFFFFF, 0x00020000);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool part = KM && (k + 1) * kStep > last + 1;
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(m, (lds_ptr)(lds + (i * (TH / 64) + wave) * 1024), 16,
+                                               part ? offset(i, last + 1 - k * kStep) : off[i], 0, 0, 0);
+  }
+  // operands of step ks of a stage: rows w N / W + 32 i + lane % 32, K 16 ks + 8 (lane / 32) and on
+  __device__ __forceinline__ void read(const char *lds, int w, int ks, u32x4 *f) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+      if constexpr (KM) {
+        const int r = (lane & 15) >> 2, col = w * (N / W) + i * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+        const char *at = lds + (ks * 16 + (lane >> 5) * 8 + r) * (N * 2) + ((col >> 3) ^ swz(r)) * 16 + (col & 4) * 2;
+        union {
+          s16x4 h[2];
+          u32x4 v;
+        } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4 * N * 2));
+        f[i] = u.v;
+      } else {
+        const int r = lane & 31;
+        f[i] = *(const u32x4 *)(lds + (w * (N / W) + i * 32 + r) * kStep * 2 + ((ks * 2 + (lane >> 5)) ^ swz(r)) * 16);
+      }
+    }
+  }
+};
+
 template <typename C, bool F16>
 struct Core {
   f32x16 acc[C::TM][C::TN];
-  int lane, wave, wm, wn, fr, fk;
+  int wm, wn, fr, fk;
 
   __device__ __forceinline__ Core() {
-    lane = threadIdx.x & 63;
-    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     wm = wave % C::WM;
     wn = wave / C::WM;
-    fr = lane & 31;
-    fk = lane >> 5;
+    fr = threadIdx.x & 31;
+    fk = (threadIdx.x & 63) >> 5;
   }
   // the tile's row of accumulator entry (i, e) of this lane, and its column of (j)
   __device__ __forceinline__ int row(int i, int e) const { return wm * (C::BM / C::WM) + i * 32 + (e >> 2) * 8 + fk * 4 + (e & 3); }
   __device__ __forceinline__ int col(int j) const { return wn * (C::BN / C::WN) + j * 32 + fr; }
 
-  // acc = sum over `steps` stages from a and b on; rows from ra (rb) on repeat the last one
-  __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int ra, int rb, int steps) {
-    constexpr int LA = C::BM / (C::NW * 8), LB = C::BN / (C::NW * 8), STAGE = (C::BM + C::BN) * kStep * 2;
-    // lane l fetches chunk l % 8 of row l / 8 of its wave's eight rows
-    const int lrow = lane >> 3, src = (lane & 7);
-    int offa[LA], offb[LB];
-#pragma unroll
-    for (int i = 0; i < LA; ++i) {
-      const int r = (i * C::NW + wave) * 8 + lrow;
-      offa[i] = min(r, ra - 1) * (int)(a.ld * 2) + (src ^ ((r >> 1) & 7)) * 16;
-    }
-#pragma unroll
-    for (int i = 0; i < LB; ++i) {
-      const int r = (i * C::NW + wave) * 8 + lrow;
-      offb[i] = min(r, rb - 1) * (int)(b.ld * 2) + (src ^ ((r >> 1) & 7)) * 16;
-    }
-    typedef __attribute__((address_space(3))) void *lds_ptr;
+  // acc = sum over `steps` stages from a and b on
+  template <bool KA, bool KB>
+  __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth_a,
+                                      int depth_b, int steps) {
+    constexpr int HALF = C::BM * kStep * 2, STAGE = HALF + C::BN * kStep * 2;
+    Side<C::BM, C::WM, C::TH, KA> sa;
+    Side<C::BN, C::WN, C::TH, KB> sb;
+    sa.init(a, rows_a, depth_a);
+    sb.init(b, rows_b, depth_b);
     int part = 0, k = 0;  // of the next stage to load; parts: hi lo, lo hi, hi hi
     auto load = [&](int st) {
-      const auto ma = __builtin_amdgcn_make_buffer_rsrc((void *)a.p[F16 && part == 1], 0, 0xFFFFFFFF, 0x00020000);
-      const auto mb = __builtin_amdgcn_make_buffer_rsrc((void *)b.p[F16 && part == 0], 0, 0xFFFFFFFF, 0x00020000);
-      char *to = lds + st * STAGE + wave * 1024;
-#pragma unroll
-      for (int i = 0; i < LA; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ma, (lds_ptr)(to + i * C::NW * 1024), 16, offa[i], k * (kStep * 2), 0, 0);
-#pragma unroll
-      for (int i = 0; i < LB; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(mb, (lds_ptr)(to + C::BM * kStep * 2 + i * C::NW * 1024), 16, offb[i],
-                                                 k * (kStep * 2), 0, 0);
+      sa.load(lds + st * STAGE, a.p[F16 && part == 1], k);
+      sb.load(lds + st * STAGE + HALF, b.p[F16 && part == 0], k);
       if (++k == steps) {
         k = 0;
         ++part;
@@ -446,16 +470,12 @@ struct Core {
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       if (s + 1 < all) load((s + 1) & 1);
-      const char *la = lds + (s & 1) * STAGE + wm * (C::BM / C::WM) * kStep * 2;
-      const char *lb = lds + (s & 1) * STAGE + (C::BM + wn * (C::BN / C::WN)) * kStep * 2;
+      const char *at = lds + (s & 1) * STAGE;
 #pragma unroll
       for (int ks = 0; ks < kStep / 16; ++ks) {
-        const int at = ((ks * 2 + fk) ^ ((fr >> 1) & 7)) * 16 + fr * kStep * 2;
         u32x4 fa[C::TM], fb[C::TN];
-#pragma unroll
-        for (int i = 0; i < C::TM; ++i) fa[i] = *(const u32x4 *)(la + i * 32 * kStep * 2 + at);
-#pragma unroll
-        for (int j = 0; j < C::TN; ++j) fb[j] = *(const u32x4 *)(lb + j * 32 * kStep * 2 + at);
+        sa.read(at, wm, ks, fa);
+        sb.read(at + HALF, wn, ks, fb);
 #pragma unroll
         for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -501,7 +521,7 @@ struct Logit {
   int64_t tcap;
   // gradient
   const RowPrm *prm;
-  uint16_t *g, *gt;  // [tcap][piece], [piece][tcap]
+  uint16_t *g;  // [tcap][piece]
   int64_t gplane, piece;
 };
 
@@ -515,7 +535,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   tile_of(blockIdx.x, mt, nt, tm, tn);
   const int m0 = tm * C::BM, n0 = tn * C::BN;
   Core<C, F16> c;
-  c.run(lds, at_row(a.w, m0), at_row(a.h, n0), a.valid - m0, np - n0, a.kp / kStep);
+  c.template run<false, false>(lds, at_row(a.w, m0), at_row(a.h, n0), a.valid - m0, np - n0, 0, 0, a.kp / kStep);
   const bool whole = m0 + C::BM <= a.valid;
 #pragma unroll
   for (int j = 0; j < C::TN; ++j) {
@@ -583,7 +603,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   }
   if (!GRAD) return;
   // G's rows leave through LDS, in whole lines (chunks of 16 bytes exchanged by the row, so that the lanes of a write meet
-  // different banks); its transpose's as they lie, 32 tokens a lane's row.
+  // different banks).
 #pragma unroll
   for (int plane = 0; plane < (F16 ? 2 : 1); ++plane) {
     constexpr int CH = C::BM / 8;
@@ -602,13 +622,6 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
           const int m = c.row(i, e);
           const u32x2 v{pair(i, j, e), pair(i, j, e + 2)};
           *(u32x2 *)(lds + n * (C::BM * 2) + ((m >> 3) ^ (n & (CH - 1))) * 16 + (m & 4) * 2) = v;
-          if (n0 + n < np) {
-            uint16_t *gt = a.gt + plane * a.gplane + (int64_t)(m0 + m) * a.tcap + n0 + n;
-            gt[0] = (uint16_t)v[0];
-            gt[a.tcap] = (uint16_t)(v[0] >> 16);
-            gt[2 * a.tcap] = (uint16_t)v[1];
-            gt[3 * a.tcap] = (uint16_t)(v[1] >> 16);
-          }
         }
     }
     __syncthreads();
@@ -774,15 +787,15 @@ struct Back {
   const Meta *meta;
   const int *seg;
   int64_t tcap;
-  // dH: acc[split] (+)= G W^T^T
-  Operand g, wt;
+  // dH: acc[split] (+)= G W
+  Operand g, w;
   int steps, per, splits;  // stages of the piece, of a split
   int blocks;              // workgroups at most, a multiple of 8 (0: not wanted)
   bool first;
   float *acc;  // [splits][tcap][kp]
   int kp;
-  // dW
-  Operand gt, ht;
+  // dW = G^T H (fp32: H times the rows' factors)
+  Operand h;
   int valid, b0;  // rows of the piece, the launch's first example
   void *out;      // rows from the piece's first on
   int64_t vocab;  // rows from example to example
@@ -807,7 +820,10 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
   const int k0 = hidden ? part * a.per * kStep : a.seg[a.b0 + part];
   const int steps = hidden ? max(0, min(a.per, a.steps - part * a.per)) : (a.seg[a.b0 + part + 1] - k0) / kStep;
   Core<C, F16> c;
-  c.run(lds, at_row(hidden ? a.g : a.gt, m0, k0), at_row(hidden ? a.wt : a.ht, n0, k0), rows - m0, a.width - n0, steps);
+  if (hidden)
+    c.template run<false, true>(lds, at_row(a.g, m0, k0), at_row(a.w, k0, n0), np - m0, a.kp - n0, 0, a.valid - k0, steps);
+  else
+    c.template run<true, true>(lds, at_row(a.g, k0, m0), at_row(a.h, k0, n0), C::BM, a.kp - n0, steps * kStep, steps * kStep, steps);
   if (hidden) {
     float *to = a.acc + (part * a.tcap + m0) * a.kp + n0;
 #pragma unroll
@@ -856,6 +872,7 @@ __global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float
     float f[8] = {};
     if (p >= 0) {
       const float *a = acc + (int64_t)p * kp + k;
+#pragma unroll 4
       for (int s = 0; s < splits; ++s, a += tcap * kp) {
 #pragma unroll
         for (int i = 0; i < 8; i += 4) {
@@ -885,7 +902,7 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Plan {
   bool f16, copy, large;
   int64_t batch, n, tcap, kp, piece, units, splits, planes;
-  int64_t list, pos, tgt, seg, cnt, meta, hc, eh, part, xt, prm, rowf, cs, ht, wc, wt, g, gt, acc, bytes;
+  int64_t list, pos, tgt, seg, cnt, meta, hc, eh, part, xt, prm, rowf, cs, hs, wc, g, acc, bytes;
 };
 
 Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
@@ -899,8 +916,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.kp = up(x->width, kStep);
   // rows that 16-byte loads in whole stages read as they lie
   p.copy = p.f16 || x->width % kStep || x->ld_weight % 8 || (uintptr_t)x->weight % 16 || x->ld_weight > (1 << 20);
-  // a piece: G and its transpose in 512 MB (4096 x 50257 x 768 bf16 one launch more for each halving: 779, 819, 895 us with
-  // 1 GB, 512 and 256 MB), a copy of W in 256 MB
+  // a piece: G in 256 MB (a launch more for each halving), a copy of W in 256 MB
   int64_t most = x->vocab;
   if (grad) most = std::min(most, ((int64_t)1 << 27) / (p.tcap * p.planes));
   if (grad || p.copy) most = std::min(most, ((int64_t)1 << 27) / (p.kp * p.planes));
@@ -940,10 +956,8 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     p.prm = take(sizeof(RowPrm) * p.tcap);
     p.rowf = take(4 * p.tcap);
     p.cs = take(4 * p.tcap);
-    if (dweight) p.ht = take(2 * p.planes * p.tcap * p.kp);
-    if (dhidden) p.wt = take(2 * p.planes * p.piece * p.kp);
+    if (dweight && p.f16) p.hs = take(2 * p.planes * p.tcap * p.kp);
     p.g = take(2 * p.planes * p.tcap * p.piece);
-    p.gt = take(2 * p.planes * p.tcap * p.piece);
     if (dhidden) p.acc = take(4 * p.splits * p.tcap * p.kp);
   }
   p.bytes = at;
@@ -997,30 +1011,25 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
     hipLaunchKernelGGL(k_gather<bf16>, dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, g);
 }
 
-// W's rows from v0 on as an operand, and their transpose
-Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, bool transpose, void *work, hipStream_t st) {
-  const int e = p.f16 ? 4 : 2;
-  const void *src = (const char *)x->weight + v0 * x->ld_weight * e;
-  if (p.copy || transpose) {
-    Prep a{};
-    a.src = src;
-    a.ld = x->ld_weight;
-    a.rows = (int)valid;
-    a.width = (int)x->width;
-    a.meta = ptr<Meta>(work, p.meta);
-    if (p.copy) a.copy = ptr<uint16_t>(work, p.wc);
-    a.cplane = a.tplane = p.piece * p.kp;
-    a.kp = (int)p.kp;
-    if (transpose) a.tr = ptr<uint16_t>(work, p.wt);
-    a.tld = p.piece;
-    const dim3 grid((unsigned)(up(valid, 64) / 64), (unsigned)(p.kp / 64));
-    if (p.f16)
-      hipLaunchKernelGGL((k_prep<float, false>), grid, dim3(256), 0, st, a);
-    else
-      hipLaunchKernelGGL((k_prep<bf16, false>), grid, dim3(256), 0, st, a);
-  }
-  if (p.copy) return planes_of(ptr<uint16_t>(work, p.wc), p.piece * p.kp, p.kp);
-  return Operand{{(const uint16_t *)src, (const uint16_t *)src}, x->ld_weight};
+// W's rows from v0 on as an operand
+Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, void *work, hipStream_t st) {
+  const void *src = (const char *)x->weight + v0 * x->ld_weight * (p.f16 ? 4 : 2);
+  if (!p.copy) return Operand{{(const uint16_t *)src, (const uint16_t *)src}, x->ld_weight};
+  Prep a{};
+  a.src = src;
+  a.ld = x->ld_weight;
+  a.rows = (int)valid;
+  a.width = (int)x->width;
+  a.kp = (int)p.kp;
+  a.meta = ptr<Meta>(work, p.meta);
+  a.out = ptr<uint16_t>(work, p.wc);
+  a.plane = p.piece * p.kp;
+  const dim3 grid((unsigned)(up(valid, 64) / 4));
+  if (p.f16)
+    hipLaunchKernelGGL((k_prep<float, false>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_prep<bf16, false>), grid, dim3(256), 0, st, a);
+  return planes_of(a.out, a.plane, p.kp);
 }
 
 Logit logit_of(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, Operand w, void *work) {
@@ -1111,7 +1120,7 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
   begin(x, p, nullptr, nullptr, logp, stats, work, st);
   for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
     const int64_t valid = std::min(p.piece, x->vocab - v0);
-    Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, false, work, st), work);
+    Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, work, st), work);
     a.part = ptr<float2>(work, p.part);
     a.xt = ptr<float>(work, p.xt);
     run_logits<false>(p, a, up(x->rows, kStep), st);
@@ -1145,7 +1154,7 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   begin(x, p, dlogp ? dlogp : (const float *)work, stats, nullptr, nullptr, work, st);
   Meta *meta = ptr<Meta>(work, p.meta);
   const int64_t width = x->width;
-  if (dweight && x->rows) {
+  if (dweight && x->rows && p.f16) {
     Prep a{};
     a.src = x->hidden;
     a.ld = x->ld_hidden;
@@ -1154,22 +1163,18 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
     a.list = ptr<int>(work, p.list);
     a.eh = ptr<int>(work, p.eh);
     a.cs = ptr<float>(work, p.cs);
-    a.tr = ptr<uint16_t>(work, p.ht);
-    a.tplane = p.tcap * p.kp;
-    a.tld = p.tcap;
-    const dim3 grid((unsigned)(p.tcap / 64), (unsigned)(p.kp / 64));
-    if (p.f16)
-      hipLaunchKernelGGL((k_prep<float, true>), grid, dim3(256), 0, st, a);
-    else
-      hipLaunchKernelGGL((k_prep<bf16, true>), grid, dim3(256), 0, st, a);
+    a.kp = (int)p.kp;
+    a.out = ptr<uint16_t>(work, p.hs);
+    a.plane = p.tcap * p.kp;
+    hipLaunchKernelGGL((k_prep<float, true>), dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, a);
   }
   for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
     const int64_t valid = std::min(p.piece, x->vocab - v0);
+    const Operand w = x->rows ? weights(x, p, v0, valid, work, st) : Operand{};
     if (x->rows) {
-      Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, dhidden != nullptr, work, st), work);
+      Logit a = logit_of(x, p, v0, valid, w, work);
       a.prm = ptr<RowPrm>(work, p.prm);
       a.g = ptr<uint16_t>(work, p.g);
-      a.gt = ptr<uint16_t>(work, p.gt);
       a.gplane = p.tcap * p.piece;
       a.piece = p.piece;
       run_logits<true>(p, a, p.tcap, st);
@@ -1180,15 +1185,14 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
     a.seg = ptr<int>(work, p.seg);
     a.tcap = p.tcap;
     a.g = planes_of(ptr<uint16_t>(work, p.g), p.tcap * p.piece, p.piece);
-    a.wt = planes_of(ptr<uint16_t>(work, p.wt), p.piece * p.kp, p.piece);
+    a.w = w;
     a.steps = (int)(up(valid, kStep) / kStep);
     a.splits = (int)p.splits;
     a.per = (int)((a.steps + p.splits - 1) / p.splits);
     a.first = v0 == 0;
     a.acc = ptr<float>(work, p.acc);
     a.kp = (int)p.kp;
-    a.gt = planes_of(ptr<uint16_t>(work, p.gt), p.tcap * p.piece, p.tcap);
-    a.ht = planes_of(ptr<uint16_t>(work, p.ht), p.tcap * p.kp, p.tcap);
+    a.h = planes_of(ptr<uint16_t>(work, p.f16 ? p.hs : p.hc), p.tcap * p.kp, p.kp);
     a.valid = (int)valid;
     a.out = (char *)dweight + v0 * width * (dweight_dtype == SK_F32 ? 4 : 2);
     a.vocab = x->vocab;
