@@ -41,14 +41,15 @@ constexpr int kTop = 13;    // split operands lie below 2^(kTop + 1)
 
 // What the kernels of a call share in its workspace.
 struct Meta {
-  int np;     // listed rows
-  int wbits;  // bits of the largest finite |W|
-  int ec;     // exponent bound of dlogp scale H
+  int np;  // listed rows
+  int ew;  // exponent of the largest finite |W|
+  int ec;  // exponent bound of dlogp scale H
 };
 
-// A listed row in the gradient: logits are acc * f, G = live ? one [v = target] + w exp(scale (x - m)) : 0.
+// A listed row in the gradient: G = one ? one [v = target] + w exp(scale (x - m)) : 0, logits being acc 2^e.
 struct RowPrm {
-  float m, w, one, f;
+  float m, w, one;
+  int e;
 };
 
 __device__ __forceinline__ int exponent_of(uint32_t bits) { return (int)((bits >> 23) & 255) - 127; }
@@ -104,32 +105,39 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {  // inclusive
   return v;
 }
 
-// One workgroup: counts of 64 rows each, their sums within the examples, the examples' starts, the list.
+// One workgroup: counts of 64 rows each, their sums within the examples, the examples' starts, the list.  A wave has four
+// chunks of 64 rows under way (8192 rows: 17 us one after another, LIVE us so).
 __global__ __launch_bounds__(1024) void k_live(Live a) {
+  constexpr int U = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per = (a.n + 63) / 64;
-  const int64_t chunks = (int64_t)per * a.batch;
-  auto target = [&](int64_t c, int64_t &t) {
-    const int i = (int)(c % per) * 64 + lane;
-    t = c / per * a.n + i;
-    if (i >= a.n) {
-      t = -1;
-      return -1;
+  const int per = (a.n + 63) / 64, chunks = per * a.batch;
+  // the row (-1: none) and target (-1: masked) of this lane in chunk c
+  auto fetch = [&](int c, int &t, int &v) {
+    const int i = c % per * 64 + lane;
+    t = c < chunks && i < a.n ? c / per * a.n + i : -1;
+    int64_t id = -1;
+    float d = 1.0f;
+    if (t >= 0) {
+      id = a.index == SK_I64 ? ((const int64_t *)a.targets)[t] : ((const int32_t *)a.targets)[t];
+      if (a.dlogp) d = a.dlogp[t];
     }
-    const int64_t v = a.index == SK_I64 ? ((const int64_t *)a.targets)[t] : ((const int32_t *)a.targets)[t];
-    if (v < 0 || v >= a.vocab || (a.dlogp && a.dlogp[t] == 0.0f)) return -1;
-    return (int)v;
+    v = id >= 0 && id < a.vocab && d != 0.0f ? (int)id : -1;
   };
-  for (int64_t c = wave; c < chunks; c += 16) {
-    int64_t t;
-    const uint64_t live = __ballot(target(c, t) >= 0);
-    if (lane == 0) a.cnt[c] = __popcll(live);
+  for (int c0 = wave * U; c0 < chunks; c0 += 16 * U) {
+    int t[U], v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) fetch(c0 + u, t[u], v[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint64_t live = __ballot(v[u] >= 0);
+      if (lane == 0 && c0 + u < chunks) a.cnt[c0 + u] = __popcll(live);
+    }
   }
   __syncthreads();
   for (int b = wave; b < a.batch; b += 16) {
     int sum = 0;
     for (int i = 0; i < per; i += 64) {
-      int *p = a.cnt + (int64_t)b * per + i + lane;
+      int *p = a.cnt + b * per + i + lane;
       const int v = i + lane < per ? *p : 0, s = wave_scan(v, lane);
       if (i + lane < per) *p = sum + s - v;
       sum += __shfl(s, 63, 64);
@@ -147,33 +155,61 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
     }
     if (lane == 0) {
       a.seg[0] = 0;
-      *a.meta = Meta{sum, 0, INT_MIN / 2};
+      *a.meta = Meta{sum, INT_MIN / 2, INT_MIN / 2};
     }
   }
   __syncthreads();
-  for (int64_t c = wave; c < chunks; c += 16) {
-    int64_t t;
-    const int v = target(c, t), b = (int)(c / per);
-    const uint64_t live = __ballot(v >= 0);
-    const int at = a.seg[b] + a.cnt[c];
-    if (v >= 0) {
-      const int p = at + __popcll(live & ((1ull << lane) - 1));
-      a.list[p] = (int)t;
-      a.tgt[p] = v;
-      a.pos[t] = p;
-    } else if (t >= 0) {
-      a.pos[t] = -1;
-      if (a.logp) {
-        a.logp[t] = 0.0f;
-        if (a.stats) a.stats[t] = float2{0.0f, 0.0f};
-      }
+  for (int c0 = wave * U; c0 < chunks; c0 += 16 * U) {
+    int t[U], v[U], at[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      fetch(c0 + u, t[u], v[u]);
+      at[u] = c0 + u < chunks ? a.seg[(c0 + u) / per] + a.cnt[c0 + u] : 0;
     }
-    if (c % per == per - 1)
-      for (int p = at + __popcll(live) + lane; p < a.seg[b + 1]; p += 64) a.list[p] = a.tgt[p] = -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint64_t live = __ballot(v[u] >= 0);
+      if (v[u] >= 0) {
+        const int p = at[u] + __popcll(live & ((1ull << lane) - 1));
+        a.list[p] = t[u];
+        a.tgt[p] = v[u];
+        a.pos[t[u]] = p;
+      } else if (t[u] >= 0) {
+        a.pos[t[u]] = -1;
+        if (a.logp) {
+          a.logp[t[u]] = 0.0f;
+          if (a.stats) a.stats[t[u]] = float2{0.0f, 0.0f};
+        }
+      }
+      if (c0 + u < chunks && (c0 + u) % per == per - 1)
+        for (int p = at[u] + __popcll(live) + lane; p < a.seg[(c0 + u) / per + 1]; p += 64) a.list[p] = a.tgt[p] = -1;
+    }
   }
 }
 
 // --- operands -----------------------------------------------------------------------------------------------
+// a wave's largest finite |x| of a row, as its exponent
+template <typename T>
+__device__ __forceinline__ int row_exponent(const T *row, int width) {
+  const int lane = threadIdx.x & 63;
+  float big = 0.0f;
+  for (int k = lane * 8; k < width; k += 1024) {
+    float f[8], g[8];
+    row_part<8>(row, k, width, f);
+    row_part<8>(row, k + 512, width, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      big = fmaxf(big, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.0f);
+      big = fmaxf(big, fabsf(g[i]) < INFINITY ? fabsf(g[i]) : 0.0f);
+    }
+  }
+  return exponent_of(wave_all(big, OpMax()));
+}
+
+__device__ __forceinline__ void raise(int *most, int v) {  // an atomic only where it can change something
+  if (v > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, v);
+}
+
 struct Gather {
   const void *hidden;
   int64_t ld;
@@ -188,7 +224,7 @@ struct Gather {
   const float *dlogp;
   float scale;
   RowPrm *prm;
-  float *rowf, *cs;
+  float *cs;
 };
 
 // Rows of H in list order, zeros to a width of kp; a wave a row.  fp32: the row's exponent, its split, and what the
@@ -203,14 +239,7 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
   uint16_t *hc = a.hc + (int64_t)n * a.kp;
   int e = 0;
   if (sizeof(T) == 4) {
-    float big = 0.0f;
-    for (int k = lane * 8; k < width; k += 512) {
-      float f[8];
-      row_part<8>(row, k, width, f);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.0f);
-    }
-    e = exponent_of(wave_all(big, OpMax()));
+    e = row_exponent(row, width);
     if (lane == 0) a.eh[n] = e;
   }
   for (int k = lane * 8; k < a.kp; k += 512) {
@@ -232,7 +261,7 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
     }
   }
   if (!a.prm || lane != 0) return;
-  RowPrm p{0.0f, 0.0f, 0.0f, 1.0f};
+  RowPrm p{0.0f, 0.0f, 0.0f, sizeof(T) == 4 ? e + a.meta->ew - 2 * kTop : 0};
   float c = 0.0f;
   if (t >= 0) {
     const float2 s = a.stats[t];
@@ -244,39 +273,42 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
     }
   }
   if (sizeof(T) == 4) {
-    const int ew = exponent_of((uint32_t)a.meta->wbits);
-    p.f = ldexpf(1.0f, e + ew - 2 * kTop);
-    a.rowf[n] = ldexpf(c, ew - 2 * kTop);
     a.cs[n] = c;
-    const int ec = e + exponent_of(c) + 1;
-    if (c != 0.0f && ec > __hip_atomic_load(&a.meta->ec, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&a.meta->ec, ec);
+    if (c != 0.0f) raise(&a.meta->ec, e + exponent_of(c) + 1);
   }
   a.prm[n] = p;
 }
 
-// The largest finite |W|, over all rows.  One atomic a workgroup, and only where it can change something: 50257 x 768 took
-// 68 us with one a wave, 40 us so (3.9 TB/s).
-__global__ __launch_bounds__(256) void k_absmax(const float *w, int64_t ld, int rows, int width, Meta *meta) {
-  __shared__ float lds[4];
-  float big = 0.0f;
+// The exponent of the largest finite |W|, over all rows; without gaps between them (a multiple of 4 entries, 16-byte
+// aligned) W is one long row.  One atomic a workgroup, and only where it can change something (50257 x 768: 68 us with one
+// a wave, ABSMAX us so).
+template <bool FLAT>
+__global__ __launch_bounds__(256) void k_largest(const float *w, int64_t ld, int64_t rows, int width, Meta *meta) {
+  __shared__ int lds[4];
   const int lane = threadIdx.x & 63;
-  auto take = [&](const float *f) {
+  int e;
+  if (FLAT) {
+    constexpr int U = 4;
+    const f32x4 *p = (const f32x4 *)w;
+    const int64_t n = rows * width / 4, step = (int64_t)gridDim.x * 256;
+    float big = 0.0f;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += U * step) {
+      f32x4 v[U];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.0f);
-  };
-  for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
-    const float *row = w + (int64_t)r * ld;
-    for (int k = lane * 8; k < width; k += 1024) {
-      float f[8], g[8];
-      row_part<8>(row, k, width, f);
-      row_part<8>(row, k + 512, width, g);
-      take(f);
-      take(g);
+      for (int u = 0; u < U; ++u) v[u] = p[i + u * step < n ? i + u * step : i];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) big = fmaxf(big, fabsf(v[u][k]) < INFINITY ? fabsf(v[u][k]) : 0.0f);
     }
+    e = exponent_of(wave_all(big, OpMax()));
+  } else {
+    e = INT_MIN / 2;
+    for (int64_t r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) e = max(e, row_exponent(w + r * ld, width));
   }
-  big = block_all<4>(big, OpMax(), lds);
-  if (threadIdx.x == 0 && (int)__float_as_uint(big) > __hip_atomic_load(&meta->wbits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
-    atomicMax(&meta->wbits, (int)__float_as_uint(big));
+  if (lane == 0) lds[threadIdx.x >> 6] = e;
+  __syncthreads();
+  if (threadIdx.x == 0) raise(&meta->ew, max(max(lds[0], lds[1]), max(lds[2], lds[3])));
 }
 
 struct Prep {
@@ -298,17 +330,17 @@ __global__ __launch_bounds__(256) void k_prep(Prep a) {
   const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (LIST && r >= a.meta->np) return;
   int64_t at = r < a.rows ? r : -1;
+  if (LIST) at = a.list[r];
+  const T *row = (const T *)a.src + (at < 0 ? 0 : at) * a.ld;
+  const int width = at < 0 ? 0 : a.width;
   float scale = 1.0f;
   int e = 0;
   if (LIST) {
-    at = a.list[r];
     e = a.eh[r];
     scale = ldexpf(a.cs[r], e - a.meta->ec);
   } else if (P == 2) {
-    e = exponent_of((uint32_t)a.meta->wbits);
+    e = a.meta->ew;
   }
-  const T *row = (const T *)a.src + (at < 0 ? 0 : at) * a.ld;
-  const int width = at < 0 ? 0 : a.width;
   uint16_t *out = a.out + (int64_t)r * a.kp;
   for (int k = lane * 8; k < a.kp; k += 512) {
     float f[8];
@@ -359,8 +391,8 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
 
 // Four columns of 16 lanes, transposed.  __restrict__ tells the compiler that the loads to LDS that are under way write
-// elsewhere (the barriers see to that): without it it waits for them before each read (4096 x 50257 x 768 bf16: 967 us,
-// TR us so).
+// elsewhere (the barriers see to that): without it it waits for them before each read (8192 x 128256 x 4096 bf16: 20.6 ms,
+// 19.7 ms so).
 __device__ __forceinline__ s16x4 read_tr(const lds_s16x4 __restrict__ p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
 
 // One operand of a tile, N of its rows, by TH threads of which a wave multiplies W of N / W rows.
@@ -548,7 +580,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
     const int n = n0 + c.col(j);
     const bool in = n < np;
     if (GRAD) {
-      const RowPrm p = in ? a.prm[n] : RowPrm{0.0f, 0.0f, 0.0f, 0.0f};
+      const RowPrm p = in ? a.prm[n] : RowPrm{0.0f, 0.0f, 0.0f, 0};
       const int tv = in ? a.tgt[n] - a.v0 - m0 : -1;
       const Power pw = power_of(a.scale);
 #pragma unroll
@@ -560,7 +592,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
           for (int q = 0; q < 4; ++q) {
             const int m = c.row(i, e + q);
             float x = c.acc[i][j][e + q];
-            if (F16) x *= p.f;
+            if (F16) x = ldexpf(x, p.e);
             g[q] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
             if (m == tv) g[q] += p.one;
             if (p.one == 0.0f || m0 + m >= a.valid) g[q] = 0.0f;
@@ -569,7 +601,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
           }
         }
     } else {
-      const float f = F16 && in ? ldexpf(1.0f, a.eh[n] + exponent_of((uint32_t)a.meta->wbits) - 2 * kTop) : 1.0f;
+      const int ex = F16 && in ? a.eh[n] + a.meta->ew - 2 * kTop : 0;
       const float k2 = power_of(a.scale).k;
       float m = -INFINITY;
 #pragma unroll
@@ -577,7 +609,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float x = c.acc[i][j][e];
-          if (F16) x *= f;
+          if (F16) x = ldexpf(x, ex);
           if (!whole && m0 + c.row(i, e) >= a.valid) x = -INFINITY;
           c.acc[i][j][e] = x;
           m = fmaxf(m, x);
@@ -761,12 +793,13 @@ __global__ __launch_bounds__(512) void k_few_join(Few a) {
   }
 }
 
-// (m, z) of the listed rows from the units' and their log-probabilities; 64 rows a workgroup, whose waves share the units.
+// (m, z) of the listed rows from the units' and their log-probabilities; 16 rows a workgroup, whose lanes share the units
+// (64 rows: 4096 x 50257 23 us, JOIN us so).
 __global__ __launch_bounds__(1024) void k_join(const Meta *meta, const int *list, const float2 *part, const float *xt,
                                                int64_t tcap, int units, float scale, float *logp, float2 *stats) {
-  __shared__ float2 lds[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
-  if ((int)blockIdx.x * 64 >= meta->np) return;
+  __shared__ float2 lds[16][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 16 + (lane & 15);
+  if ((int)blockIdx.x * 16 >= meta->np) return;
   const float k2 = power_of(scale).k;
   auto join = [&](float2 a, float2 b) {
     const float m = fmaxf(a.x, b.x), base = m == -INFINITY ? 0.0f : m;
@@ -775,10 +808,20 @@ __global__ __launch_bounds__(1024) void k_join(const Meta *meta, const int *list
                          (b.y == 0.0f ? 0.0f : b.y * __builtin_amdgcn_exp2f((b.x - base) * k2))};
   };
   float2 s{-INFINITY, 0.0f};
-  for (int u = wave; u < units; u += 16) s = join(s, part[u * tcap + n]);
-  lds[wave][lane] = s;
+  constexpr int U = 4;
+  for (int u = wave * 4 + (lane >> 4); u < units; u += 64 * U) {
+    float2 p[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) p[i] = u + i * 64 < units ? part[(u + i * 64) * tcap + n] : float2{-INFINITY, 0.0f};
+#pragma unroll
+    for (int i = 0; i < U; ++i) s = join(s, p[i]);
+  }
+#pragma unroll
+  for (int d = 16; d < 64; d <<= 1) s = join(s, float2{__shfl_xor(s.x, d, 64), __shfl_xor(s.y, d, 64)});
+  if (lane < 16) lds[wave][lane] = s;
   __syncthreads();
-  if (wave) return;
+  if (threadIdx.x >= 16) return;
+  s = lds[0][lane];
   for (int w = 1; w < 16; ++w) s = join(s, lds[w][lane]);
   const int t = list[n];
   if (t < 0) return;
@@ -798,7 +841,7 @@ struct Back {
   int steps, per, splits;  // stages of the piece, of a split
   int blocks;              // workgroups at most, a multiple of 8 (0: not wanted)
   bool first;
-  float *acc;  // [splits][tcap][kp]
+  float *acc;     // [splits][tcap][kp]
   int kp;
   // dW = G^T H (fp32: H times the rows' factors)
   Operand h;
@@ -832,6 +875,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
     c.template run<true, true>(lds, at_row(a.g, k0, m0), at_row(a.h, k0, n0), C::BM, a.kp - n0, steps * kStep, steps * kStep, steps);
   if (hidden) {
     float *to = a.acc + (part * a.tcap + m0) * a.kp + n0;
+    const int ew = F16 ? a.meta->ew - 2 * kTop : 0;
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
       if (n0 + c.col(j) >= a.kp) continue;
@@ -842,7 +886,8 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
           const int m = c.row(i, e);
           if (m0 + m >= np) continue;
           float *p = to + (int64_t)m * a.kp + c.col(j);
-          *p = a.first ? c.acc[i][j][e] : *p + c.acc[i][j][e];
+          const float v = F16 ? ldexpf(c.acc[i][j][e], ew) : c.acc[i][j][e];
+          *p = a.first ? v : *p + v;
         }
     }
   } else {
@@ -868,7 +913,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
 
 // dH: the splits' sums in order; zeros for masked rows
 template <typename T>
-__global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float *rowf, const float *acc, int64_t tcap, int kp, int splits, int rows,
+__global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float *cs, const float *acc, int64_t tcap, int kp, int splits, int rows,
                                                      int width, T *out, int64_t ld) {
   const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (t >= rows) return;
@@ -889,7 +934,7 @@ __global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float
       }
       if (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= rowf[p];
+        for (int i = 0; i < 8; ++i) f[i] *= cs[p];
       }
     }
     if (k + 8 <= width) {
@@ -907,8 +952,8 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // How a call is cut, and where its parts lie in the workspace.
 struct Plan {
   bool f16, copy, large;
-  int64_t batch, n, tcap, kp, piece, units, splits, planes;
-  int64_t list, pos, tgt, seg, cnt, meta, hc, eh, part, xt, prm, rowf, cs, hs, wc, g, acc, bytes;
+  int64_t batch, n, tcap, kp, piece, pieces, units, splits, planes;
+  int64_t list, pos, tgt, seg, cnt, meta, hc, eh, part, xt, prm, cs, hs, wc, g, acc, bytes;
 };
 
 Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
@@ -927,8 +972,8 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   if (grad) most = std::min(most, ((int64_t)1 << 27) / (p.tcap * p.planes));
   if (grad || p.copy) most = std::min(most, ((int64_t)1 << 27) / (p.kp * p.planes));
   if (most < x->vocab) most = std::max<int64_t>(most / 256 * 256, 256);
-  const int64_t pieces = (x->vocab + most - 1) / most;
-  p.piece = up((x->vocab + pieces - 1) / pieces, 256);
+  p.pieces = (x->vocab + most - 1) / most;
+  p.piece = up((x->vocab + p.pieces - 1) / p.pieces, 256);
   p.units = up(x->vocab, 128) / 64;
   p.large = x->rows > kSmallRows;
   p.splits = 1;
@@ -960,7 +1005,6 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     p.xt = take(4 * p.tcap);
   } else {
     p.prm = take(sizeof(RowPrm) * p.tcap);
-    p.rowf = take(4 * p.tcap);
     p.cs = take(4 * p.tcap);
     if (dweight && p.f16) p.hs = take(2 * p.planes * p.tcap * p.kp);
     p.g = take(2 * p.planes * p.tcap * p.piece);
@@ -1005,12 +1049,18 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
                      Live{x->targets, dlogp, (int32_t)x->index, (int32_t)x->vocab, (int32_t)p.n, (int32_t)p.batch, list,
                           ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<int>(work, p.seg), ptr<int>(work, p.cnt), meta, logp,
                           (float2 *)stats});
-  if (p.f16)
-    hipLaunchKernelGGL(k_absmax, dim3((unsigned)std::min<int64_t>(2048, (x->vocab + 3) / 4)), dim3(256), 0, st,
-                       (const float *)x->weight, x->ld_weight, (int)x->vocab, (int)x->width, meta);
+  if (p.f16) {
+    const float *w = (const float *)x->weight;
+    const bool flat = x->ld_weight == x->width && x->vocab * x->width % 4 == 0 && (uintptr_t)w % 16 == 0;
+    const dim3 grid((unsigned)std::min<int64_t>(2048, (x->vocab + 3) / 4));
+    if (flat)
+      hipLaunchKernelGGL(k_largest<true>, grid, dim3(256), 0, st, w, x->ld_weight, x->vocab, (int)x->width, meta);
+    else
+      hipLaunchKernelGGL(k_largest<false>, grid, dim3(256), 0, st, w, x->ld_weight, x->vocab, (int)x->width, meta);
+  }
   const Gather g{x->hidden, x->ld_hidden, (int)x->width, (int)p.kp, list, meta, ptr<uint16_t>(work, p.hc), p.tcap * p.kp,
                  ptr<int>(work, p.eh), (const float2 *)stats_in, dlogp, x->scale,
-                 dlogp ? ptr<RowPrm>(work, p.prm) : nullptr, ptr<float>(work, p.rowf), ptr<float>(work, p.cs)};
+                 dlogp ? ptr<RowPrm>(work, p.prm) : nullptr, ptr<float>(work, p.cs)};
   if (p.f16)
     hipLaunchKernelGGL(k_gather<float>, dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, g);
   else
@@ -1131,7 +1181,7 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
     a.xt = ptr<float>(work, p.xt);
     run_logits<false>(p, a, up(x->rows, kStep), st);
   }
-  hipLaunchKernelGGL(k_join, dim3((unsigned)(p.tcap / 64)), dim3(1024), 0, st, ptr<Meta>(work, p.meta), ptr<int>(work, p.list),
+  hipLaunchKernelGGL(k_join, dim3((unsigned)(p.tcap / 16)), dim3(1024), 0, st, ptr<Meta>(work, p.meta), ptr<int>(work, p.list),
                      ptr<float2>(work, p.part), ptr<float>(work, p.xt), p.tcap, (int)p.units, x->scale, logp,
                      (float2 *)stats);
   return train_launched();
@@ -1210,11 +1260,11 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   if (dhidden && x->rows) {
     const dim3 grid((unsigned)((x->rows + 3) / 4));
     if (p.f16)
-      hipLaunchKernelGGL(k_dhidden_out<float>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.rowf), ptr<float>(work, p.acc),
+      hipLaunchKernelGGL(k_dhidden_out<float>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.cs), ptr<float>(work, p.acc),
                          p.tcap,
                          (int)p.kp, (int)p.splits, (int)x->rows, (int)width, (float *)dhidden, ld_dhidden);
     else
-      hipLaunchKernelGGL(k_dhidden_out<bf16>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.rowf), ptr<float>(work, p.acc),
+      hipLaunchKernelGGL(k_dhidden_out<bf16>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.cs), ptr<float>(work, p.acc),
                          p.tcap,
                          (int)p.kp, (int)p.splits, (int)x->rows, (int)width, (bf16 *)dhidden, ld_dhidden);
   }
