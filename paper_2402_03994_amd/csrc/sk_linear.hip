@@ -46,7 +46,7 @@ struct Meta {
   int ec;  // exponent bound of dlogp scale H
 };
 
-// A listed row in the gradient: G = one ? one [v = target] + w exp(scale (x - m)) : 0, logits being acc 2^e.
+// A listed row in the gradient: G = one ? one [v = target] + w exp(scale (x - m)) : 0, logits being acc 2^(e + ew).
 struct RowPrm {
   float m, w, one;
   int e;
@@ -86,6 +86,24 @@ __device__ __forceinline__ void row_part(const T *row, int k, int width, float *
 }
 
 // --- the list of rows ---------------------------------------------------------------------------------------
+// a wave's largest finite |x| of a row, as its exponent
+template <typename T>
+__device__ __forceinline__ int row_exponent(const T *row, int width) {
+  const int lane = threadIdx.x & 63;
+  float big = 0.0f;
+  for (int k = lane * 8; k < width; k += 1024) {
+    float f[8], g[8];
+    row_part<8>(row, k, width, f);
+    row_part<8>(row, k + 512, width, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      big = fmaxf(big, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.0f);
+      big = fmaxf(big, fabsf(g[i]) < INFINITY ? fabsf(g[i]) : 0.0f);
+    }
+  }
+  return exponent_of(wave_all(big, OpMax()));
+}
+
 struct Live {
   const void *targets;
   const float *dlogp;  // NULL: forward
@@ -94,7 +112,15 @@ struct Live {
   Meta *meta;
   float *logp;
   float2 *stats;
+  // fp32: the workgroups behind the first look for the largest finite |W|; as one long row where its rows have no gaps
+  const float *w;
+  int64_t ldw;
+  int width;
+  bool flat;
+  int *most;  // [workgroups - 1]
 };
+constexpr int kMost = 512;
+
 
 __device__ __forceinline__ int wave_scan(int v, int lane) {  // inclusive
 #pragma unroll
@@ -105,10 +131,45 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {  // inclusive
   return v;
 }
 
-// One workgroup: counts of 64 rows each, their sums within the examples, the examples' starts, the list.  A wave has four
-// chunks of 64 rows under way (8192 rows: 17 us one after another, LIVE us so).
+// exponent of the largest finite |W| that workgroup b of n meets
+__device__ __forceinline__ void largest(const Live &a, int b, int n, int *lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int e = INT_MIN / 2;
+  if (a.flat) {
+    constexpr int U = 4;
+    const f32x4 *p = (const f32x4 *)a.w;
+    const int64_t all = (int64_t)a.vocab * a.width / 4, step = (int64_t)n * 1024;
+    float big = 0.0f;
+    for (int64_t i = (int64_t)b * 1024 + threadIdx.x; i < all; i += U * step) {
+      f32x4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = p[i + u * step < all ? i + u * step : i];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) big = fmaxf(big, fabsf(v[u][k]) < INFINITY ? fabsf(v[u][k]) : 0.0f);
+    }
+    e = exponent_of(wave_all(big, OpMax()));
+  } else {
+    for (int64_t r = b * 16 + wave; r < a.vocab; r += n * 16) e = max(e, row_exponent(a.w + r * a.ldw, a.width));
+  }
+  if (lane == 0) lds[wave] = e;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) e = max(e, lds[i]);
+    a.most[b] = e;
+  }
+}
+
+// The first workgroup: counts of 64 rows each, their sums within the examples, the examples' starts, the list.  A wave has
+// four chunks of 64 rows under way (8192 rows: 17 us one after another, 14.5 us so).
 __global__ __launch_bounds__(1024) void k_live(Live a) {
   constexpr int U = 4;
+  __shared__ int lds[16];
+  if (blockIdx.x > 0) {
+    largest(a, blockIdx.x - 1, gridDim.x - 1, lds);
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = (a.n + 63) / 64, chunks = per * a.batch;
   // the row (-1: none) and target (-1: masked) of this lane in chunk c
@@ -188,24 +249,6 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
 }
 
 // --- operands -----------------------------------------------------------------------------------------------
-// a wave's largest finite |x| of a row, as its exponent
-template <typename T>
-__device__ __forceinline__ int row_exponent(const T *row, int width) {
-  const int lane = threadIdx.x & 63;
-  float big = 0.0f;
-  for (int k = lane * 8; k < width; k += 1024) {
-    float f[8], g[8];
-    row_part<8>(row, k, width, f);
-    row_part<8>(row, k + 512, width, g);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      big = fmaxf(big, fabsf(f[i]) < INFINITY ? fabsf(f[i]) : 0.0f);
-      big = fmaxf(big, fabsf(g[i]) < INFINITY ? fabsf(g[i]) : 0.0f);
-    }
-  }
-  return exponent_of(wave_all(big, OpMax()));
-}
-
 __device__ __forceinline__ void raise(int *most, int v) {  // an atomic only where it can change something
   if (v > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, v);
 }
@@ -219,6 +262,8 @@ struct Gather {
   uint16_t *hc;
   int64_t plane;
   int *eh;
+  const int *most;
+  int parts;
   // gradient only
   const float2 *stats;
   const float *dlogp;
@@ -232,6 +277,13 @@ struct Gather {
 template <typename T>
 __global__ __launch_bounds__(256) void k_gather(Gather a) {
   const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (sizeof(T) == 4 && n == 0) {
+    int e = INT_MIN / 2;
+    for (int i = lane; i < a.parts; i += 64) e = max(e, a.most[i]);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) e = max(e, __shfl_xor(e, d, 64));
+    if (lane == 0) a.meta->ew = e;
+  }
   if (n >= a.meta->np) return;
   const int t = a.list[n];
   const T *row = (const T *)a.hidden + (int64_t)(t < 0 ? 0 : t) * a.ld;
@@ -261,7 +313,7 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
     }
   }
   if (!a.prm || lane != 0) return;
-  RowPrm p{0.0f, 0.0f, 0.0f, sizeof(T) == 4 ? e + a.meta->ew - 2 * kTop : 0};
+  RowPrm p{0.0f, 0.0f, 0.0f, e - 2 * kTop};
   float c = 0.0f;
   if (t >= 0) {
     const float2 s = a.stats[t];
@@ -279,38 +331,6 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
   a.prm[n] = p;
 }
 
-// The exponent of the largest finite |W|, over all rows; without gaps between them (a multiple of 4 entries, 16-byte
-// aligned) W is one long row.  One atomic a workgroup, and only where it can change something (50257 x 768: 68 us with one
-// a wave, ABSMAX us so).
-template <bool FLAT>
-__global__ __launch_bounds__(256) void k_largest(const float *w, int64_t ld, int64_t rows, int width, Meta *meta) {
-  __shared__ int lds[4];
-  const int lane = threadIdx.x & 63;
-  int e;
-  if (FLAT) {
-    constexpr int U = 4;
-    const f32x4 *p = (const f32x4 *)w;
-    const int64_t n = rows * width / 4, step = (int64_t)gridDim.x * 256;
-    float big = 0.0f;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += U * step) {
-      f32x4 v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = p[i + u * step < n ? i + u * step : i];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) big = fmaxf(big, fabsf(v[u][k]) < INFINITY ? fabsf(v[u][k]) : 0.0f);
-    }
-    e = exponent_of(wave_all(big, OpMax()));
-  } else {
-    e = INT_MIN / 2;
-    for (int64_t r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) e = max(e, row_exponent(w + r * ld, width));
-  }
-  if (lane == 0) lds[threadIdx.x >> 6] = e;
-  __syncthreads();
-  if (threadIdx.x == 0) raise(&meta->ew, max(max(lds[0], lds[1]), max(lds[2], lds[3])));
-}
-
 struct Prep {
   const void *src;
   int64_t ld;
@@ -325,9 +345,9 @@ struct Prep {
 
 // Rows as an operand takes them: padded with zeros to kp columns, fp32 split.  A wave a row, up to a multiple of 64 rows.
 template <typename T, bool LIST>
-__global__ __launch_bounds__(256) void k_prep(Prep a) {
+__device__ __forceinline__ void prep(const Prep &a, int block) {
   constexpr int P = sizeof(T) == 4 ? 2 : 1;
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r = block * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (LIST && r >= a.meta->np) return;
   int64_t at = r < a.rows ? r : -1;
   if (LIST) at = a.list[r];
@@ -359,6 +379,15 @@ __global__ __launch_bounds__(256) void k_prep(Prep a) {
   }
 }
 
+// H by the first `blocks` workgroups, W by the others
+template <typename T>
+__global__ __launch_bounds__(256) void k_prep(Prep h, Prep w, int blocks) {
+  if ((int)blockIdx.x < blocks)
+    prep<T, true>(h, blockIdx.x);
+  else
+    prep<T, false>(w, blockIdx.x - blocks);
+}
+
 // --- the product --------------------------------------------------------------------------------------------
 // Rows of an operand: up to two planes of 16-bit numbers, K contiguous.
 struct Operand {
@@ -371,10 +400,9 @@ struct Operand {
 // behind the barrier that frees its buffer and have the products of a whole stage to arrive.  Two workgroups share a
 // CU, so that one's epilogue lies beside the other's products.  Alone (8192^3, and 16384 x 2560 x 768, bf16): 128 x 192
 // 1150 and 803 TFLOP/s, 128 x 128 1108 and 773, one 256 x 256 a CU 1240 and 729, the library's 1290 and 817.  In the
-// operators (4096 x 50257 x 768 and 8192 x 128256 x 4096): gradients 819 us and 15.5 ms with 128 x 192, 891 us and 17.8
-// ms with 128 x 128, 1120 us and 15.9 ms with 256 x 256; log-probabilities 225 us and 4.47 ms, 243 us and 5.0 ms, 226 us
-// and 4.5 ms.  Up to 1024 rows the smaller tiles fill the chip better (gradients of 200 x 50257 x 768: 134 us, 146 with
-// the larger ones; 1000: 301 and 299).
+// operators (4096 x 50257 x 768 and 8192 x 128256 x 4096): log-probabilities 225 us and 4.47 ms with 128 x 192, 243 us and
+// 5.0 ms with 128 x 128, 226 us and 4.5 ms with 256 x 256.  Up to 1024 rows the smaller tiles fill the chip better
+// (gradients of 200 x 50257 x 768: 134 us, 146 with the larger ones; 1000: 301 and 299).
 template <int BM_, int BN_, int WM_, int WN_>
 struct Tiling {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM * WN, TH = NW * 64;
@@ -383,7 +411,14 @@ struct Tiling {
 };
 using Large = Tiling<128, 192, 2, 2>;
 using Small = Tiling<128, 128, 2, 2>;
+using Huge = Tiling<256, 256, 2, 4>;
 constexpr int64_t kSmallRows = 1024;  // rows up to which the smaller tiles are taken
+// Where the gradients' products have both rows and tiles in plenty, one 256 x 256 tile a CU asks for 0.6 times as much
+// of the caches (which the products miss by the distance their tiles drift apart: 5 TB/s at 8192 x 128256 x 4096): 15.1
+// ms, 14.1 ms there; 4096 x 50257 x 4096 3.09 and 2.87 ms; 8000 x 32000 x 5000 fp32 14.6 and 13.8 ms.  With fewer tiles
+// than four rounds of the chip, or short sums, it loses as much (16384 x 50257 x 1024: 3.53 and 3.95 ms; four examples
+// of 512 x 50257 x 4096 2.12 and 2.35 ms).
+constexpr int64_t kHugeRows = 4096, kHugeTiles = 1024;
 
 #if defined(__HIP_DEVICE_COMPILE__)
 typedef __attribute__((address_space(3))) void *lds_ptr;
@@ -402,17 +437,17 @@ __device__ __forceinline__ s16x4 read_tr(const lds_s16x4 __restrict__ p) { retur
 // KM true: the matrix has K for its rows and the operand's rows for its columns.  A stage is 64 rows of N columns, which
 // ds_read_b64_tr_b16 transposes: of 16 lanes, lane 4 r + q gives the address of four columns 4 q of row r, and lane i gets
 // column i of the four rows.  Chunks are exchanged so that the eight rows of 64 bytes that a wave reads at a time fill
-// the banks twice over: four rows lie 256 bytes (N = 128) or 384 bytes (192) apart.
+// the banks twice over: rows lie 256 bytes (N = 128), 384 (192) or 512 (256) apart.
 template <int N, int W, int TH, bool KM>
 struct Side {
   static constexpr int CH = KM ? N / 8 : kStep / 8;  // chunks of an LDS row
   static constexpr int L = N * kStep / 8 / TH;       // loads of a thread and stage
   static constexpr int T = N / W / 32;
-  static_assert(!KM || N == 128 || N == 192, "exchanges are worked out for these");
+  static_assert(!KM || N == 128 || N == 192 || N == 256, "exchanges are worked out for these");
   int off[L], ld, limit, last;
 
   static __device__ __forceinline__ int swz(int row) {
-    return !KM ? (row >> 1) & 7 : N == 128 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
+    return !KM ? (row >> 1) & 7 : N != 192 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
   }
   // rows: how many there are from the tile's first on (those behind repeat one of them; a multiple of 8 with KM); depth: K
   // rows that there are (KM)
@@ -575,6 +610,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   Core<C, F16> c;
   c.template run<false, false>(lds, at_row(a.w, m0), at_row(a.h, n0), a.valid - m0, np - n0, 0, 0, a.kp / kStep);
   const bool whole = m0 + C::BM <= a.valid;
+  const int ew = F16 ? a.meta->ew : 0;
 #pragma unroll
   for (int j = 0; j < C::TN; ++j) {
     const int n = n0 + c.col(j);
@@ -592,7 +628,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
           for (int q = 0; q < 4; ++q) {
             const int m = c.row(i, e + q);
             float x = c.acc[i][j][e + q];
-            if (F16) x = ldexpf(x, p.e);
+            if (F16) x = ldexpf(x, p.e + ew);
             g[q] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
             if (m == tv) g[q] += p.one;
             if (p.one == 0.0f || m0 + m >= a.valid) g[q] = 0.0f;
@@ -601,7 +637,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
           }
         }
     } else {
-      const int ex = F16 && in ? a.eh[n] + a.meta->ew - 2 * kTop : 0;
+      const int ex = F16 && in ? a.eh[n] + ew - 2 * kTop : 0;
       const float k2 = power_of(a.scale).k;
       float m = -INFINITY;
 #pragma unroll
@@ -951,9 +987,9 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // How a call is cut, and where its parts lie in the workspace.
 struct Plan {
-  bool f16, copy, large;
+  bool f16, copy, large, huge;
   int64_t batch, n, tcap, kp, piece, pieces, units, splits, planes;
-  int64_t list, pos, tgt, seg, cnt, meta, hc, eh, part, xt, prm, cs, hs, wc, g, acc, bytes;
+  int64_t list, pos, tgt, seg, cnt, most, meta, hc, eh, part, xt, prm, cs, hs, wc, g, acc, bytes;
 };
 
 Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
@@ -976,6 +1012,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.piece = up((x->vocab + p.pieces - 1) / p.pieces, 256);
   p.units = up(x->vocab, 128) / 64;
   p.large = x->rows > kSmallRows;
+  p.huge = p.n >= kHugeRows && (p.tcap / 256 + batch * (p.piece / 256)) * (up(x->width, 256) / 256) >= kHugeTiles;
   p.splits = 1;
   if (grad) {
     // dH has few tiles with all of the piece to sum up, dW many with the rows: a part of a dH tile takes half of what each
@@ -996,6 +1033,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.tgt = take(4 * p.tcap);
   p.seg = take(4 * (batch + 1));
   p.cnt = take(4 * batch * ((p.n + 63) / 64));
+  p.most = take(4 * kMost);
   p.meta = take(sizeof(Meta));
   p.hc = take(2 * p.planes * p.tcap * p.kp);
   p.eh = take(4 * p.tcap);
@@ -1045,21 +1083,15 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
            hipStream_t st) {
   Meta *meta = ptr<Meta>(work, p.meta);
   int *list = ptr<int>(work, p.list);
-  hipLaunchKernelGGL(k_live, dim3(1), dim3(1024), 0, st,
+  const int parts = p.f16 ? (int)std::min<int64_t>(kMost, (x->vocab * x->width + 16383) / 16384) : 0;
+  const bool flat = x->ld_weight == x->width && x->vocab * x->width % 4 == 0 && (uintptr_t)x->weight % 16 == 0;
+  int *most = ptr<int>(work, p.most);
+  hipLaunchKernelGGL(k_live, dim3(1 + parts), dim3(1024), 0, st,
                      Live{x->targets, dlogp, (int32_t)x->index, (int32_t)x->vocab, (int32_t)p.n, (int32_t)p.batch, list,
                           ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<int>(work, p.seg), ptr<int>(work, p.cnt), meta, logp,
-                          (float2 *)stats});
-  if (p.f16) {
-    const float *w = (const float *)x->weight;
-    const bool flat = x->ld_weight == x->width && x->vocab * x->width % 4 == 0 && (uintptr_t)w % 16 == 0;
-    const dim3 grid((unsigned)std::min<int64_t>(2048, (x->vocab + 3) / 4));
-    if (flat)
-      hipLaunchKernelGGL(k_largest<true>, grid, dim3(256), 0, st, w, x->ld_weight, x->vocab, (int)x->width, meta);
-    else
-      hipLaunchKernelGGL(k_largest<false>, grid, dim3(256), 0, st, w, x->ld_weight, x->vocab, (int)x->width, meta);
-  }
+                          (float2 *)stats, (const float *)x->weight, x->ld_weight, (int)x->width, flat, most});
   const Gather g{x->hidden, x->ld_hidden, (int)x->width, (int)p.kp, list, meta, ptr<uint16_t>(work, p.hc), p.tcap * p.kp,
-                 ptr<int>(work, p.eh), (const float2 *)stats_in, dlogp, x->scale,
+                 ptr<int>(work, p.eh), most, parts, (const float2 *)stats_in, dlogp, x->scale,
                  dlogp ? ptr<RowPrm>(work, p.prm) : nullptr, ptr<float>(work, p.cs)};
   if (p.f16)
     hipLaunchKernelGGL(k_gather<float>, dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, g);
@@ -1067,8 +1099,8 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
     hipLaunchKernelGGL(k_gather<bf16>, dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, g);
 }
 
-// W's rows from v0 on as an operand
-Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, void *work, hipStream_t st) {
+// W's rows from v0 on as an operand; what the same launch does for H, if anything
+Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, const Prep *h, void *work, hipStream_t st) {
   const void *src = (const char *)x->weight + v0 * x->ld_weight * (p.f16 ? 4 : 2);
   if (!p.copy) return Operand{{(const uint16_t *)src, (const uint16_t *)src}, x->ld_weight};
   Prep a{};
@@ -1080,11 +1112,12 @@ Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, vo
   a.meta = ptr<Meta>(work, p.meta);
   a.out = ptr<uint16_t>(work, p.wc);
   a.plane = p.piece * p.kp;
-  const dim3 grid((unsigned)(up(valid, 64) / 4));
+  const int blocks = h ? (int)(p.tcap / 4) : 0;
+  const dim3 grid((unsigned)(blocks + up(valid, 64) / 4));
   if (p.f16)
-    hipLaunchKernelGGL((k_prep<float, false>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_prep<float>, grid, dim3(256), 0, st, h ? *h : a, a, blocks);
   else
-    hipLaunchKernelGGL((k_prep<bf16, false>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_prep<bf16>, grid, dim3(256), 0, st, a, a, 0);
   return planes_of(a.out, a.plane, p.kp);
 }
 
@@ -1138,7 +1171,9 @@ void launch_back(const Plan &p, Back a, bool dhidden, bool dweight, sk_dtype odt
   }
 }
 void run_back(const Plan &p, const Back &a, bool dhidden, bool dweight, sk_dtype odt, hipStream_t st) {
-  if (p.large)
+  if (p.huge)
+    launch_back<Huge>(p, a, dhidden, dweight, odt, st);
+  else if (p.large)
     launch_back<Large>(p, a, dhidden, dweight, odt, st);
   else
     launch_back<Small>(p, a, dhidden, dweight, odt, st);
@@ -1176,7 +1211,7 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
   begin(x, p, nullptr, nullptr, logp, stats, work, st);
   for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
     const int64_t valid = std::min(p.piece, x->vocab - v0);
-    Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, work, st), work);
+    Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, nullptr, work, st), work);
     a.part = ptr<float2>(work, p.part);
     a.xt = ptr<float>(work, p.xt);
     run_logits<false>(p, a, up(x->rows, kStep), st);
@@ -1210,23 +1245,21 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   begin(x, p, dlogp ? dlogp : (const float *)work, stats, nullptr, nullptr, work, st);
   Meta *meta = ptr<Meta>(work, p.meta);
   const int64_t width = x->width;
-  if (dweight && x->rows && p.f16) {
-    Prep a{};
-    a.src = x->hidden;
-    a.ld = x->ld_hidden;
-    a.width = (int)width;
-    a.meta = meta;
-    a.list = ptr<int>(work, p.list);
-    a.eh = ptr<int>(work, p.eh);
-    a.cs = ptr<float>(work, p.cs);
-    a.kp = (int)p.kp;
-    a.out = ptr<uint16_t>(work, p.hs);
-    a.plane = p.tcap * p.kp;
-    hipLaunchKernelGGL((k_prep<float, true>), dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, a);
-  }
+  const bool hs = dweight && p.f16;  // dW of fp32 takes H with the rows' factors
+  Prep h{};
+  h.src = x->hidden;
+  h.ld = x->ld_hidden;
+  h.width = (int)width;
+  h.kp = (int)p.kp;
+  h.meta = meta;
+  h.list = ptr<int>(work, p.list);
+  h.eh = ptr<int>(work, p.eh);
+  h.cs = ptr<float>(work, p.cs);
+  h.out = ptr<uint16_t>(work, p.hs);
+  h.plane = p.tcap * p.kp;
   for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
     const int64_t valid = std::min(p.piece, x->vocab - v0);
-    const Operand w = x->rows ? weights(x, p, v0, valid, work, st) : Operand{};
+    const Operand w = x->rows ? weights(x, p, v0, valid, hs && v0 == 0 ? &h : nullptr, work, st) : Operand{};
     if (x->rows) {
       Logit a = logit_of(x, p, v0, valid, w, work);
       a.prm = ptr<RowPrm>(work, p.prm);
