@@ -589,12 +589,13 @@ struct Logit {
   const int *tgt, *eh;
   float scale;
   // forward
-  float2 *part;  // [vocabulary / 64][tcap]
+  float2 *part;  // [piece / 64][tcap]
   float *xt;
   int64_t tcap;
   // gradient
   const RowPrm *prm;
   uint16_t *g;  // [tcap][piece]
+  float *rest;  // [tcap], bf16: what the rounding of the target's entry has left
   int64_t gplane, piece;
 };
 
@@ -632,6 +633,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
             g[q] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
             if (m == tv) g[q] += p.one;
             if (p.one == 0.0f || m0 + m >= a.valid) g[q] = 0.0f;
+            if (!F16 && m == tv) a.rest[n] = g[q] - to_f32(bf16{(uint16_t)bf16_bits(g[q])});
             // both halves of a split number, or the bf16's bits
             c.acc[i][j][e + q] = __uint_as_float(F16 ? split(g[q]) : bf16_bits(g[q]));
           }
@@ -662,7 +664,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
       }
       z += __shfl_xor(z, 32, 64);
       if (in) {
-        const int64_t unit = (a.v0 + m0) / (C::BM / C::WM) + c.wm;
+        const int64_t unit = m0 / (C::BM / C::WM) + c.wm;
         if (c.fk == 0) a.part[unit * a.tcap + n] = float2{m, z};
         const int tv = a.tgt[n] - a.v0 - m0 - c.wm * (C::BM / C::WM);
         if (tv >= 0 && tv < C::BM / C::WM) {
@@ -729,19 +731,30 @@ struct Few {
   int units;
   float *logp;
   float2 *stats;
+  // gradient: G of a piece
+  int v0, valid;
+  const Meta *meta;
+  const int *pos, *list;
+  const RowPrm *prm;
+  uint16_t *g;
+  int64_t gplane, piece;
+  float *rest;
 };
 
 // Logits of up to 16 rows by 16 entries of the vocabulary a wave.  Lane l holds row l % 16 of both operands; its eight
 // (fp32: four) columns from 8 (l / 16) on are one operand of v_mfma_f32_16x16x32_bf16 (element i of each lane one of
-// v_mfma_f32_16x16x4_f32, in which fp32 stays fp32).  Bound by reading W: SKINNY.
-template <typename T>
+// v_mfma_f32_16x16x4_f32, in which fp32 stays fp32).  Bound by reading W: 50257 x 768 bf16
+// 19 us, 4.1 TB/s.  GRAD: G from the same logits to the bit, so that a small 1 - p of the target keeps what it has (logits of
+// the split product beside these statistics were off by 5e-6 of it where p = 0.9).
+template <typename T, bool GRAD>
 __global__ __launch_bounds__(256) void k_few(Few a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int N = Vec<T>::N, K = 4 * N, U = 4;  // columns of a lane, of a step, steps whose loads are under way together
   __shared__ float2 lds[4][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-  const int v0 = blockIdx.x * kFewUnit + wave * 16, v = v0 + r;
-  const int target = r < a.rows ? target_of(a.targets, a.index, r, a.vocab) : -1;
+  const int v0 = a.v0 + blockIdx.x * kFewUnit + wave * 16, v = v0 + r;
+  const int n = GRAD && r < a.rows ? a.pos[r] : -1;
+  const int target = r < a.rows && (!GRAD || n >= 0) ? target_of(a.targets, a.index, r, a.vocab) : -1;
   const T *w = (const T *)a.weight + (int64_t)(v < a.vocab ? v : a.vocab - 1) * a.ld_weight;
   const T *h = (const T *)a.hidden + (int64_t)(target >= 0 ? r : 0) * a.ld_hidden;
   const int hw = target >= 0 ? a.width : 0;  // masked rows are not read
@@ -774,6 +787,32 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
     }
   }
   // this lane: entries v0 + 4 q + e of row r
+  if constexpr (GRAD) {
+    constexpr bool F16 = sizeof(T) == 4;
+    const int at = v0 - a.v0 + q * 4;
+    if (n >= 0) {
+      const RowPrm p = a.prm[n];
+      const Power pw = power_of(a.scale);
+      float g[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        g[e] = p.w * entry_exp<T>(acc[e] - p.m, pw);
+        if (v0 + q * 4 + e == target) g[e] += p.one;
+        if (p.one == 0.0f || at + e >= a.valid) g[e] = 0.0f;
+        if (!F16 && v0 + q * 4 + e == target) a.rest[n] = g[e] - to_f32(bf16{(uint16_t)bf16_bits(g[e])});
+      }
+#pragma unroll
+      for (int plane = 0; plane < (F16 ? 2 : 1); ++plane)
+        *(u32x2 *)(a.g + plane * a.gplane + n * a.piece + at) = u32x2{two<F16>(g[0], g[1], plane), two<F16>(g[2], g[3], plane)};
+    }
+    // rows that only fill the list
+    for (int i = threadIdx.x >> 3; i < a.meta->np; i += 32)
+      if (a.list[i] < 0)
+#pragma unroll
+        for (int plane = 0; plane < (F16 ? 2 : 1); ++plane)
+          *(u32x4 *)(a.g + plane * a.gplane + i * a.piece + blockIdx.x * kFewUnit + (threadIdx.x & 7) * 8) = u32x4{0, 0, 0, 0};
+    return;
+  }
   const float k2 = power_of(a.scale).k;
   float m = -INFINITY;
 #pragma unroll
@@ -829,26 +868,38 @@ __global__ __launch_bounds__(512) void k_few_join(Few a) {
   }
 }
 
-// (m, z) of the listed rows from the units' and their log-probabilities; 16 rows a workgroup, whose lanes share the units
-// (64 rows: 4096 x 50257 23 us, JOIN us so).
-__global__ __launch_bounds__(1024) void k_join(const Meta *meta, const int *list, const float2 *part, const float *xt,
-                                               int64_t tcap, int units, float scale, float *logp, float2 *stats) {
+// (m, z) of the listed rows from those of a piece's units and of the pieces before, at the end their log-probabilities; 16
+// rows a workgroup, whose lanes share the units (64 rows a workgroup: 4096 x 50257 23 us, 8 us so).
+struct Join {
+  const Meta *meta;
+  const int *list;
+  const float2 *part;
+  const float *xt;
+  int64_t tcap;
+  int units;
+  float scale;
+  bool first, last;
+  float2 *run;  // [tcap]
+  float *logp;
+  float2 *stats;
+};
+__global__ __launch_bounds__(1024) void k_join(Join a) {
   __shared__ float2 lds[16][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 16 + (lane & 15);
-  if ((int)blockIdx.x * 16 >= meta->np) return;
-  const float k2 = power_of(scale).k;
-  auto join = [&](float2 a, float2 b) {
-    const float m = fmaxf(a.x, b.x), base = m == -INFINITY ? 0.0f : m;
+  if ((int)blockIdx.x * 16 >= a.meta->np) return;  // np is a multiple of 64
+  const float k2 = power_of(a.scale).k;
+  auto join = [&](float2 p, float2 q) {
+    const float m = fmaxf(p.x, q.x), base = m == -INFINITY ? 0.0f : m;
     // a sum of nothing is left out: its exponent may be a NaN
-    return float2{m, (a.y == 0.0f ? 0.0f : a.y * __builtin_amdgcn_exp2f((a.x - base) * k2)) +
-                         (b.y == 0.0f ? 0.0f : b.y * __builtin_amdgcn_exp2f((b.x - base) * k2))};
+    return float2{m, (p.y == 0.0f ? 0.0f : p.y * __builtin_amdgcn_exp2f((p.x - base) * k2)) +
+                         (q.y == 0.0f ? 0.0f : q.y * __builtin_amdgcn_exp2f((q.x - base) * k2))};
   };
   float2 s{-INFINITY, 0.0f};
   constexpr int U = 4;
-  for (int u = wave * 4 + (lane >> 4); u < units; u += 64 * U) {
+  for (int u = wave * 4 + (lane >> 4); u < a.units; u += 64 * U) {
     float2 p[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) p[i] = u + i * 64 < units ? part[(u + i * 64) * tcap + n] : float2{-INFINITY, 0.0f};
+    for (int i = 0; i < U; ++i) p[i] = u + i * 64 < a.units ? a.part[(u + i * 64) * a.tcap + n] : float2{-INFINITY, 0.0f};
 #pragma unroll
     for (int i = 0; i < U; ++i) s = join(s, p[i]);
   }
@@ -859,11 +910,16 @@ __global__ __launch_bounds__(1024) void k_join(const Meta *meta, const int *list
   if (threadIdx.x >= 16) return;
   s = lds[0][lane];
   for (int w = 1; w < 16; ++w) s = join(s, lds[w][lane]);
-  const int t = list[n];
+  if (!a.first) s = join(a.run[n], s);
+  if (!a.last) {
+    a.run[n] = s;
+    return;
+  }
+  const int t = a.list[n];
   if (t < 0) return;
   if (s.x == -INFINITY) s.x = 0.0f;
-  logp[t] = logp_of(xt[n], Stats{s.x, s.y}, scale);
-  if (stats) stats[t] = s;
+  a.logp[t] = logp_of(a.xt[n], Stats{s.x, s.y}, a.scale);
+  if (a.stats) a.stats[t] = s;
 }
 
 // What a piece adds to dH, and its rows of dW.
@@ -947,37 +1003,51 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
 #endif
 }
 
-// dH: the splits' sums in order; zeros for masked rows
+// dH: the splits' sums in order; zeros for masked rows.  fp32: times the row's factor.  bf16: with what the rounding of the
+// target's entry of G has left, since that entry is most of a row (errors of dH against 64 bits, of which 0.0017 are its
+// own rounding: 0.0022 to 0.0026 without, REST so).
+struct DHidden {
+  const int *pos, *tgt;
+  const float *cs, *rest;
+  const float *acc;
+  int64_t tcap;
+  int kp, splits, rows, width;
+  const void *w;
+  int64_t ldw;
+  void *out;
+  int64_t ld;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_dhidden_out(const int *pos, const float *cs, const float *acc, int64_t tcap, int kp, int splits, int rows,
-                                                     int width, T *out, int64_t ld) {
+__global__ __launch_bounds__(256) void k_dhidden_out(DHidden a) {
   const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (t >= rows) return;
-  const int p = pos[t];
-  T *o = out + t * ld;
-  for (int k = lane * 8; k < width; k += 512) {
-    float f[8] = {};
+  if (t >= a.rows) return;
+  const int p = a.pos[t];
+  T *o = (T *)a.out + t * a.ld;
+  const float f = p >= 0 ? (sizeof(T) == 4 ? a.cs[p] : a.rest[p]) : 0.0f;
+  const T *w = (const T *)a.w + (sizeof(T) == 2 && p >= 0 ? a.tgt[p] : 0) * a.ldw;
+  for (int k = lane * 8; k < a.width; k += 512) {
+    float v[8] = {};
     if (p >= 0) {
-      const float *a = acc + (int64_t)p * kp + k;
+      const float *x = a.acc + (int64_t)p * a.kp + k;
 #pragma unroll 4
-      for (int s = 0; s < splits; ++s, a += tcap * kp) {
+      for (int s = 0; s < a.splits; ++s, x += a.tcap * a.kp) {
 #pragma unroll
         for (int i = 0; i < 8; i += 4) {
-          const f32x4 v = *(const f32x4 *)(a + i);
+          const f32x4 y = *(const f32x4 *)(x + i);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) f[i + q] += v[q];
+          for (int q = 0; q < 4; ++q) v[i + q] += y[q];
         }
       }
-      if (sizeof(T) == 4) {
+      float r[8];
+      if (sizeof(T) == 2) row_part<8>(w, k, a.width, r);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= cs[p];
-      }
+      for (int i = 0; i < 8; ++i) v[i] = sizeof(T) == 4 ? v[i] * f : v[i] + f * r[i];
     }
-    if (k + 8 <= width) {
+    if (k + 8 <= a.width) {
 #pragma unroll
-      for (int i = 0; i < 8; i += Vec<T>::N) Vec<T>::store(o + k + i, Vec<T>::pack(f + i));
+      for (int i = 0; i < 8; i += Vec<T>::N) Vec<T>::store(o + k + i, Vec<T>::pack(v + i));
     } else {
-      for (int i = 0; k + i < width; ++i) o[k + i] = from_f32<T>(f[i]);
+      for (int i = 0; k + i < a.width; ++i) o[k + i] = from_f32<T>(v[i]);
     }
   }
 }
@@ -987,14 +1057,28 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // How a call is cut, and where its parts lie in the workspace.
 struct Plan {
-  bool f16, copy, large, huge;
+  bool f16, few, copy, large, huge;
   int64_t batch, n, tcap, kp, piece, pieces, units, splits, planes;
-  int64_t list, pos, tgt, seg, cnt, most, meta, hc, eh, part, xt, prm, cs, hs, wc, g, acc, bytes;
+  int64_t list, pos, tgt, seg, cnt, most, meta, hc, eh, part, xt, run, prm, cs, rest, hs, wc, g, acc, bytes;
 };
 
 Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
   Plan p{};
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t r = at;
+    at += up(bytes, 256);
+    return r;
+  };
   p.f16 = x->dtype == SK_F32;
+  p.units = (x->vocab + kFewUnit - 1) / kFewUnit;
+  p.few = !grad && x->rows <= kFew;
+  if (p.few) {
+    p.part = take(8 * p.units * kFew);
+    p.xt = take(4 * kFew);
+    p.bytes = at;
+    return p;
+  }
   p.planes = p.f16 ? 2 : 1;
   p.batch = batch;
   p.n = x->rows / batch;
@@ -1007,10 +1091,13 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   int64_t most = x->vocab;
   if (grad) most = std::min(most, ((int64_t)1 << 27) / (p.tcap * p.planes));
   if (grad || p.copy) most = std::min(most, ((int64_t)1 << 27) / (p.kp * p.planes));
+  // the tiles' (m, z) in 256 MB; grids below 2^32 threads
+  if (!grad) most = std::min(most, ((int64_t)1 << 31) / p.tcap);
+  most = std::min(most, ((int64_t)1 << 23) / (p.tcap / 128) * 128);
   if (most < x->vocab) most = std::max<int64_t>(most / 256 * 256, 256);
   p.pieces = (x->vocab + most - 1) / most;
   p.piece = up((x->vocab + p.pieces - 1) / p.pieces, 256);
-  p.units = up(x->vocab, 128) / 64;
+  p.units = p.piece / 64;
   p.large = x->rows > kSmallRows;
   p.huge = p.n >= kHugeRows && (p.tcap / 256 + batch * (p.piece / 256)) * (up(x->width, 256) / 256) >= kHugeTiles;
   p.splits = 1;
@@ -1022,12 +1109,6 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     const int64_t all = up(p.tcap, 128) / 128 * nt * steps + batch * (p.piece / 128) * nt * (up(p.n, kStep) / kStep);
     p.splits = std::max<int64_t>(1, std::min<int64_t>({(768 * steps + all / 2) / all, 32, steps / 4}));
   }
-  int64_t at = 0;
-  auto take = [&](int64_t bytes) {
-    const int64_t r = at;
-    at += up(bytes, 256);
-    return r;
-  };
   p.list = take(4 * p.tcap);
   p.pos = take(4 * x->rows);
   p.tgt = take(4 * p.tcap);
@@ -1041,9 +1122,11 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   if (!grad) {
     p.part = take(8 * p.units * p.tcap);
     p.xt = take(4 * p.tcap);
+    p.run = take(8 * p.tcap);
   } else {
     p.prm = take(sizeof(RowPrm) * p.tcap);
     p.cs = take(4 * p.tcap);
+    p.rest = take(4 * p.tcap);
     if (dweight && p.f16) p.hs = take(2 * p.planes * p.tcap * p.kp);
     p.g = take(2 * p.planes * p.tcap * p.piece);
     if (dhidden) p.acc = take(4 * p.splits * p.tcap * p.kp);
@@ -1197,14 +1280,15 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
   TrainGuard guard(x->device);
   if (!guard.ok) return train_no_device();
   hipStream_t st = (hipStream_t)stream;
-  if (x->rows <= kFew) {
-    const int units = (int)((x->vocab + kFewUnit - 1) / kFewUnit);
+  if (p.few) {
+    const int units = (int)p.units;
     const Few a{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)x->width,
-                (int)x->index, x->scale, ptr<float2>(work, p.part), ptr<float>(work, p.xt), units, logp, (float2 *)stats};
+                (int)x->index, x->scale, ptr<float2>(work, p.part), ptr<float>(work, p.xt), units, logp, (float2 *)stats, 0, 0, nullptr,
+                nullptr, nullptr, nullptr, nullptr, 0, 0, nullptr};
     if (p.f16)
-      hipLaunchKernelGGL(k_few<float>, dim3(units), dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_few<float, false>), dim3(units), dim3(256), 0, st, a);
     else
-      hipLaunchKernelGGL(k_few<bf16>, dim3(units), dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_few<bf16, false>), dim3(units), dim3(256), 0, st, a);
     hipLaunchKernelGGL(k_few_join, dim3((unsigned)x->rows), dim3(512), 0, st, a);
     return train_launched();
   }
@@ -1215,10 +1299,10 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
     a.part = ptr<float2>(work, p.part);
     a.xt = ptr<float>(work, p.xt);
     run_logits<false>(p, a, up(x->rows, kStep), st);
+    const Join j{a.meta, ptr<int>(work, p.list), a.part, a.xt, p.tcap, (int)up(valid, 128) / 64, x->scale, v0 == 0,
+                 v0 + valid == x->vocab, ptr<float2>(work, p.run), logp, (float2 *)stats};
+    hipLaunchKernelGGL(k_join, dim3((unsigned)(up(x->rows, kStep) / 16)), dim3(1024), 0, st, j);
   }
-  hipLaunchKernelGGL(k_join, dim3((unsigned)(p.tcap / 16)), dim3(1024), 0, st, ptr<Meta>(work, p.meta), ptr<int>(work, p.list),
-                     ptr<float2>(work, p.part), ptr<float>(work, p.xt), p.tcap, (int)p.units, x->scale, logp,
-                     (float2 *)stats);
   return train_launched();
 }
 
@@ -1264,9 +1348,21 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
       Logit a = logit_of(x, p, v0, valid, w, work);
       a.prm = ptr<RowPrm>(work, p.prm);
       a.g = ptr<uint16_t>(work, p.g);
+      a.rest = ptr<float>(work, p.rest);
       a.gplane = p.tcap * p.piece;
       a.piece = p.piece;
-      run_logits<true>(p, a, p.tcap, st);
+      if (x->rows <= kFew) {
+        const Few f{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)width,
+                    (int)x->index, x->scale, nullptr, nullptr, 0, nullptr, nullptr, (int)v0, (int)valid, meta,
+                    ptr<int>(work, p.pos), ptr<int>(work, p.list), a.prm, a.g, a.gplane, a.piece, a.rest};
+        const dim3 grid((unsigned)((valid + kFewUnit - 1) / kFewUnit));
+        if (p.f16)
+          hipLaunchKernelGGL((k_few<float, true>), grid, dim3(256), 0, st, f);
+        else
+          hipLaunchKernelGGL((k_few<bf16, true>), grid, dim3(256), 0, st, f);
+      } else {
+        run_logits<true>(p, a, p.tcap, st);
+      }
     }
     Back a{};
     a.width = (int)width;
@@ -1292,14 +1388,13 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   }
   if (dhidden && x->rows) {
     const dim3 grid((unsigned)((x->rows + 3) / 4));
+    const DHidden a{ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<float>(work, p.cs), ptr<float>(work, p.rest),
+                    ptr<float>(work, p.acc), p.tcap, (int)p.kp, (int)p.splits, (int)x->rows, (int)width, x->weight, x->ld_weight,
+                    dhidden, ld_dhidden};
     if (p.f16)
-      hipLaunchKernelGGL(k_dhidden_out<float>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.cs), ptr<float>(work, p.acc),
-                         p.tcap,
-                         (int)p.kp, (int)p.splits, (int)x->rows, (int)width, (float *)dhidden, ld_dhidden);
+      hipLaunchKernelGGL(k_dhidden_out<float>, grid, dim3(256), 0, st, a);
     else
-      hipLaunchKernelGGL(k_dhidden_out<bf16>, grid, dim3(256), 0, st, ptr<int>(work, p.pos), ptr<float>(work, p.cs), ptr<float>(work, p.acc),
-                         p.tcap,
-                         (int)p.kp, (int)p.splits, (int)x->rows, (int)width, (bf16 *)dhidden, ld_dhidden);
+      hipLaunchKernelGGL(k_dhidden_out<bf16>, grid, dim3(256), 0, st, a);
   }
   return train_launched();
 }

@@ -146,6 +146,8 @@ def test_linear(dev, T, V, d, dt):
 def test_linear_layouts(dev, dt, kw):
     check(dev, 90, 600, 192, dt, **kw)
     check(dev, 33, 210, 77, dt, **kw)
+    check(dev, 5, 300, 96, dt, **kw)  # few rows
+    check(dev, 16, 131, 33, dt, **kw)
 
 
 def test_linear_fp32_gradient_of_bf16_weights(dev):
@@ -180,6 +182,52 @@ def test_linear_in_pieces(dev, dt):
     dead = torch.ones(T, dtype=torch.bool, device=dev)
     dead[live] = False
     assert not dh[dead].any() and not logp[dead].any()
+
+
+@pytest.mark.parametrize("T", [3, 16, 60])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_gradient_of_confident_rows(dev, dt, T):
+    """1 - p of a target that is all but certain: the statistics and the gradient come from the same logits to the bit, so that
+    errors of the logits, common to p and its sum, move it by parts of 1 - p, and roundings of p by 2^-22 of p."""
+    import paper_2402_03994_amd as fw
+    V, d = 700, 448
+    h, W, t, c = make(T, V, d, dt, 21, masked=False)
+    h = (h.float() + 4.5 * d ** 0.5 * torch.nn.functional.normalize(W[t].float(), dim=1)).to(dt)
+    td = t.to(dev)
+    _, stats = fw.linear_logp(h.to(dev), W.to(dev), td)
+    dh, dw = fw.linear_logp_grad(h.to(dev), W.to(dev), td, stats, c.to(dev))
+    hn, Wn = f64(h), f64(W)
+    rh, rw, g, p = O.linear_logp_grad(hn, Wn, t.numpy(), f64(c), 1.0)
+    at = np.arange(T), t.numpy()
+    assert np.median(1 - p[at]) < 0.01
+    _, rp = errors(hn, Wn, dt, 1.0)
+    cs = np.abs(f64(c))[:, None]
+    eg = cs * p * rp
+    eg[at] = (cs[:, 0] * ((1 - p[at]) * rp.max(1) + 2.0 ** -22))
+    eg += np.abs(g) * (2.0 ** -22 if dt == F32 else HALF[BF16]) + (cs * 2.0 ** -37 if dt == F32 else 0.0)
+    ag, more = np.abs(g) + eg, 2.0 ** -20 if dt == F32 else 0.0
+    tol = eg @ np.abs(Wn) + ((3 * V + 64) * 2.0 ** -24 + more) * (ag @ np.abs(Wn)) + HALF[dt] * np.abs(rh)
+    assert (np.abs(f64(dh) - rh) <= tol).all()
+    tail = 2.0 ** -37 * T * (cs * np.abs(hn)).max() if dt == F32 else 0.0
+    tol = eg.T @ np.abs(hn) + ((3 * T + 8) * 2.0 ** -24 + more) * (ag.T @ np.abs(hn)) + HALF[dt] * np.abs(rw[0]) + tail + 1e-37
+    assert (np.abs(f64(dw) - rw[0]) <= tol).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_many_rows_in_pieces(dev, dt):
+    """So many rows that the log-probabilities come in pieces too, statistics carried from one to the next."""
+    import paper_2402_03994_amd as fw
+    T, V, d = 70000, 40000, 16  # pieces of 2^31 / 70144 entries
+    g = torch.Generator(device=dev).manual_seed(3)
+    h, W = torch.randn(T, d, generator=g, device=dev).to(dt), torch.randn(V, d, generator=g, device=dev).to(dt)
+    t = torch.randint(-3, V, (T,), generator=g, device=dev)
+    logp, stats = fw.linear_logp(h, W, t, scale=0.5)
+    for r in (slice(0, 900), slice(34000, 35000), slice(T - 700, T)):
+        x = h[r].double() @ W.double().T
+        want = torch.where(t[r] < 0, 0.0, torch.log_softmax(0.5 * x, 1).gather(1, t[r].clamp_min(0)[:, None])[:, 0])
+        # scale X: (3 * 16 + 8) 2^-24 of S < 60 (fp32 2^-21 more), twice, and E < (4 * 15 + 200) 2^-24
+        assert (logp[r].double() - want).abs().max() < 2 * 0.5 * 60 * (56 * 2.0 ** -24 + 2.0 ** -21) + 260 * 2.0 ** -24
+        assert (stats[r, 0].double() - x.max(1).values)[t[r] >= 0].abs().max() < 60 * (56 * 2.0 ** -24 + 2.0 ** -21)
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
