@@ -55,18 +55,28 @@ struct RowPrm {
 __device__ __forceinline__ int exponent_of(uint32_t bits) { return (int)((bits >> 23) & 255) - 127; }
 __device__ __forceinline__ int exponent_of(float x) { return exponent_of(__float_as_uint(x)); }
 
-// hi (low half) and lo of x, |x| < 2^15
+// What the operands of a product are: bf16; G in two bf16, beside bf16; all in two fp16.
+enum Mode { kBf16, kPair, kSplit };
+constexpr int kPairRows = 256;  // rows up to which G of bf16 inputs takes two numbers
+
+// hi (low half) and lo of x (kSplit: |x| < 2^15)
+template <Mode M>
 __device__ __forceinline__ uint32_t split(float x) {
+  if (M != kSplit) {
+    const uint32_t h = bf16_bits(x);
+    if (M == kBf16) return h;
+    const float r = x - to_f32(bf16{(uint16_t)h});
+    return h | bf16_bits(r == r ? r : 0.0f) << 16;  // of an infinity hi is all
+  }
   const _Float16 h = (_Float16)x;
   const float r = x - (float)h;
-  const _Float16 l = (_Float16)(r == r ? r : 0.0f);  // of an infinity hi is all
+  const _Float16 l = (_Float16)(r == r ? r : 0.0f);
   return (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
 }
-// plane p of two split numbers, or two bf16, side by side
-template <bool F16>
+// plane p of two of them, side by side
+template <Mode M>
 __device__ __forceinline__ uint32_t two(float a, float b, int p) {
-  if (!F16) return bf16_bits(a) | bf16_bits(b) << 16;
-  return __builtin_amdgcn_perm(split(b), split(a), p ? 0x07060302 : 0x05040100);
+  return __builtin_amdgcn_perm(split<M>(b), split<M>(a), p ? 0x07060302 : 0x05040100);
 }
 
 // N elements of a row from column k on, zeros past the width
@@ -303,8 +313,8 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
       for (int i = 0; i < 8; ++i) f[i] = ldexpf(f[i], kTop - e);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        h[i] = two<true>(f[2 * i], f[2 * i + 1], 0);
-        l[i] = two<true>(f[2 * i], f[2 * i + 1], 1);
+        h[i] = two<kSplit>(f[2 * i], f[2 * i + 1], 0);
+        l[i] = two<kSplit>(f[2 * i], f[2 * i + 1], 1);
       }
       *(u32x4 *)(hc + k) = h;
       *(u32x4 *)(hc + a.plane + k) = l;
@@ -373,7 +383,7 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
     for (int p = 0; p < P; ++p) {
       u32x4 v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = two<P == 2>(f[2 * i], f[2 * i + 1], p);
+      for (int i = 0; i < 4; ++i) v[i] = two<P == 2 ? kSplit : kBf16>(f[2 * i], f[2 * i + 1], p);
       *(u32x4 *)(out + p * a.plane + k) = v;
     }
   }
@@ -496,7 +506,7 @@ struct Side {
   }
 };
 
-template <typename C, bool F16>
+template <typename C, Mode M>
 struct Core {
   f32x16 acc[C::TM][C::TN];
   int wm, wn, fr, fk;
@@ -521,10 +531,10 @@ struct Core {
     Side<C::BN, C::WN, C::TH, KB> sb;
     sa.init(a, rows_a, depth_a);
     sb.init(b, rows_b, depth_b);
-    int part = 0, k = 0;  // of the next stage to load; parts: hi lo, lo hi, hi hi
+    int part = 0, k = 0;  // of the next stage to load; kSplit: hi lo, lo hi, hi hi; kPair: lo, hi
     auto load = [&](int st) {
-      sa.load(lds + st * STAGE, a.p[F16 && part == 1], k);
-      sb.load(lds + st * STAGE + HALF, b.p[F16 && part == 0], k);
+      sa.load(lds + st * STAGE, a.p[M == kSplit ? part == 1 : M == kPair && part == 0], k);
+      sb.load(lds + st * STAGE + HALF, b.p[M == kSplit && part == 0], k);
       if (++k == steps) {
         k = 0;
         ++part;
@@ -536,7 +546,7 @@ struct Core {
       for (int j = 0; j < C::TN; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    const int all = steps * (F16 ? 3 : 1);
+    const int all = steps * (M == kSplit ? 3 : M == kPair ? 2 : 1);
     if (all > 0) load(0);
     for (int s = 0; s < all; ++s) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -553,7 +563,7 @@ struct Core {
         for (int i = 0; i < C::TM; ++i)
 #pragma unroll
           for (int j = 0; j < C::TN; ++j) {
-            if (F16)
+            if (M == kSplit)
               acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa[i]), __builtin_bit_cast(f16x8, fb[j]),
                                                                  acc[i][j], 0, 0, 0);
             else
@@ -599,16 +609,17 @@ struct Logit {
   int64_t gplane, piece;
 };
 
-template <typename C, bool F16, bool GRAD>
+template <typename C, Mode M, bool GRAD>
 __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
 #if defined(__HIP_DEVICE_COMPILE__)
+  constexpr bool F16 = M == kSplit;
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
   const int np = a.meta->np, mt = (a.valid + C::BM - 1) / C::BM, nt = (np + C::BN - 1) / C::BN;
   if ((int)blockIdx.x >= mt * nt) return;
   int tm, tn;
   tile_of(blockIdx.x, mt, nt, tm, tn);
   const int m0 = tm * C::BM, n0 = tn * C::BN;
-  Core<C, F16> c;
+  Core<C, F16 ? kSplit : kBf16> c;  // H and W have one number or two
   c.template run<false, false>(lds, at_row(a.w, m0), at_row(a.h, n0), a.valid - m0, np - n0, 0, 0, a.kp / kStep);
   const bool whole = m0 + C::BM <= a.valid;
   const int ew = F16 ? a.meta->ew : 0;
@@ -633,9 +644,9 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
             g[q] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
             if (m == tv) g[q] += p.one;
             if (p.one == 0.0f || m0 + m >= a.valid) g[q] = 0.0f;
-            if (!F16 && m == tv) a.rest[n] = g[q] - to_f32(bf16{(uint16_t)bf16_bits(g[q])});
-            // both halves of a split number, or the bf16's bits
-            c.acc[i][j][e + q] = __uint_as_float(F16 ? split(g[q]) : bf16_bits(g[q]));
+            if (M == kBf16 && m == tv) a.rest[n] = g[q] - to_f32(bf16{(uint16_t)bf16_bits(g[q])});
+            // the one or two numbers of an entry, as bits
+            c.acc[i][j][e + q] = __uint_as_float(split<M>(g[q]));
           }
         }
     } else {
@@ -681,7 +692,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   // G's rows leave through LDS, in whole lines (chunks of 16 bytes exchanged by the row, so that the lanes of a write meet
   // different banks).
 #pragma unroll
-  for (int plane = 0; plane < (F16 ? 2 : 1); ++plane) {
+  for (int plane = 0; plane < (M == kBf16 ? 1 : 2); ++plane) {
     constexpr int CH = C::BM / 8;
     auto pair = [&](int i, int j, int e) {
       return __builtin_amdgcn_perm(__float_as_uint(c.acc[i][j][e + 1]), __float_as_uint(c.acc[i][j][e]),
@@ -738,7 +749,6 @@ struct Few {
   const RowPrm *prm;
   uint16_t *g;
   int64_t gplane, piece;
-  float *rest;
 };
 
 // Logits of up to 16 rows by 16 entries of the vocabulary a wave.  Lane l holds row l % 16 of both operands; its eight
@@ -788,7 +798,7 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
   }
   // this lane: entries v0 + 4 q + e of row r
   if constexpr (GRAD) {
-    constexpr bool F16 = sizeof(T) == 4;
+    constexpr Mode M = sizeof(T) == 4 ? kSplit : kPair;
     const int at = v0 - a.v0 + q * 4;
     if (n >= 0) {
       const RowPrm p = a.prm[n];
@@ -799,17 +809,16 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
         g[e] = p.w * entry_exp<T>(acc[e] - p.m, pw);
         if (v0 + q * 4 + e == target) g[e] += p.one;
         if (p.one == 0.0f || at + e >= a.valid) g[e] = 0.0f;
-        if (!F16 && v0 + q * 4 + e == target) a.rest[n] = g[e] - to_f32(bf16{(uint16_t)bf16_bits(g[e])});
       }
 #pragma unroll
-      for (int plane = 0; plane < (F16 ? 2 : 1); ++plane)
-        *(u32x2 *)(a.g + plane * a.gplane + n * a.piece + at) = u32x2{two<F16>(g[0], g[1], plane), two<F16>(g[2], g[3], plane)};
+      for (int plane = 0; plane < (M == kBf16 ? 1 : 2); ++plane)
+        *(u32x2 *)(a.g + plane * a.gplane + n * a.piece + at) = u32x2{two<M>(g[0], g[1], plane), two<M>(g[2], g[3], plane)};
     }
     // rows that only fill the list
     for (int i = threadIdx.x >> 3; i < a.meta->np; i += 32)
       if (a.list[i] < 0)
 #pragma unroll
-        for (int plane = 0; plane < (F16 ? 2 : 1); ++plane)
+        for (int plane = 0; plane < (M == kBf16 ? 1 : 2); ++plane)
           *(u32x4 *)(a.g + plane * a.gplane + i * a.piece + blockIdx.x * kFewUnit + (threadIdx.x & 7) * 8) = u32x4{0, 0, 0, 0};
     return;
   }
@@ -946,9 +955,10 @@ struct Back {
 // Both products of a piece in one launch: neither fills a whole number of rounds of the chip, and the longer ones (dH, K
 // is the piece) come first.  Accumulator rows are tokens (vocabulary entries), columns features, so that a store is 32
 // features of a row.
-template <typename C, bool F16, typename TO>
+template <typename C, Mode M, typename TO>
 __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
 #if defined(__HIP_DEVICE_COMPILE__)
+  constexpr bool F16 = M == kSplit;
   __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
   const bool hidden = (int)blockIdx.x < a.blocks;
   const int np = a.meta->np, rows = hidden ? np : a.valid, mt = (rows + C::BM - 1) / C::BM, nt = (a.width + C::BN - 1) / C::BN;
@@ -960,7 +970,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
   const int m0 = tm * C::BM, n0 = tn * C::BN;
   const int k0 = hidden ? part * a.per * kStep : a.seg[a.b0 + part];
   const int steps = hidden ? max(0, min(a.per, a.steps - part * a.per)) : (a.seg[a.b0 + part + 1] - k0) / kStep;
-  Core<C, F16> c;
+  Core<C, M> c;
   if (hidden)
     c.template run<false, true>(lds, at_row(a.g, m0, k0), at_row(a.w, k0, n0), np - m0, a.kp - n0, 0, a.valid - k0, steps);
   else
@@ -1023,7 +1033,7 @@ __global__ __launch_bounds__(256) void k_dhidden_out(DHidden a) {
   if (t >= a.rows) return;
   const int p = a.pos[t];
   T *o = (T *)a.out + t * a.ld;
-  const float f = p >= 0 ? (sizeof(T) == 4 ? a.cs[p] : a.rest[p]) : 0.0f;
+  const float f = p >= 0 ? (sizeof(T) == 4 ? a.cs[p] : a.rest ? a.rest[p] : 0.0f) : 0.0f;
   const T *w = (const T *)a.w + (sizeof(T) == 2 && p >= 0 ? a.tgt[p] : 0) * a.ldw;
   for (int k = lane * 8; k < a.width; k += 512) {
     float v[8] = {};
@@ -1039,9 +1049,9 @@ __global__ __launch_bounds__(256) void k_dhidden_out(DHidden a) {
         }
       }
       float r[8];
-      if (sizeof(T) == 2) row_part<8>(w, k, a.width, r);
+      if (sizeof(T) == 2 && a.rest) row_part<8>(w, k, a.width, r);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = sizeof(T) == 4 ? v[i] * f : v[i] + f * r[i];
+      for (int i = 0; i < 8; ++i) v[i] = sizeof(T) == 4 ? v[i] * f : a.rest ? v[i] + f * r[i] : v[i];
     }
     if (k + 8 <= a.width) {
 #pragma unroll
@@ -1057,8 +1067,8 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // How a call is cut, and where its parts lie in the workspace.
 struct Plan {
-  bool f16, few, copy, large, huge;
-  int64_t batch, n, tcap, kp, piece, pieces, units, splits, planes;
+  bool f16, few, pair, copy, large, huge;
+  int64_t batch, n, tcap, kp, piece, pieces, units, splits, planes, gplanes;  // numbers of an operand's entry, of G's
   int64_t list, pos, tgt, seg, cnt, most, meta, hc, eh, part, xt, run, prm, cs, rest, hs, wc, g, acc, bytes;
 };
 
@@ -1080,6 +1090,8 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     return p;
   }
   p.planes = p.f16 ? 2 : 1;
+  p.pair = !p.f16 && x->rows <= kPairRows;
+  p.gplanes = p.f16 || p.pair ? 2 : 1;
   p.batch = batch;
   p.n = x->rows / batch;
   p.tcap = up(batch * up(p.n, kStep), 256);
@@ -1089,7 +1101,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.copy = p.f16 || x->width % kStep || x->ld_weight % 8 || (uintptr_t)x->weight % 16 || x->ld_weight > (1 << 20);
   // a piece: G in 256 MB (a launch more for each halving), a copy of W in 256 MB
   int64_t most = x->vocab;
-  if (grad) most = std::min(most, ((int64_t)1 << 27) / (p.tcap * p.planes));
+  if (grad) most = std::min(most, ((int64_t)1 << 27) / (p.tcap * p.gplanes));
   if (grad || p.copy) most = std::min(most, ((int64_t)1 << 27) / (p.kp * p.planes));
   // the tiles' (m, z) in 256 MB; grids below 2^32 threads
   if (!grad) most = std::min(most, ((int64_t)1 << 31) / p.tcap);
@@ -1128,7 +1140,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     p.cs = take(4 * p.tcap);
     p.rest = take(4 * p.tcap);
     if (dweight && p.f16) p.hs = take(2 * p.planes * p.tcap * p.kp);
-    p.g = take(2 * p.planes * p.tcap * p.piece);
+    p.g = take(2 * p.gplanes * p.tcap * p.piece);
     if (dhidden) p.acc = take(4 * p.splits * p.tcap * p.kp);
   }
   p.bytes = at;
@@ -1219,47 +1231,43 @@ Logit logit_of(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, Ope
   return a;
 }
 
-template <typename C, bool GRAD>
-void launch_logits(const Plan &p, const Logit &a, int64_t rows, hipStream_t st) {
+template <typename C, Mode M, bool GRAD>
+void launch_logits(const Logit &a, int64_t rows, hipStream_t st) {
   const unsigned blocks = (unsigned)(((a.valid + C::BM - 1) / C::BM) * ((rows + C::BN - 1) / C::BN));
-  if (p.f16)
-    hipLaunchKernelGGL((k_logits<C, true, GRAD>), dim3(blocks), dim3(C::TH), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_logits<C, false, GRAD>), dim3(blocks), dim3(C::TH), 0, st, a);
+  hipLaunchKernelGGL((k_logits<C, M, GRAD>), dim3(blocks), dim3(C::TH), 0, st, a);
 }
 template <bool GRAD>
 void run_logits(const Plan &p, const Logit &a, int64_t rows, hipStream_t st) {
   if (p.large)
-    launch_logits<Large, GRAD>(p, a, rows, st);
+    p.f16 ? launch_logits<Large, kSplit, GRAD>(a, rows, st) : launch_logits<Large, kBf16, GRAD>(a, rows, st);
+  else if (p.f16)
+    launch_logits<Small, kSplit, GRAD>(a, rows, st);
+  else if (GRAD && p.pair)
+    launch_logits<Small, kPair, GRAD>(a, rows, st);
   else
-    launch_logits<Small, GRAD>(p, a, rows, st);
+    launch_logits<Small, kBf16, GRAD>(a, rows, st);
 }
 
-template <typename C>
-void launch_back(const Plan &p, Back a, bool dhidden, bool dweight, sk_dtype odt, hipStream_t st) {
+template <typename C, Mode M, typename TO>
+void launch_back(const Plan &p, Back a, bool dhidden, bool dweight, hipStream_t st) {
   const int64_t nt = (a.width + C::BN - 1) / C::BN, tiles = (a.valid + C::BM - 1) / C::BM * nt;
   a.blocks = dhidden ? (int)up((p.tcap + C::BM - 1) / C::BM * nt * a.splits, 8) : 0;
   const int64_t most = std::max<int64_t>(1, (1 << 22) / tiles);  // examples of a launch: grids below 2^32 threads
   for (int64_t b = 0; b < p.batch; b += most) {
     a.b0 = (int)b;
     const unsigned blocks = (unsigned)(a.blocks + (dweight ? tiles * std::min(most, p.batch - b) : 0));
-    if (p.f16)
-      hipLaunchKernelGGL((k_back<C, true, float>), dim3(blocks), dim3(C::TH), 0, st, a);
-    else if (odt == SK_F32)
-      hipLaunchKernelGGL((k_back<C, false, float>), dim3(blocks), dim3(C::TH), 0, st, a);
-    else
-      hipLaunchKernelGGL((k_back<C, false, bf16>), dim3(blocks), dim3(C::TH), 0, st, a);
+    hipLaunchKernelGGL((k_back<C, M, TO>), dim3(blocks), dim3(C::TH), 0, st, a);
     a.blocks = 0;  // dH came with the first
     if (!dweight) break;
   }
 }
-void run_back(const Plan &p, const Back &a, bool dhidden, bool dweight, sk_dtype odt, hipStream_t st) {
-  if (p.huge)
-    launch_back<Huge>(p, a, dhidden, dweight, odt, st);
-  else if (p.large)
-    launch_back<Large>(p, a, dhidden, dweight, odt, st);
-  else
-    launch_back<Small>(p, a, dhidden, dweight, odt, st);
+template <Mode M, typename TO>
+void run_back(const Plan &p, const Back &a, bool dhidden, bool dweight, hipStream_t st) {
+  if constexpr (M != kPair) {  // few rows
+    if (p.huge) return launch_back<Huge, M, TO>(p, a, dhidden, dweight, st);
+    if (p.large) return launch_back<Large, M, TO>(p, a, dhidden, dweight, st);
+  }
+  launch_back<Small, M, TO>(p, a, dhidden, dweight, st);
 }
 
 }  // namespace
@@ -1284,7 +1292,7 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
     const int units = (int)p.units;
     const Few a{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)x->width,
                 (int)x->index, x->scale, ptr<float2>(work, p.part), ptr<float>(work, p.xt), units, logp, (float2 *)stats, 0, 0, nullptr,
-                nullptr, nullptr, nullptr, nullptr, 0, 0, nullptr};
+                nullptr, nullptr, nullptr, nullptr, 0, 0};
     if (p.f16)
       hipLaunchKernelGGL((k_few<float, false>), dim3(units), dim3(256), 0, st, a);
     else
@@ -1354,7 +1362,7 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
       if (x->rows <= kFew) {
         const Few f{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)width,
                     (int)x->index, x->scale, nullptr, nullptr, 0, nullptr, nullptr, (int)v0, (int)valid, meta,
-                    ptr<int>(work, p.pos), ptr<int>(work, p.list), a.prm, a.g, a.gplane, a.piece, a.rest};
+                    ptr<int>(work, p.pos), ptr<int>(work, p.list), a.prm, a.g, a.gplane, a.piece};
         const dim3 grid((unsigned)((valid + kFewUnit - 1) / kFewUnit));
         if (p.f16)
           hipLaunchKernelGGL((k_few<float, true>), grid, dim3(256), 0, st, f);
@@ -1384,11 +1392,17 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
     a.accumulate = accumulate != 0;
     const bool dh = dhidden && x->rows;
     if (!dh && !dweight) continue;
-    run_back(p, a, dh, dweight, dweight_dtype, st);
+    const bool dw = dweight != nullptr, single = dweight_dtype == SK_F32;
+    if (p.f16)
+      run_back<kSplit, float>(p, a, dh, dw, st);
+    else if (p.pair)
+      single ? run_back<kPair, float>(p, a, dh, dw, st) : run_back<kPair, bf16>(p, a, dh, dw, st);
+    else
+      single ? run_back<kBf16, float>(p, a, dh, dw, st) : run_back<kBf16, bf16>(p, a, dh, dw, st);
   }
   if (dhidden && x->rows) {
     const dim3 grid((unsigned)((x->rows + 3) / 4));
-    const DHidden a{ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<float>(work, p.cs), ptr<float>(work, p.rest),
+    const DHidden a{ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<float>(work, p.cs), p.pair ? nullptr : ptr<float>(work, p.rest),
                     ptr<float>(work, p.acc), p.tcap, (int)p.kp, (int)p.splits, (int)x->rows, (int)width, x->weight, x->ld_weight,
                     dhidden, ld_dhidden};
     if (p.f16)
