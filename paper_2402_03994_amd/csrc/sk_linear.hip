@@ -10,8 +10,7 @@
 // dH and gives its rows G^T H of dW:
 //   8 n V d operations for n tokens, of which 2 n V d are the second forming.
 // Rows whose target is masked are left out of everything: k_live lists the live
-// ones, each example's padded with empty rows to a multiple of 64 so that a step
-// of the products' K lies in one example.
+// ones, each example's padded with empty rows to a multiple of 16.
 //
 // All three products are one kernel core, C[m][n] = sum_k A[m][k] B[n][k], which takes
 // its operands as they lie, with K along their rows or across them (Core below).  16-bit operands, fp32 sums.  bf16 inputs are used as they are and G is
@@ -37,6 +36,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStep = 64;   // K a stage
+constexpr int kPad = 16;    // an example's rows in the list come in multiples of it
 constexpr int kTop = 13;    // split operands lie below 2^(kTop + 1)
 
 // What the kernels of a call share in its workspace.
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
   if (wave == 0) {
     int sum = 0;
     for (int b = 0; b < a.batch; b += 64) {
-      const int v = b + lane < a.batch ? (a.seg[b + 1 + lane] + kStep - 1) / kStep * kStep : 0;
+      const int v = b + lane < a.batch ? (a.seg[b + 1 + lane] + kPad - 1) / kPad * kPad : 0;
       const int s = wave_scan(v, lane) + sum;
       if (b + lane < a.batch) a.seg[b + 1 + lane] = s;
       sum = __shfl(s, 63, 64);
@@ -454,34 +454,32 @@ struct Side {
   static constexpr int L = N * kStep / 8 / TH;       // loads of a thread and stage
   static constexpr int T = N / W / 32;
   static_assert(!KM || N == 128 || N == 192 || N == 256, "exchanges are worked out for these");
-  int off[L], ld, limit, last;
+  int off[L], ld, depth;
 
   static __device__ __forceinline__ int swz(int row) {
     return !KM ? (row >> 1) & 7 : N != 192 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
   }
-  // rows: how many there are from the tile's first on (those behind repeat one of them; a multiple of 8 with KM); depth: K
-  // rows that there are (KM)
-  __device__ __forceinline__ void init(const Operand &o, int rows, int depth) {
+  // rows: how many there are from the tile's first on (those behind repeat one of them; a multiple of 8 with KM); k: K rows
+  // that there are (KM; those behind count as zeros)
+  __device__ __forceinline__ void init(const Operand &o, int rows, int k) {
     ld = (int)(o.ld * 2);
-    limit = rows;
-    last = depth - 1;
+    depth = k;
 #pragma unroll
-    for (int i = 0; i < L; ++i) off[i] = offset(i, KM ? kStep : rows);
-  }
-  __device__ __forceinline__ int offset(int i, int rows) const {
-    const int k = i * TH + threadIdx.x, r = k / CH, c = (k % CH) ^ swz(r);
-    return min(r, rows - 1) * ld + (KM ? min(c * 16, limit * 2 - 16) : c * 16);
+    for (int i = 0; i < L; ++i) {
+      const int c = i * TH + threadIdx.x, r = c / CH, s = ((c % CH) ^ swz(r)) * 16;
+      off[i] = KM ? r * ld + min(s, rows * 2 - 16) : min(r, rows - 1) * ld + s;
+    }
   }
   // stage k of a plane to LDS
   __device__ __forceinline__ void load(char *lds, const uint16_t *plane, int k) const {
     const char *base = (const char *)plane + (int64_t)k * (KM ? (int64_t)ld * kStep : kStep * 2);
-    const auto m = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0xFFFFFFFF, 0x00020000);
+    // K rows that there are not lie past the buffer's end, where loads give zeros
+    const auto m = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, KM ? min(depth - k * kStep, kStep) * ld : 0xFFFFFFFF,
+                                                     0x00020000);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool part = KM && (k + 1) * kStep > last + 1;
 #pragma unroll
     for (int i = 0; i < L; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(m, (lds_ptr)(lds + (i * (TH / 64) + wave) * 1024), 16,
-                                               part ? offset(i, last + 1 - k * kStep) : off[i], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(m, (lds_ptr)(lds + (i * (TH / 64) + wave) * 1024), 16, off[i], 0, 0, 0);
   }
   // operands of step ks of a stage: rows w N / W + 32 i + lane % 32, K 16 ks + 8 (lane / 32) and on
   __device__ __forceinline__ void read(const char *lds, int w, int ks, u32x4 *f) const {
@@ -522,14 +520,15 @@ struct Core {
   __device__ __forceinline__ int row(int i, int e) const { return wm * (C::BM / C::WM) + i * 32 + (e >> 2) * 8 + fk * 4 + (e & 3); }
   __device__ __forceinline__ int col(int j) const { return wn * (C::BN / C::WN) + j * 32 + fr; }
 
-  // acc = sum over `steps` stages from a and b on
+  // acc = sum over `depth` of K from a and b on, a multiple of 64 (of 16 with KA); b has depth_b rows where they are K
   template <bool KA, bool KB>
-  __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth_a,
-                                      int depth_b, int steps) {
+  __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth,
+                                      int depth_b) {
     constexpr int HALF = C::BM * kStep * 2, STAGE = HALF + C::BN * kStep * 2;
     Side<C::BM, C::WM, C::TH, KA> sa;
     Side<C::BN, C::WN, C::TH, KB> sb;
-    sa.init(a, rows_a, depth_a);
+    const int steps = (depth + kStep - 1) / kStep;
+    sa.init(a, rows_a, depth);
     sb.init(b, rows_b, depth_b);
     int part = 0, k = 0;  // of the next stage to load; kSplit: hi lo, lo hi, hi hi; kPair: lo, hi
     auto load = [&](int st) {
@@ -620,7 +619,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   tile_of(blockIdx.x, mt, nt, tm, tn);
   const int m0 = tm * C::BM, n0 = tn * C::BN;
   Core<C, F16 ? kSplit : kBf16> c;  // H and W have one number or two
-  c.template run<false, false>(lds, at_row(a.w, m0), at_row(a.h, n0), a.valid - m0, np - n0, 0, 0, a.kp / kStep);
+  c.template run<false, false>(lds, at_row(a.w, m0), at_row(a.h, n0), a.valid - m0, np - n0, a.kp, 0);
   const bool whole = m0 + C::BM <= a.valid;
   const int ew = F16 ? a.meta->ew : 0;
 #pragma unroll
@@ -895,7 +894,7 @@ struct Join {
 __global__ __launch_bounds__(1024) void k_join(Join a) {
   __shared__ float2 lds[16][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 16 + (lane & 15);
-  if ((int)blockIdx.x * 16 >= a.meta->np) return;  // np is a multiple of 64
+  if ((int)blockIdx.x * 16 >= a.meta->np) return;  // np is a multiple of 16
   const float k2 = power_of(a.scale).k;
   auto join = [&](float2 p, float2 q) {
     const float m = fmaxf(p.x, q.x), base = m == -INFINITY ? 0.0f : m;
@@ -969,12 +968,12 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
   tile_of(b - part * tiles, mt, nt, tm, tn);
   const int m0 = tm * C::BM, n0 = tn * C::BN;
   const int k0 = hidden ? part * a.per * kStep : a.seg[a.b0 + part];
-  const int steps = hidden ? max(0, min(a.per, a.steps - part * a.per)) : (a.seg[a.b0 + part + 1] - k0) / kStep;
+  const int depth = hidden ? max(0, min(a.per, a.steps - part * a.per)) * kStep : a.seg[a.b0 + part + 1] - k0;
   Core<C, M> c;
   if (hidden)
-    c.template run<false, true>(lds, at_row(a.g, m0, k0), at_row(a.w, k0, n0), np - m0, a.kp - n0, 0, a.valid - k0, steps);
+    c.template run<false, true>(lds, at_row(a.g, m0, k0), at_row(a.w, k0, n0), np - m0, a.kp - n0, depth, a.valid - k0);
   else
-    c.template run<true, true>(lds, at_row(a.g, k0, m0), at_row(a.h, k0, n0), C::BM, a.kp - n0, steps * kStep, steps * kStep, steps);
+    c.template run<true, true>(lds, at_row(a.g, k0, m0), at_row(a.h, k0, n0), C::BM, a.kp - n0, depth, depth);
   if (hidden) {
     float *to = a.acc + (part * a.tcap + m0) * a.kp + n0;
     const int ew = F16 ? a.meta->ew - 2 * kTop : 0;
@@ -993,7 +992,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
         }
     }
   } else {
-    const float f = F16 && steps ? ldexpf(1.0f, max(a.meta->ec, -300) - 2 * kTop) : 1.0f;
+    const float f = F16 && depth ? ldexpf(1.0f, max(a.meta->ec, -300) - 2 * kTop) : 1.0f;
     TO *to = (TO *)a.out + ((a.b0 + part) * a.vocab + m0) * a.width + n0;
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
@@ -1094,7 +1093,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.gplanes = p.f16 || p.pair ? 2 : 1;
   p.batch = batch;
   p.n = x->rows / batch;
-  p.tcap = up(batch * up(p.n, kStep), 256);
+  p.tcap = up(batch * up(p.n, kPad), 256);
   p.tcap = std::max<int64_t>(p.tcap, 256);
   p.kp = up(x->width, kStep);
   // rows that 16-byte loads in whole stages read as they lie
@@ -1306,10 +1305,10 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
     Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, nullptr, work, st), work);
     a.part = ptr<float2>(work, p.part);
     a.xt = ptr<float>(work, p.xt);
-    run_logits<false>(p, a, up(x->rows, kStep), st);
+    run_logits<false>(p, a, up(x->rows, kPad), st);
     const Join j{a.meta, ptr<int>(work, p.list), a.part, a.xt, p.tcap, (int)up(valid, 128) / 64, x->scale, v0 == 0,
                  v0 + valid == x->vocab, ptr<float2>(work, p.run), logp, (float2 *)stats};
-    hipLaunchKernelGGL(k_join, dim3((unsigned)(up(x->rows, kStep) / 16)), dim3(1024), 0, st, j);
+    hipLaunchKernelGGL(k_join, dim3((unsigned)(up(x->rows, kPad) / 16)), dim3(1024), 0, st, j);
   }
   return train_launched();
 }
