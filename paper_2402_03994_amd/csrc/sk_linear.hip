@@ -440,24 +440,26 @@ typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
 // 19.7 ms so).
 __device__ __forceinline__ s16x4 read_tr(const lds_s16x4 __restrict__ p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
 
-// One operand of a tile, N of its rows, by TH threads of which a wave multiplies W of N / W rows.
-// KM false: K contiguous.  A stage is N rows of 128 bytes, their eight 16-byte chunks exchanged by (row / 2) & 7, so
-// that the 32 rows that a wave reads at a time lie in different banks (exchanged by row & 7: 8192^3 bf16, 256 x 256, 957
+// One operand of a tile, N of its rows, by TH threads of which a wave multiplies N / W rows.  A stage is 64 numbers of each
+// row: 64 of K, or 32 of K in two planes (P = 2).
+// KM false: K contiguous.  A stage is N rows of 128 bytes (two times N of 64), whose 16-byte chunks are exchanged by row / 2
+// so that the 32 rows that a wave reads at a time lie in different banks (exchanged by the row: 8192^3 bf16, 256 x 256, 957
 // us, 887 us so).
-// KM true: the matrix has K for its rows and the operand's rows for its columns.  A stage is 64 rows of N columns, which
-// ds_read_b64_tr_b16 transposes: of 16 lanes, lane 4 r + q gives the address of four columns 4 q of row r, and lane i gets
-// column i of the four rows.  Chunks are exchanged so that the eight rows of 64 bytes that a wave reads at a time fill
-// the banks twice over: rows lie 256 bytes (N = 128), 384 (192) or 512 (256) apart.
-template <int N, int W, int TH, bool KM>
+// KM true: the matrix has K for its rows and the operand's rows for its columns.  A stage is 64 (two times 32) rows of N
+// columns, which ds_read_b64_tr_b16 transposes: of 16 lanes, lane 4 r + q gives the address of four columns 4 q of row r,
+// and lane i gets column i of the four rows.  Chunks are exchanged so that the eight rows of 64 bytes that a wave reads at a
+// time fill the banks twice over: rows lie 256 bytes (N = 128), 384 (192) or 512 (256) apart.
+template <int N, int W, int TH, bool KM, int P>
 struct Side {
-  static constexpr int CH = KM ? N / 8 : kStep / 8;  // chunks of an LDS row
-  static constexpr int L = N * kStep / 8 / TH;       // loads of a thread and stage
-  static constexpr int T = N / W / 32;
+  static constexpr int KS = kStep / P;                      // K of a stage
+  static constexpr int CH = KM ? N / 8 : KS / 8;            // chunks of an LDS row
+  static constexpr int L = N * KS / 8 / TH;                 // loads of a thread, plane and stage
+  static constexpr int T = N / W / 32, PLANE = N * KS * 2;  // 32 x 32 blocks of a wave, bytes of a plane's part
   static_assert(!KM || N == 128 || N == 192 || N == 256, "exchanges are worked out for these");
   int off[L], ld, depth;
 
   static __device__ __forceinline__ int swz(int row) {
-    return !KM ? (row >> 1) & 7 : N != 192 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
+    return !KM ? (row >> 1) & (CH - 1) : N != 192 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
   }
   // rows: how many there are from the tile's first on (those behind repeat one of them; a multiple of 8 with KM); k: K rows
   // that there are (KM; those behind count as zeros)
@@ -472,10 +474,9 @@ struct Side {
   }
   // stage k of a plane to LDS
   __device__ __forceinline__ void load(char *lds, const uint16_t *plane, int k) const {
-    const char *base = (const char *)plane + (int64_t)k * (KM ? (int64_t)ld * kStep : kStep * 2);
+    const char *base = (const char *)plane + (int64_t)k * (KM ? (int64_t)ld * KS : KS * 2);
     // K rows that there are not lie past the buffer's end, where loads give zeros
-    const auto m = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, KM ? min(depth - k * kStep, kStep) * ld : 0xFFFFFFFF,
-                                                     0x00020000);
+    const auto m = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, KM ? min(depth - k * KS, KS) * ld : 0xFFFFFFFF, 0x00020000);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
     for (int i = 0; i < L; ++i)
@@ -498,7 +499,7 @@ struct Side {
         f[i] = u.v;
       } else {
         const int r = lane & 31;
-        f[i] = *(const u32x4 *)(lds + (w * (N / W) + i * 32 + r) * kStep * 2 + ((ks * 2 + (lane >> 5)) ^ swz(r)) * 16);
+        f[i] = *(const u32x4 *)(lds + (w * (N / W) + i * 32 + r) * KS * 2 + ((ks * 2 + (lane >> 5)) ^ swz(r)) * 16);
       }
     }
   }
@@ -520,20 +521,41 @@ struct Core {
   __device__ __forceinline__ int row(int i, int e) const { return wm * (C::BM / C::WM) + i * 32 + (e >> 2) * 8 + fk * 4 + (e & 3); }
   __device__ __forceinline__ int col(int j) const { return wn * (C::BN / C::WN) + j * 32 + fr; }
 
-  // acc = sum over `depth` of K from a and b on, a multiple of 64 (of 16 with KA); b has depth_b rows where they are K
+  __device__ __forceinline__ void multiply(const u32x4 *fa, const u32x4 *fb) {
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) {
+        if (M == kSplit)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa[i]), __builtin_bit_cast(f16x8, fb[j]),
+                                                             acc[i][j], 0, 0, 0);
+        else
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]), __builtin_bit_cast(bf16x8, fb[j]),
+                                                              acc[i][j], 0, 0, 0);
+      }
+  }
+
+  // acc = sum over `depth` of K from a and b on, a multiple of 64 (of 16 with KA); b has depth_b rows where they are K.
+  // kSplit: both planes of both operands are in a stage, each is read once for hi lo, lo hi and hi hi (one stage for each
+  // of the three: 2000 x 50257 x 768 365 us, SPLIT us so).  kPair: all of K with a's lo, then with its hi.
   template <bool KA, bool KB>
   __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth,
                                       int depth_b) {
-    constexpr int HALF = C::BM * kStep * 2, STAGE = HALF + C::BN * kStep * 2;
-    Side<C::BM, C::WM, C::TH, KA> sa;
-    Side<C::BN, C::WN, C::TH, KB> sb;
-    const int steps = (depth + kStep - 1) / kStep;
+    constexpr int P = M == kSplit ? 2 : 1, HALF = C::BM * kStep * 2, STAGE = HALF + C::BN * kStep * 2;
+    using A = Side<C::BM, C::WM, C::TH, KA, P>;
+    using B = Side<C::BN, C::WN, C::TH, KB, P>;
+    A sa;
+    B sb;
+    const int steps = (depth + A::KS - 1) / A::KS;
     sa.init(a, rows_a, depth);
     sb.init(b, rows_b, depth_b);
-    int part = 0, k = 0;  // of the next stage to load; kSplit: hi lo, lo hi, hi hi; kPair: lo, hi
+    int part = 0, k = 0;  // of the next stage to load
     auto load = [&](int st) {
-      sa.load(lds + st * STAGE, a.p[M == kSplit ? part == 1 : M == kPair && part == 0], k);
-      sb.load(lds + st * STAGE + HALF, b.p[M == kSplit && part == 0], k);
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        sa.load(lds + st * STAGE + p * A::PLANE, a.p[M == kPair ? part == 0 : p], k);
+        sb.load(lds + st * STAGE + HALF + p * B::PLANE, b.p[p], k);
+      }
       if (++k == steps) {
         k = 0;
         ++part;
@@ -545,7 +567,7 @@ struct Core {
       for (int j = 0; j < C::TN; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    const int all = steps * (M == kSplit ? 3 : M == kPair ? 2 : 1);
+    const int all = steps * (M == kPair ? 2 : 1);
     if (all > 0) load(0);
     for (int s = 0; s < all; ++s) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -554,21 +576,18 @@ struct Core {
       if (s + 1 < all) load((s + 1) & 1);
       const char *at = lds + (s & 1) * STAGE;
 #pragma unroll
-      for (int ks = 0; ks < kStep / 16; ++ks) {
-        u32x4 fa[C::TM], fb[C::TN];
-        sa.read(at, wm, ks, fa);
-        sb.read(at + HALF, wn, ks, fb);
+      for (int ks = 0; ks < A::KS / 16; ++ks) {
+        u32x4 fa[P][C::TM], fb[P][C::TN];
 #pragma unroll
-        for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-          for (int j = 0; j < C::TN; ++j) {
-            if (M == kSplit)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa[i]), __builtin_bit_cast(f16x8, fb[j]),
-                                                                 acc[i][j], 0, 0, 0);
-            else
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]),
-                                                                  __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
-          }
+        for (int p = 0; p < P; ++p) {
+          sa.read(at + p * A::PLANE, wm, ks, fa[p]);
+          sb.read(at + HALF + p * B::PLANE, wn, ks, fb[p]);
+        }
+        if (P == 2) {
+          multiply(fa[0], fb[P - 1]);
+          multiply(fa[P - 1], fb[0]);
+        }
+        multiply(fa[0], fb[0]);
       }
     }
   }
