@@ -41,9 +41,9 @@ constexpr int kTop = 13;    // split operands lie below 2^(kTop + 1)
 
 // What the kernels of a call share in its workspace.
 struct Meta {
-  int np;  // listed rows
-  int ew;  // exponent of the largest finite |W|
-  int ec;  // exponent bound of dlogp scale H
+  int np;      // listed rows
+  int ew;      // exponent of the largest finite |W|
+  int ec[64];  // exponent bounds of dlogp scale H, those of every 64th row each: its atomics would queue at one
 };
 
 // A listed row in the gradient: G = one ? one [v = target] + w exp(scale (x - m)) : 0, logits being acc 2^(e + ew).
@@ -226,8 +226,9 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
     }
     if (lane == 0) {
       a.seg[0] = 0;
-      *a.meta = Meta{sum, INT_MIN / 2, INT_MIN / 2};
+      a.meta->np = sum;
     }
+    a.meta->ec[lane] = INT_MIN / 2;
   }
   __syncthreads();
   for (int c0 = wave * U; c0 < chunks; c0 += 16 * U) {
@@ -259,6 +260,12 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
 }
 
 // --- operands -----------------------------------------------------------------------------------------------
+__device__ __forceinline__ int wave_most(int v) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v = max(v, __shfl_xor(v, d, 64));
+  return v;
+}
+
 __device__ __forceinline__ void raise(int *most, int v) {  // an atomic only where it can change something
   if (v > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, v);
 }
@@ -290,8 +297,7 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
   if (sizeof(T) == 4 && n == 0) {
     int e = INT_MIN / 2;
     for (int i = lane; i < a.parts; i += 64) e = max(e, a.most[i]);
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) e = max(e, __shfl_xor(e, d, 64));
+    e = wave_most(e);
     if (lane == 0) a.meta->ew = e;
   }
   if (n >= a.meta->np) return;
@@ -336,7 +342,7 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
   }
   if (sizeof(T) == 4) {
     a.cs[n] = c;
-    if (c != 0.0f) raise(&a.meta->ec, e + exponent_of(c) + 1);
+    if (c != 0.0f) raise(&a.meta->ec[n & 63], e + exponent_of(c) + 1);
   }
   a.prm[n] = p;
 }
@@ -367,7 +373,7 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
   int e = 0;
   if (LIST) {
     e = a.eh[r];
-    scale = ldexpf(a.cs[r], e - a.meta->ec);
+    scale = ldexpf(a.cs[r], e - wave_most(a.meta->ec[lane]));
   } else if (P == 2) {
     e = a.meta->ew;
   }
@@ -1011,7 +1017,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
         }
     }
   } else {
-    const float f = F16 && depth ? ldexpf(1.0f, max(a.meta->ec, -300) - 2 * kTop) : 1.0f;
+    const float f = F16 && depth ? ldexpf(1.0f, max(wave_most(a.meta->ec[threadIdx.x & 63]), -300) - 2 * kTop) : 1.0f;
     TO *to = (TO *)a.out + ((a.b0 + part) * a.vocab + m0) * a.width + n0;
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {

@@ -49,8 +49,9 @@ def rows(t, dev, lead=0, pad=0):
     return v
 
 
-def make(T, V, d, dt, seed, masked=True):
-    """Logits of a few units, one text's positions peaked; masked positions hold NaNs."""
+def make(T, V, d, dt, seed, masked=True, wide=False):
+    """Logits of a few units, one text's positions peaked; masked positions hold NaNs.  wide: entries, and the factors of the
+    rows, over many powers of two, beside a large column of the weight that no hidden state sees."""
     g = torch.Generator().manual_seed(seed)
     W = (torch.randn(V, d, generator=g) * (1.5 / d ** 0.5)).to(dt)
     t = torch.randint(0, V, (T,), generator=g)
@@ -60,7 +61,14 @@ def make(T, V, d, dt, seed, masked=True):
         dead = torch.rand(T, generator=g) < 0.3
         t[dead] = torch.where(torch.rand(int(dead.sum()), generator=g) < 0.5, -100, V)
         h[dead] = float("nan")
-    return h.to(dt), W, t, torch.randn(T, generator=g)
+    c = torch.randn(T, generator=g)
+    if wide:
+        power = lambda *s: torch.exp2(-torch.randint(0, 15, s, generator=g).float())  # noqa: E731
+        W, h, c = (W.float() * power(V, d)).to(dt), h * power(T, d), c * power(T) * power(T)
+        W[:, 0], h[:, 0] = 8.0, torch.where(h[:, 0].isnan(), h[:, 0], 0.0)
+        if d > 2:
+            h[:, 1] *= 40.0
+    return h.to(dt), W, t, c
 
 
 def logit_error(h, W, dt):
@@ -84,9 +92,9 @@ def errors(h, W, dt, scale):
 
 
 def check(dev, T, V, d, dt, scale=1.0, batch=1, lead=0, pad=0, wlead=0, wpad=0, seed=None, index=torch.int64, odt=None,
-          accumulate=False):
+          accumulate=False, wide=False):
     import paper_2402_03994_amd as fw
-    h, W, t, c = make(T, V, d, dt, T + V + d if seed is None else seed)
+    h, W, t, c = make(T, V, d, dt, T + V + d if seed is None else seed, wide=wide)
     hd, Wd, td, cd = rows(h, dev, lead, pad), rows(W, dev, wlead, wpad), t.to(dev).to(index), c.to(dev)
     shape = (batch, T // batch) if batch > 1 else (T,)
     hd = hd.unflatten(0, shape) if batch > 1 else hd
@@ -186,6 +194,36 @@ def test_linear_in_pieces(dev, dt):
     dead = torch.ones(T, dtype=torch.bool, device=dev)
     dead[live] = False
     assert not dh[dead].any() and not logp[dead].any()
+
+
+@pytest.mark.parametrize("T", [9, 70, 300])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_wide_entries(dev, dt, T):
+    """What is small beside the largest entries keeps its bits."""
+    check(dev, T, 500, 96, dt, wide=True)
+    if T % 3 == 0:
+        check(dev, T, 500, 33, dt, wide=True, batch=3)
+
+
+@pytest.mark.parametrize("T", [9, 70])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_of_any_powers_of_two(dev, dt, T):
+    """2^100 moved from the weight to the hidden states (and back) changes nothing but the gradients' exponents, up to what is
+    below the numbers' range in the smaller one: fp32, up to 32 parts and their sum, times dlogp (split operands are brought
+    into range), rounded to 2^-149; bf16, up to 300 products flushed below 2^-126, and the output's 2^-133."""
+    tiny = 33 * 2.0 ** -149 * 4 if dt == F32 else 300 * 2.0 ** -126 + 2.0 ** -133
+    import paper_2402_03994_amd as fw
+    h, W, t, c = (v.to(dev) for v in make(T, 300, 64, dt, 4))
+    lp, st = fw.linear_logp(h, W, t)
+    dh, dw = fw.linear_logp_grad(h, W, t, st, c)
+    for k in (100, -100):
+        p = 2.0 ** k
+        lp2, st2 = fw.linear_logp(h * p, W / p, t)
+        assert torch.equal(lp2, lp) and torch.equal(st2, st)
+        dh2, dw2 = fw.linear_logp_grad(h * p, W / p, t, st, c)
+        live = (t >= 0) & (t < 300)
+        for got, want, q in ((dh2[live], dh[live], p), (dw2, dw, 1 / p)):
+            assert (got.double() * q - want.double()).abs().max() <= (tiny * q if q > 1 else 0.0)
 
 
 @pytest.mark.parametrize("T", [3, 16, 60])
