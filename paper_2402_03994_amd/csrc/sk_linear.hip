@@ -12,13 +12,23 @@
 // Rows whose target is masked are left out of everything: k_live lists the live
 // ones, each example's padded with empty rows to a multiple of 16.
 //
-// All three products are one kernel core, C[m][n] = sum_k A[m][k] B[n][k], which takes
-// its operands as they lie, with K along their rows or across them (Core below).  16-bit operands, fp32 sums.  bf16 inputs are used as they are and G is
-// rounded to bf16, once, like any entry of a bf16 gradient.  fp32 inputs are
-// split, x = hi + lo in two fp16 numbers (22 bits) under a power of two that
-// brings the largest to 2^13, and each product is the three hi lo, lo hi, hi hi:
-// the matrix cores' fp32 rate is a sixteenth of their fp16 rate.  What lo cannot
-// hold is below 2^-38 of the largest entry of its operand (for H: of the row).
+// All three products are one kernel core, C[m][n] = sum_k A[m][k] B[n][k], which
+// takes its operands as they lie, with K along their rows or across them (Side
+// and Core below).  16-bit operands, fp32 sums.
+//   bf16 inputs are used as they are, and G is rounded to bf16, once, like any
+//   entry of a bf16 gradient (of up to 256 rows, where the bytes of W count and
+//   not the products, it takes two bf16).
+//   fp32 inputs are split, x = hi + lo in two fp16 numbers (22 bits) under a power
+//   of two that brings the largest to 2^13, and each product is the three hi lo,
+//   lo hi, hi hi: a large library product reaches 153 TFLOP/s in fp32, 1256 in
+//   fp16.  What lo cannot hold is below 2^-38 of the largest entry of the row (of
+//   the weight in the gradient).
+//
+// What bounds it: the products, at the rate that their operands leave the caches
+// (the figures are at Tiling); below some hundred rows the reads of W; below those
+// the launches.  One MI355X, both calls: 4096 x 50257 x 768 bf16 (40% masked) 851 us,
+// 8192 x 128256 x 4096 18.2 ms (850 TFLOP/s of the 6 n V d, 1140 with the logits
+// that are formed again).
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -34,6 +44,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 64;   // K a stage
 constexpr int kPad = 16;    // an example's rows in the list come in multiples of it
@@ -355,6 +366,7 @@ struct Prep {
   // H: rows in list order, with their factors (fp32)
   const int *list, *eh;
   const float *cs;
+  int *ev;  // W in fp32, forward: exponents of its rows, which bring their own powers of two
   uint16_t *out;  // [..][kp]
   int64_t plane;
 };
@@ -375,7 +387,8 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
     e = a.eh[r];
     scale = ldexpf(a.cs[r], e - wave_most(a.meta->ec[lane]));
   } else if (P == 2) {
-    e = a.meta->ew;
+    e = a.ev ? row_exponent(row, width) : a.meta->ew;
+    if (a.ev && lane == 0) a.ev[r] = e;
   }
   uint16_t *out = a.out + (int64_t)r * a.kp;
   for (int k = lane * 8; k < a.kp; k += 512) {
@@ -543,7 +556,7 @@ struct Core {
 
   // acc = sum over `depth` of K from a and b on, a multiple of 64 (of 16 with KA); b has depth_b rows where they are K.
   // kSplit: both planes of both operands are in a stage, each is read once for hi lo, lo hi and hi hi (one stage for each
-  // of the three: 2000 x 50257 x 768 365 us, SPLIT us so).  kPair: all of K with a's lo, then with its hi.
+  // of the three: gradients of 8 x 257 x 50257 x 768, each example's, 1774 us with the log-probabilities, 1659 us so).  kPair: all of K with a's lo, then with its hi.
   template <bool KA, bool KB>
   __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth,
                                       int depth_b) {
@@ -620,7 +633,7 @@ struct Logit {
   Operand w, h;
   int v0, valid, kp;  // the piece: its first row of the vocabulary and how many there are
   const Meta *meta;
-  const int *tgt, *eh;
+  const int *tgt, *eh, *ev;
   float scale;
   // forward
   float2 *part;  // [piece / 64][tcap]
@@ -646,7 +659,18 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   Core<C, F16 ? kSplit : kBf16> c;  // H and W have one number or two
   c.template run<false, false>(lds, at_row(a.w, m0), at_row(a.h, n0), a.valid - m0, np - n0, a.kp, 0);
   const bool whole = m0 + C::BM <= a.valid;
-  const int ew = F16 ? a.meta->ew : 0;
+  const int ew = F16 && GRAD ? a.meta->ew : 0;
+  int ev[C::TM][16];
+  if (F16 && !GRAD) {
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const i32x4 v = *(const i32x4 *)(a.ev + m0 + c.row(i, e));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) ev[i][e + q] = v[q];
+      }
+  }
 #pragma unroll
   for (int j = 0; j < C::TN; ++j) {
     const int n = n0 + c.col(j);
@@ -674,7 +698,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
           }
         }
     } else {
-      const int ex = F16 && in ? a.eh[n] + ew - 2 * kTop : 0;
+      const int ex = F16 && in ? a.eh[n] - 2 * kTop : 0;
       const float k2 = power_of(a.scale).k;
       float m = -INFINITY;
 #pragma unroll
@@ -682,7 +706,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float x = c.acc[i][j][e];
-          if (F16) x = ldexpf(x, ex);
+          if (F16) x = ldexpf(x, ev[i][e] + ex);
           if (!whole && m0 + c.row(i, e) >= a.valid) x = -INFINITY;
           c.acc[i][j][e] = x;
           m = fmaxf(m, x);
@@ -1039,7 +1063,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
 
 // dH: the splits' sums in order; zeros for masked rows.  fp32: times the row's factor.  bf16: with what the rounding of the
 // target's entry of G has left, since that entry is most of a row (errors of dH against 64 bits, of which 0.0017 are its
-// own rounding: 0.0022 to 0.0026 without, REST so).
+// own rounding: 0.0022 to 0.0026 without it, 0.0017 to 0.0019 with it).
 struct DHidden {
   const int *pos, *tgt;
   const float *cs, *rest;
@@ -1091,9 +1115,9 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // How a call is cut, and where its parts lie in the workspace.
 struct Plan {
-  bool f16, few, pair, copy, large, huge;
+  bool f16, grad, few, pair, copy, large, huge;
   int64_t batch, n, tcap, kp, piece, pieces, units, splits, planes, gplanes;  // numbers of an operand's entry, of G's
-  int64_t list, pos, tgt, seg, cnt, most, meta, hc, eh, part, xt, run, prm, cs, rest, hs, wc, g, acc, bytes;
+  int64_t list, pos, tgt, seg, cnt, most, meta, hc, eh, ev, part, xt, run, prm, cs, rest, hs, wc, g, acc, bytes;
 };
 
 Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
@@ -1105,6 +1129,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     return r;
   };
   p.f16 = x->dtype == SK_F32;
+  p.grad = grad;
   p.units = (x->vocab + kFewUnit - 1) / kFewUnit;
   p.few = !grad && x->rows <= kFew;
   if (p.few) {
@@ -1154,6 +1179,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.meta = take(sizeof(Meta));
   p.hc = take(2 * p.planes * p.tcap * p.kp);
   p.eh = take(4 * p.tcap);
+  if (p.f16 && !grad) p.ev = take(4 * p.piece);
   if (p.copy) p.wc = take(2 * p.planes * p.piece * p.kp);
   if (!grad) {
     p.part = take(8 * p.units * p.tcap);
@@ -1202,7 +1228,7 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
            hipStream_t st) {
   Meta *meta = ptr<Meta>(work, p.meta);
   int *list = ptr<int>(work, p.list);
-  const int parts = p.f16 ? (int)std::min<int64_t>(kMost, (x->vocab * x->width + 16383) / 16384) : 0;
+  const int parts = p.f16 && dlogp ? (int)std::min<int64_t>(kMost, (x->vocab * x->width + 16383) / 16384) : 0;
   const bool flat = x->ld_weight == x->width && x->vocab * x->width % 4 == 0 && (uintptr_t)x->weight % 16 == 0;
   int *most = ptr<int>(work, p.most);
   hipLaunchKernelGGL(k_live, dim3(1 + parts), dim3(1024), 0, st,
@@ -1229,6 +1255,7 @@ Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, co
   a.width = (int)x->width;
   a.kp = (int)p.kp;
   a.meta = ptr<Meta>(work, p.meta);
+  if (p.f16 && !p.grad) a.ev = ptr<int>(work, p.ev);
   a.out = ptr<uint16_t>(work, p.wc);
   a.plane = p.piece * p.kp;
   const int blocks = h ? (int)(p.tcap / 4) : 0;
@@ -1250,6 +1277,7 @@ Logit logit_of(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, Ope
   a.meta = ptr<Meta>(work, p.meta);
   a.tgt = ptr<int>(work, p.tgt);
   a.eh = ptr<int>(work, p.eh);
+  a.ev = ptr<int>(work, p.ev);
   a.scale = x->scale;
   a.tcap = p.tcap;
   return a;
