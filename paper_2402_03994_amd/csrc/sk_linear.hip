@@ -462,8 +462,8 @@ __device__ __forceinline__ s16x4 read_tr(const lds_s16x4 __restrict__ p) { retur
 // One operand of a tile, N of its rows, by TH threads of which a wave multiplies N / W rows.  A stage is 64 numbers of each
 // row: 64 of K, or 32 of K in two planes (P = 2).
 // KM false: K contiguous.  A stage is N rows of 128 bytes (two times N of 64), whose 16-byte chunks are exchanged by row / 2
-// so that the 32 rows that a wave reads at a time lie in different banks (exchanged by the row: 8192^3 bf16, 256 x 256, 957
-// us, 887 us so).
+// (row / 4) so that 16 rows that are read in a cycle fill the 256 bytes of the banks (128 bytes exchanged by the row: 8192^3
+// bf16, 256 x 256, 957 us, 887 us so; 64 bytes by row / 2: log-probabilities of 2000 x 50257 x 768 fp32 353 us, SWZ us so).
 // KM true: the matrix has K for its rows and the operand's rows for its columns.  A stage is 64 (two times 32) rows of N
 // columns, which ds_read_b64_tr_b16 transposes: of 16 lanes, lane 4 r + q gives the address of four columns 4 q of row r,
 // and lane i gets column i of the four rows.  Chunks are exchanged so that the eight rows of 64 bytes that a wave reads at a
@@ -478,7 +478,7 @@ struct Side {
   int off[L], ld, depth;
 
   static __device__ __forceinline__ int swz(int row) {
-    return !KM ? (row >> 1) & (CH - 1) : N != 192 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
+    return !KM ? (P == 1 ? (row >> 1) & 7 : (row >> 2) & 3) : N != 192 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
   }
   // rows: how many there are from the tile's first on (those behind repeat one of them; a multiple of 8 with KM); k: K rows
   // that there are (KM; those behind count as zeros)
