@@ -90,6 +90,10 @@ __device__ __forceinline__ uint32_t two(float a, float b, int p) {
   return __builtin_amdgcn_perm(split<M>(b), split<M>(a), p ? 0x07060302 : 0x05040100);
 }
 
+// Split operands keep 32 hi and the 32 lo that belong to them side by side, a line of 128 bytes: the place of number p of
+// column k in a row.
+__device__ __forceinline__ int64_t split_at(int64_t k, int p) { return (k >> 5) * 64 + p * 32 + (k & 31); }
+
 // N elements of a row from column k on, zeros past the width
 template <int N, typename T>
 __device__ __forceinline__ void row_part(const T *row, int k, int width, float *f) {
@@ -288,7 +292,6 @@ struct Gather {
   const int *list;
   Meta *meta;
   uint16_t *hc;
-  int64_t plane;
   int *eh;
   const int *most;
   int parts;
@@ -315,7 +318,7 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
   const int t = a.list[n];
   const T *row = (const T *)a.hidden + (int64_t)(t < 0 ? 0 : t) * a.ld;
   const int width = t < 0 ? 0 : a.width;
-  uint16_t *hc = a.hc + (int64_t)n * a.kp;
+  uint16_t *hc = a.hc + (int64_t)n * a.kp * (sizeof(T) == 4 ? 2 : 1);
   int e = 0;
   if (sizeof(T) == 4) {
     e = row_exponent(row, width);
@@ -333,8 +336,8 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
         h[i] = two<kSplit>(f[2 * i], f[2 * i + 1], 0);
         l[i] = two<kSplit>(f[2 * i], f[2 * i + 1], 1);
       }
-      *(u32x4 *)(hc + k) = h;
-      *(u32x4 *)(hc + a.plane + k) = l;
+      *(u32x4 *)(hc + split_at(k, 0)) = h;
+      *(u32x4 *)(hc + split_at(k, 1)) = l;
     } else {
       *(u32x4 *)(hc + k) = Vec<bf16>::pack(f);
     }
@@ -367,8 +370,7 @@ struct Prep {
   const int *list, *eh;
   const float *cs;
   int *ev;  // W in fp32, forward: exponents of its rows, which bring their own powers of two
-  uint16_t *out;  // [..][kp]
-  int64_t plane;
+  uint16_t *out;  // [..][kp] numbers
 };
 
 // Rows as an operand takes them: padded with zeros to kp columns, fp32 split.  A wave a row, up to a multiple of 64 rows.
@@ -390,7 +392,7 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
     e = a.ev ? row_exponent(row, width) : a.meta->ew;
     if (a.ev && lane == 0) a.ev[r] = e;
   }
-  uint16_t *out = a.out + (int64_t)r * a.kp;
+  uint16_t *out = a.out + (int64_t)r * a.kp * P;
   for (int k = lane * 8; k < a.kp; k += 512) {
     float f[8];
     row_part<8>(row, k, width, f);
@@ -403,7 +405,7 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
       u32x4 v;
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = two<P == 2 ? kSplit : kBf16>(f[2 * i], f[2 * i + 1], p);
-      *(u32x4 *)(out + p * a.plane + k) = v;
+      *(u32x4 *)(out + (P == 2 ? split_at(k, p) : k)) = v;
     }
   }
 }
@@ -418,10 +420,10 @@ __global__ __launch_bounds__(256) void k_prep(Prep h, Prep w, int blocks) {
 }
 
 // --- the product --------------------------------------------------------------------------------------------
-// Rows of an operand: up to two planes of 16-bit numbers, K contiguous.
+// Rows of an operand, K or the operand's rows contiguous; kPair: G's lo in a matrix of its own.
 struct Operand {
   const uint16_t *p[2];
-  int64_t ld;  // elements
+  int64_t ld;  // 16-bit numbers
 };
 
 // A BM x BN tile by WM x WN waves, each (BM / WM) x (BN / WN) in 32 x 32 accumulators of v_mfma_f32_32x32x16.  Stages of
@@ -460,25 +462,26 @@ typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
 __device__ __forceinline__ s16x4 read_tr(const lds_s16x4 __restrict__ p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
 
 // One operand of a tile, N of its rows, by TH threads of which a wave multiplies N / W rows.  A stage is 64 numbers of each
-// row: 64 of K, or 32 of K in two planes (P = 2).
-// KM false: K contiguous.  A stage is N rows of 128 bytes (two times N of 64), whose 16-byte chunks are exchanged by row / 2
-// (row / 4) so that 16 rows that are read in a cycle fill the 256 bytes of the banks (128 bytes exchanged by the row: 8192^3
-// bf16, 256 x 256, 957 us, 887 us so; 64 bytes by row / 2: log-probabilities of 2000 x 50257 x 768 fp32 353 us, SWZ us so).
-// KM true: the matrix has K for its rows and the operand's rows for its columns.  A stage is 64 (two times 32) rows of N
-// columns, which ds_read_b64_tr_b16 transposes: of 16 lanes, lane 4 r + q gives the address of four columns 4 q of row r,
-// and lane i gets column i of the four rows.  Chunks are exchanged so that the eight rows of 64 bytes that a wave reads at a
-// time fill the banks twice over: rows lie 256 bytes (N = 128), 384 (192) or 512 (256) apart.
+// row: 64 of K, or (P = 2, split operands) hi and lo of 32 of K.
+// KM false: K contiguous.  A stage is N rows of 128 bytes, whose 16-byte chunks are exchanged by row / 2 so that 16 rows
+// that are read in a cycle fill the 256 bytes of the banks (exchanged by the row: 8192^3 bf16, 256 x 256, 957 us, 887 us
+// so).
+// KM true: the matrix has K for its rows and the operand's rows for its columns.  A stage is 64 rows of N columns (32 of
+// hi, 32 of lo), which ds_read_b64_tr_b16 transposes: of 16 lanes, lane 4 r + q gives the address of four columns 4 q of row
+// r, and lane i gets column i of the four rows.  Chunks are exchanged so that the eight rows of 64 bytes that a wave reads
+// at a time fill the banks twice over: rows lie 256 bytes (N = 128), 384 (192) or 512 (256) apart.
 template <int N, int W, int TH, bool KM, int P>
 struct Side {
-  static constexpr int KS = kStep / P;                      // K of a stage
-  static constexpr int CH = KM ? N / 8 : KS / 8;            // chunks of an LDS row
-  static constexpr int L = N * KS / 8 / TH;                 // loads of a thread, plane and stage
-  static constexpr int T = N / W / 32, PLANE = N * KS * 2;  // 32 x 32 blocks of a wave, bytes of a plane's part
+  static constexpr int KS = kStep / P;                   // K of a stage
+  static constexpr int CH = KM ? N / 8 : kStep / 8;      // chunks of an LDS row
+  static constexpr int PASS = KM ? P : 1;                // hi's and lo's rows are loaded apart
+  static constexpr int L = N * kStep / 8 / TH / PASS;    // loads of a thread, pass and stage
+  static constexpr int T = N / W / 32, LO = N * KS * 2;  // 32 x 32 blocks of a wave; where lo's rows begin (KM)
   static_assert(!KM || N == 128 || N == 192 || N == 256, "exchanges are worked out for these");
   int off[L], ld, depth;
 
   static __device__ __forceinline__ int swz(int row) {
-    return !KM ? (P == 1 ? (row >> 1) & 7 : (row >> 2) & 3) : N != 192 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
+    return !KM ? (row >> 1) & 7 : N != 192 ? (row & 3) * 4 : ((row >> 1) & 1) * 4;
   }
   // rows: how many there are from the tile's first on (those behind repeat one of them; a multiple of 8 with KM); k: K rows
   // that there are (KM; those behind count as zeros)
@@ -487,28 +490,37 @@ struct Side {
     depth = k;
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-      const int c = i * TH + threadIdx.x, r = c / CH, s = ((c % CH) ^ swz(r)) * 16;
-      off[i] = KM ? r * ld + min(s, rows * 2 - 16) : min(r, rows - 1) * ld + s;
+      const int c = i * TH + threadIdx.x, r = c / CH, s = (c % CH) ^ swz(r);
+      if (KM) {
+        const int col = min(s * 8, rows - 8);
+        off[i] = r * ld + (int)(P == 2 ? split_at(col, 0) : col) * 2;
+      } else {
+        off[i] = min(r, rows - 1) * ld + s * 16;
+      }
     }
   }
-  // stage k of a plane to LDS
-  __device__ __forceinline__ void load(char *lds, const uint16_t *plane, int k) const {
-    const char *base = (const char *)plane + (int64_t)k * (KM ? (int64_t)ld * KS : KS * 2);
-    // K rows that there are not lie past the buffer's end, where loads give zeros
-    const auto m = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, KM ? min(depth - k * KS, KS) * ld : 0xFFFFFFFF, 0x00020000);
+  // stage k to LDS
+  __device__ __forceinline__ void load(char *lds, const uint16_t *from, int k) const {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(m, (lds_ptr)(lds + (i * (TH / 64) + wave) * 1024), 16, off[i], 0, 0, 0);
+    for (int p = 0; p < PASS; ++p) {
+      const char *base = (const char *)from + (KM ? (int64_t)k * ld * KS + p * 64 : (int64_t)k * kStep * 2);
+      // K rows that there are not lie past the buffer's end, where loads give zeros
+      const auto m =
+          __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, KM ? min(depth - k * KS, KS) * ld : 0xFFFFFFFF, 0x00020000);
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(m, (lds_ptr)(lds + p * LO + (i * (TH / 64) + wave) * 1024), 16, off[i], 0, 0, 0);
+    }
   }
-  // operands of step ks of a stage: rows w N / W + 32 i + lane % 32, K 16 ks + 8 (lane / 32) and on
-  __device__ __forceinline__ void read(const char *lds, int w, int ks, u32x4 *f) const {
+  // operands of step ks of a stage, number p: rows w N / W + 32 i + lane % 32, K 16 ks + 8 (lane / 32) and on
+  __device__ __forceinline__ void read(const char *lds, int w, int ks, int p, u32x4 *f) const {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int i = 0; i < T; ++i) {
       if constexpr (KM) {
         const int r = (lane & 15) >> 2, col = w * (N / W) + i * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-        const char *at = lds + (ks * 16 + (lane >> 5) * 8 + r) * (N * 2) + ((col >> 3) ^ swz(r)) * 16 + (col & 4) * 2;
+        const char *at = lds + p * LO + (ks * 16 + (lane >> 5) * 8 + r) * (N * 2) + ((col >> 3) ^ swz(r)) * 16 + (col & 4) * 2;
         union {
           s16x4 h[2];
           u32x4 v;
@@ -518,7 +530,7 @@ struct Side {
         f[i] = u.v;
       } else {
         const int r = lane & 31;
-        f[i] = *(const u32x4 *)(lds + (w * (N / W) + i * 32 + r) * KS * 2 + ((ks * 2 + (lane >> 5)) ^ swz(r)) * 16);
+        f[i] = *(const u32x4 *)(lds + (w * (N / W) + i * 32 + r) * 128 + ((p * 4 + ks * 2 + (lane >> 5)) ^ swz(r)) * 16);
       }
     }
   }
@@ -555,7 +567,7 @@ struct Core {
   }
 
   // acc = sum over `depth` of K from a and b on, a multiple of 64 (of 16 with KA); b has depth_b rows where they are K.
-  // kSplit: both planes of both operands are in a stage, each is read once for hi lo, lo hi and hi hi (one stage for each
+  // kSplit: both numbers of both operands are in a stage, each is read once for hi lo, lo hi and hi hi (one stage for each
   // of the three: gradients of 8 x 257 x 50257 x 768, each example's, 1774 us with the log-probabilities, 1659 us so).  kPair: all of K with a's lo, then with its hi.
   template <bool KA, bool KB>
   __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth,
@@ -570,11 +582,8 @@ struct Core {
     sb.init(b, rows_b, depth_b);
     int part = 0, k = 0;  // of the next stage to load
     auto load = [&](int st) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        sa.load(lds + st * STAGE + p * A::PLANE, a.p[M == kPair ? part == 0 : p], k);
-        sb.load(lds + st * STAGE + HALF + p * B::PLANE, b.p[p], k);
-      }
+      sa.load(lds + st * STAGE, a.p[M == kPair && part == 0], k);
+      sb.load(lds + st * STAGE + HALF, b.p[0], k);
       if (++k == steps) {
         k = 0;
         ++part;
@@ -599,8 +608,8 @@ struct Core {
         u32x4 fa[P][C::TM], fb[P][C::TN];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-          sa.read(at + p * A::PLANE, wm, ks, fa[p]);
-          sb.read(at + HALF + p * B::PLANE, wn, ks, fb[p]);
+          sa.read(at, wm, ks, p, fa[p]);
+          sb.read(at + HALF, wn, ks, p, fb[p]);
         }
         if (P == 2) {
           multiply(fa[0], fb[P - 1]);
@@ -613,10 +622,18 @@ struct Core {
 };
 #endif
 
+// from a row, and a column that is a multiple of 32, on
+template <Mode M>
 __device__ __forceinline__ Operand at_row(Operand a, int64_t row, int64_t k = 0) {
-  a.p[0] += row * a.ld + k;
-  a.p[1] += row * a.ld + k;
+  a.p[0] += row * a.ld + (M == kSplit ? 2 * k : k);
+  a.p[1] += row * a.ld + (M == kSplit ? 2 * k : k);
   return a;
+}
+
+// the place of number p of G's entry (n, v)
+template <Mode M>
+__device__ __forceinline__ int64_t g_at(int64_t plane, int64_t piece, int64_t n, int64_t v, int p) {
+  return M == kSplit ? n * piece * 2 + split_at(v, p) : p * plane + n * piece + v;
 }
 
 // Tile number b of mt x nt: workgroups go to the eight XCDs in turn, and each XCD takes a run of tiles, in groups of
@@ -641,7 +658,7 @@ struct Logit {
   int64_t tcap;
   // gradient
   const RowPrm *prm;
-  uint16_t *g;  // [tcap][piece]
+  uint16_t *g;  // [tcap][piece] entries
   float *rest;  // [tcap], bf16: what the rounding of the target's entry has left
   int64_t gplane, piece;
 };
@@ -657,7 +674,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   tile_of(blockIdx.x, mt, nt, tm, tn);
   const int m0 = tm * C::BM, n0 = tn * C::BN;
   Core<C, F16 ? kSplit : kBf16> c;  // H and W have one number or two
-  c.template run<false, false>(lds, at_row(a.w, m0), at_row(a.h, n0), a.valid - m0, np - n0, a.kp, 0);
+  c.template run<false, false>(lds, at_row<M>(a.w, m0), at_row<M>(a.h, n0), a.valid - m0, np - n0, a.kp, 0);
   const bool whole = m0 + C::BM <= a.valid;
   const int ew = F16 && GRAD ? a.meta->ew : 0;
   int ev[C::TM][16];
@@ -764,7 +781,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
     for (int k = threadIdx.x; k < C::BN * CH; k += C::TH) {
       const int n = k / CH, m = k % CH;
       if (n0 + n < np)
-        *(u32x4 *)(a.g + plane * a.gplane + (int64_t)(n0 + n) * a.piece + m0 + m * 8) =
+        *(u32x4 *)(a.g + g_at<M>(a.gplane, a.piece, n0 + n, m0 + m * 8, plane)) =
             *(const u32x4 *)(lds + n * (C::BM * 2) + (m ^ (n & (CH - 1))) * 16);
     }
   }
@@ -860,14 +877,14 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
       }
 #pragma unroll
       for (int plane = 0; plane < (M == kBf16 ? 1 : 2); ++plane)
-        *(u32x2 *)(a.g + plane * a.gplane + n * a.piece + at) = u32x2{two<M>(g[0], g[1], plane), two<M>(g[2], g[3], plane)};
+        *(u32x2 *)(a.g + g_at<M>(a.gplane, a.piece, n, at, plane)) = u32x2{two<M>(g[0], g[1], plane), two<M>(g[2], g[3], plane)};
     }
     // rows that only fill the list
     for (int i = threadIdx.x >> 3; i < a.meta->np; i += 32)
       if (a.list[i] < 0)
 #pragma unroll
-        for (int plane = 0; plane < (M == kBf16 ? 1 : 2); ++plane)
-          *(u32x4 *)(a.g + plane * a.gplane + i * a.piece + blockIdx.x * kFewUnit + (threadIdx.x & 7) * 8) = u32x4{0, 0, 0, 0};
+        for (int plane = 0; plane < 2; ++plane)
+          *(u32x4 *)(a.g + g_at<M>(a.gplane, a.piece, i, blockIdx.x * kFewUnit + (threadIdx.x & 7) * 8, plane)) = u32x4{0, 0, 0, 0};
     return;
   }
   const float k2 = power_of(a.scale).k;
@@ -1021,9 +1038,9 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
   const int depth = hidden ? max(0, min(a.per, a.steps - part * a.per)) * kStep : a.seg[a.b0 + part + 1] - k0;
   Core<C, M> c;
   if (hidden)
-    c.template run<false, true>(lds, at_row(a.g, m0, k0), at_row(a.w, k0, n0), np - m0, a.kp - n0, depth, a.valid - k0);
+    c.template run<false, true>(lds, at_row<M>(a.g, m0, k0), at_row<M>(a.w, k0, n0), np - m0, a.kp - n0, depth, a.valid - k0);
   else
-    c.template run<true, true>(lds, at_row(a.g, k0, m0), at_row(a.h, k0, n0), C::BM, a.kp - n0, depth, depth);
+    c.template run<true, true>(lds, at_row<M>(a.g, k0, m0), at_row<M>(a.h, k0, n0), C::BM, a.kp - n0, depth, depth);
   if (hidden) {
     float *to = a.acc + (part * a.tcap + m0) * a.kp + n0;
     const int ew = F16 ? a.meta->ew - 2 * kTop : 0;
@@ -1232,7 +1249,6 @@ T *ptr(void *work, int64_t at) {
   return (T *)((char *)work + at);
 }
 
-Operand planes_of(uint16_t *p, int64_t plane, int64_t ld) { return Operand{{p, p + plane}, ld}; }
 
 // list, |W|, rows of H: what both directions begin with
 void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *stats_in, float *logp, float *stats, void *work,
@@ -1246,7 +1262,7 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
                      Live{x->targets, dlogp, (int32_t)x->index, (int32_t)x->vocab, (int32_t)p.n, (int32_t)p.batch, list,
                           ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<int>(work, p.seg), ptr<int>(work, p.cnt), meta, logp,
                           (float2 *)stats, (const float *)x->weight, x->ld_weight, (int)x->width, flat, most});
-  const Gather g{x->hidden, x->ld_hidden, (int)x->width, (int)p.kp, list, meta, ptr<uint16_t>(work, p.hc), p.tcap * p.kp,
+  const Gather g{x->hidden, x->ld_hidden, (int)x->width, (int)p.kp, list, meta, ptr<uint16_t>(work, p.hc),
                  ptr<int>(work, p.eh), most, parts, (const float2 *)stats_in, dlogp, x->scale,
                  dlogp ? ptr<RowPrm>(work, p.prm) : nullptr, ptr<float>(work, p.cs)};
   if (p.f16)
@@ -1268,20 +1284,20 @@ Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, co
   a.meta = ptr<Meta>(work, p.meta);
   if (p.f16 && !p.grad) a.ev = ptr<int>(work, p.ev);
   a.out = ptr<uint16_t>(work, p.wc);
-  a.plane = p.piece * p.kp;
   const int blocks = h ? (int)(p.tcap / 4) : 0;
   const dim3 grid((unsigned)(blocks + up(valid, 64) / 4));
   if (p.f16)
     hipLaunchKernelGGL(k_prep<float>, grid, dim3(256), 0, st, h ? *h : a, a, blocks);
   else
     hipLaunchKernelGGL(k_prep<bf16>, grid, dim3(256), 0, st, a, a, 0);
-  return planes_of(a.out, a.plane, p.kp);
+  return Operand{{a.out, a.out}, p.kp * p.planes};
 }
 
 Logit logit_of(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, Operand w, void *work) {
   Logit a{};
   a.w = w;
-  a.h = planes_of(ptr<uint16_t>(work, p.hc), p.tcap * p.kp, p.kp);
+  const uint16_t *h = ptr<uint16_t>(work, p.hc);
+  a.h = Operand{{h, h}, p.kp * p.planes};
   a.v0 = (int)v0;
   a.valid = (int)valid;
   a.kp = (int)p.kp;
@@ -1411,7 +1427,6 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   h.eh = ptr<int>(work, p.eh);
   h.cs = ptr<float>(work, p.cs);
   h.out = ptr<uint16_t>(work, p.hs);
-  h.plane = p.tcap * p.kp;
   for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
     const int64_t valid = std::min(p.piece, x->vocab - v0);
     const Operand w = x->rows ? weights(x, p, v0, valid, hs && v0 == 0 ? &h : nullptr, work, st) : Operand{};
@@ -1440,7 +1455,8 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
     a.meta = meta;
     a.seg = ptr<int>(work, p.seg);
     a.tcap = p.tcap;
-    a.g = planes_of(ptr<uint16_t>(work, p.g), p.tcap * p.piece, p.piece);
+    const uint16_t *g = ptr<uint16_t>(work, p.g), *hd = ptr<uint16_t>(work, p.f16 ? p.hs : p.hc);
+    a.g = Operand{{g, g + (p.pair ? p.tcap * p.piece : 0)}, p.piece * p.planes};
     a.w = w;
     a.steps = (int)(up(valid, kStep) / kStep);
     a.splits = (int)p.splits;
@@ -1448,7 +1464,7 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
     a.first = v0 == 0;
     a.acc = ptr<float>(work, p.acc);
     a.kp = (int)p.kp;
-    a.h = planes_of(ptr<uint16_t>(work, p.f16 ? p.hs : p.hc), p.tcap * p.kp, p.kp);
+    a.h = Operand{{hd, hd}, p.kp * p.planes};
     a.valid = (int)valid;
     a.out = (char *)dweight + v0 * width * (dweight_dtype == SK_F32 ? 4 : 2);
     a.vocab = x->vocab;
