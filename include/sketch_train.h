@@ -6,9 +6,10 @@
  * run steps omega on the sketched gradient of one.  These entry points are the
  * parts of such a step that lie outside the model's blocks: the embedding
  * lookup and its gradient (per example, as sketch_apply takes it, or summed),
- * the log-probabilities of given tokens, the clipped policy loss and the
- * preference loss with their gradients with respect to the logits, and AdamW
- * over a parameter list.
+ * the log-probabilities of given tokens, from logits or from hidden states and the
+ * output matrix, the clipped policy loss and the preference loss with their
+ * gradients, dropout, the balance loss of a router, and AdamW over a parameter
+ * list.
  *
  * Conventions: return 0 or a negative SK_E* code (sketch_last_error() gives
  * the message); arguments are validated before any device work is queued;
@@ -163,11 +164,11 @@ typedef struct {
 
 /*
  * logp[t] = log softmax(scale x_t)[targets[t]] (fp32) and stats [rows, 2] fp32
- * (NULL if not wanted), as sketch_token_logp gives them for these logits.  bf16
- * products and the sums are exact to fp32; of fp32 inputs each product is taken
- * from two numbers of 11 bits an operand (22 bits; what lies below 2^-38 of the
- * largest entry of weight, or of the row of hidden, is lost), so that infinities
- * and NaNs in them give NaNs.
+ * (NULL if not wanted), as sketch_token_logp gives them for these logits.  Sums are
+ * fp32.  bf16 products are exact; of fp32 inputs (more than 16 rows) each product is
+ * taken from two numbers of 11 bits an operand: 22 bits, what lies below 2^-38 of the
+ * largest entry of a row of hidden or weight is lost, and infinities and NaNs give
+ * NaNs in what they reach.
  *   work     sketch_linear_logp_work_bytes(x) bytes (0 if x is refused), 256-byte
  *            aligned.
  */
@@ -183,9 +184,12 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
  *                [batch, vocab, width] contiguous, NULL if not wanted: rows are
  *                `batch` examples of rows / batch each, batch > 1 gives one gradient
  *                per example.  Of fp32 weights it is fp32, of bf16 weights either.
- * Sums are fp32 and rounded once.  bf16 inputs have g rounded to bf16 before the
- * products, whatever the type of dweight.  Rows with dlogp = 0 are masked.  Outputs
- * may not overlap inputs.
+ * Sums are fp32 and rounded once.  bf16 inputs: g is rounded to bf16 before the
+ * products, whatever the type of dweight (up to 256 rows: to two bf16, 2^-16; dhidden
+ * gets back what the target's entry has lost).  fp32 inputs: products as above, with
+ * 2^-38 of the largest entry of weight, and of dlogp times hidden.  A weight that is
+ * not finite gives NaNs.  Rows with dlogp = 0 are masked.  Outputs may not overlap
+ * inputs.
  *   work     sketch_linear_logp_grad_work_bytes(x, batch, dhidden wanted, dweight
  *            wanted) bytes (0 if refused), 256-byte aligned.
  * SK_EUNSUPPORTED for batch > 2^14.

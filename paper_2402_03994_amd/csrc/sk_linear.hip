@@ -57,7 +57,8 @@ struct Meta {
   int ec[64];  // exponent bounds of dlogp scale H, those of every 64th row each: its atomics would queue at one
 };
 
-// A listed row in the gradient: G = one ? one [v = target] + w exp(scale (x - m)) : 0, logits being acc 2^(e + ew).
+// A listed row in the gradient: G = one [v = target] + w exp(scale (x - m)), logits being acc 2^(e + ew).  A row that only
+// fills the list, or has no logit above -inf, has m = inf, w = one = 0.
 struct RowPrm {
   float m, w, one;
   int e;
@@ -343,7 +344,7 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
     }
   }
   if (!a.prm || lane != 0) return;
-  RowPrm p{0.0f, 0.0f, 0.0f, e - 2 * kTop};
+  RowPrm p{INFINITY, 0.0f, 0.0f, e - 2 * kTop};
   float c = 0.0f;
   if (t >= 0) {
     const float2 s = a.stats[t];
@@ -693,27 +694,40 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
     const int n = n0 + c.col(j);
     const bool in = n < np;
     if (GRAD) {
-      const RowPrm p = in ? a.prm[n] : RowPrm{0.0f, 0.0f, 0.0f, 0};
-      const int tv = in ? a.tgt[n] - a.v0 - m0 : -1;
+      const RowPrm p = in ? a.prm[n] : RowPrm{INFINITY, 0.0f, 0.0f, 0};
+      const int tv = in ? a.tgt[n] - a.v0 - m0 - c.wm * (C::BM / C::WM) : -1;
       const Power pw = power_of(a.scale);
 #pragma unroll
       for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-          float g[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int m = c.row(i, e + q);
-            float x = c.acc[i][j][e + q];
-            if (F16) x = ldexpf(x, p.e + ew);
-            g[q] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
-            if (m == tv) g[q] += p.one;
-            if (p.one == 0.0f || m0 + m >= a.valid) g[q] = 0.0f;
-            if (M == kBf16 && m == tv) a.rest[n] = g[q] - to_f32(bf16{(uint16_t)bf16_bits(g[q])});
-            // the one or two numbers of an entry, as bits
-            c.acc[i][j][e + q] = __uint_as_float(split<M>(g[q]));
-          }
+        for (int e = 0; e < 16; ++e) {
+          float x = c.acc[i][j][e];
+          if (F16) x = ldexpf(x, p.e + ew);
+          c.acc[i][j][e] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
         }
+      if (__any(tv >= 0 && tv < C::BM / C::WM)) {  // few tiles have one of their rows' targets
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (c.row(i, e) - c.wm * (C::BM / C::WM) == tv) {
+              const float g = c.acc[i][j][e] + p.one;
+              c.acc[i][j][e] = g;
+              if (M == kBf16) a.rest[n] = g - to_f32(bf16{(uint16_t)bf16_bits(g)});
+            }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (m0 + c.row(i, e) >= a.valid) c.acc[i][j][e] = 0.0f;
+      }
+      // the one or two numbers of an entry, as bits
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) c.acc[i][j][e] = __uint_as_float(split<M>(c.acc[i][j][e]));
     } else {
       const int ex = F16 && in ? a.eh[n] - 2 * kTop : 0;
       const float k2 = power_of(a.scale).k;
@@ -873,7 +887,7 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
       for (int e = 0; e < 4; ++e) {
         g[e] = p.w * entry_exp<T>(acc[e] - p.m, pw);
         if (v0 + q * 4 + e == target) g[e] += p.one;
-        if (p.one == 0.0f || at + e >= a.valid) g[e] = 0.0f;
+        if (at + e >= a.valid) g[e] = 0.0f;
       }
 #pragma unroll
       for (int plane = 0; plane < (M == kBf16 ? 1 : 2); ++plane)

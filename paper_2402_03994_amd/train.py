@@ -1,8 +1,9 @@
 """Binding of the training-step operators (include/sketch_train.h) for torch tensors.
 
 Argument marshalling only: the embedding lookup and its gradient, the token
-log-probabilities, the policy and preference losses with their gradients and
-the AdamW step run in the HIP kernels of libsketch.so on torch's current
+log-probabilities (from logits, or from hidden states and the output matrix), the
+policy and preference losses and a router's balance loss with their gradients,
+dropout and the AdamW step run in the HIP kernels of libsketch.so on torch's current
 stream.  The losses return the gradient with respect to the logits next to the
 loss: a model continues with logits.backward(dlogits).  No call records itself for
 autograd (embed() of a weight that requires a gradient gives a tensor without one);
@@ -233,8 +234,8 @@ def linear_logp(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tenso
 
     hidden [*targets.shape, width] and weight [vocab, width], float32 or bfloat16 alike, rows of one stride each; a target
     outside [0, vocab) masks its position (logp 0, its hidden state is not read).  The logits live tile by tile in
-    registers; what a call needs beside its inputs is a few numbers for each position and 128 entries of the vocabulary,
-    and for float32 (or rows that 16-byte loads do not fit) a copy of a piece of the weight."""
+    registers; what a call needs beside its inputs is up to 256 MB of their statistics, a copy of the hidden states, and
+    for float32 (or rows that 16-byte loads do not fit) a copy of a piece of the weight."""
     x = _linear(hidden, weight, targets, scale)
     device, lib = hidden.device, _lib.load()
     logp = torch.empty(targets.shape, dtype=torch.float32, device=device)
@@ -258,8 +259,8 @@ def linear_logp_grad(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.
     Sketch.apply takes.  dweight has the weight's type; out_dtype (or an out of it) may be float32 for a bfloat16 weight.
     accumulate adds to `out` (with tied weights embed_grad can add to it too).
 
-    The logits are formed again, a piece of the vocabulary at a time; the gradients at them are rounded to bfloat16 where the
-    inputs are.  Positions with a masked target or dlogp = 0 are not read and get zeros."""
+    The logits are formed again, a piece of the vocabulary at a time (256 MB of gradients at them); these are rounded to
+    bfloat16 where the inputs are (up to 256 positions: to two numbers).  Positions with a masked target or dlogp = 0 are not read and get zeros."""
     x = _linear(hidden, weight, targets, scale)
     device, lib = hidden.device, _lib.load()
     if stats.dtype != torch.float32 or stats.device != device or stats.shape != (*targets.shape, 2) or \
