@@ -116,6 +116,18 @@ def test_dropout_past_32_bits(dev):
     assert abs(float((x[:1 << 24] != 0).float().mean()) - 0.5) < 5 * 0.5 / 4096
 
 
+def test_dropout_of_the_most_elements(dev):
+    """2^35 of them (64 GiB), more groups of eight than a grid has threads."""
+    import paper_2402_03994_amd as fw
+    n = 1 << 35
+    x = torch.ones(n, dtype=BF16, device=dev)
+    fw.dropout(x, 0.5, 3, 4, 5, out=x)
+    for at in (0, (1 << 34) - 2048, n - 4096):
+        i = np.arange(at, at + 4096)
+        w = O.philox(i // 8, 4, 5, 13, 3)[np.arange(4096), (i // 2) % 4]
+        assert np.array_equal(f64(x[at:at + 4096]) != 0, np.where(i % 2, w >> 16, w & 0xFFFF) >= 32768)
+
+
 # --- balance ----------------------------------------------------------------------------------------------
 def check_balance(dev, T, E, k, dt, lead=0, pad=0, index=torch.int64, coef=0.3, seed=0):
     import paper_2402_03994_amd as fw
