@@ -357,7 +357,8 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
   }
   if (sizeof(T) == 4) {
     a.cs[n] = c;
-    if (c != 0.0f) raise(&a.meta->ec[n & 63], e + exponent_of(c) + 1);
+    // a factor that is not finite makes NaNs by itself, and leaves the other examples their range
+    if (c != 0.0f && fabsf(c) < INFINITY) raise(&a.meta->ec[n & 63], e + exponent_of(c) + 1);
   }
   a.prm[n] = p;
 }
@@ -507,8 +508,8 @@ struct Side {
     for (int p = 0; p < PASS; ++p) {
       const char *base = (const char *)from + (KM ? (int64_t)k * ld * KS + p * 64 : (int64_t)k * kStep * 2);
       // K rows that there are not lie past the buffer's end, where loads give zeros
-      const auto m =
-          __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, KM ? min(depth - k * KS, KS) * ld : 0xFFFFFFFF, 0x00020000);
+      const int there = KM ? max(0, min(depth - k * KS, KS)) * ld : -1;
+      const auto m = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, there, 0x00020000);
 #pragma unroll
       for (int i = 0; i < L; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(m, (lds_ptr)(lds + p * LO + (i * (TH / 64) + wave) * 1024), 16, off[i], 0, 0, 0);
@@ -569,7 +570,8 @@ struct Core {
 
   // acc = sum over `depth` of K from a and b on, a multiple of 64 (of 16 with KA); b has depth_b rows where they are K.
   // kSplit: both numbers of both operands are in a stage, each is read once for hi lo, lo hi and hi hi (one stage for each
-  // of the three: gradients of 8 x 257 x 50257 x 768, each example's, 1774 us with the log-probabilities, 1659 us so).  kPair: all of K with a's lo, then with its hi.
+  // of the three: gradients of 8 x 257 x 50257 x 768, each example's, 1774 us with the log-probabilities, 1659 us so).
+  // kPair: all of K with a's lo, then with its hi.
   template <bool KA, bool KB>
   __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth,
                                       int depth_b) {

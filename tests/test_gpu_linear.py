@@ -256,6 +256,48 @@ def test_linear_gradient_of_confident_rows(dev, dt, T):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_gradient_of_many_rows_and_features(dev, dt):
+    """Enough of both for the gradients' largest tiles, against the same in fp64 on the device, row by row.  Roundings are
+    independent and add up at random.  bf16: 2^-8 of each entry of g, and of the output.  fp32: 3 V / 16 additions of 2^-24
+    in a row, sqrt(3 * 30720 / 16) 2^-24 = 4.5e-6 of what they add up to.  A row of dW that no target hits can rest on its one
+    largest p, so that the error of that logit is the row's: of 1.3e8 logits with a deviation of 1.5 the largest is 5.8
+    deviations, 8.7, and 3 * 4096 / 16 = 768 additions of that size make sqrt(768) 2^-24 8.7 = 1.4e-5: 1.9e-5 together."""
+    import paper_2402_03994_amd as fw
+    T, V, d = 4200, 30720, 4096
+    g = torch.Generator(device=dev).manual_seed(6)
+    h = torch.randn(T, d, generator=g, device=dev).to(dt)
+    W = (torch.randn(V, d, generator=g, device=dev) * (1.5 / d ** 0.5)).to(dt)
+    t, c = torch.randint(-300, V, (T,), generator=g, device=dev), torch.randn(T, generator=g, device=dev)
+    _, stats = fw.linear_logp(h, W, t)
+    dh, dw = fw.linear_logp_grad(h, W, t, stats, c)
+    live = (t >= 0).nonzero()[:, 0]
+    G = torch.softmax(h[live].double() @ W.double().T, 1).neg_()
+    G.scatter_add_(1, t[live][:, None], torch.ones(len(live), 1, dtype=torch.float64, device=dev)).mul_(c[live].double()[:, None])
+    for got, want in ((dh[live], G @ W.double()), (dw, G.T.contiguous() @ h[live].double())):
+        err = (got.double() - want).norm(dim=1) / want.norm(dim=1)
+        assert err.max() <= (2.0 ** -7.5 if dt == BF16 else 1.9e-5), err.max()
+    assert not dh[t < 0].any()
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_factor_that_is_not_finite(dev, dt, bad):
+    """It spoils the gradients of its own example and hidden state, not one bit of the others."""
+    import paper_2402_03994_amd as fw
+    h, W, t, c = make(60, 200, 64, dt, 12, masked=False)
+    h, W, t, c = h.to(dev).view(3, 20, 64), W.to(dev), t.to(dev).view(3, 20), c.to(dev).view(3, 20)
+    _, stats = fw.linear_logp(h, W, t)
+    c[1, 4] = 0.0
+    dh, dw = fw.linear_logp_grad(h, W, t, stats, c, per_example=True)
+    c[1, 4] = bad
+    dh2, dw2 = fw.linear_logp_grad(h, W, t, stats, c, per_example=True)
+    assert torch.equal(dw2[0], dw[0]) and torch.equal(dw2[2], dw[2]) and not dw2[1].isfinite().any()
+    ok = torch.ones(3, 20, dtype=torch.bool, device=dev)
+    ok[1, 4] = False
+    assert torch.equal(dh2[ok], dh[ok]) and not dh2[1, 4].isfinite().any()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
 def test_linear_many_rows_in_pieces(dev, dt):
     """So many rows that the log-probabilities come in pieces too, statistics carried from one to the next."""
     import paper_2402_03994_amd as fw
