@@ -228,8 +228,8 @@ int sketch_dropout(const void *x, sk_dtype dtype, int64_t rows, int64_t width, i
  *   P_e = mean over those tokens of softmax(logits)_e (probs),  f_e = c_e / (n k)
  *   loss = coef E sum_e f_e P_e  (coef where f or P is even)
  *   dlogits_te = coef E / n p_te (f_e - sum_e' f_e' p_te')
- * (c_e has no gradient).  A token without an id in [0, E) is masked: its logits are
- * not read, its gradient is a row of zeros.  An id counts as often as it stands.
+ * (c_e has no gradient).  A token without an id in [0, E) is masked: its logits may
+ * be anything, its gradient is a row of zeros.  An id counts as often as it stands.
  * With n = 0 everything is 0.  A row of -inf alone counts with probabilities 0.
  *   logits   [tokens, E], row stride ld >= E;  ids [tokens, k] contiguous
  *   loss, probs [E]  fp32;  counts [E] int64

@@ -1,6 +1,7 @@
 """MI355X (gfx950) structured sketches (FJL, FFD, AFFD, AFJL, QK and the Q-pre-conditioned kinds) and
 the sketched HVP operator with Arnoldi in the sketched space, and the training-step operators around them
-(embedding, token log-probabilities, policy and preference losses, AdamW), behind a C ABI.
+(embedding, token log-probabilities from logits or hidden states, policy, preference and balance losses, dropout,
+AdamW), behind a C ABI.
 
 The kernels live in libsketch.so (csrc/, built by build.py); this package only
 marshals torch tensors into that library.

@@ -260,7 +260,8 @@ def linear_logp_grad(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.
     accumulate adds to `out` (with tied weights embed_grad can add to it too).
 
     The logits are formed again, a piece of the vocabulary at a time (256 MB of gradients at them); these are rounded to
-    bfloat16 where the inputs are (up to 256 positions: to two numbers).  Positions with a masked target or dlogp = 0 are not read and get zeros."""
+    bfloat16 where the inputs are (up to 256 positions: to two numbers).  Positions with a masked target or dlogp = 0 are
+    not read and get zeros."""
     x = _linear(hidden, weight, targets, scale)
     device, lib = hidden.device, _lib.load()
     if stats.dtype != torch.float32 or stats.device != device or stats.shape != (*targets.shape, 2) or \
