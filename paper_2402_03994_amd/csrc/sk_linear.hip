@@ -601,7 +601,8 @@ struct Core {
     const int all = steps * (M == kPair ? 2 : 1);
     if (all > 0) load(0);
     for (int s = 0; s < all; ++s) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      // the loads of this stage, and the reads of the buffer that the next one gets
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       if (s + 1 < all) load((s + 1) & 1);
