@@ -508,7 +508,7 @@ struct Side {
     for (int p = 0; p < PASS; ++p) {
       const char *base = (const char *)from + (KM ? (int64_t)k * ld * KS + p * 64 : (int64_t)k * kStep * 2);
       // K rows that there are not lie past the buffer's end, where loads give zeros
-      const int there = KM ? max(0, min(depth - k * KS, KS)) * ld : -1;
+      const int there = KM ? min(depth - k * KS, KS) * ld : -1;
       const auto m = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, there, 0x00020000);
 #pragma unroll
       for (int i = 0; i < L; ++i)
@@ -568,7 +568,8 @@ struct Core {
       }
   }
 
-  // acc = sum over `depth` of K from a and b on, a multiple of 64 (of 16 with KA); b has depth_b rows where they are K.
+  // acc = sum over `depth` of K from a and b on, a multiple of 64 (of 16 with KA); b has depth_b rows where they are K,
+  // some in every stage.
   // kSplit: both numbers of both operands are in a stage, each is read once for hi lo, lo hi and hi hi (one stage for each
   // of the three: gradients of 8 x 257 x 50257 x 768, each example's, 1774 us with the log-probabilities, 1659 us so).
   // kPair: all of K with a's lo, then with its hi.
@@ -1054,8 +1055,10 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
   const int k0 = hidden ? part * a.per * kStep : a.seg[a.b0 + part];
   const int depth = hidden ? max(0, min(a.per, a.steps - part * a.per)) * kStep : a.seg[a.b0 + part + 1] - k0;
   Core<C, M> c;
+  // split weights bring rows of zeros up to a multiple of 64
   if (hidden)
-    c.template run<false, true>(lds, at_row<M>(a.g, m0, k0), at_row<M>(a.w, k0, n0), np - m0, a.kp - n0, depth, a.valid - k0);
+    c.template run<false, true>(lds, at_row<M>(a.g, m0, k0), at_row<M>(a.w, k0, n0), np - m0, a.kp - n0, depth,
+                                F16 ? a.steps * kStep - k0 : a.valid - k0);
   else
     c.template run<true, true>(lds, at_row<M>(a.g, k0, m0), at_row<M>(a.h, k0, n0), C::BM, a.kp - n0, depth, depth);
   if (hidden) {
