@@ -9,7 +9,7 @@
 // G = dlogp scale (onehot - p) in the tile's epilogue, and the piece adds G W to
 // dH and gives its rows G^T H of dW:
 //   8 n V d operations for n tokens, of which 2 n V d are the second forming.
-// Rows whose target is masked are left out of everything: k_live lists the live
+// Rows whose target is masked are left out of everything: k_front (many rows: k_live) lists the live
 // ones, each example's padded with empty rows to a multiple of 16.
 //
 // All three products are one kernel core, C[m][n] = sum_k A[m][k] B[n][k], which
@@ -49,6 +49,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = 64;   // K a stage
 constexpr int kPad = 16;    // an example's rows in the list come in multiples of it
 constexpr int kTop = 13;    // split operands lie below 2^(kTop + 1)
+constexpr int kNone = INT_MIN / 2;  // the exponent of nothing
 
 // What the kernels of a call share in its workspace.
 struct Meta {
@@ -160,7 +161,7 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {  // inclusive
 // exponent of the largest finite |W| that workgroup b of n meets
 __device__ __forceinline__ void largest(const Live &a, int b, int n, int *lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int e = INT_MIN / 2;
+  int e = kNone;
   if (a.flat) {
     constexpr int U = 4;
     const f32x4 *p = (const f32x4 *)a.w;
@@ -187,6 +188,27 @@ __device__ __forceinline__ void largest(const Live &a, int b, int n, int *lds) {
   }
 }
 
+// the row (-1: none) and target (-1: masked) of this lane in chunk c; an example has `per` of them
+__device__ __forceinline__ void fetch(const Live &a, int per, int chunks, int c, int &t, int &v) {
+  const int i = c % per * 64 + (threadIdx.x & 63);
+  t = c < chunks && i < a.n ? c / per * a.n + i : -1;
+  int64_t id = -1;
+  float d = 1.0f;
+  if (t >= 0) {
+    id = a.index == SK_I64 ? ((const int64_t *)a.targets)[t] : ((const int32_t *)a.targets)[t];
+    if (a.dlogp) d = a.dlogp[t];
+  }
+  v = id >= 0 && id < a.vocab && d != 0.0f ? (int)id : -1;
+}
+
+__device__ __forceinline__ void masked(const Live &a, int row) {
+  a.pos[row] = -1;
+  if (a.logp) {
+    a.logp[row] = 0.0f;
+    if (a.stats) a.stats[row] = float2{0.0f, 0.0f};
+  }
+}
+
 // The first workgroup: counts of 64 rows each, their sums within the examples, the examples' starts, the list.  A wave has
 // four chunks of 64 rows under way (8192 rows: 17 us one after another, 14.5 us so).
 __global__ __launch_bounds__(1024) void k_live(Live a) {
@@ -198,22 +220,10 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = (a.n + 63) / 64, chunks = per * a.batch;
-  // the row (-1: none) and target (-1: masked) of this lane in chunk c
-  auto fetch = [&](int c, int &t, int &v) {
-    const int i = c % per * 64 + lane;
-    t = c < chunks && i < a.n ? c / per * a.n + i : -1;
-    int64_t id = -1;
-    float d = 1.0f;
-    if (t >= 0) {
-      id = a.index == SK_I64 ? ((const int64_t *)a.targets)[t] : ((const int32_t *)a.targets)[t];
-      if (a.dlogp) d = a.dlogp[t];
-    }
-    v = id >= 0 && id < a.vocab && d != 0.0f ? (int)id : -1;
-  };
   for (int c0 = wave * U; c0 < chunks; c0 += 16 * U) {
     int t[U], v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) fetch(c0 + u, t[u], v[u]);
+    for (int u = 0; u < U; ++u) fetch(a, per, chunks, c0 + u, t[u], v[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint64_t live = __ballot(v[u] >= 0);
@@ -244,14 +254,14 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
       a.seg[0] = 0;
       a.meta->np = sum;
     }
-    a.meta->ec[lane] = INT_MIN / 2;
+    a.meta->ec[lane] = kNone;
   }
   __syncthreads();
   for (int c0 = wave * U; c0 < chunks; c0 += 16 * U) {
     int t[U], v[U], at[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      fetch(c0 + u, t[u], v[u]);
+      fetch(a, per, chunks, c0 + u, t[u], v[u]);
       at[u] = c0 + u < chunks ? a.seg[(c0 + u) / per] + a.cnt[c0 + u] : 0;
     }
 #pragma unroll
@@ -263,11 +273,7 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
         a.tgt[p] = v[u];
         a.pos[t[u]] = p;
       } else if (t[u] >= 0) {
-        a.pos[t[u]] = -1;
-        if (a.logp) {
-          a.logp[t[u]] = 0.0f;
-          if (a.stats) a.stats[t[u]] = float2{0.0f, 0.0f};
-        }
+        masked(a, t[u]);
       }
       if (c0 + u < chunks && (c0 + u) % per == per - 1)
         for (int p = at[u] + __popcll(live) + lane; p < a.seg[(c0 + u) / per + 1]; p += 64) a.list[p] = a.tgt[p] = -1;
@@ -304,19 +310,11 @@ struct Gather {
   float *cs;
 };
 
-// Rows of H in list order, zeros to a width of kp; a wave a row.  fp32: the row's exponent, its split, and what the
-// gradient needs to know of it.
+// Row t of H at place n of the list (t < 0: a row of zeros), zeros to a width of kp, by a wave.  fp32: the row's exponent,
+// its split; in the gradient what that needs to know of it.  Gives the exponent bound of dlogp scale H.
 template <typename T>
-__global__ __launch_bounds__(256) void k_gather(Gather a) {
-  const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (sizeof(T) == 4 && n == 0) {
-    int e = INT_MIN / 2;
-    for (int i = lane; i < a.parts; i += 64) e = max(e, a.most[i]);
-    e = wave_most(e);
-    if (lane == 0) a.meta->ew = e;
-  }
-  if (n >= a.meta->np) return;
-  const int t = a.list[n];
+__device__ __forceinline__ int gather(const Gather &a, int n, int t) {
+  const int lane = threadIdx.x & 63;
   const T *row = (const T *)a.hidden + (int64_t)(t < 0 ? 0 : t) * a.ld;
   const int width = t < 0 ? 0 : a.width;
   uint16_t *hc = a.hc + (int64_t)n * a.kp * (sizeof(T) == 4 ? 2 : 1);
@@ -343,7 +341,7 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
       *(u32x4 *)(hc + k) = Vec<bf16>::pack(f);
     }
   }
-  if (!a.prm || lane != 0) return;
+  if (!a.prm) return kNone;
   RowPrm p{INFINITY, 0.0f, 0.0f, e - 2 * kTop};
   float c = 0.0f;
   if (t >= 0) {
@@ -355,19 +353,43 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
       p.w = -p.one / s.y;
     }
   }
-  if (sizeof(T) == 4) {
-    a.cs[n] = c;
-    // a factor that is not finite makes NaNs by itself, and leaves the other examples their range
-    if (c != 0.0f && fabsf(c) < INFINITY) raise(&a.meta->ec[n & 63], e + exponent_of(c) + 1);
+  if (lane == 0) {
+    if (sizeof(T) == 4) a.cs[n] = c;
+    a.prm[n] = p;
   }
-  a.prm[n] = p;
+  // a factor that is not finite makes NaNs by itself, and leaves the other examples their range
+  return c != 0.0f && fabsf(c) < INFINITY ? e + exponent_of(c) + 1 : kNone;
+}
+
+// the largest of n numbers, by a wave
+__device__ __forceinline__ int most_of(const int *p, int n) {
+  int v = kNone;
+#pragma unroll 4
+  for (int i = threadIdx.x & 63; i < n; i += 64) v = max(v, p[i]);
+  return wave_most(v);
+}
+
+// a wave a row
+template <typename T>
+__global__ __launch_bounds__(256) void k_gather(Gather a) {
+  const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (sizeof(T) == 4 && n == 0) {
+    const int e = most_of(a.most, a.parts);
+    if (lane == 0) a.meta->ew = e;
+  }
+  if (n >= a.meta->np) return;
+  const int e = gather<T>(a, n, a.list[n]);
+  if (sizeof(T) == 4 && lane == 0 && e != kNone) raise(&a.meta->ec[n & 63], e);
 }
 
 struct Prep {
   const void *src;
   int64_t ld;
   int rows, width, kp;  // what there is, zeros up to kp columns
-  const Meta *meta;
+  Meta *meta;
+  // behind k_front: the parts of the weight's exponent and of that of dlogp scale H, which become meta's
+  const int *most, *ecs;
+  int parts, eparts;
   // H: rows in list order, with their factors (fp32)
   const int *list, *eh;
   const float *cs;
@@ -375,12 +397,13 @@ struct Prep {
   uint16_t *out;  // [..][kp] numbers
 };
 
-// Rows as an operand takes them: padded with zeros to kp columns, fp32 split.  A wave a row, up to a multiple of 64 rows.
-template <typename T, bool LIST>
+// Rows as an operand takes them: padded with zeros to kp columns, fp32 split.  A wave a row, up to a multiple of 64 rows;
+// `block` counts groups of WAVES rows.
+template <typename T, bool LIST, int WAVES>
 __device__ __forceinline__ void prep(const Prep &a, int block) {
   constexpr int P = sizeof(T) == 4 ? 2 : 1;
-  const int r = block * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (LIST && r >= a.meta->np) return;
+  const int r = block * WAVES + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (LIST ? r >= a.meta->np : r >= (a.rows + 63) / 64 * 64) return;
   int64_t at = r < a.rows ? r : -1;
   if (LIST) at = a.list[r];
   const T *row = (const T *)a.src + (at < 0 ? 0 : at) * a.ld;
@@ -388,11 +411,20 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
   float scale = 1.0f;
   int e = 0;
   if (LIST) {
+    const int most = a.ecs ? most_of(a.ecs, a.eparts) : wave_most(a.meta->ec[lane]);
+    if (a.ecs && r == 0) a.meta->ec[lane] = most;
     e = a.eh[r];
-    scale = ldexpf(a.cs[r], e - wave_most(a.meta->ec[lane]));
+    scale = ldexpf(a.cs[r], e - most);
   } else if (P == 2) {
-    e = a.ev ? row_exponent(row, width) : a.meta->ew;
-    if (a.ev && lane == 0) a.ev[r] = e;
+    if (a.ev) {
+      e = row_exponent(row, width);
+      if (lane == 0) a.ev[r] = e;
+    } else if (a.most) {
+      e = most_of(a.most, a.parts);
+      if (r == 0 && lane == 0) a.meta->ew = e;
+    } else {
+      e = a.meta->ew;
+    }
   }
   uint16_t *out = a.out + (int64_t)r * a.kp * P;
   for (int k = lane * 8; k < a.kp; k += 512) {
@@ -416,9 +448,93 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
 template <typename T>
 __global__ __launch_bounds__(256) void k_prep(Prep h, Prep w, int blocks) {
   if ((int)blockIdx.x < blocks)
-    prep<T, true>(h, blockIdx.x);
+    prep<T, true, 4>(h, blockIdx.x);
   else
-    prep<T, false>(w, blockIdx.x - blocks);
+    prep<T, false, 4>(w, blockIdx.x - blocks);
+}
+
+// The list, H's rows and what of W waits for neither, in one launch, for up to 64 chunks of 64 rows: each workgroup counts
+// the live rows by itself and takes 16 rows of a chunk, a wave each.  `blocks` of those; the workgroups behind them look for
+// the largest |W| (gradient of fp32), or prepare W.  Beside k_live, k_gather and k_prep one after another: 61 x 8000 x 250
+// fp32 with gradients 78.7 us, 68.1 us so; 2000 x 50257 x 768 fp32 345 and 329 us; 4096 x 50257 x 768 bf16 with gradients
+// 868 and 855 us.
+struct Front {
+  Live l;
+  Gather g;
+  Prep w;
+  int blocks;
+  int *ecs;  // [blocks]
+};
+constexpr int kFrontChunks = 64;
+
+template <typename T>
+__global__ __launch_bounds__(1024) void k_front(Front a) {
+  __shared__ int lds[16], cnt[kFrontChunks], ids[64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if ((int)blockIdx.x >= a.blocks) {
+    const int b = blockIdx.x - a.blocks;
+    if (sizeof(T) == 4 && a.g.prm)
+      largest(a.l, b, gridDim.x - a.blocks, lds);
+    else
+      prep<T, false, 16>(a.w, b);
+    return;
+  }
+  constexpr int U = kFrontChunks / 16;
+  const int per = (a.l.n + 63) / 64, chunks = per * a.l.batch, mine = blockIdx.x >> 2;
+  int t[U], v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) fetch(a.l, per, chunks, wave * U + u, t[u], v[u]);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int c = wave * U + u;
+    const uint64_t live = __ballot(v[u] >= 0);
+    if (lane == 0) cnt[c] = __popcll(live);
+    if (c == mine) ids[lane] = v[u];
+  }
+  __syncthreads();
+  // lane c: live rows before the end of chunk c; lane b: places before the end of example b
+  const int sum = wave_scan(cnt[lane], lane), before = sum - cnt[lane];
+  const int all = __shfl(sum, min(lane * per + per - 1, 63), 64) - __shfl(before, min(lane * per, 63), 64);
+  const int ends = wave_scan(lane < a.l.batch ? (all + kPad - 1) / kPad * kPad : 0, lane);
+  const int ex = mine / per, end = __shfl(ends, ex, 64);
+  const int at = (ex ? __shfl(ends, ex - 1, 64) : 0) + __shfl(before, mine, 64) - __shfl(before, ex * per, 64);
+  if (blockIdx.x == 0 && wave == 0) {
+    if (lane < a.l.batch) a.l.seg[lane + 1] = ends;
+    if (lane == 0) a.l.seg[0] = 0;
+    if (lane == 63) a.l.meta->np = ends;
+  }
+  const int r = (blockIdx.x & 3) * 16 + wave, i = mine % per * 64 + r;
+  const uint64_t live = __ballot(ids[lane] >= 0);
+  int e = kNone;
+  if (i < a.l.n) {
+    const int row = ex * a.l.n + i, target = ids[r];
+    if (target >= 0) {
+      const int p = at + __popcll(live & ((1ull << r) - 1));
+      if (lane == 0) {
+        a.l.list[p] = row;
+        a.l.tgt[p] = target;
+        a.l.pos[row] = p;
+      }
+      e = gather<T>(a.g, p, row);
+    } else if (lane == 0) {
+      masked(a.l, row);
+    }
+  }
+  if ((int)blockIdx.x % (4 * per) == 4 * per - 1) {  // an example's last: the rows that only fill the list
+    const int p = at + __popcll(live) + wave;
+    if (p < end) {
+      if (lane == 0) a.l.list[p] = a.l.tgt[p] = -1;
+      gather<T>(a.g, p, -1);
+    }
+  }
+  if (sizeof(T) == 4 && a.g.prm) {
+    if (lane == 0) lds[wave] = e;
+    __syncthreads();
+    if (wave == 0) {
+      const int m = wave_most(lds[lane & 15]);
+      if (lane == 0) a.ecs[blockIdx.x] = m;
+    }
+  }
 }
 
 // --- the product --------------------------------------------------------------------------------------------
@@ -1163,9 +1279,9 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // How a call is cut, and where its parts lie in the workspace.
 struct Plan {
-  bool f16, grad, few, pair, copy, large, huge;
-  int64_t batch, n, tcap, kp, piece, pieces, units, splits, planes, gplanes;  // numbers of an operand's entry, of G's
-  int64_t list, pos, tgt, seg, cnt, most, meta, hc, eh, ev, part, xt, run, prm, cs, rest, hs, wc, g, acc, bytes;
+  bool f16, grad, few, pair, copy, large, huge, front;
+  int64_t batch, n, chunks, tcap, kp, piece, pieces, units, splits, planes, gplanes;  // numbers of an operand's entry, of G's
+  int64_t list, pos, tgt, seg, cnt, most, ecs, meta, hc, eh, ev, part, xt, run, prm, cs, rest, hs, wc, g, acc, bytes;
 };
 
 Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
@@ -1193,6 +1309,8 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.n = x->rows / batch;
   p.tcap = up(batch * up(p.n, kPad), 256);
   p.tcap = std::max<int64_t>(p.tcap, 256);
+  p.chunks = batch * ((p.n + 63) / 64);
+  p.front = p.chunks >= 1 && p.chunks <= kFrontChunks;
   p.kp = up(x->width, kStep);
   // rows that 16-byte loads in whole stages read as they lie
   p.copy = p.f16 || x->width % kStep || x->ld_weight % 8 || (uintptr_t)x->weight % 16 || x->ld_weight > (1 << 20);
@@ -1222,8 +1340,9 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.pos = take(4 * x->rows);
   p.tgt = take(4 * p.tcap);
   p.seg = take(4 * (batch + 1));
-  p.cnt = take(4 * batch * ((p.n + 63) / 64));
+  p.cnt = take(4 * p.chunks);
   p.most = take(4 * kMost);
+  p.ecs = take(4 * 4 * kFrontChunks);
   p.meta = take(sizeof(Meta));
   p.hc = take(2 * p.planes * p.tcap * p.kp);
   p.eh = take(4 * p.tcap);
@@ -1270,21 +1389,52 @@ T *ptr(void *work, int64_t at) {
 }
 
 
+// W's rows from v0 on, as prep() takes them
+Prep weights_of(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, void *work) {
+  Prep a{};
+  a.src = (const char *)x->weight + v0 * x->ld_weight * (p.f16 ? 4 : 2);
+  a.ld = x->ld_weight;
+  a.rows = (int)valid;
+  a.width = (int)x->width;
+  a.kp = (int)p.kp;
+  a.meta = ptr<Meta>(work, p.meta);
+  if (p.f16 && !p.grad) a.ev = ptr<int>(work, p.ev);
+  a.out = ptr<uint16_t>(work, p.wc);
+  return a;
+}
+
+// parts of the search for the largest |W|
+int parts_of(const sk_linear *x, const Plan &p) {
+  return p.f16 && p.grad ? (int)std::min<int64_t>(kMost, (x->vocab * x->width + 16383) / 16384) : 0;
+}
+// whether W's first piece is prepared by the launch that begins
+bool in_front(const Plan &p) { return p.front && p.copy && !(p.f16 && p.grad); }
+
 // list, |W|, rows of H: what both directions begin with
 void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *stats_in, float *logp, float *stats, void *work,
            hipStream_t st) {
   Meta *meta = ptr<Meta>(work, p.meta);
   int *list = ptr<int>(work, p.list);
-  const int parts = p.f16 && dlogp ? (int)std::min<int64_t>(kMost, (x->vocab * x->width + 16383) / 16384) : 0;
+  const int parts = parts_of(x, p);
   const bool flat = x->ld_weight == x->width && x->vocab * x->width % 4 == 0 && (uintptr_t)x->weight % 16 == 0;
   int *most = ptr<int>(work, p.most);
-  hipLaunchKernelGGL(k_live, dim3(1 + parts), dim3(1024), 0, st,
-                     Live{x->targets, dlogp, (int32_t)x->index, (int32_t)x->vocab, (int32_t)p.n, (int32_t)p.batch, list,
-                          ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<int>(work, p.seg), ptr<int>(work, p.cnt), meta, logp,
-                          (float2 *)stats, (const float *)x->weight, x->ld_weight, (int)x->width, flat, most});
+  const Live l{x->targets, dlogp, (int32_t)x->index, (int32_t)x->vocab, (int32_t)p.n, (int32_t)p.batch, list,
+               ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<int>(work, p.seg), ptr<int>(work, p.cnt), meta, logp,
+               (float2 *)stats, (const float *)x->weight, x->ld_weight, (int)x->width, flat, most};
   const Gather g{x->hidden, x->ld_hidden, (int)x->width, (int)p.kp, list, meta, ptr<uint16_t>(work, p.hc),
                  ptr<int>(work, p.eh), most, parts, (const float2 *)stats_in, dlogp, x->scale,
-                 dlogp ? ptr<RowPrm>(work, p.prm) : nullptr, ptr<float>(work, p.cs)};
+                 p.grad ? ptr<RowPrm>(work, p.prm) : nullptr, ptr<float>(work, p.cs)};
+  if (p.front) {
+    const int64_t valid = std::min(p.piece, x->vocab);
+    const Front f{l, g, weights_of(x, p, 0, valid, work), (int)p.chunks * 4, ptr<int>(work, p.ecs)};
+    const dim3 grid((unsigned)(f.blocks + (in_front(p) ? up(valid, 64) / 16 : parts))), block(1024);
+    if (p.f16)
+      hipLaunchKernelGGL(k_front<float>, grid, block, 0, st, f);
+    else
+      hipLaunchKernelGGL(k_front<bf16>, grid, block, 0, st, f);
+    return;
+  }
+  hipLaunchKernelGGL(k_live, dim3(1 + parts), dim3(1024), 0, st, l);
   if (p.f16)
     hipLaunchKernelGGL(k_gather<float>, dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, g);
   else
@@ -1293,24 +1443,21 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
 
 // W's rows from v0 on as an operand; what the same launch does for H, if anything
 Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, const Prep *h, void *work, hipStream_t st) {
-  const void *src = (const char *)x->weight + v0 * x->ld_weight * (p.f16 ? 4 : 2);
-  if (!p.copy) return Operand{{(const uint16_t *)src, (const uint16_t *)src}, x->ld_weight};
-  Prep a{};
-  a.src = src;
-  a.ld = x->ld_weight;
-  a.rows = (int)valid;
-  a.width = (int)x->width;
-  a.kp = (int)p.kp;
-  a.meta = ptr<Meta>(work, p.meta);
-  if (p.f16 && !p.grad) a.ev = ptr<int>(work, p.ev);
-  a.out = ptr<uint16_t>(work, p.wc);
+  Prep a = weights_of(x, p, v0, valid, work);
+  if (!p.copy) return Operand{{(const uint16_t *)a.src, (const uint16_t *)a.src}, x->ld_weight};
+  const Operand o{{a.out, a.out}, p.kp * p.planes};
+  if (v0 == 0 && in_front(p)) return o;
+  if (p.front && p.f16 && p.grad) {
+    a.most = ptr<int>(work, p.most);
+    a.parts = parts_of(x, p);
+  }
   const int blocks = h ? (int)(p.tcap / 4) : 0;
   const dim3 grid((unsigned)(blocks + up(valid, 64) / 4));
   if (p.f16)
     hipLaunchKernelGGL(k_prep<float>, grid, dim3(256), 0, st, h ? *h : a, a, blocks);
   else
     hipLaunchKernelGGL(k_prep<bf16>, grid, dim3(256), 0, st, a, a, 0);
-  return Operand{{a.out, a.out}, p.kp * p.planes};
+  return o;
 }
 
 Logit logit_of(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, Operand w, void *work) {
@@ -1432,7 +1579,7 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   TrainGuard guard(x->device);
   if (!guard.ok) return train_no_device();
   hipStream_t st = (hipStream_t)stream;
-  // k_live takes dlogp = NULL for the forward direction; without rows nothing is read from it
+  // the list takes dlogp = NULL for the forward direction; without rows nothing is read from it
   begin(x, p, dlogp ? dlogp : (const float *)work, stats, nullptr, nullptr, work, st);
   Meta *meta = ptr<Meta>(work, p.meta);
   const int64_t width = x->width;
@@ -1446,6 +1593,10 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   h.list = ptr<int>(work, p.list);
   h.eh = ptr<int>(work, p.eh);
   h.cs = ptr<float>(work, p.cs);
+  if (p.front) {
+    h.ecs = ptr<int>(work, p.ecs);
+    h.eparts = (int)p.chunks * 4;
+  }
   h.out = ptr<uint16_t>(work, p.hs);
   for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
     const int64_t valid = std::min(p.piece, x->vocab - v0);
