@@ -560,6 +560,7 @@ struct Tiling {
 };
 using Large = Tiling<128, 192, 2, 2>;
 using Small = Tiling<128, 128, 2, 2>;
+using Narrow = Tiling<128, 64, 2, 2>;  // logits of up to 64 rows (61 x 8000 x 250 fp32, both calls: 67.2 us with Small, 62.4 us so)
 using Huge = Tiling<256, 256, 2, 4>;
 constexpr int64_t kSmallRows = 1024;  // rows up to which the smaller tiles are taken
 // Where the gradients' products have both rows and tiles in plenty, one 256 x 256 tile a CU asks for 0.6 times as much
@@ -1482,16 +1483,24 @@ void launch_logits(const Logit &a, int64_t rows, hipStream_t st) {
   const unsigned blocks = (unsigned)(((a.valid + C::BM - 1) / C::BM) * ((rows + C::BN - 1) / C::BN));
   hipLaunchKernelGGL((k_logits<C, M, GRAD>), dim3(blocks), dim3(C::TH), 0, st, a);
 }
+template <typename C, bool GRAD>
+void run_logits_in(const Plan &p, const Logit &a, int64_t rows, hipStream_t st) {
+  if (p.f16)
+    launch_logits<C, kSplit, GRAD>(a, rows, st);
+  else if (GRAD && p.pair)
+    launch_logits<C, kPair, GRAD>(a, rows, st);
+  else
+    launch_logits<C, kBf16, GRAD>(a, rows, st);
+}
 template <bool GRAD>
-void run_logits(const Plan &p, const Logit &a, int64_t rows, hipStream_t st) {
+void run_logits(const Plan &p, const Logit &a, hipStream_t st) {
+  const int64_t rows = p.batch * up(p.n, kPad);
   if (p.large)
     p.f16 ? launch_logits<Large, kSplit, GRAD>(a, rows, st) : launch_logits<Large, kBf16, GRAD>(a, rows, st);
-  else if (p.f16)
-    launch_logits<Small, kSplit, GRAD>(a, rows, st);
-  else if (GRAD && p.pair)
-    launch_logits<Small, kPair, GRAD>(a, rows, st);
+  else if (rows <= Narrow::BN)
+    run_logits_in<Narrow, GRAD>(p, a, rows, st);
   else
-    launch_logits<Small, kBf16, GRAD>(a, rows, st);
+    run_logits_in<Small, GRAD>(p, a, rows, st);
 }
 
 template <typename C, Mode M, typename TO>
@@ -1552,7 +1561,7 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
     Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, nullptr, work, st), work);
     a.part = ptr<float2>(work, p.part);
     a.xt = ptr<float>(work, p.xt);
-    run_logits<false>(p, a, up(x->rows, kPad), st);
+    run_logits<false>(p, a, st);
     const Join j{a.meta, ptr<int>(work, p.list), a.part, a.xt, p.tcap, (int)up(valid, 128) / 64, x->scale, v0 == 0,
                  v0 + valid == x->vocab, ptr<float2>(work, p.run), logp, (float2 *)stats};
     hipLaunchKernelGGL(k_join, dim3((unsigned)(up(x->rows, kPad) / 16)), dim3(1024), 0, st, j);
@@ -1618,7 +1627,7 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
         else
           hipLaunchKernelGGL((k_few<bf16, true>), grid, dim3(256), 0, st, f);
       } else {
-        run_logits<true>(p, a, p.tcap, st);
+        run_logits<true>(p, a, st);
       }
     }
     Back a{};
