@@ -26,8 +26,8 @@
 //
 // What bounds it: the products, at the rate that their operands leave the caches
 // (the figures are at Tiling); below some hundred rows the reads of W; below those
-// the launches.  One MI355X, both calls: 4096 x 50257 x 768 bf16 (40% masked) 869 us,
-// 8192 x 128256 x 4096 18.6 ms (835 TFLOP/s of the 6 n V d, 1110 with the logits
+// the launches.  One MI355X, both calls: 4096 x 50257 x 768 bf16 (40% masked) 867 us,
+// 8192 x 128256 x 4096 18.4 ms (840 TFLOP/s of the 6 n V d, 1110 with the logits
 // that are formed again).
 #include <algorithm>
 #include <climits>
