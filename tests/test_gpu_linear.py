@@ -174,6 +174,41 @@ def test_linear_per_example(dev, dt, T, batch):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("T,batch", [(4096, 1), (4097, 1), (4096, 64), (192, 64), (195, 65), (4 * 961, 4), (63, 63), (320, 64)])
+def test_linear_lists_of_rows(dev, dt, T, batch):
+    """Around the 64 chunks of 64 rows up to which a call's list is made by the launch that uses it."""
+    check(dev, T, 70, 40, dt, batch=batch)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("T", [200, 5000])
+def test_linear_list_of_few_live_rows(dev, dt, T):
+    """One live row at either end or in the middle, and none."""
+    import paper_2402_03994_amd as fw
+    h, W, t, c = make(T, 150, 64, dt, 8, masked=False)
+    hd, Wd, cd = h.to(dev), W.to(dev), c.to(dev)
+    for at in ([0], [T - 1], [T // 2], [63, 64], [T - 17, T - 1], []):
+        td = torch.full((T,), 150, device=dev)
+        td[at] = t[at].to(dev)
+        lp, st = fw.linear_logp(hd, Wd, td)
+        dh, dw = fw.linear_logp_grad(hd, Wd, td, st, cd)
+        lone, some = fw.linear_logp(hd[at], Wd, td[at]), torch.zeros(T, dtype=torch.bool, device=dev)
+        some[at] = True
+        assert not lp[~some].any() and not dh[~some].any() and not st[~some].any()
+        # the same numbers by the kernel of up to 16 rows, which has fp32 products (2^-21 of |h| |w| < 90 apart) for split ones
+        assert at == [] or (lp[at] - lone[0]).abs().max() < 90 * 2.0 ** -20 + 2.0 ** -18
+        x = hd[at].double() @ Wd.double().T
+        g = torch.softmax(x, 1).neg_()
+        g[range(len(at)), td[at]] += 1
+        g *= cd[at].double()[:, None]
+        want = g.T @ hd[at].double() if at else torch.zeros(150, 64, dtype=torch.float64, device=dev)
+        # of a confident row 1 - p is a difference of two numbers near 1, each rounded by 2^-24 of it after an exponential and a
+        # quotient that are (2^-22 together): absolute, in one entry of g, times h
+        low = 2.0 ** -22 * float((cd[at].double().abs() * hd[at].double().norm(dim=1)).sum())
+        assert (dw.double() - want).norm() <= (2.0 ** -7 if dt == BF16 else 2.0 ** -15) * want.norm() + low
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
 def test_linear_in_pieces(dev, dt):
     """More than one piece of the vocabulary, against the same in fp64 on the device."""
     import paper_2402_03994_amd as fw
