@@ -169,7 +169,8 @@ def check_balance(dev, T, E, k, dt, lead=0, pad=0, index=torch.int64, coef=0.3, 
 
 @pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 8, 2), (61, 8, 2), (5, 3, 4), (300, 9, 1), (1000, 33, 3), (513, 60, 4), (700, 64, 8),
                                    (129, 65, 5), (333, 128, 2), (2000, 200, 6), (40, 257, 8), (600, 512, 3), (100, 513, 70),
-                                   (50, 1025, 2), (20, 2048, 9), (20000, 16, 2), (70000, 7, 1)])
+                                   (50, 1025, 2), (20, 2048, 9), (20000, 16, 2), (70000, 7, 1), (3000, 2048, 9), (6144, 60, 4),
+                                   (6145, 60, 4), (9000, 512, 3), (9000, 513, 3), (66000, 130, 1)])
 @pytest.mark.parametrize("dt", [F32, BF16])
 def test_balance(dev, T, E, k, dt):
     check_balance(dev, T, E, k, dt)
