@@ -294,11 +294,11 @@ def test_linear_gradient_of_confident_rows(dev, dt, T):
 def test_linear_gradient_of_many_rows_and_features(dev, dt):
     """Enough of both for the gradients' largest tiles, against the same in fp64 on the device, row by row.  Roundings are
     independent and add up at random.  bf16: 2^-8 of each entry of g, and of the output.  fp32: 3 V / 16 additions of 2^-24
-    in a row, sqrt(3 * 30720 / 16) 2^-24 = 4.5e-6 of what they add up to.  A row of dW that no target hits can rest on its one
+    in a row, sqrt(3 * 30000 / 16) 2^-24 = 4.5e-6 of what they add up to.  A row of dW that no target hits can rest on its one
     largest p, so that the error of that logit is the row's: of 1.3e8 logits with a deviation of 1.5 the largest is 5.8
     deviations, 8.7, and 3 * 4096 / 16 = 768 additions of that size make sqrt(768) 2^-24 8.7 = 1.4e-5: 1.9e-5 together."""
     import paper_2402_03994_amd as fw
-    T, V, d = 4200, 30720, 4096
+    T, V, d = 4200, 30000, 4096
     g = torch.Generator(device=dev).manual_seed(6)
     h = torch.randn(T, d, generator=g, device=dev).to(dt)
     W = (torch.randn(V, d, generator=g, device=dev) * (1.5 / d ** 0.5)).to(dt)
