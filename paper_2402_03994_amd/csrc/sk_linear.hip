@@ -9,8 +9,8 @@
 // G = dlogp scale (onehot - p) in the tile's epilogue, and the piece adds G W to
 // dH and gives its rows G^T H of dW:
 //   8 n V d operations for n tokens, of which 2 n V d are the second forming.
-// Rows whose target is masked are left out of everything: k_front (many rows: k_live) lists the live
-// ones, each example's padded with empty rows to a multiple of 16.
+// Rows whose target is masked are left out of everything: k_front (k_live, of many
+// rows) lists the live ones, each example's padded with empty rows to a multiple of 16.
 //
 // All three products are one kernel core, C[m][n] = sum_k A[m][k] B[n][k], which
 // takes its operands as they lie, with K along their rows or across them (Side
