@@ -22,7 +22,9 @@
 //   of two that brings the largest to 2^13, and each product is the three hi lo,
 //   lo hi, hi hi: a large library product reaches 153 TFLOP/s in fp32, 1256 in
 //   fp16.  What lo cannot hold is below 2^-38 of the largest entry of the row (of
-//   the weight in the gradient).
+//   the weight in the gradient).  For dW G is split under powers of two of its own
+//   (Powers below), so that a vocabulary entry that no token finds likely, and an
+//   example whose factors are small, keep their bits.
 //
 // What bounds it: the products, at the rate that their operands leave the caches
 // (the figures are at Tiling); below some hundred rows the reads of W; below those
@@ -50,12 +52,13 @@ constexpr int kStep = 64;   // K a stage
 constexpr int kPad = 16;    // an example's rows in the list come in multiples of it
 constexpr int kTop = 13;    // split operands lie below 2^(kTop + 1)
 constexpr int kNone = INT_MIN / 2;  // the exponent of nothing
+// G's entries under Powers lie below 2^(kTopG + 1), in a product below 2^kSlack times that
+[[maybe_unused]] constexpr int kTopG = 12, kSlack = 2;
 
 // What the kernels of a call share in its workspace.
 struct Meta {
-  int np;      // listed rows
-  int ew;      // exponent of the largest finite |W|
-  int ec[64];  // exponent bounds of dlogp scale H, those of every 64th row each: its atomics would queue at one
+  int np;  // listed rows
+  int ew;  // exponent of the largest finite |W|
 };
 
 // A listed row in the gradient: G = one [v = target] + w exp(scale (x - m)), logits being acc 2^(e + ew).  A row that only
@@ -95,6 +98,16 @@ __device__ __forceinline__ uint32_t two(float a, float b, int p) {
 // Split operands keep 32 hi and the 32 lo that belong to them side by side, a line of 128 bytes: the place of number p of
 // column k in a row.
 __device__ __forceinline__ int64_t split_at(int64_t k, int p) { return (k >> 5) * 64 + p * 32 + (k & 31); }
+
+// Powers of two of a split operand whose rows may hold anything from 1 down: 16 columns (K of the product) of a row share
+// one, that of the largest.  The product brings a group to the power of the largest that its row has had, so that what is
+// lost lies below 2^-37 of the row's largest entry.  The other operand's row at column k has left its own power to the entries of
+// that column, so that rows of any size meet in a sum.  G is the sum over t's operand: 16 rows of the list (one example's,
+// which come in multiples of 16) by an entry of the vocabulary.
+struct Powers {
+  const int *p;  // exponents [K / 16][rows]
+  int64_t ld;
+};
 
 // N elements of a row from column k on, zeros past the width
 template <int N, typename T>
@@ -254,7 +267,6 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
       a.seg[0] = 0;
       a.meta->np = sum;
     }
-    a.meta->ec[lane] = kNone;
   }
   __syncthreads();
   for (int c0 = wave * U; c0 < chunks; c0 += 16 * U) {
@@ -288,10 +300,6 @@ __device__ __forceinline__ int wave_most(int v) {
   return v;
 }
 
-__device__ __forceinline__ void raise(int *most, int v) {  // an atomic only where it can change something
-  if (v > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, v);
-}
-
 struct Gather {
   const void *hidden;
   int64_t ld;
@@ -311,9 +319,9 @@ struct Gather {
 };
 
 // Row t of H at place n of the list (t < 0: a row of zeros), zeros to a width of kp, by a wave.  fp32: the row's exponent,
-// its split; in the gradient what that needs to know of it.  Gives the exponent bound of dlogp scale H.
+// its split; in the gradient what that needs to know of it.
 template <typename T>
-__device__ __forceinline__ int gather(const Gather &a, int n, int t) {
+__device__ __forceinline__ void gather(const Gather &a, int n, int t) {
   const int lane = threadIdx.x & 63;
   const T *row = (const T *)a.hidden + (int64_t)(t < 0 ? 0 : t) * a.ld;
   const int width = t < 0 ? 0 : a.width;
@@ -341,7 +349,7 @@ __device__ __forceinline__ int gather(const Gather &a, int n, int t) {
       *(u32x4 *)(hc + k) = Vec<bf16>::pack(f);
     }
   }
-  if (!a.prm) return kNone;
+  if (!a.prm) return;
   RowPrm p{INFINITY, 0.0f, 0.0f, e - 2 * kTop};
   float c = 0.0f;
   if (t >= 0) {
@@ -357,8 +365,6 @@ __device__ __forceinline__ int gather(const Gather &a, int n, int t) {
     if (sizeof(T) == 4) a.cs[n] = c;
     a.prm[n] = p;
   }
-  // a factor that is not finite makes NaNs by itself, and leaves the other examples their range
-  return c != 0.0f && fabsf(c) < INFINITY ? e + exponent_of(c) + 1 : kNone;
 }
 
 // the largest of n numbers, by a wave
@@ -378,8 +384,7 @@ __global__ __launch_bounds__(256) void k_gather(Gather a) {
     if (lane == 0) a.meta->ew = e;
   }
   if (n >= a.meta->np) return;
-  const int e = gather<T>(a, n, a.list[n]);
-  if (sizeof(T) == 4 && lane == 0 && e != kNone) raise(&a.meta->ec[n & 63], e);
+  gather<T>(a, n, a.list[n]);
 }
 
 struct Prep {
@@ -387,35 +392,24 @@ struct Prep {
   int64_t ld;
   int rows, width, kp;  // what there is, zeros up to kp columns
   Meta *meta;
-  // behind k_front: the parts of the weight's exponent and of that of dlogp scale H, which become meta's
-  const int *most, *ecs;
-  int parts, eparts;
-  // H: rows in list order, with their factors (fp32)
-  const int *list, *eh;
-  const float *cs;
+  // behind k_front: the parts of the weight's exponent, which become meta's
+  const int *most;
+  int parts;
   int *ev;  // W in fp32, forward: exponents of its rows, which bring their own powers of two
   uint16_t *out;  // [..][kp] numbers
 };
 
-// Rows as an operand takes them: padded with zeros to kp columns, fp32 split.  A wave a row, up to a multiple of 64 rows;
+// Rows of W as an operand takes them: padded with zeros to kp columns, fp32 split.  A wave a row, up to a multiple of 64 rows;
 // `block` counts groups of WAVES rows.
-template <typename T, bool LIST, int WAVES>
+template <typename T, int WAVES>
 __device__ __forceinline__ void prep(const Prep &a, int block) {
   constexpr int P = sizeof(T) == 4 ? 2 : 1;
   const int r = block * WAVES + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (LIST ? r >= a.meta->np : r >= (a.rows + 63) / 64 * 64) return;
-  int64_t at = r < a.rows ? r : -1;
-  if (LIST) at = a.list[r];
-  const T *row = (const T *)a.src + (at < 0 ? 0 : at) * a.ld;
-  const int width = at < 0 ? 0 : a.width;
-  float scale = 1.0f;
+  if (r >= (a.rows + 63) / 64 * 64) return;
+  const T *row = (const T *)a.src + (r < a.rows ? r : 0) * a.ld;
+  const int width = r < a.rows ? a.width : 0;
   int e = 0;
-  if (LIST) {
-    const int most = a.ecs ? most_of(a.ecs, a.eparts) : wave_most(a.meta->ec[lane]);
-    if (a.ecs && r == 0) a.meta->ec[lane] = most;
-    e = a.eh[r];
-    scale = ldexpf(a.cs[r], e - most);
-  } else if (P == 2) {
+  if (P == 2) {
     if (a.ev) {
       e = row_exponent(row, width);
       if (lane == 0) a.ev[r] = e;
@@ -432,7 +426,7 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
     row_part<8>(row, k, width, f);
     if (P == 2) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = LIST ? ldexpf(f[i], kTop - e) * (at < 0 ? 0.0f : scale) : ldexpf(f[i], kTop - e);
+      for (int i = 0; i < 8; ++i) f[i] = ldexpf(f[i], kTop - e);
     }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -444,13 +438,9 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
   }
 }
 
-// H by the first `blocks` workgroups, W by the others
 template <typename T>
-__global__ __launch_bounds__(256) void k_prep(Prep h, Prep w, int blocks) {
-  if ((int)blockIdx.x < blocks)
-    prep<T, true, 4>(h, blockIdx.x);
-  else
-    prep<T, false, 4>(w, blockIdx.x - blocks);
+__global__ __launch_bounds__(256) void k_prep(Prep a) {
+  prep<T, 4>(a, blockIdx.x);
 }
 
 // The list, H's rows and what of W waits for neither, in one launch, for up to 64 chunks of 64 rows: each workgroup counts
@@ -463,7 +453,6 @@ struct Front {
   Gather g;
   Prep w;
   int blocks;
-  int *ecs;  // [blocks]
 };
 constexpr int kFrontChunks = 64;
 
@@ -476,7 +465,7 @@ __global__ __launch_bounds__(1024) void k_front(Front a) {
     if (sizeof(T) == 4 && a.g.prm)
       largest(a.l, b, gridDim.x - a.blocks, lds);
     else
-      prep<T, false, 16>(a.w, b);
+      prep<T, 16>(a.w, b);
     return;
   }
   constexpr int U = kFrontChunks / 16;
@@ -505,7 +494,6 @@ __global__ __launch_bounds__(1024) void k_front(Front a) {
   }
   const int r = (blockIdx.x & 3) * 16 + wave, i = mine % per * 64 + r;
   const uint64_t live = __ballot(ids[lane] >= 0);
-  int e = kNone;
   if (i < a.l.n) {
     const int row = ex * a.l.n + i, target = ids[r];
     if (target >= 0) {
@@ -515,7 +503,7 @@ __global__ __launch_bounds__(1024) void k_front(Front a) {
         a.l.tgt[p] = target;
         a.l.pos[row] = p;
       }
-      e = gather<T>(a.g, p, row);
+      gather<T>(a.g, p, row);
     } else if (lane == 0) {
       masked(a.l, row);
     }
@@ -525,14 +513,6 @@ __global__ __launch_bounds__(1024) void k_front(Front a) {
     if (p < end) {
       if (lane == 0) a.l.list[p] = a.l.tgt[p] = -1;
       gather<T>(a.g, p, -1);
-    }
-  }
-  if (sizeof(T) == 4 && a.g.prm) {
-    if (lane == 0) lds[wave] = e;
-    __syncthreads();
-    if (wave == 0) {
-      const int m = wave_most(lds[lane & 15]);
-      if (lane == 0) a.ecs[blockIdx.x] = m;
     }
   }
 }
@@ -655,9 +635,24 @@ struct Side {
   }
 };
 
+// the largest of 16 lanes', in each of them
+__device__ __forceinline__ int most16(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, true));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, true));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xF, 0xF, true));
+  return max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xF, 0xF, true));
+}
+
+// eight fp16 numbers times 2^d, -14 <= d <= 15
+__device__ __forceinline__ u32x4 times_power(u32x4 v, int d) {
+  const _Float16 f = __builtin_bit_cast(_Float16, (uint16_t)((15 + d) << 10));
+  return __builtin_bit_cast(u32x4, __builtin_bit_cast(f16x8, v) * f16x8{f, f, f, f, f, f, f, f});
+}
+
 template <typename C, Mode M>
 struct Core {
   f32x16 acc[C::TM][C::TN];
+  int top[C::TM];  // with Powers: the exponent of row 32 i + lane % 32 in the sums so far
   int wm, wn, fr, fk;
 
   __device__ __forceinline__ Core() {
@@ -670,6 +665,35 @@ struct Core {
   // the tile's row of accumulator entry (i, e) of this lane, and its column of (j)
   __device__ __forceinline__ int row(int i, int e) const { return wm * (C::BM / C::WM) + i * 32 + (e >> 2) * 8 + fk * 4 + (e & 3); }
   __device__ __forceinline__ int col(int j) const { return wn * (C::BN / C::WN) + j * 32 + fr; }
+  // what lane `row % 32` of the 32 x 32 accumulators holds, for entry e's row
+  template <typename T>
+  __device__ __forceinline__ T of_row(T v, int e) const {
+    return __shfl(v, (e >> 2) * 8 + fk * 4 + (e & 3), 64);
+  }
+
+  // Block i of a, a group under the power of e, comes to its rows' power; where it would not fit, the sums come down first.
+  template <int P>
+  __device__ __forceinline__ void align(int i, int e, u32x4 (&f)[P][C::TM]) {
+    if (__any(e > top[i] + kSlack)) {
+      const int t = e > top[i] + kSlack ? e : top[i];
+      const float down = ldexpf(1.0f, max(top[i] - t, -300));
+      top[i] = t;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const float g = of_row(down, q);
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) acc[i][j][q] *= g;
+      }
+    }
+    const int d = e - top[i], first = max(d, -14);
+#pragma unroll
+    for (int p = 0; p < P; ++p) f[p][i] = times_power(f[p][i], first);
+    if (__any(d < -14)) {  // 2^-28 of the row's largest has nothing left to add
+      const int rest = max(d - first, -15);
+#pragma unroll
+      for (int p = 0; p < P; ++p) f[p][i] = times_power(f[p][i], rest);
+    }
+  }
 
   __device__ __forceinline__ void multiply(const u32x4 *fa, const u32x4 *fb) {
 #pragma unroll
@@ -690,9 +714,11 @@ struct Core {
   // kSplit: both numbers of both operands are in a stage, each is read once for hi lo, lo hi and hi hi (one stage for each
   // of the three: gradients of 8 x 257 x 50257 x 768, each example's, 1774 us with the log-probabilities, 1659 us so).
   // kPair: all of K with a's lo, then with its hi.
-  template <bool KA, bool KB>
+  // POW: a has Powers.  Each row begins at the largest of its first 256 columns (one trip to the caches), so that few groups
+  // bring the sums down.
+  template <bool KA, bool KB, bool POW = false>
   __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth,
-                                      int depth_b) {
+                                      int depth_b, Powers pw = Powers{}) {
     constexpr int P = M == kSplit ? 2 : 1, HALF = C::BM * kStep * 2, STAGE = HALF + C::BN * kStep * 2;
     using A = Side<C::BM, C::WM, C::TH, KA, P>;
     using B = Side<C::BN, C::WN, C::TH, KB, P>;
@@ -717,21 +743,58 @@ struct Core {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     const int all = steps * (M == kPair ? 2 : 1);
+    constexpr int G = A::KS / 16;  // groups of a stage
+    const int groups = depth / 16;
+    int next[G][C::TM];
+    auto powers = [&](int k) {
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+          next[g][i] = pw.p[min(k * G + g, groups - 1) * pw.ld + wm * (C::BM / C::WM) + i * 32 + fr];
+    };
+    if (POW) {
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i) {
+        top[i] = kNone;
+        for (int g = 0; g < min(groups, 16); g += 4)
+#pragma unroll
+          for (int h = 0; h < 4; ++h)
+            top[i] = max(top[i], pw.p[min(g + h, groups - 1) * pw.ld + wm * (C::BM / C::WM) + i * 32 + fr]);
+      }
+      if (groups) powers(0);
+    }
     if (all > 0) load(0);
     for (int s = 0; s < all; ++s) {
       // the loads of this stage, and the reads of the buffer that the next one gets
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
+      int now[G][C::TM];
+      if (POW) {
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i) {
+            now[g][i] = next[g][i];
+            asm volatile("" : "+v"(now[g][i]));  // they have arrived: not waited for behind the loads that follow
+          }
+        if (s + 1 < all) powers(s + 1);
+      }
       if (s + 1 < all) load((s + 1) & 1);
       const char *at = lds + (s & 1) * STAGE;
 #pragma unroll
       for (int ks = 0; ks < A::KS / 16; ++ks) {
+        if (POW && s * G + ks >= groups) break;
         u32x4 fa[P][C::TM], fb[P][C::TN];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           sa.read(at, wm, ks, p, fa[p]);
           sb.read(at + HALF, wn, ks, p, fb[p]);
+        }
+        if constexpr (POW) {
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i) align(i, now[ks][i], fa);
         }
         if (P == 2) {
           multiply(fa[0], fb[P - 1]);
@@ -758,6 +821,7 @@ __device__ __forceinline__ int64_t g_at(int64_t plane, int64_t piece, int64_t n,
   return M == kSplit ? n * piece * 2 + split_at(v, p) : p * plane + n * piece + v;
 }
 
+#if defined(__HIP_DEVICE_COMPILE__)
 // Tile number b of mt x nt: workgroups go to the eight XCDs in turn, and each XCD takes a run of tiles, in groups of
 // eight of m, so that its L2 holds the rows that its CUs share.
 __device__ __forceinline__ void tile_of(int b, int mt, int nt, int &tm, int &tn) {
@@ -767,6 +831,7 @@ __device__ __forceinline__ void tile_of(int b, int mt, int nt, int &tm, int &tn)
   tm = g * 8 + (b - g * per) % gm;
   tn = (b - g * per) / gm;
 }
+#endif
 
 struct Logit {
   Operand w, h;
@@ -783,6 +848,10 @@ struct Logit {
   uint16_t *g;  // [tcap][piece] entries
   float *rest;  // [tcap], bf16: what the rounding of the target's entry has left
   int64_t gplane, piece;
+  // fp32: G for dH (g, beside a factor of the row; NULL if not wanted) and for dW (gw, whole, under the powers pw)
+  uint16_t *gw;
+  int *pw;  // [tcap / 16][piece]
+  const float *cs;
 };
 
 template <typename C, Mode M, bool GRAD>
@@ -845,10 +914,11 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
             if (m0 + c.row(i, e) >= a.valid) c.acc[i][j][e] = 0.0f;
       }
       // the one or two numbers of an entry, as bits
+      if (!F16)
 #pragma unroll
-      for (int i = 0; i < C::TM; ++i)
+        for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) c.acc[i][j][e] = __uint_as_float(split<M>(c.acc[i][j][e]));
+          for (int e = 0; e < 16; ++e) c.acc[i][j][e] = __uint_as_float(split<M>(c.acc[i][j][e]));
     } else {
       const int ex = F16 && in ? a.eh[n] - 2 * kTop : 0;
       const float k2 = power_of(a.scale).k;
@@ -891,6 +961,66 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   if (!GRAD) return;
   // G's rows leave through LDS, in whole lines (chunks of 16 bytes exchanged by the row, so that the lanes of a write meet
   // different banks).
+  if constexpr (F16) {  // hi and lo of 32 columns of the waves' accumulators at a time, in two places by turns
+    constexpr int RW = C::BM * 4, CH = RW / 16, ROWS = 32 * C::WN;
+    static_assert(ROWS * RW <= C::LDS, "a turn fits");
+    constexpr int PLACES = 2 * ROWS * RW <= C::LDS ? 2 : 1;
+    int turn = 0;
+    auto leave = [&](int j, const uint32_t (&bits)[C::TM][16], uint16_t *to) {
+      char *at = lds + (turn % PLACES) * ROWS * RW;
+      if (PLACES == 1 || turn == 0) __syncthreads();
+      ++turn;
+      const int n = c.wn * 32 + c.fr;
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const int m = c.row(i, e), ch = (m >> 5) * 8 + p * 4 + ((m & 31) >> 3);
+            const uint32_t sel = p ? 0x07060302 : 0x05040100;
+            *(u32x2 *)(at + n * RW + (ch ^ (n & 31)) * 16 + (m & 4) * 2) =
+                u32x2{__builtin_amdgcn_perm(bits[i][e + 1], bits[i][e], sel), __builtin_amdgcn_perm(bits[i][e + 3], bits[i][e + 2], sel)};
+          }
+      __syncthreads();
+#pragma unroll 4
+      for (int k = threadIdx.x; k < ROWS * CH; k += C::TH) {
+        const int r = k / CH, ch = k % CH, row = n0 + (r >> 5) * (C::BN / C::WN) + j * 32 + (r & 31);
+        if (row < np)
+          *(u32x4 *)(to + (int64_t)row * a.piece * 2 + m0 * 2 + ch * 8) = *(const u32x4 *)(at + r * RW + (ch ^ (r & 31)) * 16);
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+      uint32_t bits[C::TM][16];
+      if (a.g) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) bits[i][e] = split<M>(c.acc[i][j][e]);
+        leave(j, bits, a.g);
+      }
+      if (a.gw) {
+        const int n = n0 + c.col(j);
+        const int eh = n < np ? a.eh[n] : 0;
+        const float f = n < np ? a.cs[n] * (1.0f / (1 << kTop)) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) {
+          int mine = kNone;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float y = c.acc[i][j][e] * f;
+            const int most = most16(exponent_of(y) + eh);
+            bits[i][e] = split<M>(ldexpf(y, eh + kTopG - most));
+            if ((c.fr & 15) == e) mine = most;
+          }
+          if (n < np) a.pw[(int64_t)(n >> 4) * a.piece + m0 + c.row(i, c.fr & 15)] = mine;
+        }
+        leave(j, bits, a.gw);
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int plane = 0; plane < (M == kBf16 ? 1 : 2); ++plane) {
     constexpr int CH = C::BM / 8;
@@ -949,6 +1079,10 @@ struct Few {
   const RowPrm *prm;
   uint16_t *g;
   int64_t gplane, piece;
+  uint16_t *gw;  // fp32, as in Logit
+  int *pw;
+  const int *eh;
+  const float *cs;
 };
 
 // Logits of up to 16 rows by 16 entries of the vocabulary a wave.  Lane l holds row l % 16 of both operands; its eight
@@ -1000,26 +1134,55 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
   if constexpr (GRAD) {
     constexpr Mode M = sizeof(T) == 4 ? kSplit : kPair;
     const int at = v0 - a.v0 + q * 4;
+    float g[4];
+    auto leave = [&](uint16_t *to, const float *x) {
+#pragma unroll
+      for (int plane = 0; plane < 2; ++plane)
+        *(u32x2 *)(to + g_at<M>(a.gplane, a.piece, n, at, plane)) = u32x2{two<M>(x[0], x[1], plane), two<M>(x[2], x[3], plane)};
+    };
     if (n >= 0) {
       const RowPrm p = a.prm[n];
       const Power pw = power_of(a.scale);
-      float g[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         g[e] = p.w * entry_exp<T>(acc[e] - p.m, pw);
         if (v0 + q * 4 + e == target) g[e] += p.one;
         if (at + e >= a.valid) g[e] = 0.0f;
       }
+      if (a.g) leave(a.g, g);
+    }
+    const int np = a.meta->np;
+    if (M == kSplit && a.gw) {  // up to 16 groups of rows, by the unit's entries of the vocabulary
+      __shared__ int most[kFew][kFewUnit];
+      for (int i = threadIdx.x; i < kFew * kFewUnit; i += 256) (&most[0][0])[i] = kNone;
+      __syncthreads();
+      const int eh = n >= 0 ? a.eh[n] : 0;
+      const float f = n >= 0 ? a.cs[n] * (1.0f / (1 << kTop)) : 0.0f;
+      int *mine = &most[n >= 0 ? n >> 4 : 0][wave * 16 + q * 4];
+      if (n >= 0)
 #pragma unroll
-      for (int plane = 0; plane < (M == kBf16 ? 1 : 2); ++plane)
-        *(u32x2 *)(a.g + g_at<M>(a.gplane, a.piece, n, at, plane)) = u32x2{two<M>(g[0], g[1], plane), two<M>(g[2], g[3], plane)};
+        for (int e = 0; e < 4; ++e) {
+          g[e] *= f;
+          atomicMax(mine + e, exponent_of(g[e]) + eh);
+        }
+      __syncthreads();
+      if (n >= 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g[e] = ldexpf(g[e], eh + kTopG - mine[e]);
+        leave(a.gw, g);
+      }
+      for (int i = threadIdx.x; i < np / 16 * kFewUnit; i += 256)
+        a.pw[(int64_t)(i / kFewUnit) * a.piece + blockIdx.x * kFewUnit + i % kFewUnit] = most[i / kFewUnit][i % kFewUnit];
     }
     // rows that only fill the list
-    for (int i = threadIdx.x >> 3; i < a.meta->np; i += 32)
+    for (int i = threadIdx.x >> 3; i < np; i += 32)
       if (a.list[i] < 0)
 #pragma unroll
-        for (int plane = 0; plane < 2; ++plane)
-          *(u32x4 *)(a.g + g_at<M>(a.gplane, a.piece, i, blockIdx.x * kFewUnit + (threadIdx.x & 7) * 8, plane)) = u32x4{0, 0, 0, 0};
+        for (int plane = 0; plane < 2; ++plane) {
+          const int64_t to = g_at<M>(a.gplane, a.piece, i, blockIdx.x * kFewUnit + (threadIdx.x & 7) * 8, plane);
+          if (a.g) *(u32x4 *)(a.g + to) = u32x4{0, 0, 0, 0};
+          if (M == kSplit && a.gw) *(u32x4 *)(a.gw + to) = u32x4{0, 0, 0, 0};
+        }
     return;
   }
   const float k2 = power_of(a.scale).k;
@@ -1144,8 +1307,9 @@ struct Back {
   bool first;
   float *acc;     // [splits][tcap][kp]
   int kp;
-  // dW = G^T H (fp32: H times the rows' factors)
-  Operand h;
+  // dW = G^T H (fp32: of its own G, under Powers)
+  Operand gw, h;
+  Powers pw;
   int valid, b0;  // rows of the piece, the launch's first example
   void *out;      // rows from the piece's first on
   int64_t vocab;  // rows from example to example
@@ -1177,7 +1341,8 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
     c.template run<false, true>(lds, at_row<M>(a.g, m0, k0), at_row<M>(a.w, k0, n0), np - m0, a.kp - n0, depth,
                                 F16 ? a.steps * kStep - k0 : a.valid - k0);
   else
-    c.template run<true, true>(lds, at_row<M>(a.g, k0, m0), at_row<M>(a.h, k0, n0), C::BM, a.kp - n0, depth, depth);
+    c.template run<true, true, F16>(lds, at_row<M>(a.gw, k0, m0), at_row<M>(a.h, k0, n0), C::BM, a.kp - n0, depth, depth,
+                                    Powers{a.pw.p + k0 / 16 * a.pw.ld + m0, a.pw.ld});
   if (hidden) {
     float *to = a.acc + (part * a.tcap + m0) * a.kp + n0;
     const int ew = F16 ? a.meta->ew - 2 * kTop : 0;
@@ -1196,7 +1361,12 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
         }
     }
   } else {
-    const float f = F16 && depth ? ldexpf(1.0f, max(wave_most(a.meta->ec[threadIdx.x & 63]), -300) - 2 * kTop) : 1.0f;
+    int power[C::TM][16];  // by all lanes, before those of columns that there are not leave
+    if (F16)
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) power[i][e] = c.of_row(c.top[i], e) - kTopG - kTop;
     TO *to = (TO *)a.out + ((a.b0 + part) * a.vocab + m0) * a.width + n0;
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
@@ -1208,7 +1378,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
           const int m = c.row(i, e);
           if (m0 + m >= a.valid) continue;
           TO *p = to + (int64_t)m * a.width + c.col(j);
-          const float v = F16 ? c.acc[i][j][e] * f : c.acc[i][j][e];
+          const float v = F16 ? ldexpf(c.acc[i][j][e], power[i][e]) : c.acc[i][j][e];
           const TO r = from_f32<TO>(a.accumulate ? v + to_f32(*p) : v);
           if (a.past) {
             asm volatile("");  // or the compiler makes one ordinary store of the two
@@ -1282,7 +1452,7 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Plan {
   bool f16, grad, few, pair, copy, large, huge, front;
   int64_t batch, n, chunks, tcap, kp, piece, pieces, units, splits, planes, gplanes;  // numbers of an operand's entry, of G's
-  int64_t list, pos, tgt, seg, cnt, most, ecs, meta, hc, eh, ev, part, xt, run, prm, cs, rest, hs, wc, g, acc, bytes;
+  int64_t list, pos, tgt, seg, cnt, most, meta, hc, eh, ev, part, xt, run, prm, cs, rest, wc, g, gw, pw, acc, bytes;
 };
 
 Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
@@ -1343,7 +1513,6 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.seg = take(4 * (batch + 1));
   p.cnt = take(4 * p.chunks);
   p.most = take(4 * kMost);
-  p.ecs = take(4 * 4 * kFrontChunks);
   p.meta = take(sizeof(Meta));
   p.hc = take(2 * p.planes * p.tcap * p.kp);
   p.eh = take(4 * p.tcap);
@@ -1357,8 +1526,11 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     p.prm = take(sizeof(RowPrm) * p.tcap);
     p.cs = take(4 * p.tcap);
     p.rest = take(4 * p.tcap);
-    if (dweight && p.f16) p.hs = take(2 * p.planes * p.tcap * p.kp);
-    p.g = take(2 * p.gplanes * p.tcap * p.piece);
+    if (dhidden || !p.f16) p.g = take(2 * p.gplanes * p.tcap * p.piece);
+    if (dweight && p.f16) {
+      p.gw = take(2 * p.gplanes * p.tcap * p.piece);
+      p.pw = take(4 * (p.tcap / 16) * p.piece);
+    }
     if (dhidden) p.acc = take(4 * p.splits * p.tcap * p.kp);
   }
   p.bytes = at;
@@ -1427,7 +1599,7 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
                  p.grad ? ptr<RowPrm>(work, p.prm) : nullptr, ptr<float>(work, p.cs)};
   if (p.front) {
     const int64_t valid = std::min(p.piece, x->vocab);
-    const Front f{l, g, weights_of(x, p, 0, valid, work), (int)p.chunks * 4, ptr<int>(work, p.ecs)};
+    const Front f{l, g, weights_of(x, p, 0, valid, work), (int)p.chunks * 4};
     const dim3 grid((unsigned)(f.blocks + (in_front(p) ? up(valid, 64) / 16 : parts))), block(1024);
     if (p.f16)
       hipLaunchKernelGGL(k_front<float>, grid, block, 0, st, f);
@@ -1442,8 +1614,8 @@ void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *s
     hipLaunchKernelGGL(k_gather<bf16>, dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, g);
 }
 
-// W's rows from v0 on as an operand; what the same launch does for H, if anything
-Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, const Prep *h, void *work, hipStream_t st) {
+// W's rows from v0 on as an operand
+Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, void *work, hipStream_t st) {
   Prep a = weights_of(x, p, v0, valid, work);
   if (!p.copy) return Operand{{(const uint16_t *)a.src, (const uint16_t *)a.src}, x->ld_weight};
   const Operand o{{a.out, a.out}, p.kp * p.planes};
@@ -1452,12 +1624,11 @@ Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, co
     a.most = ptr<int>(work, p.most);
     a.parts = parts_of(x, p);
   }
-  const int blocks = h ? (int)(p.tcap / 4) : 0;
-  const dim3 grid((unsigned)(blocks + up(valid, 64) / 4));
+  const dim3 grid((unsigned)(up(valid, 64) / 4));
   if (p.f16)
-    hipLaunchKernelGGL(k_prep<float>, grid, dim3(256), 0, st, h ? *h : a, a, blocks);
+    hipLaunchKernelGGL(k_prep<float>, grid, dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL(k_prep<bf16>, grid, dim3(256), 0, st, a, a, 0);
+    hipLaunchKernelGGL(k_prep<bf16>, grid, dim3(256), 0, st, a);
   return o;
 }
 
@@ -1547,7 +1718,7 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
     const int units = (int)p.units;
     const Few a{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)x->width,
                 (int)x->index, x->scale, ptr<float2>(work, p.part), ptr<float>(work, p.xt), units, logp, (float2 *)stats, 0, 0, nullptr,
-                nullptr, nullptr, nullptr, nullptr, 0, 0};
+                nullptr, nullptr, nullptr, nullptr, 0, 0, nullptr, nullptr, nullptr, nullptr};
     if (p.f16)
       hipLaunchKernelGGL((k_few<float, false>), dim3(units), dim3(256), 0, st, a);
     else
@@ -1558,7 +1729,7 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
   begin(x, p, nullptr, nullptr, logp, stats, work, st);
   for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
     const int64_t valid = std::min(p.piece, x->vocab - v0);
-    Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, nullptr, work, st), work);
+    Logit a = logit_of(x, p, v0, valid, weights(x, p, v0, valid, work, st), work);
     a.part = ptr<float2>(work, p.part);
     a.xt = ptr<float>(work, p.xt);
     run_logits<false>(p, a, st);
@@ -1592,35 +1763,25 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   begin(x, p, dlogp ? dlogp : (const float *)work, stats, nullptr, nullptr, work, st);
   Meta *meta = ptr<Meta>(work, p.meta);
   const int64_t width = x->width;
-  const bool hs = dweight && p.f16;  // dW of fp32 takes H with the rows' factors
-  Prep h{};
-  h.src = x->hidden;
-  h.ld = x->ld_hidden;
-  h.width = (int)width;
-  h.kp = (int)p.kp;
-  h.meta = meta;
-  h.list = ptr<int>(work, p.list);
-  h.eh = ptr<int>(work, p.eh);
-  h.cs = ptr<float>(work, p.cs);
-  if (p.front) {
-    h.ecs = ptr<int>(work, p.ecs);
-    h.eparts = (int)p.chunks * 4;
-  }
-  h.out = ptr<uint16_t>(work, p.hs);
+  uint16_t *g = dhidden || !p.f16 ? ptr<uint16_t>(work, p.g) : nullptr;
+  uint16_t *gw = dweight && p.f16 ? ptr<uint16_t>(work, p.gw) : nullptr;
   for (int64_t v0 = 0; v0 < x->vocab; v0 += p.piece) {
     const int64_t valid = std::min(p.piece, x->vocab - v0);
-    const Operand w = x->rows ? weights(x, p, v0, valid, hs && v0 == 0 ? &h : nullptr, work, st) : Operand{};
+    const Operand w = x->rows ? weights(x, p, v0, valid, work, st) : Operand{};
     if (x->rows) {
       Logit a = logit_of(x, p, v0, valid, w, work);
       a.prm = ptr<RowPrm>(work, p.prm);
-      a.g = ptr<uint16_t>(work, p.g);
+      a.g = g;
       a.rest = ptr<float>(work, p.rest);
       a.gplane = p.tcap * p.piece;
       a.piece = p.piece;
+      a.gw = gw;
+      a.pw = ptr<int>(work, p.pw);
+      a.cs = ptr<float>(work, p.cs);
       if (x->rows <= kFew) {
         const Few f{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)width,
                     (int)x->index, x->scale, nullptr, nullptr, 0, nullptr, nullptr, (int)v0, (int)valid, meta,
-                    ptr<int>(work, p.pos), ptr<int>(work, p.list), a.prm, a.g, a.gplane, a.piece};
+                    ptr<int>(work, p.pos), ptr<int>(work, p.list), a.prm, a.g, a.gplane, a.piece, a.gw, a.pw, a.eh, a.cs};
         const dim3 grid((unsigned)((valid + kFewUnit - 1) / kFewUnit));
         if (p.f16)
           hipLaunchKernelGGL((k_few<float, true>), grid, dim3(256), 0, st, f);
@@ -1635,7 +1796,7 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
     a.meta = meta;
     a.seg = ptr<int>(work, p.seg);
     a.tcap = p.tcap;
-    const uint16_t *g = ptr<uint16_t>(work, p.g), *hd = ptr<uint16_t>(work, p.f16 ? p.hs : p.hc);
+    const uint16_t *hd = ptr<uint16_t>(work, p.hc);
     a.g = Operand{{g, g + (p.pair ? p.tcap * p.piece : 0)}, p.piece * p.planes};
     a.w = w;
     a.steps = (int)(up(valid, kStep) / kStep);
@@ -1644,6 +1805,8 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
     a.first = v0 == 0;
     a.acc = ptr<float>(work, p.acc);
     a.kp = (int)p.kp;
+    a.gw = gw ? Operand{{gw, gw}, p.piece * p.planes} : a.g;
+    a.pw = Powers{ptr<int>(work, p.pw), p.piece};
     a.h = Operand{{hd, hd}, p.kp * p.planes};
     a.valid = (int)valid;
     a.out = (char *)dweight + v0 * width * (dweight_dtype == SK_F32 ? 4 : 2);
