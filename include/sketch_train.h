@@ -188,7 +188,7 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
  * products, whatever the type of dweight (up to 256 rows: to two bf16, 2^-16; dhidden
  * gets back what the target's entry has lost).  fp32 inputs: products as above; of dweight[b][v]
  * what lies below 2^-37 of its largest |g_tv| max |hidden[t]| is lost, of dhidden[t]
- * what lies below 2^-38 of dlogp[t] times the largest entry of weight.  A weight that
+ * what lies below 2^-36 of dlogp[t] times the largest entry of weight.  A weight that
  * is not finite gives NaNs.  Rows with dlogp = 0 are masked.  Outputs may not overlap
  * inputs.
  *   work     sketch_linear_logp_grad_work_bytes(x, batch, dhidden wanted, dweight

@@ -21,10 +21,10 @@
 //   fp32 inputs are split, x = hi + lo in two fp16 numbers (22 bits) under a power
 //   of two that brings the largest to 2^13, and each product is the three hi lo,
 //   lo hi, hi hi: a large library product reaches 153 TFLOP/s in fp32, 1256 in
-//   fp16.  What lo cannot hold is below 2^-38 of the largest entry of the row (of
-//   the weight in the gradient).  For dW G is split under powers of two of its own
-//   (Powers below), so that a vocabulary entry that no token finds likely, and an
-//   example whose factors are small, keep their bits.
+//   fp16.  What lo cannot hold is below 2^-38 of the largest entry of the row.  G
+//   is split under powers of two of its own for each of its products (Powers
+//   below), so that a vocabulary entry that no token finds likely, and an example
+//   whose factors are small, keep their bits.
 //
 // What bounds it: the products, at the rate that their operands leave the caches
 // (the figures are at Tiling); below some hundred rows the reads of W; below those
@@ -51,21 +51,19 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = 64;   // K a stage
 constexpr int kPad = 16;    // an example's rows in the list come in multiples of it
 constexpr int kTop = 13;    // split operands lie below 2^(kTop + 1)
-constexpr int kNone = INT_MIN / 2;  // the exponent of nothing
-// G's entries under Powers lie below 2^(kTopG + 1), in a product below 2^kSlack times that
+[[maybe_unused]] constexpr int kNone = INT_MIN / 2;  // the exponent of nothing
+// Split entries of G lie below 2^(kTopG + 1), in a product below 2^(kTopG + 1 + kSlack)
 [[maybe_unused]] constexpr int kTopG = 12, kSlack = 2;
 
 // What the kernels of a call share in its workspace.
 struct Meta {
   int np;  // listed rows
-  int ew;  // exponent of the largest finite |W|
 };
 
-// A listed row in the gradient: G = one [v = target] + w exp(scale (x - m)), logits being acc 2^(e + ew).  A row that only
+// A listed row in the gradient: G = one [v = target] + w exp(scale (x - m)).  A row that only
 // fills the list, or has no logit above -inf, has m = inf, w = one = 0.
 struct RowPrm {
-  float m, w, one;
-  int e;
+  float m, w, one;  // fp32: without the factor dlogp scale, which is in cs
 };
 
 __device__ __forceinline__ int exponent_of(uint32_t bits) { return (int)((bits >> 23) & 255) - 127; }
@@ -99,15 +97,18 @@ __device__ __forceinline__ uint32_t two(float a, float b, int p) {
 // column k in a row.
 __device__ __forceinline__ int64_t split_at(int64_t k, int p) { return (k >> 5) * 64 + p * 32 + (k & 31); }
 
-// Powers of two of a split operand whose rows may hold anything from 1 down: 16 columns (K of the product) of a row share
-// one, that of the largest.  The product brings a group to the power of the largest that its row has had, so that what is
-// lost lies below 2^-37 of the row's largest entry.  The other operand's row at column k has left its own power to the entries of
-// that column, so that rows of any size meet in a sum.  G is the sum over t's operand: 16 rows of the list (one example's,
-// which come in multiples of 16) by an entry of the vocabulary.
+// Powers of two of a split G.  The other operand's row at column k has left its own power to the entries of that column.
+//   kRows (dW): G's entries may be anything from 1 down.  16 columns (tokens of one example: they come in multiples of 16)
+//   of a row (an entry of the vocabulary) share the power of the largest of them; the product brings each group to that of
+//   the largest that its row has had.  What is lost lies below 2^-37 of the row's largest entry.
+//   kBlocks (dH): G is a fixed-point number beside 1; 64 columns (entries of the vocabulary) of all rows share the power of
+//   the largest row of W among them, in steps of 2^4, so that the powers of most weights are all the same.
+enum Scaling { kPlain, kRows, kBlocks };
 struct Powers {
-  const int *p;  // exponents [K / 16][rows]
+  const int *p;  // exponents [K / 16][rows], [K / 64]
   int64_t ld;
 };
+[[maybe_unused]] constexpr int kCoarse = 4;
 
 // N elements of a row from column k on, zeros past the width
 template <int N, typename T>
@@ -152,15 +153,7 @@ struct Live {
   Meta *meta;
   float *logp;
   float2 *stats;
-  // fp32: the workgroups behind the first look for the largest finite |W|; as one long row where its rows have no gaps
-  const float *w;
-  int64_t ldw;
-  int width;
-  bool flat;
-  int *most;  // [workgroups - 1]
 };
-constexpr int kMost = 512;
-
 
 __device__ __forceinline__ int wave_scan(int v, int lane) {  // inclusive
 #pragma unroll
@@ -169,36 +162,6 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {  // inclusive
     if (lane >= d) v += o;
   }
   return v;
-}
-
-// exponent of the largest finite |W| that workgroup b of n meets
-__device__ __forceinline__ void largest(const Live &a, int b, int n, int *lds) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int e = kNone;
-  if (a.flat) {
-    constexpr int U = 4;
-    const f32x4 *p = (const f32x4 *)a.w;
-    const int64_t all = (int64_t)a.vocab * a.width / 4, step = (int64_t)n * 1024;
-    float big = 0.0f;
-    for (int64_t i = (int64_t)b * 1024 + threadIdx.x; i < all; i += U * step) {
-      f32x4 v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = p[i + u * step < all ? i + u * step : i];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) big = fmaxf(big, fabsf(v[u][k]) < INFINITY ? fabsf(v[u][k]) : 0.0f);
-    }
-    e = exponent_of(wave_all(big, OpMax()));
-  } else {
-    for (int64_t r = b * 16 + wave; r < a.vocab; r += n * 16) e = max(e, row_exponent(a.w + r * a.ldw, a.width));
-  }
-  if (lane == 0) lds[wave] = e;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < 16; ++i) e = max(e, lds[i]);
-    a.most[b] = e;
-  }
 }
 
 // the row (-1: none) and target (-1: masked) of this lane in chunk c; an example has `per` of them
@@ -222,15 +185,10 @@ __device__ __forceinline__ void masked(const Live &a, int row) {
   }
 }
 
-// The first workgroup: counts of 64 rows each, their sums within the examples, the examples' starts, the list.  A wave has
+// Counts of 64 rows each, their sums within the examples, the examples' starts, the list.  A wave has
 // four chunks of 64 rows under way (8192 rows: 17 us one after another, 14.5 us so).
 __global__ __launch_bounds__(1024) void k_live(Live a) {
   constexpr int U = 4;
-  __shared__ int lds[16];
-  if (blockIdx.x > 0) {
-    largest(a, blockIdx.x - 1, gridDim.x - 1, lds);
-    return;
-  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = (a.n + 63) / 64, chunks = per * a.batch;
   for (int c0 = wave * U; c0 < chunks; c0 += 16 * U) {
@@ -294,12 +252,6 @@ __global__ __launch_bounds__(1024) void k_live(Live a) {
 }
 
 // --- operands -----------------------------------------------------------------------------------------------
-__device__ __forceinline__ int wave_most(int v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = max(v, __shfl_xor(v, d, 64));
-  return v;
-}
-
 struct Gather {
   const void *hidden;
   int64_t ld;
@@ -308,8 +260,6 @@ struct Gather {
   Meta *meta;
   uint16_t *hc;
   int *eh;
-  const int *most;
-  int parts;
   // gradient only
   const float2 *stats;
   const float *dlogp;
@@ -350,14 +300,14 @@ __device__ __forceinline__ void gather(const Gather &a, int n, int t) {
     }
   }
   if (!a.prm) return;
-  RowPrm p{INFINITY, 0.0f, 0.0f, e - 2 * kTop};
+  RowPrm p{INFINITY, 0.0f, 0.0f};
   float c = 0.0f;
   if (t >= 0) {
     const float2 s = a.stats[t];
     if (s.y != 0.0f) {
       c = a.dlogp[t] * a.scale;
       p.m = s.x;
-      p.one = sizeof(T) == 4 ? (float)(1 << kTop) : c;
+      p.one = sizeof(T) == 4 ? 1.0f : c;
       p.w = -p.one / s.y;
     }
   }
@@ -367,22 +317,10 @@ __device__ __forceinline__ void gather(const Gather &a, int n, int t) {
   }
 }
 
-// the largest of n numbers, by a wave
-__device__ __forceinline__ int most_of(const int *p, int n) {
-  int v = kNone;
-#pragma unroll 4
-  for (int i = threadIdx.x & 63; i < n; i += 64) v = max(v, p[i]);
-  return wave_most(v);
-}
-
 // a wave a row
 template <typename T>
 __global__ __launch_bounds__(256) void k_gather(Gather a) {
-  const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (sizeof(T) == 4 && n == 0) {
-    const int e = most_of(a.most, a.parts);
-    if (lane == 0) a.meta->ew = e;
-  }
+  const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (n >= a.meta->np) return;
   gather<T>(a, n, a.list[n]);
 }
@@ -391,11 +329,7 @@ struct Prep {
   const void *src;
   int64_t ld;
   int rows, width, kp;  // what there is, zeros up to kp columns
-  Meta *meta;
-  // behind k_front: the parts of the weight's exponent, which become meta's
-  const int *most;
-  int parts;
-  int *ev;  // W in fp32, forward: exponents of its rows, which bring their own powers of two
+  int *ev;  // W in fp32: exponents of its rows, which bring their own powers of two
   uint16_t *out;  // [..][kp] numbers
 };
 
@@ -410,15 +344,8 @@ __device__ __forceinline__ void prep(const Prep &a, int block) {
   const int width = r < a.rows ? a.width : 0;
   int e = 0;
   if (P == 2) {
-    if (a.ev) {
-      e = row_exponent(row, width);
-      if (lane == 0) a.ev[r] = e;
-    } else if (a.most) {
-      e = most_of(a.most, a.parts);
-      if (r == 0 && lane == 0) a.meta->ew = e;
-    } else {
-      e = a.meta->ew;
-    }
+    e = row_exponent(row, width);
+    if (lane == 0) a.ev[r] = e;
   }
   uint16_t *out = a.out + (int64_t)r * a.kp * P;
   for (int k = lane * 8; k < a.kp; k += 512) {
@@ -443,9 +370,8 @@ __global__ __launch_bounds__(256) void k_prep(Prep a) {
   prep<T, 4>(a, blockIdx.x);
 }
 
-// The list, H's rows and what of W waits for neither, in one launch, for up to 64 chunks of 64 rows: each workgroup counts
-// the live rows by itself and takes 16 rows of a chunk, a wave each.  `blocks` of those; the workgroups behind them look for
-// the largest |W| (gradient of fp32), or prepare W.  Beside k_live, k_gather and k_prep one after another: 61 x 8000 x 250
+// The list, H's rows and W's in one launch, for up to 64 chunks of 64 rows: each workgroup counts the live rows by itself and
+// takes 16 rows of a chunk, a wave each.  `blocks` of those; the workgroups behind them prepare W.  Beside k_live, k_gather and k_prep one after another: 61 x 8000 x 250
 // fp32 with gradients 78.7 us, 68.1 us so; 2000 x 50257 x 768 fp32 345 and 329 us; 4096 x 50257 x 768 bf16 with gradients
 // 868 and 855 us.
 struct Front {
@@ -458,14 +384,10 @@ constexpr int kFrontChunks = 64;
 
 template <typename T>
 __global__ __launch_bounds__(1024) void k_front(Front a) {
-  __shared__ int lds[16], cnt[kFrontChunks], ids[64];
+  __shared__ int cnt[kFrontChunks], ids[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int)blockIdx.x >= a.blocks) {
-    const int b = blockIdx.x - a.blocks;
-    if (sizeof(T) == 4 && a.g.prm)
-      largest(a.l, b, gridDim.x - a.blocks, lds);
-    else
-      prep<T, 16>(a.w, b);
+    prep<T, 16>(a.w, blockIdx.x - a.blocks);
     return;
   }
   constexpr int U = kFrontChunks / 16;
@@ -598,14 +520,14 @@ struct Side {
       }
     }
   }
-  // stage k to LDS
-  __device__ __forceinline__ void load(char *lds, const uint16_t *from, int k) const {
+  // stage k to LDS; none: zeros (K contiguous)
+  __device__ __forceinline__ void load(char *lds, const uint16_t *from, int k, bool none = false) const {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {
       const char *base = (const char *)from + (KM ? (int64_t)k * ld * KS + p * 64 : (int64_t)k * kStep * 2);
       // K rows that there are not lie past the buffer's end, where loads give zeros
-      const int there = KM ? min(depth - k * KS, KS) * ld : -1;
+      const int there = KM ? min(depth - k * KS, KS) * ld : __builtin_amdgcn_readfirstlane(none ? 0 : -1);
       const auto m = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, there, 0x00020000);
 #pragma unroll
       for (int i = 0; i < L; ++i)
@@ -643,9 +565,13 @@ __device__ __forceinline__ int most16(int v) {
   return max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xF, 0xF, true));
 }
 
-// eight fp16 numbers times 2^d, -14 <= d <= 15
+// G's entries in a block lie below 2^(kTopG + kCoarse), 2^15
+static_assert(kTopG + 1 + kSlack <= 15 && kTopG - 1 + kCoarse <= 15, "fp16");
+__device__ __forceinline__ int coarse_of(int e) { return e & ~(kCoarse - 1); }
+
+// eight fp16 numbers times 2^d, d <= 15 (0 below 2^-24)
 __device__ __forceinline__ u32x4 times_power(u32x4 v, int d) {
-  const _Float16 f = __builtin_bit_cast(_Float16, (uint16_t)((15 + d) << 10));
+  const _Float16 f = __builtin_amdgcn_ldexph((_Float16)1.0f, d);
   return __builtin_bit_cast(u32x4, __builtin_bit_cast(f16x8, v) * f16x8{f, f, f, f, f, f, f, f});
 }
 
@@ -671,27 +597,60 @@ struct Core {
     return __shfl(v, (e >> 2) * 8 + fk * 4 + (e & 3), 64);
   }
 
-  // Block i of a, a group under the power of e, comes to its rows' power; where it would not fit, the sums come down first.
-  template <int P>
-  __device__ __forceinline__ void align(int i, int e, u32x4 (&f)[P][C::TM]) {
-    if (__any(e > top[i] + kSlack)) {
-      const int t = e > top[i] + kSlack ? e : top[i];
-      const float down = ldexpf(1.0f, max(top[i] - t, -300));
-      top[i] = t;
+  // The sums of block i come down to the power of t.
+  __device__ __forceinline__ void come_down(int i, int t) {
+    const float down = ldexpf(1.0f, max(top[i] - t, -300));
+    top[i] = t;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const float g = of_row(down, q);
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) acc[i][j][q] *= g;
+    }
+  }
+
+  // The sums as they are, without the powers that their operands had.
+  __device__ __forceinline__ void level() {
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i) {
 #pragma unroll
       for (int q = 0; q < 16; ++q) {
-        const float g = of_row(down, q);
+        const int power = of_row(top[i], q) - kTopG - kTop;
 #pragma unroll
-        for (int j = 0; j < C::TN; ++j) acc[i][j][q] *= g;
+        for (int j = 0; j < C::TN; ++j) acc[i][j][q] = ldexpf(acc[i][j][q], power);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    const int d = e - top[i], first = max(d, -14);
+  }
+
+  // The products of a stage.  TIMES: a's blocks times 2^(d[ks][i]), in one or two factors (below 2^-38 nothing is left of them).
+  template <int TIMES, int KSTEPS, int P, typename A, typename B>
+  __device__ __forceinline__ void stage(const char *at, const char *bt, const A &sa, const B &sb, const int (&d)[KSTEPS][C::TM]) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) f[p][i] = times_power(f[p][i], first);
-    if (__any(d < -14)) {  // 2^-28 of the row's largest has nothing left to add
-      const int rest = max(d - first, -15);
+    for (int ks = 0; ks < KSTEPS; ++ks) {
+      u32x4 fa[P][C::TM], fb[P][C::TN];
 #pragma unroll
-      for (int p = 0; p < P; ++p) f[p][i] = times_power(f[p][i], rest);
+      for (int p = 0; p < P; ++p) {
+        sa.read(at, wm, ks, p, fa[p]);
+        sb.read(bt, wn, ks, p, fb[p]);
+      }
+      if (TIMES > 0) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) {
+          const int first = max(d[ks][i], -14);
+#pragma unroll
+          for (int p = 0; p < P; ++p) {
+            fa[p][i] = times_power(fa[p][i], first);
+            if (TIMES > 1) fa[p][i] = times_power(fa[p][i], max(d[ks][i] - first, -25));
+          }
+        }
+      }
+      if (P == 2) {
+        multiply(fa[0], fb[P - 1]);
+        multiply(fa[P - 1], fb[0]);
+      }
+      multiply(fa[0], fb[0]);
+      if (TIMES > 0 && ks + 1 < KSTEPS) __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -714,9 +673,9 @@ struct Core {
   // kSplit: both numbers of both operands are in a stage, each is read once for hi lo, lo hi and hi hi (one stage for each
   // of the three: gradients of 8 x 257 x 50257 x 768, each example's, 1774 us with the log-probabilities, 1659 us so).
   // kPair: all of K with a's lo, then with its hi.
-  // POW: a has Powers.  Each row begins at the largest of its first 256 columns (one trip to the caches), so that few groups
-  // bring the sums down.
-  template <bool KA, bool KB, bool POW = false>
+  // kRows: each row begins at the largest of its first 256 columns (one trip to the caches), so that few groups bring the sums
+  // down; what a stage's blocks are times is settled a stage before, since the products would wait for it.
+  template <bool KA, bool KB, Scaling S = kPlain>
   __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth,
                                       int depth_b, Powers pw = Powers{}) {
     constexpr int P = M == kSplit ? 2 : 1, HALF = C::BM * kStep * 2, STAGE = HALF + C::BN * kStep * 2;
@@ -728,8 +687,8 @@ struct Core {
     sa.init(a, rows_a, depth);
     sb.init(b, rows_b, depth_b);
     int part = 0, k = 0;  // of the next stage to load
-    auto load = [&](int st) {
-      sa.load(lds + st * STAGE, a.p[M == kPair && part == 0], k);
+    auto load = [&](int st, bool none = false) {
+      sa.load(lds + st * STAGE, a.p[M == kPair && part == 0], k, none);
       sb.load(lds + st * STAGE + HALF, b.p[0], k);
       if (++k == steps) {
         k = 0;
@@ -743,9 +702,10 @@ struct Core {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     const int all = steps * (M == kPair ? 2 : 1);
+    if (all > 0) load(0);
     constexpr int G = A::KS / 16;  // groups of a stage
     const int groups = depth / 16;
-    int next[G][C::TM];
+    int next[G][C::TM], d[G][C::TM];  // kRows: powers of the stage behind the next one; what this stage's blocks are times
     auto powers = [&](int k) {
 #pragma unroll
       for (int g = 0; g < G; ++g)
@@ -753,7 +713,10 @@ struct Core {
         for (int i = 0; i < C::TM; ++i)
           next[g][i] = pw.p[min(k * G + g, groups - 1) * pw.ld + wm * (C::BM / C::WM) + i * 32 + fr];
     };
-    if (POW) {
+    // kBlocks: the powers of the stage whose loads are under way and of the one behind it, the largest so far.  The sums go from
+    // block to block's power, up to 2^60 above what they are under the largest; blocks below that count as zeros.
+    int block = 0, behind = 0, most = 0;
+    if (S == kRows) {
 #pragma unroll
       for (int i = 0; i < C::TM; ++i) {
         top[i] = kNone;
@@ -762,45 +725,78 @@ struct Core {
           for (int h = 0; h < 4; ++h)
             top[i] = max(top[i], pw.p[min(g + h, groups - 1) * pw.ld + wm * (C::BM / C::WM) + i * 32 + fr]);
       }
-      if (groups) powers(0);
+      if (groups) {
+        powers(0);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i) d[g][i] = next[g][i] - top[i];
+        powers(1);
+      }
+    } else if (S == kBlocks) {
+      top[0] = kNone;
+      if (all > 0) block = most = top[0] = __builtin_amdgcn_readfirstlane(pw.p[0]);
+      if (all > 1) behind = pw.p[A::KS / 64];
     }
-    if (all > 0) load(0);
     for (int s = 0; s < all; ++s) {
       // the loads of this stage, and the reads of the buffer that the next one gets
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      int now[G][C::TM];
-      if (POW) {
+      int to[C::TM], then[G][C::TM];
+      bool up = false;
+      if (S == kRows) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) {
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            then[g][i] = next[g][i];
+            asm volatile("" : "+v"(then[g][i]));  // they have arrived: not waited for behind the loads that follow
+          }
+          to[i] = then[0][i];
+#pragma unroll
+          for (int g = 1; g < G; ++g) to[i] = max(to[i], then[g][i]);
+          up = up || to[i] > top[i] + kSlack;
+          to[i] = to[i] > top[i] + kSlack ? to[i] : top[i];
+        }
+        up = __any(up);
+        if (s + 2 < all) powers(s + 2);
+      }
+      const int e = block;
+      if (S == kBlocks) {
+        asm volatile("" : "+v"(behind));
+        const int b = __builtin_amdgcn_readfirstlane(behind);
+        most = max(most, b);
+        block = max(b, most - 60);
+        if (s + 2 < all) behind = pw.p[(s + 2) * A::KS / 64];
+        if (s + 1 < all) load((s + 1) & 1, b < most - 60);
+      } else if (s + 1 < all) {
+        load((s + 1) & 1);
+      }
+      const char *at = lds + (s & 1) * STAGE, *bt = at + HALF;
+      if constexpr (S == kRows) {
+        stage<2, G, P>(at, bt, sa, sb, d);
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-          for (int i = 0; i < C::TM; ++i) {
-            now[g][i] = next[g][i];
-            asm volatile("" : "+v"(now[g][i]));  // they have arrived: not waited for behind the loads that follow
-          }
-        if (s + 1 < all) powers(s + 1);
-      }
-      if (s + 1 < all) load((s + 1) & 1);
-      const char *at = lds + (s & 1) * STAGE;
+          for (int i = 0; i < C::TM; ++i) d[g][i] = then[g][i] - to[i];
+        if (up)
 #pragma unroll
-      for (int ks = 0; ks < A::KS / 16; ++ks) {
-        if (POW && s * G + ks >= groups) break;
-        u32x4 fa[P][C::TM], fb[P][C::TN];
+          for (int i = 0; i < C::TM; ++i) come_down(i, to[i]);
+      } else if constexpr (S == kBlocks) {
+        if (e != top[0]) {
+          const float f = ldexpf(1.0f, max(top[0] - e, -300));
+          top[0] = e;
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          sa.read(at, wm, ks, p, fa[p]);
-          sb.read(at + HALF, wn, ks, p, fb[p]);
-        }
-        if constexpr (POW) {
+          for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-          for (int i = 0; i < C::TM; ++i) align(i, now[ks][i], fa);
+            for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+              for (int q = 0; q < 16; ++q) acc[i][j][q] *= f;
         }
-        if (P == 2) {
-          multiply(fa[0], fb[P - 1]);
-          multiply(fa[P - 1], fb[0]);
-        }
-        multiply(fa[0], fb[0]);
+        stage<0, G, P>(at, bt, sa, sb, d);
+      } else {
+        stage<0, G, P>(at, bt, sa, sb, d);
       }
     }
   }
@@ -848,9 +844,9 @@ struct Logit {
   uint16_t *g;  // [tcap][piece] entries
   float *rest;  // [tcap], bf16: what the rounding of the target's entry has left
   int64_t gplane, piece;
-  // fp32: G for dH (g, beside a factor of the row; NULL if not wanted) and for dW (gw, whole, under the powers pw)
+  // fp32: G for dH without the rows' factors cs (g; NULL if not wanted) and for dW (gw), under the powers ph and pw
   uint16_t *gw;
-  int *pw;  // [tcap / 16][piece]
+  int *ph, *pw;  // [piece / 64], [tcap / 16][piece]
   const float *cs;
 };
 
@@ -867,9 +863,8 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   Core<C, F16 ? kSplit : kBf16> c;  // H and W have one number or two
   c.template run<false, false>(lds, at_row<M>(a.w, m0), at_row<M>(a.h, n0), a.valid - m0, np - n0, a.kp, 0);
   const bool whole = m0 + C::BM <= a.valid;
-  const int ew = F16 && GRAD ? a.meta->ew : 0;
   int ev[C::TM][16];
-  if (F16 && !GRAD) {
+  if (F16) {
 #pragma unroll
     for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -883,8 +878,9 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
   for (int j = 0; j < C::TN; ++j) {
     const int n = n0 + c.col(j);
     const bool in = n < np;
+    const int ex = F16 && in ? a.eh[n] - 2 * kTop : 0;
     if (GRAD) {
-      const RowPrm p = in ? a.prm[n] : RowPrm{INFINITY, 0.0f, 0.0f, 0};
+      const RowPrm p = in ? a.prm[n] : RowPrm{INFINITY, 0.0f, 0.0f};
       const int tv = in ? a.tgt[n] - a.v0 - m0 - c.wm * (C::BM / C::WM) : -1;
       const Power pw = power_of(a.scale);
 #pragma unroll
@@ -892,7 +888,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float x = c.acc[i][j][e];
-          if (F16) x = ldexpf(x, p.e + ew);
+          if (F16) x = ldexpf(x, ev[i][e] + ex);
           c.acc[i][j][e] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
         }
       if (__any(tv >= 0 && tv < C::BM / C::WM)) {  // few tiles have one of their rows' targets
@@ -920,7 +916,6 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) c.acc[i][j][e] = __uint_as_float(split<M>(c.acc[i][j][e]));
     } else {
-      const int ex = F16 && in ? a.eh[n] - 2 * kTop : 0;
       const float k2 = power_of(a.scale).k;
       float m = -INFINITY;
 #pragma unroll
@@ -990,6 +985,16 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
           *(u32x4 *)(to + (int64_t)row * a.piece * 2 + m0 * 2 + ch * 8) = *(const u32x4 *)(at + r * RW + (ch ^ (r & 31)) * 16);
       }
     };
+    int coarse = kNone;  // the wave's 64 entries of the vocabulary
+    if (a.g) {
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) coarse = max(coarse, ev[i][e]);
+      static_assert(C::BM / C::WM == 64, "a block of kBlocks");
+      coarse = coarse_of(max(coarse, __shfl_xor(coarse, 32, 64)));
+      if (tn == 0) a.ph[(m0 >> 6) + c.wm] = coarse;
+    }
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
       uint32_t bits[C::TM][16];
@@ -997,13 +1002,12 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
 #pragma unroll
         for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) bits[i][e] = split<M>(c.acc[i][j][e]);
+          for (int e = 0; e < 16; ++e) bits[i][e] = split<M>(ldexpf(c.acc[i][j][e], ev[i][e] + kTopG - coarse));
         leave(j, bits, a.g);
       }
       if (a.gw) {
-        const int n = n0 + c.col(j);
-        const int eh = n < np ? a.eh[n] : 0;
-        const float f = n < np ? a.cs[n] * (1.0f / (1 << kTop)) : 0.0f;
+        const int n = n0 + c.col(j), eh = n < np ? a.eh[n] : 0;
+        const float f = n < np ? a.cs[n] : 0.0f;
 #pragma unroll
         for (int i = 0; i < C::TM; ++i) {
           int mine = kNone;
@@ -1080,8 +1084,8 @@ struct Few {
   uint16_t *g;
   int64_t gplane, piece;
   uint16_t *gw;  // fp32, as in Logit
-  int *pw;
-  const int *eh;
+  int *ph, *pw;
+  const int *eh, *ev;
   const float *cs;
 };
 
@@ -1134,7 +1138,7 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
   if constexpr (GRAD) {
     constexpr Mode M = sizeof(T) == 4 ? kSplit : kPair;
     const int at = v0 - a.v0 + q * 4;
-    float g[4];
+    float g[4] = {};
     auto leave = [&](uint16_t *to, const float *x) {
 #pragma unroll
       for (int plane = 0; plane < 2; ++plane)
@@ -1149,7 +1153,20 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
         if (v0 + q * 4 + e == target) g[e] += p.one;
         if (at + e >= a.valid) g[e] = 0.0f;
       }
-      if (a.g) leave(a.g, g);
+    }
+    if (M != kSplit && n >= 0) leave(a.g, g);
+    if (M == kSplit && a.g) {
+      int coarse = a.ev[blockIdx.x * kFewUnit + lane];
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) coarse = max(coarse, __shfl_xor(coarse, d, 64));
+      coarse = coarse_of(coarse);
+      if (threadIdx.x == 0) a.ph[blockIdx.x] = coarse;
+      if (n >= 0) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = ldexpf(g[e], a.ev[at + e] + kTopG - coarse);
+        leave(a.g, x);
+      }
     }
     const int np = a.meta->np;
     if (M == kSplit && a.gw) {  // up to 16 groups of rows, by the unit's entries of the vocabulary
@@ -1157,7 +1174,7 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
       for (int i = threadIdx.x; i < kFew * kFewUnit; i += 256) (&most[0][0])[i] = kNone;
       __syncthreads();
       const int eh = n >= 0 ? a.eh[n] : 0;
-      const float f = n >= 0 ? a.cs[n] * (1.0f / (1 << kTop)) : 0.0f;
+      const float f = n >= 0 ? a.cs[n] : 0.0f;
       int *mine = &most[n >= 0 ? n >> 4 : 0][wave * 16 + q * 4];
       if (n >= 0)
 #pragma unroll
@@ -1307,7 +1324,8 @@ struct Back {
   bool first;
   float *acc;     // [splits][tcap][kp]
   int kp;
-  // dW = G^T H (fp32: of its own G, under Powers)
+  const int *ph;  // fp32
+  // dW = G^T H (fp32: of its own G)
   Operand gw, h;
   Powers pw;
   int valid, b0;  // rows of the piece, the launch's first example
@@ -1338,14 +1356,14 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
   Core<C, M> c;
   // split weights bring rows of zeros up to a multiple of 64
   if (hidden)
-    c.template run<false, true>(lds, at_row<M>(a.g, m0, k0), at_row<M>(a.w, k0, n0), np - m0, a.kp - n0, depth,
-                                F16 ? a.steps * kStep - k0 : a.valid - k0);
+    c.template run<false, true, F16 ? kBlocks : kPlain>(lds, at_row<M>(a.g, m0, k0), at_row<M>(a.w, k0, n0), np - m0, a.kp - n0, depth,
+                                                        F16 ? a.steps * kStep - k0 : a.valid - k0, Powers{a.ph + k0 / 64, 0});
   else
-    c.template run<true, true, F16>(lds, at_row<M>(a.gw, k0, m0), at_row<M>(a.h, k0, n0), C::BM, a.kp - n0, depth, depth,
-                                    Powers{a.pw.p + k0 / 16 * a.pw.ld + m0, a.pw.ld});
+    c.template run<true, true, F16 ? kRows : kPlain>(lds, at_row<M>(a.gw, k0, m0), at_row<M>(a.h, k0, n0), C::BM, a.kp - n0, depth,
+                                                     depth, Powers{a.pw.p + k0 / 16 * a.pw.ld + m0, a.pw.ld});
   if (hidden) {
     float *to = a.acc + (part * a.tcap + m0) * a.kp + n0;
-    const int ew = F16 ? a.meta->ew - 2 * kTop : 0;
+    const int power = c.top[0] - kTopG - kTop;  // kBlocks: the same for all rows
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
       if (n0 + c.col(j) >= a.kp) continue;
@@ -1356,17 +1374,12 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
           const int m = c.row(i, e);
           if (m0 + m >= np) continue;
           float *p = to + (int64_t)m * a.kp + c.col(j);
-          const float v = F16 ? ldexpf(c.acc[i][j][e], ew) : c.acc[i][j][e];
+          const float v = F16 ? ldexpf(c.acc[i][j][e], power) : c.acc[i][j][e];
           *p = a.first ? v : *p + v;
         }
     }
   } else {
-    int power[C::TM][16];  // by all lanes, before those of columns that there are not leave
-    if (F16)
-#pragma unroll
-      for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) power[i][e] = c.of_row(c.top[i], e) - kTopG - kTop;
+    if constexpr (F16) c.level();
     TO *to = (TO *)a.out + ((a.b0 + part) * a.vocab + m0) * a.width + n0;
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
@@ -1378,7 +1391,7 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
           const int m = c.row(i, e);
           if (m0 + m >= a.valid) continue;
           TO *p = to + (int64_t)m * a.width + c.col(j);
-          const float v = F16 ? ldexpf(c.acc[i][j][e], power[i][e]) : c.acc[i][j][e];
+          const float v = c.acc[i][j][e];
           const TO r = from_f32<TO>(a.accumulate ? v + to_f32(*p) : v);
           if (a.past) {
             asm volatile("");  // or the compiler makes one ordinary store of the two
@@ -1452,7 +1465,7 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Plan {
   bool f16, grad, few, pair, copy, large, huge, front;
   int64_t batch, n, chunks, tcap, kp, piece, pieces, units, splits, planes, gplanes;  // numbers of an operand's entry, of G's
-  int64_t list, pos, tgt, seg, cnt, most, meta, hc, eh, ev, part, xt, run, prm, cs, rest, wc, g, gw, pw, acc, bytes;
+  int64_t list, pos, tgt, seg, cnt, meta, hc, eh, ev, part, xt, run, prm, cs, rest, wc, g, gw, ph, pw, acc, bytes;
 };
 
 Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
@@ -1485,9 +1498,12 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.kp = up(x->width, kStep);
   // rows that 16-byte loads in whole stages read as they lie
   p.copy = p.f16 || x->width % kStep || x->ld_weight % 8 || (uintptr_t)x->weight % 16 || x->ld_weight > (1 << 20);
-  // a piece: G in 256 MB (a launch more for each halving), a copy of W in 256 MB
+  // a piece: G in 256 MB (a launch more for each halving), a copy of W in 256 MB.  fp32 has G twice where both gradients are
+  // wanted: in 256 MB together up to a width of 1024 (4096 x 50257 x 768 2867 us, 2725 us so), in twice as much above, where
+  // more pieces cost more sums of dH (4 examples of 512 x 32000 x 2048 2336 us, 2396 us; 8000 x 32000 x 5000 18.5 and 19.1 ms).
   int64_t most = x->vocab;
-  if (grad) most = std::min(most, ((int64_t)1 << 27) / (p.tcap * p.gplanes));
+  const int64_t copies = p.f16 && dhidden && dweight && x->width <= 1024 ? 2 : 1;
+  if (grad) most = std::min(most, ((int64_t)1 << 27) / (p.tcap * p.gplanes * copies));
   if (grad || p.copy) most = std::min(most, ((int64_t)1 << 27) / (p.kp * p.planes));
   // the tiles' (m, z) in 256 MB; grids below 2^32 threads
   if (!grad) most = std::min(most, ((int64_t)1 << 31) / p.tcap);
@@ -1512,11 +1528,10 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.tgt = take(4 * p.tcap);
   p.seg = take(4 * (batch + 1));
   p.cnt = take(4 * p.chunks);
-  p.most = take(4 * kMost);
   p.meta = take(sizeof(Meta));
   p.hc = take(2 * p.planes * p.tcap * p.kp);
   p.eh = take(4 * p.tcap);
-  if (p.f16 && !grad) p.ev = take(4 * p.piece);
+  if (p.f16) p.ev = take(4 * p.piece);
   if (p.copy) p.wc = take(2 * p.planes * p.piece * p.kp);
   if (!grad) {
     p.part = take(8 * p.units * p.tcap);
@@ -1527,6 +1542,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     p.cs = take(4 * p.tcap);
     p.rest = take(4 * p.tcap);
     if (dhidden || !p.f16) p.g = take(2 * p.gplanes * p.tcap * p.piece);
+    if (dhidden && p.f16) p.ph = take(4 * (p.piece / 64));
     if (dweight && p.f16) {
       p.gw = take(2 * p.gplanes * p.tcap * p.piece);
       p.pw = take(4 * (p.tcap / 16) * p.piece);
@@ -1570,44 +1586,36 @@ Prep weights_of(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, vo
   a.rows = (int)valid;
   a.width = (int)x->width;
   a.kp = (int)p.kp;
-  a.meta = ptr<Meta>(work, p.meta);
-  if (p.f16 && !p.grad) a.ev = ptr<int>(work, p.ev);
+  if (p.f16) a.ev = ptr<int>(work, p.ev);
   a.out = ptr<uint16_t>(work, p.wc);
   return a;
 }
 
-// parts of the search for the largest |W|
-int parts_of(const sk_linear *x, const Plan &p) {
-  return p.f16 && p.grad ? (int)std::min<int64_t>(kMost, (x->vocab * x->width + 16383) / 16384) : 0;
-}
 // whether W's first piece is prepared by the launch that begins
-bool in_front(const Plan &p) { return p.front && p.copy && !(p.f16 && p.grad); }
+bool in_front(const Plan &p) { return p.front && p.copy; }
 
-// list, |W|, rows of H: what both directions begin with
+// list, rows of H: what both directions begin with
 void begin(const sk_linear *x, const Plan &p, const float *dlogp, const float *stats_in, float *logp, float *stats, void *work,
            hipStream_t st) {
   Meta *meta = ptr<Meta>(work, p.meta);
   int *list = ptr<int>(work, p.list);
-  const int parts = parts_of(x, p);
-  const bool flat = x->ld_weight == x->width && x->vocab * x->width % 4 == 0 && (uintptr_t)x->weight % 16 == 0;
-  int *most = ptr<int>(work, p.most);
   const Live l{x->targets, dlogp, (int32_t)x->index, (int32_t)x->vocab, (int32_t)p.n, (int32_t)p.batch, list,
                ptr<int>(work, p.pos), ptr<int>(work, p.tgt), ptr<int>(work, p.seg), ptr<int>(work, p.cnt), meta, logp,
-               (float2 *)stats, (const float *)x->weight, x->ld_weight, (int)x->width, flat, most};
+               (float2 *)stats};
   const Gather g{x->hidden, x->ld_hidden, (int)x->width, (int)p.kp, list, meta, ptr<uint16_t>(work, p.hc),
-                 ptr<int>(work, p.eh), most, parts, (const float2 *)stats_in, dlogp, x->scale,
+                 ptr<int>(work, p.eh), (const float2 *)stats_in, dlogp, x->scale,
                  p.grad ? ptr<RowPrm>(work, p.prm) : nullptr, ptr<float>(work, p.cs)};
   if (p.front) {
     const int64_t valid = std::min(p.piece, x->vocab);
     const Front f{l, g, weights_of(x, p, 0, valid, work), (int)p.chunks * 4};
-    const dim3 grid((unsigned)(f.blocks + (in_front(p) ? up(valid, 64) / 16 : parts))), block(1024);
+    const dim3 grid((unsigned)(f.blocks + (in_front(p) ? up(valid, 64) / 16 : 0))), block(1024);
     if (p.f16)
       hipLaunchKernelGGL(k_front<float>, grid, block, 0, st, f);
     else
       hipLaunchKernelGGL(k_front<bf16>, grid, block, 0, st, f);
     return;
   }
-  hipLaunchKernelGGL(k_live, dim3(1 + parts), dim3(1024), 0, st, l);
+  hipLaunchKernelGGL(k_live, dim3(1), dim3(1024), 0, st, l);
   if (p.f16)
     hipLaunchKernelGGL(k_gather<float>, dim3((unsigned)(p.tcap / 4)), dim3(256), 0, st, g);
   else
@@ -1620,10 +1628,6 @@ Operand weights(const sk_linear *x, const Plan &p, int64_t v0, int64_t valid, vo
   if (!p.copy) return Operand{{(const uint16_t *)a.src, (const uint16_t *)a.src}, x->ld_weight};
   const Operand o{{a.out, a.out}, p.kp * p.planes};
   if (v0 == 0 && in_front(p)) return o;
-  if (p.front && p.f16 && p.grad) {
-    a.most = ptr<int>(work, p.most);
-    a.parts = parts_of(x, p);
-  }
   const dim3 grid((unsigned)(up(valid, 64) / 4));
   if (p.f16)
     hipLaunchKernelGGL(k_prep<float>, grid, dim3(256), 0, st, a);
@@ -1718,7 +1722,7 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
     const int units = (int)p.units;
     const Few a{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)x->width,
                 (int)x->index, x->scale, ptr<float2>(work, p.part), ptr<float>(work, p.xt), units, logp, (float2 *)stats, 0, 0, nullptr,
-                nullptr, nullptr, nullptr, nullptr, 0, 0, nullptr, nullptr, nullptr, nullptr};
+                nullptr, nullptr, nullptr, nullptr, 0, 0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
     if (p.f16)
       hipLaunchKernelGGL((k_few<float, false>), dim3(units), dim3(256), 0, st, a);
     else
@@ -1776,12 +1780,13 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
       a.gplane = p.tcap * p.piece;
       a.piece = p.piece;
       a.gw = gw;
+      a.ph = ptr<int>(work, p.ph);
       a.pw = ptr<int>(work, p.pw);
       a.cs = ptr<float>(work, p.cs);
       if (x->rows <= kFew) {
         const Few f{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)width,
                     (int)x->index, x->scale, nullptr, nullptr, 0, nullptr, nullptr, (int)v0, (int)valid, meta,
-                    ptr<int>(work, p.pos), ptr<int>(work, p.list), a.prm, a.g, a.gplane, a.piece, a.gw, a.pw, a.eh, a.cs};
+                    ptr<int>(work, p.pos), ptr<int>(work, p.list), a.prm, a.g, a.gplane, a.piece, a.gw, a.ph, a.pw, a.eh, a.ev, a.cs};
         const dim3 grid((unsigned)((valid + kFewUnit - 1) / kFewUnit));
         if (p.f16)
           hipLaunchKernelGGL((k_few<float, true>), grid, dim3(256), 0, st, f);
@@ -1806,6 +1811,7 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
     a.acc = ptr<float>(work, p.acc);
     a.kp = (int)p.kp;
     a.gw = gw ? Operand{{gw, gw}, p.piece * p.planes} : a.g;
+    a.ph = ptr<int>(work, p.ph);
     a.pw = Powers{ptr<int>(work, p.pw), p.piece};
     a.h = Operand{{hd, hd}, p.kp * p.planes};
     a.valid = (int)valid;

@@ -98,6 +98,18 @@ def test_examples_far_apart(dev, T, batch):
     check(dev, h, W, t, c, batch, alone=range(batch))
 
 
+@pytest.mark.parametrize("far", [10, 20, 30])
+def test_positions_far_apart_in_features_of_their_own(dev, far):
+    """The last 16 of 32 positions have 2^-far of the others' factors and all that there is of half the features."""
+    h, W, t, c = make(32, 300, 64, far, 2.0)
+    h[:16, 32:] = 0.0
+    h[16:, :32] = 0.0
+    c[16:] *= 2.0 ** -far
+    g, _ = check(dev, h, W, t, c, 1)
+    # a quarter of these features' largest entries is above what the check lets pass
+    assert 32 * 2.0 ** -37 * (np.abs(g) * f64(h).max(1, keepdims=True)).max() < np.abs(g.T @ f64(h))[:, 32:].max() / 4
+
+
 @pytest.mark.parametrize("T", [9, 70, 1300])
 def test_hidden_states_far_apart(dev, T):
     """Positions whose hidden states are 2^-20 and 2^15 of others', with logits of the same size: what they add to a row of
@@ -106,3 +118,52 @@ def test_hidden_states_far_apart(dev, T):
     W[:, 90:] = 0.0  # features that no logit sees
     h[:, 90:] *= torch.exp2(torch.randint(-20, 16, (T, 1), generator=torch.Generator().manual_seed(T)).float())
     check(dev, h, W, t, c, 1)
+
+
+@pytest.mark.parametrize("T,batch", [(9, 1), (70, 1), (120, 3), (1300, 1)])
+def test_weight_with_a_row_far_above_the_others(dev, T, batch):
+    """A row 2^15 above the others, in a feature that the hidden states do not have: the others keep their bits."""
+    for pull in (4.0, 9.0):
+        h, W, t, c = make(T, 500, 128, T + 2, pull)
+        h[:, 0] = 0.0
+        W[:, 0] = 0.0
+        W[450] = 0.0
+        W[450, 0] = 2.0 ** 15
+        check(dev, h, W, t, c, batch)
+
+
+@pytest.mark.parametrize("T,batch", [(9, 1), (70, 1), (120, 3), (1300, 1)])
+@pytest.mark.parametrize("powers", [(0, 16, 0, -70, 20, 0, -100), (20, 0, -70, -100, 0, 16, 0), (-100, -70, 0, 0, 16, 20, 20)])
+def test_weight_of_blocks_far_apart(dev, T, batch, powers):
+    """Every 64 rows another power of two: large ones in a feature that the hidden states do not have, small ones altogether."""
+    h, W, t, c = make(T, 64 * len(powers) - 5, 128, T + 3, 4.0)
+    h[:, 0], W[:, 0] = 0.0, 0.0
+    for b, k in enumerate(powers):
+        if k > 0:
+            W[64 * b:64 * b + 64, 0] = 2.0 ** k
+        else:
+            W[64 * b:64 * b + 64] *= 2.0 ** k
+    check(dev, h, W, t, c, batch)
+
+
+@pytest.mark.parametrize("dt", [F32])
+@pytest.mark.parametrize("T", [9, 40, 1200])
+def test_statistics_and_gradient_from_the_same_logits(dev, T, dt):
+    """Positions with one hidden state and targets 0, 1, ..: example b's gradient has -p_v h in row v, and log p_v is
+    position v's.  Both come from the same logit and statistics, whatever errors these have: log p rounds to 2^-24 of itself and
+    twice of the logit's distance to the largest, which is no more; p, 1 / z, log z, g and dweight to 16 2^-24 together (bf16: g
+    to 2^-16).  A row of the weight 2^22 above the others, in a feature that the hidden state does not have."""
+    import paper_2402_03994_amd as fw
+    V, d, n = 300, 64, min(T, 40)
+    h, W, _, _ = make(1, V, d, T)
+    h[:, 0], W[:, 0], W[290] = 0.0, 0.0, 0.0
+    W[290, 0] = 2.0 ** 22
+    h, W, t = h.expand(T, d).to(dt).contiguous().to(dev), W.to(dt).to(dev), torch.arange(T, device=dev) % V
+    logp, stats = fw.linear_logp(h[:, None], W, t[:, None])
+    _, dw = fw.linear_logp_grad(h[:, None], W, t[:, None], stats, torch.ones(T, 1, device=dev), per_example=True, out_dtype=F32)
+    k = int(h[0].abs().argmax())
+    p = f64(-dw[:, :n, k] / h[0, k].float())[n - 1:]  # of the last position among the n, and those behind
+    want = f64(logp)[:n, 0]
+    tol = (3 * np.abs(want) + 16) * 2.0 ** -24 + (2.0 ** -16 if dt == BF16 else 0.0)
+    other = np.arange(n)[None] != (np.arange(n - 1, T) % V)[:, None]
+    assert (np.abs(p * np.exp(-want) - 1) <= tol)[other].all(), (np.abs(p * np.exp(-want) - 1) / tol)[other].max()
