@@ -185,8 +185,8 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
  *                `batch` examples of rows / batch each, batch > 1 gives one gradient
  *                per example.  Of fp32 weights it is fp32, of bf16 weights either.
  * Sums are fp32 and rounded once.  bf16 inputs: g is rounded to bf16 before the
- * products, whatever the type of dweight (up to 256 rows: to two bf16, 2^-16; dhidden
- * gets back what the target's entry has lost).  fp32 inputs: products as above; of dweight[b][v]
+ * products (up to 256 rows: to two bf16, 2^-16), and what the targets' entries have
+ * lost is returned to both gradients, whatever the type of dweight.  fp32 inputs: products as above; of dweight[b][v]
  * what lies below 2^-37 of its largest |g_tv| max |hidden[t]| is lost, of dhidden[t]
  * what lies below 2^-36 of dlogp[t] times the largest entry of weight.  A weight that
  * is not finite gives NaNs.  Rows with dlogp = 0 are masked.  Outputs may not overlap

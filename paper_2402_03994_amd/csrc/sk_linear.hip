@@ -16,8 +16,9 @@
 // takes its operands as they lie, with K along their rows or across them (Side
 // and Core below).  16-bit operands, fp32 sums.
 //   bf16 inputs are used as they are, and G is rounded to bf16, once, like any
-//   entry of a bf16 gradient (of up to 256 rows, where the bytes of W count and
-//   not the products, it takes two bf16).
+//   entry of a bf16 gradient (of few rows it takes two bf16: kPairRows).  What the
+//   rounding of a target's entry, most of its row of G, has left is returned to
+//   both gradients.
 //   fp32 inputs are split, x = hi + lo in two fp16 numbers (22 bits) under a power
 //   of two that brings the largest to 2^13, and each product is the three hi lo,
 //   lo hi, hi hi: a large library product reaches 153 TFLOP/s in fp32, 1256 in
@@ -109,6 +110,15 @@ struct Powers {
   int64_t ld;
 };
 [[maybe_unused]] constexpr int kCoarse = 4;
+// What the rounding of the targets' entries of G in bf16 has left, as another term of dW: rest[k] stands in the row of entry
+// tgt[k] of the vocabulary.  marks, [rows / 64][K / 32], say where there is one: few stages of a tile.
+struct Rest {
+  const int *tgt;
+  const float *rest;
+  const uint8_t *marks;  // of the tile's first row and the matrix's first k
+  int64_t ld;
+  int first, k0;  // entry of the vocabulary and k that the tile begins with
+};
 
 // N elements of a row from column k on, zeros past the width
 template <int N, typename T>
@@ -654,18 +664,20 @@ struct Core {
     }
   }
 
+  __device__ __forceinline__ void multiply_row(int i, const u32x4 &fa, const u32x4 *fb) {
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+      if (M == kSplit)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa), __builtin_bit_cast(f16x8, fb[j]),
+                                                           acc[i][j], 0, 0, 0);
+      else
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa), __builtin_bit_cast(bf16x8, fb[j]),
+                                                            acc[i][j], 0, 0, 0);
+    }
+  }
   __device__ __forceinline__ void multiply(const u32x4 *fa, const u32x4 *fb) {
 #pragma unroll
-    for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-      for (int j = 0; j < C::TN; ++j) {
-        if (M == kSplit)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa[i]), __builtin_bit_cast(f16x8, fb[j]),
-                                                             acc[i][j], 0, 0, 0);
-        else
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]), __builtin_bit_cast(bf16x8, fb[j]),
-                                                              acc[i][j], 0, 0, 0);
-      }
+    for (int i = 0; i < C::TM; ++i) multiply_row(i, fa[i], fb);
   }
 
   // acc = sum over `depth` of K from a and b on, a multiple of 64 (of 16 with KA); b has depth_b rows where they are K,
@@ -675,9 +687,9 @@ struct Core {
   // kPair: all of K with a's lo, then with its hi.
   // kRows: each row begins at the largest of its first 256 columns (one trip to the caches), so that few groups bring the sums
   // down; what a stage's blocks are times is settled a stage before, since the products would wait for it.
-  template <bool KA, bool KB, Scaling S = kPlain>
+  template <bool KA, bool KB, Scaling S = kPlain, bool REST = false>
   __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth,
-                                      int depth_b, Powers pw = Powers{}) {
+                                      int depth_b, Powers pw = Powers{}, Rest r = Rest{}) {
     constexpr int P = M == kSplit ? 2 : 1, HALF = C::BM * kStep * 2, STAGE = HALF + C::BN * kStep * 2;
     using A = Side<C::BM, C::WM, C::TH, KA, P>;
     using B = Side<C::BN, C::WN, C::TH, KB, P>;
@@ -702,7 +714,34 @@ struct Core {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     const int all = steps * (M == kPair ? 2 : 1);
+    // REST: target and number of row `lane` of the next stage, where that is marked
+    int next_target = -1, chunk = r.k0 >> 5;
+    float next_rest = 0.0f;
+    uint64_t marks = 0;  // of 64 blocks of 32 rows from `chunk` on
+    auto read_marks = [&]() {
+      constexpr int V = C::BM / C::WM / 64;
+      const int b = chunk + (threadIdx.x & 63), last = (r.k0 + depth - 1) >> 5;
+      int m = 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v) m |= r.marks[(wm * V + v) * r.ld + min(b, last)];
+      marks = __ballot(b <= last && m);
+    };
+    auto read_rest = [&](int s) {
+      if (((r.k0 + s * kStep) >> 5) - chunk > 61) {
+        chunk = (r.k0 + s * kStep) >> 5;
+        read_marks();
+      }
+      next_target = -1;
+      if (!(marks >> (((r.k0 + s * kStep) >> 5) - chunk) & (r.k0 & 31 ? 7 : 3))) return;
+      const int k = s * kStep + (threadIdx.x & 63), at = min(k, depth - 1);
+      if (k < depth) next_target = r.tgt[at] - r.first - wm * (C::BM / C::WM);
+      next_rest = r.rest[at];
+    };
     if (all > 0) load(0);
+    if (REST && all > 0) {
+      read_marks();
+      read_rest(0);
+    }
     constexpr int G = A::KS / 16;  // groups of a stage
     const int groups = depth / 16;
     int next[G][C::TM], d[G][C::TM];  // kRows: powers of the stage behind the next one; what this stage's blocks are times
@@ -762,6 +801,12 @@ struct Core {
         up = __any(up);
         if (s + 2 < all) powers(s + 2);
       }
+      int target = next_target;
+      float left = next_rest;
+      if (REST) {
+        asm volatile("" : "+v"(target), "+v"(left));
+        if (s + 1 < all) read_rest(s + 1);
+      }
       const int e = block;
       if (S == kBlocks) {
         asm volatile("" : "+v"(behind));
@@ -797,6 +842,39 @@ struct Core {
         stage<0, G, P>(at, bt, sa, sb, d);
       } else {
         stage<0, G, P>(at, bt, sa, sb, d);
+      }
+      if constexpr (REST) {
+        // few stages have a row whose target is among the wave's: their 16 rows once more, a made in registers
+        const uint32_t place = (unsigned)target < (unsigned)(C::BM / C::WM) ? target : 0xFFFF;
+        const uint32_t word = place << 16 | bf16_bits(left);
+        uint64_t hit[C::TM], any = 0;
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) {
+          hit[i] = __ballot(place >> 5 == i);
+          any |= hit[i];
+        }
+        if (any) {
+#pragma unroll 1
+          for (int ks = 0; ks < kStep / 16; ++ks) {
+            if (!(any >> (ks * 16) & 0xFFFF)) continue;
+            u32x4 fa[C::TM], fb[C::TN];
+            uint32_t w[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) w[q] = __shfl(word, ks * 16 + fk * 8 + q, 64);
+            sb.read(bt, wn, ks, 0, fb);
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i) {
+              if (!(hit[i] >> (ks * 16) & 0xFFFF)) continue;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const uint32_t lo = w[2 * q] >> 16 == i * 32 + fr ? w[2 * q] & 0xFFFF : 0;
+                const uint32_t hi = w[2 * q + 1] >> 16 == i * 32 + fr ? w[2 * q + 1] << 16 : 0;
+                fa[i][q] = lo | hi;
+              }
+              multiply_row(i, fa[i], fb);
+            }
+          }
+        }
       }
     }
   }
@@ -842,7 +920,8 @@ struct Logit {
   // gradient
   const RowPrm *prm;
   uint16_t *g;  // [tcap][piece] entries
-  float *rest;  // [tcap], bf16: what the rounding of the target's entry has left
+  float *rest;     // [tcap], bf16: what the rounding of the target's entry has left
+  uint8_t *marks;  // [piece / 64][tcap / 32], bf16: whether a row of the 32 has its target among the 64 entries
   int64_t gplane, piece;
   // fp32: G for dH without the rows' factors cs (g; NULL if not wanted) and for dW (gw), under the powers ph and pw
   uint16_t *gw;
@@ -891,7 +970,12 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
           if (F16) x = ldexpf(x, ev[i][e] + ex);
           c.acc[i][j][e] = p.w * (F16 ? entry_exp<float>(x - p.m, pw) : entry_exp<bf16>(x - p.m, pw));
         }
-      if (__any(tv >= 0 && tv < C::BM / C::WM)) {  // few tiles have one of their rows' targets
+      const bool any = __any(tv >= 0 && tv < C::BM / C::WM);
+      if (M == kBf16 && (threadIdx.x & 63) == 0 && in) {
+        static_assert(C::BM / C::WM == 64, "a row of marks");
+        a.marks[((m0 >> 6) + c.wm) * (a.tcap >> 5) + (n >> 5)] = any;
+      }
+      if (any) {  // few tiles have one of their rows' targets
 #pragma unroll
         for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -1328,7 +1412,10 @@ struct Back {
   // dW = G^T H (fp32: of its own G)
   Operand gw, h;
   Powers pw;
-  int valid, b0;  // rows of the piece, the launch's first example
+  const int *tgt;     // bf16, one number, as in Rest
+  const float *rest;
+  const uint8_t *marks;
+  int v0, valid, b0;  // the piece's first row and how many, the launch's first example
   void *out;      // rows from the piece's first on
   int64_t vocab;  // rows from example to example
   bool accumulate;
@@ -1359,8 +1446,11 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
     c.template run<false, true, F16 ? kBlocks : kPlain>(lds, at_row<M>(a.g, m0, k0), at_row<M>(a.w, k0, n0), np - m0, a.kp - n0, depth,
                                                         F16 ? a.steps * kStep - k0 : a.valid - k0, Powers{a.ph + k0 / 64, 0});
   else
-    c.template run<true, true, F16 ? kRows : kPlain>(lds, at_row<M>(a.gw, k0, m0), at_row<M>(a.h, k0, n0), C::BM, a.kp - n0, depth,
-                                                     depth, Powers{a.pw.p + k0 / 16 * a.pw.ld + m0, a.pw.ld});
+    c.template run<true, true, F16 ? kRows : kPlain, M == kBf16>(lds, at_row<M>(a.gw, k0, m0), at_row<M>(a.h, k0, n0), C::BM,
+                                                                 a.kp - n0, depth, depth,
+                                                                 Powers{a.pw.p + k0 / 16 * a.pw.ld + m0, a.pw.ld},
+                                                                 Rest{a.tgt + k0, a.rest + k0, a.marks + (m0 >> 6) * (a.tcap >> 5), a.tcap >> 5,
+                                                                      a.v0 + m0, k0});
   if (hidden) {
     float *to = a.acc + (part * a.tcap + m0) * a.kp + n0;
     const int power = c.top[0] - kTopG - kTop;  // kBlocks: the same for all rows
@@ -1465,7 +1555,7 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Plan {
   bool f16, grad, few, pair, copy, large, huge, front;
   int64_t batch, n, chunks, tcap, kp, piece, pieces, units, splits, planes, gplanes;  // numbers of an operand's entry, of G's
-  int64_t list, pos, tgt, seg, cnt, meta, hc, eh, ev, part, xt, run, prm, cs, rest, wc, g, gw, ph, pw, acc, bytes;
+  int64_t list, pos, tgt, seg, cnt, meta, hc, eh, ev, part, xt, run, prm, cs, rest, marks, wc, g, gw, ph, pw, acc, bytes;
 };
 
 Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
@@ -1487,10 +1577,10 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     return p;
   }
   p.planes = p.f16 ? 2 : 1;
-  p.pair = !p.f16 && x->rows <= kPairRows;
-  p.gplanes = p.f16 || p.pair ? 2 : 1;
   p.batch = batch;
   p.n = x->rows / batch;
+  p.pair = !p.f16 && x->rows <= kPairRows;
+  p.gplanes = p.f16 || p.pair ? 2 : 1;
   p.tcap = up(batch * up(p.n, kPad), 256);
   p.tcap = std::max<int64_t>(p.tcap, 256);
   p.chunks = batch * ((p.n + 63) / 64);
@@ -1541,6 +1631,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
     p.prm = take(sizeof(RowPrm) * p.tcap);
     p.cs = take(4 * p.tcap);
     p.rest = take(4 * p.tcap);
+    if (!p.f16 && !p.pair) p.marks = take(p.piece / 64 * (p.tcap / 32));
     if (dhidden || !p.f16) p.g = take(2 * p.gplanes * p.tcap * p.piece);
     if (dhidden && p.f16) p.ph = take(4 * (p.piece / 64));
     if (dweight && p.f16) {
@@ -1660,18 +1751,16 @@ void launch_logits(const Logit &a, int64_t rows, hipStream_t st) {
 }
 template <typename C, bool GRAD>
 void run_logits_in(const Plan &p, const Logit &a, int64_t rows, hipStream_t st) {
-  if (p.f16)
-    launch_logits<C, kSplit, GRAD>(a, rows, st);
-  else if (GRAD && p.pair)
-    launch_logits<C, kPair, GRAD>(a, rows, st);
-  else
-    launch_logits<C, kBf16, GRAD>(a, rows, st);
+  if (p.f16) return launch_logits<C, kSplit, GRAD>(a, rows, st);
+  if constexpr (GRAD)
+    if (p.pair) return launch_logits<C, kPair, GRAD>(a, rows, st);
+  launch_logits<C, kBf16, GRAD>(a, rows, st);
 }
 template <bool GRAD>
 void run_logits(const Plan &p, const Logit &a, hipStream_t st) {
   const int64_t rows = p.batch * up(p.n, kPad);
   if (p.large)
-    p.f16 ? launch_logits<Large, kSplit, GRAD>(a, rows, st) : launch_logits<Large, kBf16, GRAD>(a, rows, st);
+    run_logits_in<Large, GRAD>(p, a, rows, st);
   else if (rows <= Narrow::BN)
     run_logits_in<Narrow, GRAD>(p, a, rows, st);
   else
@@ -1693,10 +1782,10 @@ void launch_back(const Plan &p, Back a, bool dhidden, bool dweight, hipStream_t 
 }
 template <Mode M, typename TO>
 void run_back(const Plan &p, const Back &a, bool dhidden, bool dweight, hipStream_t st) {
-  if constexpr (M != kPair) {  // few rows
+  if constexpr (M != kPair)  // few rows an example
     if (p.huge) return launch_back<Huge, M, TO>(p, a, dhidden, dweight, st);
+  if constexpr (M != kPair)
     if (p.large) return launch_back<Large, M, TO>(p, a, dhidden, dweight, st);
-  }
   launch_back<Small, M, TO>(p, a, dhidden, dweight, st);
 }
 
@@ -1777,6 +1866,7 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
       a.prm = ptr<RowPrm>(work, p.prm);
       a.g = g;
       a.rest = ptr<float>(work, p.rest);
+      a.marks = ptr<uint8_t>(work, p.marks);
       a.gplane = p.tcap * p.piece;
       a.piece = p.piece;
       a.gw = gw;
@@ -1814,6 +1904,10 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
     a.ph = ptr<int>(work, p.ph);
     a.pw = Powers{ptr<int>(work, p.pw), p.piece};
     a.h = Operand{{hd, hd}, p.kp * p.planes};
+    a.tgt = ptr<int>(work, p.tgt);
+    a.rest = ptr<float>(work, p.rest);
+    a.marks = ptr<uint8_t>(work, p.marks);
+    a.v0 = (int)v0;
     a.valid = (int)valid;
     a.out = (char *)dweight + v0 * width * (dweight_dtype == SK_F32 ? 4 : 2);
     a.vocab = x->vocab;

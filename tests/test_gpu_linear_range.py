@@ -35,8 +35,8 @@ def make(T, V, d, seed, pull=0.0):
     return h, W, t, torch.randn(T, generator=g)
 
 
-def check(dev, h, W, t, c, batch, dt=F32, g_bits=22, odt=None, alone=None):
-    """Both gradients, each row against its own size.  g_bits: to which g is held; alone: examples that are compared with the
+def check(dev, h, W, t, c, batch, dt=F32, g_bits=22, odt=None, alone=None, t_bits=None):
+    """Both gradients, each row against its own size.  g_bits: to which g is held, t_bits: its targets' entries; alone: examples that are compared with the
     same ones in a call of their own."""
     import paper_2402_03994_amd as fw
     T, (V, d) = len(t), W.shape
@@ -57,7 +57,7 @@ def check(dev, h, W, t, c, batch, dt=F32, g_bits=22, odt=None, alone=None):
     _, rp = errors(hn, Wn, dt, 1.0)
     at = np.flatnonzero(live)
     eg = cs * p * rp + np.abs(g) * 2.0 ** -g_bits
-    eg[at, tn[at]] = cs[at, 0] * ((1 - p[at, tn[at]]) * (rp[at].max(1) + 2.0 ** -g_bits) + (4 + 39) * 2.0 ** -24)
+    eg[at, tn[at]] = cs[at, 0] * ((1 - p[at, tn[at]]) * (rp[at].max(1) + 2.0 ** -(t_bits or g_bits)) + (4 + 39) * 2.0 ** -24)
     ag, aW, ah = np.abs(g) + eg, np.abs(Wn), np.abs(hn)
     more, floor = (2.0 ** -20, 2.0 ** -37) if dt == F32 else (0.0, 0.0)
     odt = odt or dt
@@ -167,3 +167,40 @@ def test_statistics_and_gradient_from_the_same_logits(dev, T, dt):
     tol = (3 * np.abs(want) + 16) * 2.0 ** -24 + (2.0 ** -16 if dt == BF16 else 0.0)
     other = np.arange(n)[None] != (np.arange(n - 1, T) % V)[:, None]
     assert (np.abs(p * np.exp(-want) - 1) <= tol)[other].all(), (np.abs(p * np.exp(-want) - 1) / tol)[other].max()
+
+
+@pytest.mark.parametrize("T,batch,odt", [(300, 1, F32), (700, 1, F32), (1400, 1, F32), (1400, 1, BF16), (1200, 4, F32),
+                                         (264, 8, BF16), (2600, 2, F32), (66000, 1, F32)])
+def test_bf16_targets_of_many_positions(dev, T, batch, odt):
+    """Above that g's entries round to bf16, but the targets', most of their rows, are held to 2^-16 in both gradients."""
+    V = 300 if T < 60000 else 40
+    h, W, t, c = make(T, V, 72, 6, 6.0)
+    t[::7] = -1
+    t[1::7] = V
+    check(dev, h.to(BF16), W.to(BF16), t, c, batch, BF16, g_bits=8, t_bits=16, odt=odt)
+
+
+def test_bf16_targets_of_many_rows_and_features(dev):
+    """The largest tiles: rows of dweight that one position has for its target, against fp64 on the device.  The target's entry
+    is held to 2^-16; the others round by 2^-8 of themselves at most, independently: 2^-8 of the root of the sum of their
+    terms' squares (a p can be e^8.7 / (30000 e^1.1) = 0.07, so that no bound fits all rows); the logits of deviation 1.5 move
+    an entry by 2^-17 of itself."""
+    import paper_2402_03994_amd as fw
+    T, V, d = 4200, 30000, 4096
+    g = torch.Generator(device=dev).manual_seed(16)
+    h = torch.randn(T, d, generator=g, device=dev).to(BF16)
+    W = (torch.randn(V, d, generator=g, device=dev) * (1.5 / d ** 0.5)).to(BF16)
+    t, c = torch.randint(-300, V, (T,), generator=g, device=dev), torch.rand(T, generator=g, device=dev) + 0.5
+    _, stats = fw.linear_logp(h, W, t)
+    _, dw = fw.linear_logp_grad(h, W, t, stats, c, hidden_grad=False, out_dtype=F32)
+    live = (t >= 0).nonzero()[:, 0]
+    G = torch.softmax(h[live].double() @ W.double().T, 1).neg_()
+    G.scatter_add_(1, t[live][:, None], torch.ones(len(live), 1, dtype=torch.float64, device=dev)).mul_(c[live].double()[:, None])
+    want = G.T.contiguous() @ h[live].double()
+    once = torch.bincount(t[live], minlength=V) == 1
+    one = torch.zeros_like(G).scatter_(1, t[live][:, None], 1.0) * G
+    size = h[live].double().square().sum(1)  # of the hidden states, squared
+    tol = (2.0 ** -16 + 2.0 ** -17) * (one.square().T.contiguous() @ size).sqrt() + 2.0 ** -8 * ((G - one).square().T.contiguous() @ size).sqrt()
+    err = (dw.double() - want).norm(dim=1)
+    assert int(once.sum()) > 3000 and (err / tol)[once].max() <= 1, (err / tol)[once].max()
+    assert (tol / want.norm(dim=1))[once].median() < 2.0 ** -13
