@@ -72,7 +72,11 @@ __device__ __forceinline__ int exponent_of(float x) { return exponent_of(__float
 
 // What the operands of a product are: bf16; G in two bf16, beside bf16; all in two fp16.
 enum Mode { kBf16, kPair, kSplit };
-constexpr int kPairRows = 256;  // rows up to which G of bf16 inputs takes two numbers
+// G of bf16 inputs takes two numbers up to so many rows, where the reads of W count and not the products; and where dW is
+// wanted in fp32, up to so many rows of an example, whatever the others: there few tokens make a row of dW, and what their
+// number costs in precision would show (gradients of 16 examples of 200 x 50257 x 768 868 us, 1225 us so; of 8 of 250 x 32000
+// x 2048 816 and 1274 us).
+constexpr int kPairRows = 256;
 
 // hi (low half) and lo of x (kSplit: |x| < 2^15)
 template <Mode M>
@@ -1558,7 +1562,8 @@ struct Plan {
   int64_t list, pos, tgt, seg, cnt, meta, hc, eh, ev, part, xt, run, prm, cs, rest, marks, wc, g, gw, ph, pw, acc, bytes;
 };
 
-Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight) {
+// single: dW in fp32
+Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dweight, bool single) {
   Plan p{};
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -1579,7 +1584,7 @@ Plan plan_of(const sk_linear *x, int64_t batch, bool grad, bool dhidden, bool dw
   p.planes = p.f16 ? 2 : 1;
   p.batch = batch;
   p.n = x->rows / batch;
-  p.pair = !p.f16 && x->rows <= kPairRows;
+  p.pair = !p.f16 && (x->rows <= kPairRows || (single && p.n <= kPairRows));
   p.gplanes = p.f16 || p.pair ? 2 : 1;
   p.tcap = up(batch * up(p.n, kPad), 256);
   p.tcap = std::max<int64_t>(p.tcap, 256);
@@ -1784,7 +1789,7 @@ template <Mode M, typename TO>
 void run_back(const Plan &p, const Back &a, bool dhidden, bool dweight, hipStream_t st) {
   if constexpr (M != kPair)  // few rows an example
     if (p.huge) return launch_back<Huge, M, TO>(p, a, dhidden, dweight, st);
-  if constexpr (M != kPair)
+  if constexpr (M != kPair || sizeof(TO) == 4)
     if (p.large) return launch_back<Large, M, TO>(p, a, dhidden, dweight, st);
   launch_back<Small, M, TO>(p, a, dhidden, dweight, st);
 }
@@ -1795,14 +1800,14 @@ extern "C" {
 
 int64_t sketch_linear_logp_work_bytes(const sk_linear *x) {
   if (check_linear(x) != SK_OK) return 0;
-  return plan_of(x, 1, false, false, false).bytes;
+  return plan_of(x, 1, false, false, false, false).bytes;
 }
 
 int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work, int64_t work_bytes, void *stream) {
   int rc = check_linear(x);
   if (rc != SK_OK || x->rows == 0) return rc;
   if (!logp || !work) return train_fail(SK_EINVAL, "NULL argument");
-  const Plan p = plan_of(x, 1, false, false, false);
+  const Plan p = plan_of(x, 1, false, false, false, false);
   if (work_bytes < p.bytes) return train_fail(SK_EINVAL, "work is smaller than sketch_linear_logp_work_bytes");
   TrainGuard guard(x->device);
   if (!guard.ok) return train_no_device();
@@ -1835,7 +1840,8 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
 
 int64_t sketch_linear_logp_grad_work_bytes(const sk_linear *x, int64_t batch, int32_t dhidden, int32_t dweight) {
   if (check_linear(x) != SK_OK || check_batch(x, batch) != SK_OK) return 0;
-  return plan_of(x, batch, true, dhidden, dweight).bytes;
+  // either type of dW
+  return std::max(plan_of(x, batch, true, dhidden, dweight, false).bytes, plan_of(x, batch, true, dhidden, dweight, true).bytes);
 }
 
 int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stats, const float *dlogp, void *dhidden,
@@ -1847,8 +1853,8 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   if (x->dtype == SK_F32 && dweight_dtype != SK_F32) return train_fail(SK_EDTYPE, "dweight of fp32 weights is fp32");
   if (!work || (x->rows && (!stats || !dlogp)) || (!dhidden && !dweight)) return train_fail(SK_EINVAL, "NULL argument");
   if (dhidden && ld_dhidden < x->width) return train_fail(SK_EINVAL, "need ld_dhidden >= width");
-  const Plan p = plan_of(x, batch, true, dhidden != nullptr, dweight != nullptr);
-  if (work_bytes < p.bytes) return train_fail(SK_EINVAL, "work is smaller than sketch_linear_logp_grad_work_bytes");
+  if (work_bytes < sketch_linear_logp_grad_work_bytes(x, batch, dhidden != nullptr, dweight != nullptr)) return train_fail(SK_EINVAL, "work is smaller than sketch_linear_logp_grad_work_bytes");
+  const Plan p = plan_of(x, batch, true, dhidden != nullptr, dweight != nullptr, dweight && dweight_dtype == SK_F32);
   TrainGuard guard(x->device);
   if (!guard.ok) return train_no_device();
   hipStream_t st = (hipStream_t)stream;

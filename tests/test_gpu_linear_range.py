@@ -146,7 +146,7 @@ def test_weight_of_blocks_far_apart(dev, T, batch, powers):
     check(dev, h, W, t, c, batch)
 
 
-@pytest.mark.parametrize("dt", [F32])
+@pytest.mark.parametrize("dt", [F32, BF16])
 @pytest.mark.parametrize("T", [9, 40, 1200])
 def test_statistics_and_gradient_from_the_same_logits(dev, T, dt):
     """Positions with one hidden state and targets 0, 1, ..: example b's gradient has -p_v h in row v, and log p_v is
@@ -167,6 +167,14 @@ def test_statistics_and_gradient_from_the_same_logits(dev, T, dt):
     tol = (3 * np.abs(want) + 16) * 2.0 ** -24 + (2.0 ** -16 if dt == BF16 else 0.0)
     other = np.arange(n)[None] != (np.arange(n - 1, T) % V)[:, None]
     assert (np.abs(p * np.exp(-want) - 1) <= tol)[other].all(), (np.abs(p * np.exp(-want) - 1) / tol)[other].max()
+
+
+@pytest.mark.parametrize("T,batch", [(33, 1), (231, 7), (264, 8), (1320, 40), (16 * 256, 16), (40, 40)])
+def test_bf16_examples_in_any_company(dev, T, batch):
+    """dweight in fp32: up to 256 positions an example g is held in two bf16, however many examples there are."""
+    h, W, t, c = make(T, 300, 64, 5, 4.0)
+    check(dev, h.to(BF16), W.to(BF16), t, c, batch, BF16, g_bits=16, odt=F32,
+          alone=range(0, batch, 5) if batch > 1 and T // batch > 16 else None)
 
 
 @pytest.mark.parametrize("T,batch,odt", [(300, 1, F32), (700, 1, F32), (1400, 1, F32), (1400, 1, BF16), (1200, 4, F32),
