@@ -1181,7 +1181,9 @@ struct Few {
 // (fp32: four) columns from 8 (l / 16) on are one operand of v_mfma_f32_16x16x32_bf16 (element i of each lane one of
 // v_mfma_f32_16x16x4_f32, in which fp32 stays fp32).  Bound by reading W: 50257 x 768 bf16
 // 19 us, 4.1 TB/s.  GRAD: G from the same logits to the bit, so that a small 1 - p of the target keeps what it has (logits of
-// the split product beside these statistics were off by 5e-6 of it where p = 0.9).
+// the split product beside these statistics were off by 5e-6 of it where p = 0.9).  A logit is eight sums (bf16: four), since
+// one of 4096 products in a row rounds to 8e-6 at random (log p of 16 x 20000 x 4096 fp32, relative: 1.3e-6 with one, 4.4e-7
+// with four, 1.7e-7 with eight; sixteen take 60 us instead of 47 for 1 x 50257 x 768).
 template <typename T, bool GRAD>
 __global__ __launch_bounds__(256) void k_few(Few a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -1194,7 +1196,8 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
   const T *w = (const T *)a.weight + (int64_t)(v < a.vocab ? v : a.vocab - 1) * a.ld_weight;
   const T *h = (const T *)a.hidden + (int64_t)(target >= 0 ? r : 0) * a.ld_hidden;
   const int hw = target >= 0 ? a.width : 0;  // masked rows are not read
-  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  constexpr int S = sizeof(T) == 2 ? U : 8;  // sums, joined at the end
+  f32x4 sum[S] = {};
   for (int k0 = q * N; k0 - q * N < a.width; k0 += K * U) {
     u32x4 fw[U], fh[U];
 #pragma unroll
@@ -1213,15 +1216,21 @@ __global__ __launch_bounds__(256) void k_few(Few a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if constexpr (sizeof(T) == 2) {
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[u]), __builtin_bit_cast(bf16x8, fh[u]), acc, 0,
-                                                      0, 0);
+        sum[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[u]), __builtin_bit_cast(bf16x8, fh[u]),
+                                                         sum[u], 0, 0, 0);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fw[u][i]), __uint_as_float(fh[u][i]), acc, 0, 0, 0);
+          sum[(u * 4 + i) % S] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fw[u][i]), __uint_as_float(fh[u][i]),
+                                                                      sum[(u * 4 + i) % S], 0, 0, 0);
       }
     }
   }
+#pragma unroll
+  for (int n = S / 2; n >= 1; n >>= 1)
+#pragma unroll
+    for (int i = 0; i < n; ++i) sum[i] += sum[i + n];
+  f32x4 acc = sum[0];
   // this lane: entries v0 + 4 q + e of row r
   if constexpr (GRAD) {
     constexpr Mode M = sizeof(T) == 4 ? kSplit : kPair;

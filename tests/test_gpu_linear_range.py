@@ -212,3 +212,19 @@ def test_bf16_targets_of_many_rows_and_features(dev):
     err = (dw.double() - want).norm(dim=1)
     assert int(once.sum()) > 3000 and (err / tol)[once].max() <= 1, (err / tol)[once].max()
     assert (tol / want.norm(dim=1))[once].median() < 2.0 ** -13
+
+
+def test_few_rows_add_up_in_several_sums(dev):
+    """fp32, up to 16 rows: logits of 4096 products and a deviation of 5.  A sum of n products in a row, of which it is the root of
+    k / n behind k of them, rounds to 2^-24 / sqrt(3) of that each time: sqrt(n / 6) 2^-24 of the whole.  Eight sums of 512 add up to
+    sqrt(4096 / 48) 2^-24 = 9.2 2^-24 of the deviation, one sum to 26 2^-24; log p and log z themselves, of size 20, to 12 2^-24.
+    Half as much again for the mean of 640 of them."""
+    import paper_2402_03994_amd as fw
+    g = torch.Generator().manual_seed(8)
+    h, W = torch.randn(16, 4096, generator=g).to(dev), (torch.randn(64, 4096, generator=g) * (5 / 64)).to(dev)
+    x = h.double() @ W.double().T
+    err = []
+    for v in range(0, 40):
+        t = torch.full((16,), v, device=dev)
+        err.append(fw.linear_logp(h, W, t)[0].double() - torch.log_softmax(x, 1)[:, v])
+    assert torch.stack(err).square().mean().sqrt() <= 1.5 * (46.0 ** 2 + 12.0 ** 2) ** 0.5 * 2.0 ** -24
