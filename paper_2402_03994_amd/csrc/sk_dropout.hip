@@ -126,7 +126,9 @@ extern "C" int sketch_dropout(const void *x, sk_dtype dtype, int64_t rows, int64
   Drop a{x, residual, out, rows * width, width, ld, ld_residual, ld_out, 0, 0, drop, (uint32_t)step, (uint32_t)site, step_at,
          drop < 65536 ? 65536.0f / (float)(65536 - drop) : 0.0f, make_key(seed), false};
   a.groups = (a.n + 7) / 8;
-  a.past = a.n * (dtype == SK_F32 ? 4 : 2) > kPastBytes;
+  // fp32 leaves in two stores of 16 bytes of every 32, which the caches put together (32768 x 4096 with residual past them 538
+  // us, 304 us so; bf16 136 us either way)
+  a.past = dtype == SK_BF16 && a.n * 2 > kPastBytes;
   const bool flat = rows == 1 || (ld == width && ld_out == width && (!residual || ld_residual == width));
   if (dtype == SK_F32)
     run<float>(a, flat, (hipStream_t)stream);
