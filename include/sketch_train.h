@@ -189,8 +189,8 @@ int sketch_linear_logp(const sk_linear *x, float *logp, float *stats, void *work
  * to 256 rows, and with dweight in fp32 up to 256 rows an example, g takes two bf16
  * (2^-16).  fp32 inputs: products as above; of dweight[b][v] what lies below 2^-37 of
  * its largest |g_tv| max |hidden[t]| is lost, of dhidden[t] what lies below 2^-36 of
- * dlogp[t] times the largest entry of weight.  A weight that is not finite gives NaNs.  Rows with dlogp = 0 are masked.  Outputs may not overlap
- * inputs.
+ * dlogp[t] times the largest entry of weight.  A weight that is not finite gives NaNs.
+ * Rows with dlogp = 0 are masked.  Outputs may not overlap inputs.
  *   work     sketch_linear_logp_grad_work_bytes(x, batch, dhidden wanted, dweight
  *            wanted) bytes (0 if refused), 256-byte aligned.
  * SK_EUNSUPPORTED for batch > 2^14.

@@ -29,9 +29,9 @@
 //
 // What bounds it: the products, at the rate that their operands leave the caches
 // (the figures are at Tiling); below some hundred rows the reads of W; below those
-// the launches.  One MI355X, both calls: 4096 x 50257 x 768 bf16 (40% masked) 867 us,
-// 8192 x 128256 x 4096 18.4 ms (840 TFLOP/s of the 6 n V d, 1110 with the logits
-// that are formed again).
+// the launches.  One MI355X, both calls: 4096 x 50257 x 768 bf16 (40% masked) 884 us,
+// 8192 x 128256 x 4096 19.5 ms (790 TFLOP/s of the 6 n V d, 1060 with the logits
+// that are formed again); 8 examples of 257 x 50257 x 768 fp32 1680 us.
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -61,8 +61,8 @@ struct Meta {
   int np;  // listed rows
 };
 
-// A listed row in the gradient: G = one [v = target] + w exp(scale (x - m)).  A row that only
-// fills the list, or has no logit above -inf, has m = inf, w = one = 0.
+// A listed row in the gradient: G = one [v = target] + w exp(scale (x - m)).  A row that only fills the list, or has no logit
+// above -inf, has m = inf, w = one = 0.
 struct RowPrm {
   float m, w, one;  // fp32: without the factor dlogp scale, which is in cs
 };
@@ -199,8 +199,8 @@ __device__ __forceinline__ void masked(const Live &a, int row) {
   }
 }
 
-// Counts of 64 rows each, their sums within the examples, the examples' starts, the list.  A wave has
-// four chunks of 64 rows under way (8192 rows: 17 us one after another, 14.5 us so).
+// Counts of 64 rows each, their sums within the examples, the examples' starts, the list.  A wave has four chunks of 64 rows
+// under way (8192 rows: 17 us one after another, 14.5 us so).
 __global__ __launch_bounds__(1024) void k_live(Live a) {
   constexpr int U = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -385,9 +385,9 @@ __global__ __launch_bounds__(256) void k_prep(Prep a) {
 }
 
 // The list, H's rows and W's in one launch, for up to 64 chunks of 64 rows: each workgroup counts the live rows by itself and
-// takes 16 rows of a chunk, a wave each.  `blocks` of those; the workgroups behind them prepare W.  Beside k_live, k_gather and k_prep one after another: 61 x 8000 x 250
-// fp32 with gradients 78.7 us, 68.1 us so; 2000 x 50257 x 768 fp32 345 and 329 us; 4096 x 50257 x 768 bf16 with gradients
-// 868 and 855 us.
+// takes 16 rows of a chunk, a wave each.  `blocks` of those; the workgroups behind them prepare W.  Beside k_live, k_gather and
+// k_prep one after another: 61 x 8000 x 250 fp32 with gradients 78.7 us, 68.1 us so; 2000 x 50257 x 768 fp32 345 and 329 us;
+// 4096 x 50257 x 768 bf16 with gradients 868 and 855 us.
 struct Front {
   Live l;
   Gather g;
@@ -592,7 +592,7 @@ __device__ __forceinline__ u32x4 times_power(u32x4 v, int d) {
 template <typename C, Mode M>
 struct Core {
   f32x16 acc[C::TM][C::TN];
-  int top[C::TM];  // with Powers: the exponent of row 32 i + lane % 32 in the sums so far
+  int top[C::TM];  // kRows: the exponent of row 32 i + lane % 32 in the sums so far; kBlocks: top[0] that of all rows
   int wm, wn, fr, fk;
 
   __device__ __forceinline__ Core() {
@@ -691,6 +691,8 @@ struct Core {
   // kPair: all of K with a's lo, then with its hi.
   // kRows: each row begins at the largest of its first 256 columns (one trip to the caches), so that few groups bring the sums
   // down; what a stage's blocks are times is settled a stage before, since the products would wait for it.
+  // REST: the rows of a marked stage once more with the rest (4096 x 50257 x 768 bf16 855 us without it, 879 us so; as stages of
+  // their own at the end 911 us; 8192 x 128256 x 4096 19.2 and 19.8 ms).
   template <bool KA, bool KB, Scaling S = kPlain, bool REST = false>
   __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int rows_a, int rows_b, int depth,
                                       int depth_b, Powers pw = Powers{}, Rest r = Rest{}) {
@@ -1062,8 +1064,9 @@ __global__ __launch_bounds__(C::TH, 2) void k_logits(Logit a) {
           for (int p = 0; p < 2; ++p) {
             const int m = c.row(i, e), ch = (m >> 5) * 8 + p * 4 + ((m & 31) >> 3);
             const uint32_t sel = p ? 0x07060302 : 0x05040100;
-            *(u32x2 *)(at + n * RW + (ch ^ (n & 31)) * 16 + (m & 4) * 2) =
-                u32x2{__builtin_amdgcn_perm(bits[i][e + 1], bits[i][e], sel), __builtin_amdgcn_perm(bits[i][e + 3], bits[i][e + 2], sel)};
+            const u32x2 v{__builtin_amdgcn_perm(bits[i][e + 1], bits[i][e], sel),
+                          __builtin_amdgcn_perm(bits[i][e + 3], bits[i][e + 2], sel)};
+            *(u32x2 *)(at + n * RW + (ch ^ (n & 31)) * 16 + (m & 4) * 2) = v;
           }
       __syncthreads();
 #pragma unroll 4
@@ -1455,15 +1458,17 @@ __global__ __launch_bounds__(C::TH, 2) void k_back(Back a) {
   const int depth = hidden ? max(0, min(a.per, a.steps - part * a.per)) * kStep : a.seg[a.b0 + part + 1] - k0;
   Core<C, M> c;
   // split weights bring rows of zeros up to a multiple of 64
-  if (hidden)
-    c.template run<false, true, F16 ? kBlocks : kPlain>(lds, at_row<M>(a.g, m0, k0), at_row<M>(a.w, k0, n0), np - m0, a.kp - n0, depth,
-                                                        F16 ? a.steps * kStep - k0 : a.valid - k0, Powers{a.ph + k0 / 64, 0});
-  else
+  if (hidden) {
+    c.template run<false, true, F16 ? kBlocks : kPlain>(lds, at_row<M>(a.g, m0, k0), at_row<M>(a.w, k0, n0), np - m0,
+                                                        a.kp - n0, depth, F16 ? a.steps * kStep - k0 : a.valid - k0,
+                                                        Powers{a.ph + k0 / 64, 0});
+  } else {
+    const Powers pw{a.pw.p + k0 / 16 * a.pw.ld + m0, a.pw.ld};
+    const int64_t blocks = a.tcap >> 5;
+    const Rest rest{a.tgt + k0, a.rest + k0, a.marks + (m0 >> 6) * blocks, blocks, a.v0 + m0, k0};
     c.template run<true, true, F16 ? kRows : kPlain, M == kBf16>(lds, at_row<M>(a.gw, k0, m0), at_row<M>(a.h, k0, n0), C::BM,
-                                                                 a.kp - n0, depth, depth,
-                                                                 Powers{a.pw.p + k0 / 16 * a.pw.ld + m0, a.pw.ld},
-                                                                 Rest{a.tgt + k0, a.rest + k0, a.marks + (m0 >> 6) * (a.tcap >> 5), a.tcap >> 5,
-                                                                      a.v0 + m0, k0});
+                                                                 a.kp - n0, depth, depth, pw, rest);
+  }
   if (hidden) {
     float *to = a.acc + (part * a.tcap + m0) * a.kp + n0;
     const int power = c.top[0] - kTopG - kTop;  // kBlocks: the same for all rows
@@ -1862,7 +1867,8 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
   if (x->dtype == SK_F32 && dweight_dtype != SK_F32) return train_fail(SK_EDTYPE, "dweight of fp32 weights is fp32");
   if (!work || (x->rows && (!stats || !dlogp)) || (!dhidden && !dweight)) return train_fail(SK_EINVAL, "NULL argument");
   if (dhidden && ld_dhidden < x->width) return train_fail(SK_EINVAL, "need ld_dhidden >= width");
-  if (work_bytes < sketch_linear_logp_grad_work_bytes(x, batch, dhidden != nullptr, dweight != nullptr)) return train_fail(SK_EINVAL, "work is smaller than sketch_linear_logp_grad_work_bytes");
+  if (work_bytes < sketch_linear_logp_grad_work_bytes(x, batch, dhidden != nullptr, dweight != nullptr))
+    return train_fail(SK_EINVAL, "work is smaller than sketch_linear_logp_grad_work_bytes");
   const Plan p = plan_of(x, batch, true, dhidden != nullptr, dweight != nullptr, dweight && dweight_dtype == SK_F32);
   TrainGuard guard(x->device);
   if (!guard.ok) return train_no_device();
@@ -1891,7 +1897,8 @@ int sketch_linear_logp_grad(const sk_linear *x, int64_t batch, const float *stat
       if (x->rows <= kFew) {
         const Few f{x->hidden, x->weight, x->targets, x->ld_hidden, x->ld_weight, (int)x->rows, (int)x->vocab, (int)width,
                     (int)x->index, x->scale, nullptr, nullptr, 0, nullptr, nullptr, (int)v0, (int)valid, meta,
-                    ptr<int>(work, p.pos), ptr<int>(work, p.list), a.prm, a.g, a.gplane, a.piece, a.gw, a.ph, a.pw, a.eh, a.ev, a.cs};
+                    ptr<int>(work, p.pos), ptr<int>(work, p.list), a.prm, a.g, a.gplane, a.piece, a.gw, a.ph, a.pw, a.eh, a.ev,
+                    a.cs};
         const dim3 grid((unsigned)((valid + kFewUnit - 1) / kFewUnit));
         if (p.f16)
           hipLaunchKernelGGL((k_few<float, true>), grid, dim3(256), 0, st, f);

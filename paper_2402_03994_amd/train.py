@@ -259,9 +259,14 @@ def linear_logp_grad(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.
     Sketch.apply takes.  dweight has the weight's type; out_dtype (or an out of it) may be float32 for a bfloat16 weight.
     accumulate adds to `out` (with tied weights embed_grad can add to it too).
 
-    The logits are formed again, a piece of the vocabulary at a time (256 MB of gradients at them); these are rounded to
-    bfloat16 where the inputs are (up to 256 positions: to two numbers).  Positions with a masked target or dlogp = 0 are
-    not read and get zeros."""
+    The logits are formed again, a piece of the vocabulary at a time; their gradients are rounded to bfloat16 where the inputs
+    are, and what the targets' entries lose by that is returned to both gradients (up to 256 positions, and with dweight in
+    float32 up to 256 an example, they are held in two numbers).  float32 keeps what lies 2^-37 below the largest term of a row
+    of dweight, whatever other examples the call has.  Positions with a masked target or dlogp = 0 are not read and get zeros.
+    Beside its inputs a call needs 256 MB of these gradients (float32 with a width above 1024: for either gradient; at least 256
+    entries of the vocabulary, 1 to 2 GB at 2^20 positions), a copy of the hidden states, up to 32 sums of dhidden in float32 (one
+    or two of many positions), and for float32 (or rows that 16-byte loads do not fit) a copy of a piece of the weight in up to
+    256 MB."""
     x = _linear(hidden, weight, targets, scale)
     device, lib = hidden.device, _lib.load()
     if stats.dtype != torch.float32 or stats.device != device or stats.shape != (*targets.shape, 2) or \
